@@ -18,7 +18,8 @@ BINDING_PATH = os.path.join(PKG_DIR, "_binding.so")
 # attn_mfma_*.hip: the instantiations of the MFMA kernel template (attn_mfma.h), one slice per
 # element type and head_dim, so that the slow part of the build runs side by side
 SOURCES = ["grat_api.hip", "block_lists.hip", "attn_f32.hip", "mfma_probe.hip", "attn_mfma.hip",
-           "attn_mfma_bf16_d128.hip", "attn_mfma_bf16_d64.hip", "attn_mfma_f16_d128.hip", "attn_mfma_f16_d64.hip"]
+           "attn_mfma_bf16_d128.hip", "attn_mfma_bf16_d64.hip", "attn_mfma_f16_d128.hip", "attn_mfma_f16_d64.hip",
+           "sequence_api.hip", "sequence_rotary.hip", "sequence_scores.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,197 @@
+// Host side of the token-sequence operators: argument validation and dispatch.  No allocation, no synchronisation.
+#include <cmath>
+#include <cstdint>
+
+#include "sequence_common.h"
+
+namespace grat {
+namespace {
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+bool is16(grat_dtype t) { return t == GRAT_BF16 || t == GRAT_F16; }
+bool known(grat_dtype t) { return is16(t) || t == GRAT_F32; }
+
+// A tensor whose rows are read or written as 16-byte vectors.
+grat_status check_tensor(const grat_tensor* t, grat_dtype dtype, int32_t head_dim) {
+    if (!t || !t->data) return GRAT_ERR_NULL;
+    if (t->stride_n < head_dim || t->stride_b < 0 || t->stride_h < 0) return GRAT_ERR_BAD_DIMS;
+    const int vec = is16(dtype) ? 8 : 4;
+    if (t->stride_n % vec || t->stride_b % vec || t->stride_h % vec || !aligned16(t->data)) return GRAT_ERR_UNSUPPORTED;
+    if (t->stride_n >= ((int64_t)1 << 24) || t->stride_b >= ((int64_t)1 << 46) || t->stride_h >= ((int64_t)1 << 46))
+        return GRAT_ERR_UNSUPPORTED;
+    return GRAT_OK;
+}
+
+SeqTensor of(const grat_tensor* t) { return {(uint8_t*)t->data, t->stride_b, t->stride_h, t->stride_n}; }
+
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
+
+// The parts of a grat_sequence that every operator on lists reads.
+grat_status make_shape(const grat_sequence* s, SeqShape* out) {
+    if (!s) return GRAT_ERR_NULL;
+    if (s->batch < 1 || s->kv_heads < 1 || s->q_heads < 1 || s->n_q < 1 || s->n_k < 1 || s->q_group < 1 || s->block < 1) return GRAT_ERR_BAD_DIMS;
+    if (s->q_heads % s->kv_heads) return GRAT_ERR_BAD_DIMS;
+    if (s->block % 32 || s->block > 4096) return GRAT_ERR_UNSUPPORTED;
+    if (s->n_q >= kMaxRows || s->n_k >= kMaxRows || (int64_t)s->batch * s->kv_heads > 65535 || s->q_heads > 65535) return GRAT_ERR_UNSUPPORTED;
+    *out = SeqShape{s->batch, s->q_heads, s->kv_heads, s->q_heads / s->kv_heads, s->n_q, s->n_k,
+                    s->q_group < s->n_q ? s->q_group : s->n_q, s->block, 0, 0, s->causal ? 1 : 0, s->d_k_len, s->d_q_pos};
+    out->n_groups = (out->n_q + out->q_group - 1) / out->q_group;
+    out->n_blocks = (out->n_k + out->block - 1) / out->block;
+    return GRAT_OK;
+}
+
+// For the operators that do not read all of it.
+grat_sequence with_heads(const grat_sequence& s) {
+    grat_sequence t = s;
+    t.q_heads = t.kv_heads;
+    return t;
+}
+
+grat_status status_of(hipError_t e) { return e == hipSuccess ? GRAT_OK : GRAT_ERR_HIP; }
+
+grat_status make_rotary(const grat_rotary_args* a, bool with_k, RotaryParams* out) {
+    if (!a || !a->d_table) return GRAT_ERR_NULL;
+    if (a->batch < 1 || a->q_heads < 1 || a->n_tokens < 1 || a->head_dim < 1 || a->rot < 1 || a->rot > a->head_dim || a->n_pos < 1)
+        return GRAT_ERR_BAD_DIMS;
+    if (with_k && a->kv_heads < 1) return GRAT_ERR_BAD_DIMS;
+    if (a->axes < 1 || a->axes > 3) return GRAT_ERR_BAD_DIMS;
+    int64_t pairs = 0;
+    RotaryParams p{};
+    for (int k = 0; k < 3; ++k) {
+        if (k < a->axes) {
+            if (a->axis_pairs[k] < 1) return GRAT_ERR_BAD_DIMS;
+            pairs += a->axis_pairs[k];
+        }
+        p.axis_end[k] = (int32_t)(pairs < kMaxRows ? pairs : kMaxRows);
+    }
+    if (2 * pairs != a->rot) return GRAT_ERR_BAD_DIMS;
+    if (a->axes > 1 && !a->d_positions) return GRAT_ERR_NULL;
+    if (a->positions_stride_b < 0) return GRAT_ERR_BAD_DIMS;
+    if (!known(a->dtype)) return GRAT_ERR_UNSUPPORTED;
+    if (a->head_dim % 16 || a->rot % 16 || a->head_dim > 1024 || !aligned16(a->d_table)) return GRAT_ERR_UNSUPPORTED;
+    if ((int64_t)a->batch * a->n_tokens >= kMaxRows || (int64_t)a->q_heads + 2 * (int64_t)(with_k ? a->kv_heads : 0) > 65535) return GRAT_ERR_UNSUPPORTED;
+    p.heads[0] = a->q_heads;
+    p.heads[1] = with_k ? a->kv_heads : 0;
+    p.batch = a->batch;
+    p.n_tokens = a->n_tokens;
+    p.items = a->head_dim;   // (the launcher divides by what a piece holds)
+    p.rot = a->rot;
+    p.interleaved = a->interleaved ? 1 : 0;
+    p.inverse = a->inverse ? 1 : 0;
+    p.n_pos = a->n_pos;
+    p.axes = a->axes;
+    p.table = a->d_table;
+    p.positions = a->d_positions;
+    p.positions_stride_b = a->positions_stride_b;
+    p.start = a->d_start;
+    *out = p;
+    return GRAT_OK;
+}
+
+}  // namespace
+}  // namespace grat
+
+using namespace grat;
+
+extern "C" grat_status grat_rotary_table(const grat_rotary_spec* spec, int32_t n_pos, int32_t axes, const int32_t* axis_pairs,
+                                         float* d_table, void* hip_stream) {
+    if (!spec || !axis_pairs || !d_table) return GRAT_ERR_NULL;
+    if (n_pos < 1 || axes < 1 || axes > 3) return GRAT_ERR_BAD_DIMS;
+    int64_t pairs = 0;
+    for (int k = 0; k < axes; ++k) {
+        if (axis_pairs[k] < 1) return GRAT_ERR_BAD_DIMS;
+        pairs += axis_pairs[k];
+    }
+    if (spec->scaling != GRAT_ROTARY_PLAIN && spec->scaling != GRAT_ROTARY_LINEAR && spec->scaling != GRAT_ROTARY_BASE &&
+        spec->scaling != GRAT_ROTARY_RAMP)
+        return GRAT_ERR_BAD_PATTERN;
+    auto positive = [](double v) { return v > 0.0 && std::isfinite(v); };
+    if (!positive(spec->base) || !positive(spec->magnitude)) return GRAT_ERR_BAD_DIMS;
+    if (spec->scaling != GRAT_ROTARY_PLAIN && !positive(spec->factor)) return GRAT_ERR_BAD_DIMS;
+    if (spec->scaling == GRAT_ROTARY_RAMP && (!positive(spec->trained) || !(spec->low < spec->high) || !std::isfinite(spec->high - spec->low)))
+        return GRAT_ERR_BAD_DIMS;
+    if (pairs > 512 || (int64_t)n_pos * pairs >= kMaxRows || !aligned16(d_table)) return GRAT_ERR_UNSUPPORTED;
+    return status_of(launch_rotary_table(*spec, n_pos, axes, axis_pairs, d_table, (hipStream_t)hip_stream));
+}
+
+extern "C" grat_status grat_rotary(const grat_rotary_args* args, const grat_tensor* Q, const grat_tensor* Q_out, const grat_tensor* K,
+                                   const grat_tensor* K_out, void* hip_stream) {
+    RotaryParams p;
+    const bool with_k = K || K_out;
+    grat_status st = make_rotary(args, with_k, &p);
+    const grat_tensor* const tensors[4] = {Q, Q_out, K, K_out};
+    for (int i = 0; st == GRAT_OK && i < (with_k ? 4 : 2); ++i) st = check_tensor(tensors[i], args->dtype, args->head_dim);
+    if (st != GRAT_OK) return st;
+    p.in[0] = of(Q);
+    p.out[0] = of(Q_out);
+    if (with_k) {
+        p.in[1] = of(K);
+        p.out[1] = of(K_out);
+    }
+    return status_of(launch_rotary(p, args->dtype, (hipStream_t)hip_stream));
+}
+
+extern "C" grat_status grat_rotary_append(const grat_rotary_args* args, const grat_tensor* Q, const grat_tensor* Q_out, const grat_tensor* K,
+                                          const grat_tensor* V, const grat_tensor* K_cache, const grat_tensor* V_cache, int32_t n_cache,
+                                          void* hip_stream) {
+    RotaryParams p;
+    grat_status st = make_rotary(args, true, &p);
+    const grat_tensor* const tensors[6] = {Q, Q_out, K, K_cache, V, V_cache};
+    for (int i = 0; st == GRAT_OK && i < 6; ++i) st = check_tensor(tensors[i], args->dtype, args->head_dim);
+    if (st != GRAT_OK) return st;
+    if (!args->d_start) return GRAT_ERR_NULL;
+    if (n_cache < 1 || args->axes != 1 || args->d_positions || args->inverse) return GRAT_ERR_BAD_DIMS;
+    for (int t = 0; t < 3; ++t) {
+        p.in[t] = of(tensors[2 * t]);
+        p.out[t] = of(tensors[2 * t + 1]);
+    }
+    p.heads[2] = p.heads[1];
+    p.n_cache = n_cache;
+    return status_of(launch_rotary(p, args->dtype, (hipStream_t)hip_stream));
+}
+
+extern "C" grat_status grat_block_means(const grat_sequence* seq, const grat_tensor* K, int32_t n_new, float* d_means, void* hip_stream) {
+    if (!seq || !d_means) return GRAT_ERR_NULL;
+    grat_sequence q = with_heads(*seq);   // what is not read here
+    q.n_q = q.q_group = 1;
+    SeqShape s;
+    grat_status st = make_shape(&q, &s);
+    if (st != GRAT_OK) return st;
+    if (n_new < 0) return GRAT_ERR_BAD_DIMS;
+    if (!known(seq->dtype) || (seq->head_dim != 64 && seq->head_dim != 128)) return GRAT_ERR_UNSUPPORTED;
+    st = check_tensor(K, seq->dtype, seq->head_dim);
+    if (st != GRAT_OK) return st;
+    return status_of(launch_block_means(s, of(K), seq->dtype, seq->head_dim, n_new, d_means, (hipStream_t)hip_stream));
+}
+
+extern "C" int64_t grat_block_scores_work(const grat_sequence* seq) {
+    SeqShape s;
+    return make_shape(seq, &s) == GRAT_OK && seq->head_dim > 0 ? block_scores_work(s, seq->head_dim) : 0;
+}
+
+extern "C" grat_status grat_block_scores(const grat_sequence* seq, const grat_tensor* Q, const float* d_means, float scale, float* d_scores,
+                                         void* d_work, void* hip_stream) {
+    if (!d_means || !d_scores) return GRAT_ERR_NULL;
+    SeqShape s;
+    grat_status st = make_shape(seq, &s);
+    if (st != GRAT_OK) return st;
+    if (!std::isfinite(scale)) return GRAT_ERR_BAD_DIMS;
+    if (!known(seq->dtype) || (seq->head_dim != 64 && seq->head_dim != 128)) return GRAT_ERR_UNSUPPORTED;
+    if ((int64_t)s.n_groups > 65535 * (int64_t)64 || !aligned16(d_means) || !aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;
+    st = check_tensor(Q, seq->dtype, seq->head_dim);
+    if (st != GRAT_OK) return st;
+    if (!d_work && block_scores_work(s, seq->head_dim) > 0) return GRAT_ERR_NULL;
+    return status_of(launch_block_scores(s, of(Q), seq->dtype, seq->head_dim, d_means, scale, d_scores, (float*)d_work, (hipStream_t)hip_stream));
+}
+
+extern "C" grat_status grat_select_blocks(const grat_sequence* seq, const float* d_scores, int32_t top, int32_t first, int32_t local,
+                                          int32_t* d_count, int32_t* d_index, void* hip_stream) {
+    if (!seq || !d_scores || !d_count || !d_index) return GRAT_ERR_NULL;
+    const grat_sequence q = with_heads(*seq);
+    SeqShape s;
+    const grat_status st = make_shape(&q, &s);
+    if (st != GRAT_OK) return st;
+    if (top < 1 || first < 0 || local < 0 || (int64_t)first + local > top) return GRAT_ERR_BAD_DIMS;
+    if (s.n_blocks > 32768 || top > 8192 || (int64_t)s.batch * s.kv_heads * s.n_groups >= (1 << 26)) return GRAT_ERR_UNSUPPORTED;
+    return status_of(launch_select_blocks(s, d_scores, top, first, local, d_count, d_index, (hipStream_t)hip_stream));
+}

@@ -25,7 +25,10 @@ PATTERNS = {"block": 0, "cross": 1, "cross_planes": 2, "dense": 3}
 DTYPES = {torch.bfloat16: 0, torch.float32: 1, torch.float16: 2}
 EXPORTS = ("grat_block_list_shape", "grat_build_block_lists", "grat_validate_block_lists", "grat_attention_fwd",
            "grat_attention_global_fwd", "grat_attention_packed_fwd", "grat_dense_attention_fwd",
-           "grat_status_string", "grat_probe_mfma", "grat_probe_launch")
+           "grat_status_string", "grat_probe_mfma", "grat_probe_launch",
+           # token sequences: sequence.py
+           "grat_rotary_table", "grat_rotary", "grat_rotary_append", "grat_block_means", "grat_block_scores_work",
+           "grat_block_scores", "grat_select_blocks")
 
 _i32, _i64, _f32, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
 _pi32 = ctypes.POINTER(ctypes.c_int32)
