@@ -1,5 +1,5 @@
 /*
- * libgrat — token sequences: rotary positions, and lists of key blocks that a score selects.
+ * libgrat — token sequences: rotary positions, and attention over key blocks that a score selects.
  *
  * grat.h attends lists of key groups that follow from positions on a grid.  Here the lists follow from the data, as
  * long sequences of a language model need them: every group of queries attends the key blocks whose mean key it
@@ -9,6 +9,7 @@
  *   grat_block_means                    mean key of every key block
  *   grat_block_scores                   score of every query group for every key block
  *   grat_select_blocks                  the lists
+ *   grat_selected_attention_fwd / _bwd  attention over the lists, and its gradient
  *
  * Conventions of grat.h hold: plain C, device pointers owned by the caller, nothing allocated, nothing synchronised,
  * work enqueued on `hip_stream`, every check on the host ahead of the first launch, errors as return codes.  The
@@ -149,6 +150,40 @@ grat_status grat_block_scores(const grat_sequence* seq, const grat_tensor* Q, co
  */
 grat_status grat_select_blocks(const grat_sequence* seq, const float* d_scores, int32_t top, int32_t first, int32_t local,
                                int32_t* d_count, int32_t* d_index, void* hip_stream);
+
+/*
+ * O = softmax(scale * Q K^T over the listed keys that the row sees) V, row by row.
+ *   O          strides of its own; must not alias Q, K or V.  A row that sees no listed key gets 0.
+ *   d_lse      [batch][q_heads][n_q] (fp32, or NULL): the natural logarithm of the row's sum of exp(scale q.k), -infinity
+ *              for a row that sees no listed key
+ *   d_count, d_index, max_blocks   lists as grat_select_blocks writes them (max_blocks = top).  Callers may make their
+ *              own: any order, blocks of a list distinct.  Counts are forced into [0, max_blocks]; entries outside
+ *              [0, n_blocks) are skipped.
+ *   d_work     scratch memory of grat_selected_attention_work(seq, max_blocks, 0) bytes (NULL where that is 0), 16-byte
+ *              aligned
+ * Supported: GRAT_BF16, GRAT_F16; head_dim 64 or 128; block a multiple of 32; max_blocks * block <= 2^18; stride_n
+ * < 2^24; every other stride as in grat.h.  scale > 0.
+ * Scores, reference maximum, sum and output accumulate in fp32; the weights are rounded to the element type (nearest-even)
+ * for the product with V, their sum is not.  A NaN or infinite V of a key that some row of a query group sees reaches
+ * all rows of that group (0 * NaN); keys that no row of the group sees are never read.
+ */
+int64_t grat_selected_attention_work(const grat_sequence* seq, int32_t max_blocks, int32_t backward);
+grat_status grat_selected_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K, const grat_tensor* V,
+                                        const grat_tensor* O, float* d_lse, float scale, const int32_t* d_count,
+                                        const int32_t* d_index, int32_t max_blocks, void* d_work, void* hip_stream);
+
+/*
+ * The gradient of grat_selected_attention_fwd (the lists are given, not differentiated): dQ, dK, dV for dO, with O and
+ * d_lse as the forward call wrote them.  Heads that share a K/V head add up in its dK and dV.  Rows of dK and dV that
+ * no query attends, also those behind the valid keys, get 0.  Every output is written once, nothing is added
+ * atomically: the same inputs give the same bits.
+ *   d_work     grat_selected_attention_work(seq, max_blocks, 1) bytes, 16-byte aligned
+ * The softmax weights and the score gradients are rounded to the element type for the products; all sums in fp32.
+ */
+grat_status grat_selected_attention_bwd(const grat_sequence* seq, const grat_tensor* dO, const grat_tensor* Q, const grat_tensor* K,
+                                        const grat_tensor* V, const grat_tensor* O, const float* d_lse, const grat_tensor* dQ,
+                                        const grat_tensor* dK, const grat_tensor* dV, float scale, const int32_t* d_count,
+                                        const int32_t* d_index, int32_t max_blocks, void* d_work, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,9 @@ BINDING_PATH = os.path.join(PKG_DIR, "_binding.so")
 # element type and head_dim, so that the slow part of the build runs side by side
 SOURCES = ["grat_api.hip", "block_lists.hip", "attn_f32.hip", "mfma_probe.hip", "attn_mfma.hip",
            "attn_mfma_bf16_d128.hip", "attn_mfma_bf16_d64.hip", "attn_mfma_f16_d128.hip", "attn_mfma_f16_d64.hip",
-           "sequence_api.hip", "sequence_rotary.hip", "sequence_scores.hip"]
+           "sequence_api.hip", "sequence_rotary.hip", "sequence_scores.hip", "sequence_bwd.hip",
+           "sequence_fwd_bf16_d128.hip", "sequence_fwd_bf16_d64.hip", "sequence_fwd_f16_d128.hip", "sequence_fwd_f16_d64.hip",
+           "sequence_bwd_bf16_d128.hip", "sequence_bwd_bf16_d64.hip", "sequence_bwd_f16_d128.hip", "sequence_bwd_f16_d64.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

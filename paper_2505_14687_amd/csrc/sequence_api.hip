@@ -1,8 +1,9 @@
 // Host side of the token-sequence operators: argument validation and dispatch.  No allocation, no synchronisation.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
-#include "sequence_common.h"
+#include "sequence_attn.h"
 
 namespace grat {
 namespace {
@@ -85,6 +86,96 @@ grat_status make_rotary(const grat_rotary_args* a, bool with_k, RotaryParams* ou
     p.positions_stride_b = a->positions_stride_b;
     p.start = a->d_start;
     *out = p;
+    return GRAT_OK;
+}
+
+// ---- attention over lists --------------------------------------------------------------------
+// Rows of a forward workgroup.  (rows = those of a group)
+int fwd_tile_rows(const SeqShape& s, int head_dim, int64_t rows) {
+    if (rows <= 32) return 32;
+    if (rows <= 64) return 64;
+    const int64_t lists = (int64_t)s.batch * s.kv_heads * s.n_groups;
+    if (head_dim == 128 && (rows % 256 == 0 || rows % 256 > 128) && lists * ((rows + 255) / 256) >= 256) return 256;
+    return 128;
+}
+int bwd_tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+int bwd_tile_keys(int block) { return block % 128 == 0 ? 128 : block % 64 == 0 ? 64 : 32; }
+
+// A checked call on lists, with everything that is decided about its launches.
+struct SelPlan {
+    SelParams p{};
+    GradParams g{};
+    int tile_rows = 0, tile_keys = 0;
+    int64_t work = 0;   // bytes of scratch memory
+};
+
+// Takes a share of the scratch memory: returns its place, counted from the start.
+int64_t take(SelPlan& plan, int64_t bytes) {
+    const int64_t at = plan.work;
+    plan.work = at + (bytes + 255) / 256 * 256;
+    return at;
+}
+
+grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks, bool backward, uint8_t* work, SelPlan* out) {
+    SelPlan plan;
+    SelParams& p = plan.p;
+    const grat_status st = make_shape(seq, &p.s);
+    if (st != GRAT_OK) return st;
+    const SeqShape& s = p.s;
+    if (max_blocks < 1) return GRAT_ERR_BUFFER_TOO_SMALL;
+    if (!(scale > 0.f) || !std::isfinite(scale)) return GRAT_ERR_BAD_DIMS;
+    if (!is16(seq->dtype) || (seq->head_dim != 64 && seq->head_dim != 128)) return GRAT_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)s.q_group * s.share, lists = (int64_t)s.batch * s.kv_heads * s.n_groups;
+    const int64_t blocks = (int64_t)s.batch * s.kv_heads * s.n_blocks, D = seq->head_dim;
+    if ((int64_t)max_blocks * s.block > (1 << 18) || lists * max_blocks >= kMaxRows || blocks >= (1 << 24)) return GRAT_ERR_UNSUPPORTED;
+    if ((int64_t)s.batch * s.q_heads * s.n_q >= kMaxRows || lists * rows >= 2 * kMaxRows || lists * ((rows + 31) / 32) >= (1 << 23))
+        return GRAT_ERR_UNSUPPORTED;
+    p.max_blocks = max_blocks;
+    p.scale = scale;
+    p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    p.rows = (int32_t)rows;
+    plan.tile_rows = backward ? bwd_tile_rows(rows) : fwd_tile_rows(s, (int)D, rows);
+    p.row_tiles = (int32_t)((rows + plan.tile_rows - 1) / plan.tile_rows);
+    const int64_t items = lists * p.row_tiles, key_tiles = ((int64_t)max_blocks * (s.block / kUnit) + 1) / 2;
+    // A forward launch that leaves compute units idle (each takes two workgroups) has lists shared by several workgroups.
+    p.splits = backward || items >= 512 ? 1 : (int32_t)std::min<int64_t>(std::min<int64_t>((512 + items - 1) / items, key_tiles), 64);
+    p.items = (int32_t)(items * p.splits);
+    p.per_xcd = (p.items + 7) / 8;
+    p.fd_splits = make_fastdiv((uint32_t)p.splits);
+    p.fd_row_tiles = make_fastdiv((uint32_t)p.row_tiles);
+    p.fd_groups = make_fastdiv((uint32_t)s.n_groups);
+    p.fd_kv_heads = make_fastdiv((uint32_t)s.kv_heads);
+    p.fd_q_group = make_fastdiv((uint32_t)s.q_group);
+    p.fd_units = make_fastdiv((uint32_t)(s.block / kUnit));
+    if (p.splits > 1) {
+        const int64_t part_rows = (int64_t)p.items * plan.tile_rows;
+        p.part_o = (float*)(work + take(plan, part_rows * D * 4));
+        p.part_ml = (float*)(work + take(plan, part_rows * 8));
+    }
+    if (backward) {
+        GradParams& g = plan.g;
+        plan.tile_keys = bwd_tile_keys(s.block);
+        g.blocks = (int32_t)blocks;
+        g.words = (s.n_groups + 31) / 32;
+        g.fd_rows = make_fastdiv((uint32_t)rows);
+        g.fd_tiles = make_fastdiv((uint32_t)(s.block / plan.tile_keys));
+        // Parts of twice the rows that a block has on average: entries of all lists times the rows of a group, over all blocks.
+        const int64_t entries = lists * std::min(max_blocks, s.n_blocks), all_rows = entries * rows;
+        const int64_t part = std::max<int64_t>(1024, (2 * all_rows / blocks + 63) / 64 * 64);
+        g.part_rows = (int32_t)std::min<int64_t>(part, kMaxRows);
+        const int64_t most_parts = blocks + all_rows / g.part_rows, most_slots = 2 * (all_rows / g.part_rows) + 1;
+        if (most_parts * (s.block / plan.tile_keys) >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+        g.most_parts = (int32_t)most_parts;
+        g.delta = (float*)(work + take(plan, (int64_t)s.batch * s.q_heads * s.n_q * 4));
+        g.bits = (uint32_t*)(work + take(plan, blocks * g.words * 4));
+        g.counters = (int32_t*)(work + take(plan, 3 * 4));
+        g.groups = (int32_t*)(work + take(plan, entries * 4));
+        g.parts = (int4*)(work + take(plan, most_parts * 16));
+        g.part_slot = (int32_t*)(work + take(plan, most_parts * 4));
+        g.joins = (int2*)(work + take(plan, blocks * 8));
+        g.slots = (float*)(work + take(plan, most_slots * s.block * 2 * D * 4));
+    }
+    *out = plan;
     return GRAT_OK;
 }
 
@@ -194,4 +285,65 @@ extern "C" grat_status grat_select_blocks(const grat_sequence* seq, const float*
     if (top < 1 || first < 0 || local < 0 || (int64_t)first + local > top) return GRAT_ERR_BAD_DIMS;
     if (s.n_blocks > 32768 || top > 8192 || (int64_t)s.batch * s.kv_heads * s.n_groups >= (1 << 26)) return GRAT_ERR_UNSUPPORTED;
     return status_of(launch_select_blocks(s, d_scores, top, first, local, d_count, d_index, (hipStream_t)hip_stream));
+}
+
+extern "C" int64_t grat_selected_attention_work(const grat_sequence* seq, int32_t max_blocks, int32_t backward) {
+    SelPlan plan;
+    return make_plan(seq, 1.f, max_blocks, backward != 0, nullptr, &plan) == GRAT_OK ? plan.work : 0;
+}
+
+extern "C" grat_status grat_selected_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K, const grat_tensor* V,
+                                                   const grat_tensor* O, float* d_lse, float scale, const int32_t* d_count,
+                                                   const int32_t* d_index, int32_t max_blocks, void* d_work, void* hip_stream) {
+    if (!d_count || !d_index) return GRAT_ERR_NULL;
+    SelPlan plan;
+    grat_status st = make_plan(seq, scale, max_blocks, false, (uint8_t*)d_work, &plan);
+    for (const grat_tensor* t : {Q, K, V, O})
+        if (st == GRAT_OK) st = check_tensor(t, seq->dtype, seq->head_dim);
+    if (st != GRAT_OK) return st;
+    if (plan.work > 0 && !d_work) return GRAT_ERR_NULL;
+    if (!aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;
+    SelParams& p = plan.p;
+    p.Q = of(Q);
+    p.K = of(K);
+    p.V = of(V);
+    p.O = of(O);
+    p.lse = d_lse;
+    p.count = d_count;
+    p.index = d_index;
+    const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
+    const auto launch = f16 ? (wide ? launch_selected_fwd_f16_d128 : launch_selected_fwd_f16_d64)
+                            : (wide ? launch_selected_fwd_bf16_d128 : launch_selected_fwd_bf16_d64);
+    return status_of(launch(p, plan.tile_rows, (hipStream_t)hip_stream));
+}
+
+extern "C" grat_status grat_selected_attention_bwd(const grat_sequence* seq, const grat_tensor* dO, const grat_tensor* Q, const grat_tensor* K,
+                                                   const grat_tensor* V, const grat_tensor* O, const float* d_lse, const grat_tensor* dQ,
+                                                   const grat_tensor* dK, const grat_tensor* dV, float scale, const int32_t* d_count,
+                                                   const int32_t* d_index, int32_t max_blocks, void* d_work, void* hip_stream) {
+    if (!d_lse || !d_count || !d_index) return GRAT_ERR_NULL;
+    SelPlan plan;
+    grat_status st = make_plan(seq, scale, max_blocks, true, (uint8_t*)d_work, &plan);
+    for (const grat_tensor* t : {dO, Q, K, V, O, dQ, dK, dV})
+        if (st == GRAT_OK) st = check_tensor(t, seq->dtype, seq->head_dim);
+    if (st != GRAT_OK) return st;
+    if (!d_work) return GRAT_ERR_NULL;
+    if (!aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;
+    SelParams& p = plan.p;
+    p.Q = of(Q);
+    p.K = of(K);
+    p.V = of(V);
+    p.O = of(O);
+    p.lse = const_cast<float*>(d_lse);
+    p.count = d_count;
+    p.index = d_index;
+    GradParams& g = plan.g;
+    g.dO = of(dO);
+    g.dQ = of(dQ);
+    g.dK = of(dK);
+    g.dV = of(dV);
+    const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
+    const auto launch = f16 ? (wide ? launch_selected_bwd_f16_d128 : launch_selected_bwd_f16_d64)
+                            : (wide ? launch_selected_bwd_bf16_d128 : launch_selected_bwd_bf16_d64);
+    return status_of(launch(p, g, plan.tile_rows, plan.tile_keys, (hipStream_t)hip_stream));
 }

@@ -1,0 +1,257 @@
+// Attention over lists of key blocks, on the matrix cores of gfx950: what the forward and the gradient kernels share.
+//
+// The rows of a query group - q_group queries of each of the heads that share a K/V head, head by head - all walk the group's list, so every
+// (row tile, key unit) product is a dense one; only the newest keys and the end of a sequence need a mask.  The products are the
+// "transposed" ones of attn_mfma.h: with X the operand that streams through LDS and Y the one whose rows a wave owns (its 32
+// columns of the instruction, in registers as B fragments), T = X Y^T leaves lane (c = lane % 32, half = lane / 32) with the 16 streamed
+// rows 8 (r / 4) + 4 half + r % 4 of its own row c per 32, and that layout, packed to 16 bits, is the B operand of
+// Z^T += X'^T T if the contraction index is enumerated in the same order.  X'^T fragments come out of row-major tiles
+// through the LDS transpose read.
+#pragma once
+#include "mfma_elem.h"
+#include "sequence_common.h"
+
+namespace grat {
+
+struct SelParams {
+    SeqShape s;
+    SeqTensor Q, K, V, O;
+    float* lse;
+    const int32_t* count;
+    const int32_t* index;
+    int32_t max_blocks;
+    float scale, scale_log2;
+    int32_t rows, row_tiles;      // rows of a group (q_group * share), workgroups they are cut into
+    int32_t splits;               // workgroups that share a list
+    int32_t items, per_xcd;       // workgroups with work, those of an XCD
+    FastDiv fd_splits, fd_row_tiles, fd_groups, fd_kv_heads, fd_q_group, fd_units;   // fd_units: by block / 32
+    float* part_o;                // splits > 1: [items][rows of a tile][D], with part_ml [items][rows of a tile][2]
+    float* part_ml;
+};
+
+// What the gradient needs beside SelParams, in the caller's scratch memory.
+struct GradParams {
+    SeqTensor dO, dQ, dK, dV;
+    float* delta;          // [batch][q_heads][n_q]: D
+    uint32_t* bits;        // [blocks of all heads][words]
+    int32_t* counters;     // entries of `groups` in use, parts, slots in use
+    int32_t* groups;       // the groups that list a block, block after block
+    int4* parts;           // block (of all heads), first group's place in `groups`, rows from and to
+    int32_t* part_slot;    // of every part: its slot, -1: its block has no other
+    int2* joins;           // of every block: first slot, parts
+    float* slots;          // sums of a part: [key tile of the block][dK, dV][key][D]
+    int32_t words, blocks, most_parts, part_rows;
+    FastDiv fd_rows, fd_tiles;   // by rows of a group; by key tiles of a block
+};
+
+// Dispatch by element type and head_dim (sequence_fwd_*.hip, sequence_bwd_*.hip).
+hipError_t launch_selected_fwd_bf16_d128(const SelParams& p, int tile_rows, hipStream_t stream);
+hipError_t launch_selected_fwd_bf16_d64(const SelParams& p, int tile_rows, hipStream_t stream);
+hipError_t launch_selected_fwd_f16_d128(const SelParams& p, int tile_rows, hipStream_t stream);
+hipError_t launch_selected_fwd_f16_d64(const SelParams& p, int tile_rows, hipStream_t stream);
+hipError_t launch_selected_bwd_bf16_d128(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream);
+hipError_t launch_selected_bwd_bf16_d64(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream);
+hipError_t launch_selected_bwd_f16_d128(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream);
+hipError_t launch_selected_bwd_f16_d64(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream);
+void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stream);
+
+constexpr int kUnit = 32;         // keys that are looked up, masked and skipped together
+constexpr int kNoUnit = 0x7fffff00;   // start of a unit that only fills a tile: behind every key
+
+// ---- LDS tiles -------------------------------------------------------------------------------
+// Tiles are unpadded, rows of D / 8 chunks of 16 bytes; chunk c of a row lies at c ^ swizzle(row).  One swizzle serves both
+// reads.  ds_read_b128, lanes = consecutive rows (and the two halves of a wave neighbouring chunks): 8 rows x 2 chunks, and 16 rows,
+// fall on the 16 chunk positions of a 256-byte line.  The transpose read takes 4 rows x 4 neighbouring chunks at a time: rows e = 0 .. 3 go to
+// different groups of 4 positions.  head_dim 64 has two rows in a line.
+template <int D>
+__device__ __forceinline__ int tile_swizzle(int row) {
+    return D == 128 ? (row & 3) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1) : ((row >> 1) & 1) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1);
+}
+
+// Addresses of a wave's fragments inside a tile (see the two reads above).
+template <int D>
+struct TileReader {
+    static constexpr int kRow = 2 * D;
+    int row_base, row_x;              // b128: chunk (2 ks + half) ^ swizzle
+    int col_lo, col_hi;               // transpose read: rows 4 half + e and 8 more
+    int col_x;
+    __device__ __forceinline__ explicit TileReader(int lane) {
+        const int c = lane & 31, half = lane >> 5;
+        row_base = c * kRow;
+        row_x = tile_swizzle<D>(c) ^ half;
+        const int e = (lane & 15) >> 2, cq = lane & 3, dsel = (lane >> 4) & 1, row = 4 * half + e;
+        const int sw = tile_swizzle<D>(row);   // (8 rows on: the lowest bit as well)
+        col_x = sw >> 2;
+        const int low = (2 * dsel + (cq >> 1)) ^ (sw & 3);
+        col_lo = row * kRow + (low << 4) + 8 * (cq & 1);
+        col_hi = (row + 8) * kRow + ((low ^ 1) << 4) + 8 * (cq & 1);
+    }
+    // A operand, rows = tile rows 32 block + c, dims 16 ks + 8 half .. + 7
+    __device__ __forceinline__ frag8 rows(const uint8_t* tile, int block, int ks) const {
+        return *(LDS_PTR(const frag8))(tile + 32 * block * kRow + row_base + (((2 * ks) ^ row_x) << 4));
+    }
+    // A operand, rows = dims 32 db + c, contracted over 16 tile rows: 32 block + 16 s2 + accumulator order
+    __device__ __forceinline__ frag8 cols(const uint8_t* tile, int block, int s2, int db) const {
+        const uint8_t* src = tile + (32 * block + 16 * s2) * kRow + ((4 * (db ^ col_x)) << 4);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(src + col_lo));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(src + col_hi));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// 1 KiB, one 16-byte chunk a lane, from per-lane offsets against a uniform address straight into LDS (at dst + 16 lane).  Inline
+// assembly on purpose: a load into LDS that the compiler can see makes it wait for all of them ahead of the next LDS
+// read.  The caller waits (s_waitcnt) ahead of the barrier that publishes the tile.
+__device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t off, uint8_t* dst) {
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_PTR(uint8_t))dst);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+// ... from a 64-bit address of every lane's own
+__device__ __forceinline__ void load_lds(const uint8_t* src, uint8_t* dst) {
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_PTR(uint8_t))dst);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+}
+
+// This wave's direct loads have landed, everyone's have, and everyone is done with the buffers that are filled next.
+__device__ __forceinline__ void tile_barrier() {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+}
+
+// ---- the list of a group -----------------------------------------------------------------------
+// First keys of the units of a group's list that hold a key below `seen`, in list order, into LDS; returns their number (every
+// thread of the workgroup calls it, it ends with a barrier), followed by one kNoUnit.
+__device__ __forceinline__ int list_units(const SelParams& p, int64_t list, int seen, int32_t* s_units, int32_t* s_n) {
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x;
+        const int n = min(max(p.count[list], 0), p.max_blocks) * (int)p.fd_units.d;
+        const int32_t* const entries = p.index + list * p.max_blocks;
+        int have = 0;
+        for (int u0 = 0; u0 < n; u0 += 64) {
+            const int u = u0 + lane;
+            uint32_t entry, part;
+            fdivmod((uint32_t)min(u, n - 1), p.fd_units, entry, part);
+            const int block = entries[entry];
+            const int start = min(max(block, 0), p.s.n_blocks - 1) * p.s.block + (int)part * kUnit;
+            const bool in = u < n && block >= 0 && block < p.s.n_blocks && start < seen;
+            const uint64_t all = __ballot(in);
+            if (in) s_units[have + __popcll(all & ((1ull << lane) - 1ull))] = start;
+            have += __popcll(all);
+        }
+        if (lane == 0) {
+            s_units[have] = kNoUnit;
+            *s_n = have;
+        }
+    }
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(*s_n);
+}
+
+// Which part of the launch a workgroup is: consecutive items go to one XCD, whose L2 then holds the K and V of few heads.
+struct Item {
+    int item, b, h, g, tile, split;
+    __device__ __forceinline__ explicit Item(const SelParams& p) {
+        item = ((int)blockIdx.x & 7) * p.per_xcd + ((int)blockIdx.x >> 3);
+        uint32_t t, s, m, bh, gg, bb, hh;
+        fdivmod((uint32_t)item, p.fd_splits, t, s);
+        fdivmod(t, p.fd_row_tiles, t, m);
+        fdivmod(t, p.fd_groups, bh, gg);
+        fdivmod(bh, p.fd_kv_heads, bb, hh);
+        b = (int)bb; h = (int)hh; g = (int)gg; tile = (int)m; split = (int)s;
+    }
+    __device__ __forceinline__ bool idle(const SelParams& p) const { return (int)(blockIdx.x >> 3) >= p.per_xcd || item >= p.items; }
+    __device__ __forceinline__ int64_t list(const SelParams& p) const { return ((int64_t)b * p.s.kv_heads + h) * p.s.n_groups + g; }
+};
+
+// Row r of a group: its head and query row; not there where it is behind the group's or the tensor's last.
+struct GroupRow {
+    int head, query;
+    bool there;
+    __device__ __forceinline__ GroupRow(const SelParams& p, int h, int g, int r) {
+        uint32_t e, i;
+        fdivmod((uint32_t)min(r, p.rows - 1), p.fd_q_group, e, i);
+        head = h * p.s.share + (int)e;
+        query = g * p.s.q_group + (int)i;
+        there = r < p.rows && query < p.s.n_q;
+        query = min(query, p.s.n_q - 1);
+    }
+};
+
+__device__ __forceinline__ const uint8_t* row_address(const SeqTensor& t, int b, int head, int row) {
+    return t.data + 2 * (b * t.stride_b + head * t.stride_h + row * t.stride_n);
+}
+
+// ---- the walk over a list ------------------------------------------------------------------------
+// K and V tiles of 64 keys (two units), double buffered.  NW waves fetch 1-KiB pieces; a wave's pieces lie in one unit.
+template <int NW, int D>
+struct KeyLoader {
+    static constexpr int kPieces = 64 * D * 2 / 1024, LPW = kPieces / NW, kPerUnit = kPieces / 2, kRows = 1024 / (2 * D), kChunks = D / 8;
+    static_assert(LPW >= 1 && kPerUnit % LPW == 0, "a wave's pieces lie in one unit");
+    const uint8_t *K, *V;        // of the head
+    int64_t pitch_k, pitch_v;    // bytes
+    int last;                    // last key that may be read
+    int my_unit, row[LPW], col[LPW];
+    __device__ __forceinline__ KeyLoader(const SelParams& p, const Item& it, int seen, int wave, int lane) {
+        K = row_address(p.K, it.b, it.h, 0);
+        V = row_address(p.V, it.b, it.h, 0);
+        pitch_k = 2 * p.K.stride_n;
+        pitch_v = 2 * p.V.stride_n;
+        last = seen - 1;
+        my_unit = wave * LPW / kPerUnit;
+#pragma unroll
+        for (int k = 0; k < LPW; ++k) {
+            const int r = (wave * LPW + k) * kRows + lane / kChunks;   // in the tile
+            row[k] = r & (kUnit - 1);
+            col[k] = ((lane % kChunks) ^ tile_swizzle<D>(r)) << 4;
+        }
+    }
+    // Keys behind the last that some row sees are not read: the last one stands for them, and they are masked.
+    __device__ __forceinline__ void issue(int start, uint8_t* k_tile, uint8_t* v_tile, int wave) const {
+        const int first = min(start, last), left = last - first;
+        const uint8_t *kb = K + first * pitch_k, *vb = V + first * pitch_v;
+#pragma unroll
+        for (int k = 0; k < LPW; ++k) load_lds(kb, (uint32_t)min(row[k], left) * (uint32_t)pitch_k + col[k], k_tile + (wave * LPW + k) * 1024);
+#pragma unroll
+        for (int k = 0; k < LPW; ++k) load_lds(vb, (uint32_t)min(row[k], left) * (uint32_t)pitch_v + col[k], v_tile + (wave * LPW + k) * 1024);
+    }
+};
+
+// Rows from accumulators: a lane holds 4 consecutive dims at a time of its row (dims 32 db + 8 q + 4 half ..).  A wave turns its 32 rows
+// through 4 KiB of LDS, 64 dims at a time, so that a store instruction covers 8 rows of 128 bytes.  row_of(i): address of row i of
+// the 32, or null.  Only the wave itself uses `stage`.
+template <bool F16, int D, typename F>
+__device__ __forceinline__ void store_rows(uint8_t* stage, const f32x16* acc, float factor, int lane, F&& row_of) {
+    using E = Elem<F16>;
+#pragma unroll
+    for (int pass = 0; pass < D / 64; ++pass) {
+#pragma unroll
+        for (int dbp = 0; dbp < 2; ++dbp)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x16& o = acc[2 * pass + dbp];
+                uint2 v;
+                v.x = E::pack(o[4 * q] * factor, o[4 * q + 1] * factor);
+                v.y = E::pack(o[4 * q + 2] * factor, o[4 * q + 3] * factor);
+                *(uint2*)(stage + (lane & 31) * 128 + 8 * (lane >> 5) + (((4 * dbp + q) ^ (lane & 7)) << 4)) = v;
+            }
+        __builtin_amdgcn_wave_barrier();   // (compiler: keep the reads below the writes above)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 8 * i + (lane >> 3);
+            const uint4 x = *(const uint4*)(stage + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+            uint8_t* const to = row_of(r);
+            if (to) *(uint4*)(to + pass * 128 + (lane & 7) * 16) = x;
+        }
+        __builtin_amdgcn_wave_barrier();   // (... and the next pass's writes below these reads)
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void clear(f32x16 (&acc)[D / 32]) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
+}
+
+}  // namespace grat

@@ -1,0 +1,243 @@
+// Attention over lists of key blocks, forward: O = softmax(scale Q K^T) V over the listed keys that a row sees.
+//
+// One pass over the keys with a running reference maximum and sum (base 2, scale * log2 e folded into one FMA a score; the reference
+// is refreshed only where a block's sum leaves the safe range, as in attn_mfma.h).  A workgroup is RW waves of 32 rows of ONE group and
+// TEAMS such sets that take the two units of a tile each (few rows), and walks the list, or with `splits` a share of
+// it, in tiles of 64 keys through double-buffered LDS.
+#pragma once
+#include "sequence_attn.h"
+
+namespace grat {
+
+template <int RW, int TEAMS, bool F16, int D>
+__global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void selected_fwd_kernel(SelParams p) {
+    using E = Elem<F16>;
+    constexpr int NW = RW * TEAMS, kTile = 64 * D * 2;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][kTile];   // K, K, V, V
+    __shared__ int32_t s_n;
+    extern __shared__ int32_t s_units[];
+    const Item it(p);
+    if (it.idle(p)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int team = TEAMS == 1 ? 0 : wave / RW, row_wave = wave % RW;
+    const int half = lane >> 5;
+    const SeqShape& s = p.s;
+
+    // this lane's row
+    const int r = (it.tile * RW + row_wave) * 32 + (lane & 31);
+    const GroupRow row(p, it.h, it.g, r);
+    const uint8_t* const q_src = row_address(p.Q, it.b, row.head, row.query) + 16 * half;
+    frag8 qf[D / 16];
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const frag8*)(q_src + 32 * ks);
+    const int len = seq_len(s, it.b);
+    const int64_t pos = seq_pos(s, it.b, len);
+    const int seen = group_seen(s, len, pos, it.g);
+    const int limit = row.there ? row_seen(s, len, pos, row.query) : 0;   // keys below it are seen
+    int least = row.there ? limit : 0x7fffffff, most = limit;              // of the wave's rows
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) {
+        least = min(least, __shfl_xor(least, m));
+        most = max(most, __shfl_xor(most, m));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
+
+    const int all_units = seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
+    int u_first = 0, n_units = all_units;
+    if (p.splits > 1) {   // an even number of units a part
+        const int per = ((all_units + p.splits - 1) / p.splits + 1) & ~1;
+        u_first = min(it.split * per, all_units);
+        n_units = min(per, all_units - u_first);
+    }
+    const int n_tiles = (n_units + 1) / 2;
+
+    f32x16 oacc[D / 32];
+    clear<D>(oacc);
+    const float c = p.scale_log2;
+    float m_ref = -1e38f / fmaxf(c, 1.f);   // (finite, so that a block without a seen key weighs 0)
+    float l_run = 0.f;
+
+    const KeyLoader<NW, D> load(p, it, seen, wave, lane);
+    const TileReader<D> read(lane);
+    // (a list's last tile may lack its second unit; one of a part that ends inside the list does not)
+    auto unit_start = [&](int i) { return i < n_units ? __builtin_amdgcn_readfirstlane(s_units[u_first + i]) : kNoUnit; };
+
+    auto block = [&](const uint8_t* k_tile, const uint8_t* v_tile, int hb, int start) {
+        if (start >= most) return;   // nobody in this wave sees the unit
+        f32x16 S;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(k_tile, hb, ks), qf[ks], S);
+        if (start + kUnit > least) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (start + 8 * (i >> 2) + 4 * half + (i & 3) >= limit) S[i] = -INFINITY;
+        }
+        uint32_t pw[8];
+        float ls0 = 0.f, ls1 = 0.f;
+        auto weigh = [&]() {
+            const float mc = m_ref * c;
+            ls0 = ls1 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float a = __builtin_amdgcn_exp2f(fmaf(S[i], c, -mc)), b = __builtin_amdgcn_exp2f(fmaf(S[i + 1], c, -mc));
+                pw[i >> 1] = E::pack(a, b);
+                ls0 += a;
+                ls1 += b;
+            }
+        };
+        weigh();
+        if (__builtin_amdgcn_ballot_w64(!(ls0 + ls1 < E::kSumLimit)) != 0) {   // the rare path: the true maximum, and everything against it
+            float mx = S[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i]);
+            const float m_new = fmaxf(m_ref, max_across_halves(mx));
+            const float alpha = __builtin_amdgcn_exp2f((m_ref - m_new) * c);
+            m_ref = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
+            weigh();
+        }
+        l_run += ls0 + ls1;
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+            const frag8 w = __builtin_bit_cast(frag8, make_uint4(pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]));
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) oacc[db] = E::mfma(read.cols(v_tile, hb, s2, db), w, oacc[db]);
+        }
+    };
+
+    if (n_tiles > 0) {
+        load.issue(unit_start(load.my_unit), lds[0], lds[2], wave);
+        for (int t = 0; t < n_tiles; ++t) {
+            const int next = unit_start(2 * t + 2 + load.my_unit);
+            tile_barrier();
+            if (t + 1 < n_tiles) load.issue(next, lds[(t + 1) & 1], lds[2 + ((t + 1) & 1)], wave);
+            if constexpr (TEAMS == 1) {
+                block(lds[t & 1], lds[2 + (t & 1)], 0, unit_start(2 * t));
+                block(lds[t & 1], lds[2 + (t & 1)], 1, unit_start(2 * t + 1));
+            } else {
+                block(lds[t & 1], lds[2 + (t & 1)], team, unit_start(2 * t + team));
+            }
+        }
+    }
+    float l = sum_across_halves(l_run);
+
+    // ---- the second team's share, lane by lane -----------------------------------------------------
+    if constexpr (TEAMS == 2) {
+        __shared__ float s_m[RW][64], s_l[RW][64];
+        float* const part = (float*)&lds[0][0] + row_wave * 64 * (D / 2) + lane;   // [register][lane]
+        static_assert(RW * 64 * (D / 2) * 4 <= 2 * kTile && RW * 4096 <= 2 * kTile, "the partial results, and behind them the output");
+        __syncthreads();
+        if (team == 1) {
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[(db * 16 + i) * 64] = oacc[db][i];
+            s_m[row_wave][lane] = m_ref;
+            s_l[row_wave][lane] = l;
+        }
+        __syncthreads();
+        if (team == 1) return;
+        const float m2 = s_m[row_wave][lane], m = fmaxf(m_ref, m2);
+        const float f1 = __builtin_amdgcn_exp2f((m_ref - m) * c), f2 = __builtin_amdgcn_exp2f((m2 - m) * c);
+        m_ref = m;
+        l = l * f1 + s_l[row_wave][lane] * f2;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[db][i] = oacc[db][i] * f1 + part[(db * 16 + i) * 64] * f2;
+    } else {
+        __syncthreads();   // everyone is done with the tiles: the output is turned through them
+    }
+
+    if (p.splits > 1) {   // parts are joined by selected_join_kernel
+        const int64_t at = (int64_t)it.item * (RW * 32) + row_wave * 32 + (lane & 31);
+        float* const dst = p.part_o + at * D + 4 * half;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(float4*)(dst + 32 * db + 8 * q) = make_float4(oacc[db][4 * q], oacc[db][4 * q + 1], oacc[db][4 * q + 2], oacc[db][4 * q + 3]);
+        if (half == 0) *(float2*)(p.part_ml + 2 * at) = make_float2(m_ref, l);
+        return;
+    }
+    const float inv = l > 0.f ? 1.f / l : l;   // (a row that attends nothing: 0; NaN stays)
+    if (p.lse && half == 0 && row.there)
+        p.lse[((int64_t)it.b * s.q_heads + row.head) * s.n_q + row.query] = (m_ref * c + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+
+    uint8_t* const stage = &lds[0][0] + (TEAMS == 2 ? 2 * kTile : 0) + row_wave * 4096;   // (two teams: behind what team 0 still reads)
+    store_rows<F16, D>(stage, oacc, inv, lane, [&](int i) -> uint8_t* {
+        const GroupRow to(p, it.h, it.g, (it.tile * RW + row_wave) * 32 + i);
+        return to.there ? (uint8_t*)row_address(p.O, it.b, to.head, to.query) : nullptr;
+    });
+}
+
+// Joins the parts of a split list: a row's D / 4 lanes add up its parts, weighted by 2^(c (m - max m)).
+template <bool F16, int D>
+__global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int tile_rows, FastDiv fd_rows) {
+    constexpr int L = D / 4;
+    const SeqShape& s = p.s;
+    const int lane = threadIdx.x % L;
+    const int64_t n = (int64_t)s.batch * s.kv_heads * s.n_groups * p.rows;
+    const int64_t at = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    if (at >= n) return;
+    uint32_t list, r, bh, g, b, h;
+    fdivmod((uint32_t)at, fd_rows, list, r);
+    fdivmod(list, p.fd_groups, bh, g);
+    fdivmod(bh, p.fd_kv_heads, b, h);
+    const GroupRow row(p, (int)h, (int)g, (int)r);
+    if (!row.there) return;
+    const int64_t first = (((int64_t)list * p.row_tiles + r / tile_rows) * p.splits) * tile_rows + r % tile_rows;   // + split * tile_rows
+    const float2* const ml = (const float2*)p.part_ml + first;
+    const float4* const po = (const float4*)p.part_o + first * L + lane;
+    float m = -INFINITY;
+    for (int i = 0; i < p.splits; ++i) m = fmaxf(m, ml[(int64_t)i * tile_rows].x);
+    float l = 0.f, x = 0.f, y = 0.f, z = 0.f, w = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < p.splits; ++i) {
+        const float2 v = ml[(int64_t)i * tile_rows];
+        const float4 o = po[(int64_t)i * tile_rows * L];
+        const float f = __builtin_amdgcn_exp2f((v.x - m) * p.scale_log2);
+        l = fmaf(f, v.y, l);
+        x = fmaf(f, o.x, x);
+        y = fmaf(f, o.y, y);
+        z = fmaf(f, o.z, z);
+        w = fmaf(f, o.w, w);
+    }
+    const float inv = l > 0.f ? 1.f / l : l;
+    uint2 v;
+    v.x = Elem<F16>::pack(x * inv, y * inv);
+    v.y = Elem<F16>::pack(z * inv, w * inv);
+    *(uint2*)((uint8_t*)row_address(p.O, (int)b, row.head, row.query) + 8 * lane) = v;
+    if (p.lse && lane == 0)
+        p.lse[((int64_t)b * s.q_heads + row.head) * s.n_q + row.query] = (m * p.scale_log2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int RW, int TEAMS, bool F16, int D>
+inline void launch_fwd_tile(const SelParams& p, hipStream_t stream) {
+    const size_t dyn = sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1);
+    hipLaunchKernelGGL((selected_fwd_kernel<RW, TEAMS, F16, D>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p);
+}
+
+// tile_rows: 256, 128, 64 or 32
+template <bool F16, int D>
+inline hipError_t launch_fwd(const SelParams& p, int tile_rows, hipStream_t stream) {
+    if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D>(p, stream);
+    else if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D>(p, stream);
+    else if (tile_rows == 64) launch_fwd_tile<2, 2, F16, D>(p, stream);
+    else launch_fwd_tile<1, 2, F16, D>(p, stream);
+    if (p.splits > 1) {
+        const int64_t rows = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.rows;
+        hipLaunchKernelGGL((selected_join_kernel<F16, D>), dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, p, tile_rows,
+                           make_fastdiv((uint32_t)p.rows));
+    }
+    return hipGetLastError();
+}
+
+}  // namespace grat

@@ -28,7 +28,8 @@ EXPORTS = ("grat_block_list_shape", "grat_build_block_lists", "grat_validate_blo
            "grat_status_string", "grat_probe_mfma", "grat_probe_launch",
            # token sequences: sequence.py
            "grat_rotary_table", "grat_rotary", "grat_rotary_append", "grat_block_means", "grat_block_scores_work",
-           "grat_block_scores", "grat_select_blocks")
+           "grat_block_scores", "grat_select_blocks", "grat_selected_attention_work", "grat_selected_attention_fwd",
+           "grat_selected_attention_bwd")
 
 _i32, _i64, _f32, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
 _pi32 = ctypes.POINTER(ctypes.c_int32)

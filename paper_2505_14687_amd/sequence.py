@@ -1,4 +1,4 @@
-"""Token sequences: rotary positions, and lists of key blocks that a score selects (include/grat_sequence.h).
+"""Token sequences: rotary positions, and attention over key blocks that a score selects (include/grat_sequence.h).
 
 Marshalling only, like grat.py: every step runs in the library's kernels, on the current stream or the one that is given.
 Results and scratch memory are allocated for the stream that the call runs on.
@@ -8,6 +8,7 @@ Results and scratch memory are allocated for the stream that the call runs on.
     means = grat_block_means(K, block)
     scores = grat_block_scores(Q, means, scale, q_group, block, n_k=K.shape[2])
     count, index = grat_select_blocks(scores, top, first=1, local=2, n_q=Q.shape[2], n_k=K.shape[2], q_group=q_group, block=block)
+    O = grat_selected_attention_fwd(Q, K, V, scale, count, index, q_group, block)
 
 Q is [B, Hq, N, d], K and V are [B, Hkv, M, d] views (any strides with d contiguous); Hkv divides Hq.  k_len (int32 [B]): valid keys of
 each sequence; q_pos (int32 [B]): position of its first query, by default the queries are the newest tokens.
@@ -54,6 +55,9 @@ _SIGNATURES = {
     "grat_block_scores_work": (_i64, [_ps]),
     "grat_block_scores": (_i32, [_ps, _pt, _vp, _f32, _vp, _vp, _vp]),
     "grat_select_blocks": (_i32, [_ps, _vp, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "grat_selected_attention_work": (_i64, [_ps, _i32, _i32]),
+    "grat_selected_attention_fwd": (_i32, [_ps, _pt, _pt, _pt, _pt, _vp, _f32, _vp, _vp, _i32, _vp, _vp]),
+    "grat_selected_attention_bwd": (_i32, [_ps] + [_pt] * 5 + [_vp] + [_pt] * 3 + [_f32, _vp, _vp, _i32, _vp, _vp]),
 }
 _lib = None
 
@@ -287,3 +291,63 @@ def grat_select_blocks(scores, top: int, first: int, local: int, n_q: int, n_k: 
         index = torch.empty((B, Hkv, groups, int(top)), dtype=torch.int32, device=scores.device)
     _call("grat_select_blocks", ctypes.byref(seq), where, int(top), int(first), int(local), count.data_ptr(), index.data_ptr(), s)
     return count, index
+
+
+# ---- attention --------------------------------------------------------------------------------
+
+def _attention_args(Q, K, V, count, index, q_group, block, causal, k_len, q_pos):
+    _check("Q", Q)
+    _check("K", K, None, Q)
+    _positive(q_group=q_group, block=block)
+    B, Hq, N, d = Q.shape
+    Hkv, M = K.shape[1], K.shape[2]
+    _check("K", K, (B, Hkv, M, d), Q)
+    _check("V", V, K.shape, Q)
+    _shared(Hq, Hkv)
+    groups = _ceil(N, int(q_group))
+    if not isinstance(index, torch.Tensor) or index.dim() != 4 or index.shape[3] < 1:
+        raise ValueError(f"index must have shape [{B}, {Hkv}, {groups}, top]")
+    lists = (_flat("count", count, torch.int32, (B, Hkv, groups), Q.device),
+             _flat("index", index, torch.int32, (B, Hkv, groups, index.shape[3]), Q.device), int(index.shape[3]))
+    seq = _Sequence(DTYPES[Q.dtype], B, Hq, Hkv, d, N, M, int(q_group), int(block), int(bool(causal)),
+                    _ints("k_len", k_len, B, Q.device), _ints("q_pos", q_pos, B, Q.device))
+    return seq, lists
+
+
+def _work(seq: _Sequence, top: int, backward: int, device):
+    need = _library().grat_selected_attention_work(ctypes.byref(seq), top, backward)
+    return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+
+
+def grat_selected_attention_fwd(Q, K, V, scale: float, count, index, q_group: int, block: int, causal: bool = True, k_len=None,
+                                q_pos=None, return_lse: bool = False, out=None, stream=None):
+    """O = softmax(scale * Q K^T over the listed keys that a row sees) V; with return_lse also the rows' log-sum-exp, fp32 [B, Hq, N]."""
+    seq, lists = _attention_args(Q, K, V, count, index, q_group, block, causal, k_len, q_pos)
+    context, s = _on(stream, Q.device)
+    with context:
+        work = _work(seq, lists[2], 0, Q.device)
+        O = torch.empty_like(Q) if out is None else out
+        lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if return_lse else None
+    _check("out", O, Q.shape, Q)
+    _call("grat_selected_attention_fwd", ctypes.byref(seq), *(ctypes.byref(_tensor(t)) for t in (Q, K, V, O)),
+          lse.data_ptr() if return_lse else None, float(scale), *lists, work.data_ptr() if work is not None else None, s)
+    return (O, lse) if return_lse else O
+
+
+def grat_selected_attention_bwd(dO, Q, K, V, O, lse, scale: float, count, index, q_group: int, block: int, causal: bool = True,
+                                k_len=None, q_pos=None, out=None, stream=None):
+    """(dQ, dK, dV) of grat_selected_attention_fwd for dO; O and lse as it returned them.  out: three tensors to write to."""
+    seq, lists = _attention_args(Q, K, V, count, index, q_group, block, causal, k_len, q_pos)
+    _check("dO", dO, Q.shape, Q)
+    _check("O", O, Q.shape, Q)
+    where = _flat("lse", lse, torch.float32, Q.shape[:3], Q.device)
+    context, s = _on(stream, Q.device)
+    with context:
+        work = _work(seq, lists[2], 1, Q.device)
+        grads = (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)) if out is None else tuple(out)
+    for name, t, like in zip(("out[0]", "out[1]", "out[2]"), grads, (Q, K, V)):
+        _check(name, t, like.shape, Q)
+    dQ, dK, dV = grads
+    _call("grat_selected_attention_bwd", ctypes.byref(seq), *(ctypes.byref(_tensor(t)) for t in (dO, Q, K, V, O)), where,
+          *(ctypes.byref(_tensor(t)) for t in (dQ, dK, dV)), float(scale), *lists, work.data_ptr() if work is not None else None, s)
+    return dQ, dK, dV

@@ -1,0 +1,310 @@
+"""Attention over lists of key blocks and its gradient vs the float64 oracle.
+
+Bounds, element by element, with u the unit roundoff of the element type, e = 2^-24, n the keys of a row and
+   w = (d + 8) e scale max|q||k| + n e      the relative error of a weight: fp32 dot products of d terms, fp32 sums of n weights
+   A = P |V|                                what weights of relative error 1 could change O by
+O:   u A (weights rounded) + u |O| (result rounded) + 4 w A;            lse: 4 w + 4 e (1 + |lse|)
+dP = dO V^T is off by (d + 1) e |dO||V|^T, D = sum dO O by |dO| . (the bound of O) + d e |dO| . |O|, so with E = P (both of these)
+dS:  u |dS| (rounded) + 4 w |dS| + E, and dQ, dK the products of that with |K|, |Q|, plus n e |dS||K| and the result's rounding
+dV:  P^T |dO| (u + 4 w + n e) + u |dV|
+(w counts twice in every quotient of a weight and a sum, hence 4.)"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_14687_amd as grat
+from oracle import sequence_oracle as orc
+from sequence_util import ROUND, TINY, f64, ints, nan_like, normal
+
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
+
+
+def random_lists(gen, B, Hkv, groups, blocks, top, full=False, junk=False):
+    """Distinct blocks in any order; counts from 0; behind the count, and with junk also among the entries, what has to be ignored."""
+    index = np.full((B, Hkv, groups, top), -1, np.int32)
+    count = np.zeros((B, Hkv, groups), np.int32)
+    for at in np.ndindex(B, Hkv, groups):
+        n = min(top, blocks) if full else int(gen.integers(0, min(top, blocks) + 1))
+        index[at][:n] = gen.permutation(blocks)[:n]
+        count[at] = n
+        if junk and n > 2:
+            index[at][int(gen.integers(0, n))] = int(gen.choice([-1, -7, blocks, 2 ** 31 - 1]))
+        if junk and n < top:
+            index[at][n:] = int(gen.integers(0, blocks))
+    return count, index
+
+
+def bounds(Q, K, V, scale, mask, dtype, dO=None):
+    """Expected results and their bounds (see above); arrays in float64."""
+    u, tiny = ROUND[dtype], TINY[dtype]
+    O, lse, P = orc.attention(Q, K, V, scale, mask)
+    B, Hq, N, d = Q.shape
+    Hkv = K.shape[1]
+    share = Hq // Hkv
+    keys = mask.any(2)[..., None]
+    K, V = np.where(keys, K, 0.0), np.where(keys, V, 0.0)
+    n = max(1, int(mask.sum(-1).max()))
+    bO, blse = np.zeros_like(O), np.zeros_like(lse)
+    grads = [np.zeros_like(Q), np.zeros_like(K), np.zeros_like(V)]
+    bG = [np.zeros_like(Q), np.zeros_like(K), np.zeros_like(V)]
+    for b in range(B):
+        for h in range(Hq):
+            k, v, q, p = K[b, h // share], V[b, h // share], Q[b, h], P[b, h]
+            w = (d + 8) * EPS * scale * (np.abs(q) @ np.abs(k).T).max(initial=0) + n * EPS
+            bO[b, h] = u * (p @ np.abs(v)) + u * np.abs(O[b, h]) + 4 * w * (p @ np.abs(v)) + tiny
+            blse[b, h] = 4 * w + 4 * EPS * (1 + np.where(np.isfinite(lse[b, h]), np.abs(lse[b, h]), 0))
+            if dO is None:
+                continue
+            do, g = dO[b, h], h // share
+            dp = do @ v.T
+            ds = p * (dp - (do * O[b, h]).sum(1, keepdims=True))
+            E = p * ((d + 1) * EPS * (np.abs(do) @ np.abs(v).T) + (np.abs(do) * (bO[b, h] + d * EPS * np.abs(O[b, h]))).sum(1, keepdims=True))
+            bs = (u + 4 * w) * np.abs(ds) + E + tiny
+            grads[0][b, h] = scale * (ds @ k)
+            bG[0][b, h] = scale * ((bs + n * EPS * np.abs(ds)) @ np.abs(k))
+            grads[1][b, g] += scale * (ds.T @ q)
+            bG[1][b, g] += scale * ((bs + N * share * EPS * np.abs(ds)).T @ np.abs(q))
+            grads[2][b, g] += p.T @ do
+            bG[2][b, g] += ((u + 4 * w + N * share * EPS) * p.T + tiny) @ np.abs(do)
+    bG = [x + u * np.abs(g) + tiny for x, g in zip(bG, grads)]
+    return O, lse, bO, blse, grads, bG
+
+
+def within(got, want, lim, what):
+    assert np.isfinite(got).all(), f"{what}: not finite"
+    over = np.abs(got - want) - lim
+    assert (over <= 0).all(), f"{what}: over the bound by {over.max():.3e} at {np.unravel_index(over.argmax(), over.shape)}"
+
+
+# B, Hq, Hkv, N, M, q_group, block, top, k_len, q_pos, causal
+TOKENS = [
+    (1, 4, 4, 1, 1, 1, 32, 1, None, None, True),                       # one key
+    (3, 8, 2, 1, 700, 1, 64, 6, [700, 1, 65], None, True),             # serving, lists shared by several workgroups
+    (2, 16, 1, 1, 3000, 1, 128, 9, [2999, 130], None, True),           # 16 heads to a K/V head
+    (2, 40, 1, 1, 900, 1, 32, 12, [900, 0], None, True),               # more heads than a row tile; an empty cache
+    (1, 6, 2, 5, 400, 1, 64, 4, None, None, False),                    # a few tokens with a list each
+]
+GROUPS = [
+    (2, 4, 4, 100, 100, 32, 32, 4, None, None, True),                  # 32 rows a group, ends inside one
+    (2, 4, 2, 130, 130, 32, 64, 2, [130, 70], None, True),             # 64 rows; rows ahead of the first key
+    (1, 6, 2, 300, 300, 48, 64, 5, None, None, True),                  # 144 rows: two row tiles, the second mostly empty
+    (1, 3, 3, 257, 500, 100, 96, 5, None, None, True),                 # blocks of three units, a chunk behind a prefix
+    (1, 2, 1, 200, 333, 200, 256, 2, None, None, False),               # one group, large blocks, no mask but the end
+    (2, 2, 2, 150, 150, 1, 32, 3, None, None, True),                   # a list of its own for every query
+    (2, 4, 1, 70, 200, 16, 64, 4, [200, 33], [-20, 300], True),        # positions that are given: before the first key, behind the last
+    (1, 16, 1, 33, 1000, 1, 128, 8, [999], None, True),
+]
+
+
+def tensors(shape, dtype, d, where, seed, gain=1.0):
+    B, Hq, Hkv, N, M = shape[:5]
+    return (normal((B, Hq, N, d), dtype, seed, where, gain), normal((B, Hkv, M, d), dtype, seed + 1, where),
+            normal((B, Hkv, M, d), dtype, seed + 2, where))
+
+
+def spoil(K, V, k_len):
+    """What is not valid has to stay unread."""
+    if k_len is not None:
+        for b, n in enumerate(k_len):
+            K[b, :, n:] = float("nan")
+            V[b, :, n:] = float("inf")
+
+
+def run_case(shape, dtype, d, where="heads", gain=1.0, junk=False, backward=False, seed=31, full=False, pick=None):
+    B, Hq, Hkv, N, M, q_group, block, top, k_len, q_pos, causal = shape
+    gen = np.random.default_rng(seed)
+    groups, blocks = -(-N // q_group), -(-M // block)
+    count, index = random_lists(gen, B, Hkv, groups, blocks, top, full=full, junk=junk)
+    Q, K, V = tensors(shape, dtype, d, where, seed, gain)
+    spoil(K, V, k_len)
+    scale = 1.0 / math.sqrt(d)
+    args = dict(q_group=q_group, block=block, causal=causal, k_len=ints(k_len), q_pos=ints(q_pos))
+    lists = torch.from_numpy(count).cuda(), torch.from_numpy(index).cuda()
+    out = nan_like(Q)
+    O, lse = grat.grat_selected_attention_fwd(Q, K, V, scale, *lists, return_lse=True, out=out, **args)
+    assert O is out
+    again = grat.grat_selected_attention_fwd(Q, K, V, scale, *lists, **args)
+    assert torch.equal(O, again)
+    dO = normal((B, Hq, N, d), dtype, seed + 5, where) if backward else None
+    if backward:
+        grads = tuple(nan_like(t) for t in (Q, K, V))
+        grat.grat_selected_attention_bwd(dO, Q, K, V, O, lse, scale, *lists, out=grads, **args)
+        twice = grat.grat_selected_attention_bwd(dO, Q, K, V, O, lse, scale, *lists, **args)
+        assert all(torch.equal(x, y) for x, y in zip(grads, twice))
+    share = Hq // Hkv
+    for b, h in pick or [(slice(0, B), slice(0, Hkv))]:
+        b, h = (slice(b, b + 1) if isinstance(b, int) else b), (slice(h, h + 1) if isinstance(h, int) else h)
+        hq = slice(h.start * share, h.stop * share)
+        mask = orc.attended(count[b, h], index[b, h], N, M, q_group, block, causal, k_len and k_len[b], q_pos and q_pos[b])
+        with np.errstate(invalid="ignore"):
+            want = bounds(f64(Q[b, hq]), f64(K[b, h]), f64(V[b, h]), scale, mask, dtype, f64(dO[b, hq]) if backward else None)
+        Ow, lw, bO, bl, gw, bG = want
+        within(f64(O[b, hq]), Ow, bO, "O")
+        got = f64(lse[b, hq])
+        assert np.array_equal(np.isneginf(got), np.isneginf(lw)), "rows that attend nothing"
+        fin = np.isfinite(lw)
+        within(got[fin], lw[fin], bl[fin], "lse")
+        if backward:
+            for name, t, w, lim, head in zip(("dQ", "dK", "dV"), grads, gw, bG, (hq, h, h)):
+                within(f64(t[b, head]), w, lim, name)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("bf16", 64), ("f16", 128)])
+@pytest.mark.parametrize("shape", TOKENS + GROUPS)
+def test_forward(dtype, d, shape):
+    run_case(shape, dtype, d, where="tokens" if d == 128 else "wide", junk=True)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("bf16", 64), ("f16", 128)])
+@pytest.mark.parametrize("shape", TOKENS[:3] + GROUPS)
+def test_gradient(dtype, d, shape):
+    run_case(shape, dtype, d, where="wide" if d == 128 else "tokens", junk=True, backward=True, seed=41)
+
+
+@pytest.mark.parametrize("dtype,gain", [("bf16", 16.0), ("f16", 8.0)])
+@pytest.mark.parametrize("shape", [TOKENS[1], GROUPS[1], GROUPS[2]])
+def test_peaked_weights(dtype, gain, shape):
+    """Scores far apart: the reference maximum is refreshed on the way."""
+    run_case(shape, dtype, 128, gain=gain, backward=True, seed=51, full=True)
+
+
+@pytest.mark.parametrize("shape,pick", [
+    ((4, 32, 8, 512, 512, 64, 64, 5, None, None, True), [(0, 0), (3, 7)]),              # 256-row workgroups
+    ((1, 8, 2, 1000, 1000, 125, 128, 4, None, None, True), [(0, 1)]),                   # 500 rows a group, 128-key tiles
+    ((1, 2, 1, 2100, 2100, 1, 32, 4, None, None, True), None),                          # lists of many groups, turned round
+])
+def test_larger(shape, pick):
+    run_case(shape, "bf16", 128, backward=True, seed=61, full=True, pick=pick)
+
+
+def test_a_block_that_every_group_lists_is_cut_into_parts():
+    B, Hq, Hkv, N, M, q_group, block, top = 1, 4, 1, 1500, 1500, 16, 64, 3
+    groups, blocks = -(-N // q_group), -(-M // block)
+    gen = np.random.default_rng(71)
+    index = np.stack([np.concatenate([[0], 1 + gen.permutation(blocks - 1)[:top - 1]]) for _ in range(groups)])[None, None].astype(np.int32)
+    count = np.full((1, 1, groups), top, np.int32)
+    Q, K, V = tensors((B, Hq, Hkv, N, M), "bf16", 128, "heads", 72)
+    dO, scale = normal((B, Hq, N, 128), "bf16", 75), 1 / math.sqrt(128)
+    args = dict(q_group=q_group, block=block, causal=False)
+    lists = torch.from_numpy(count).cuda(), torch.from_numpy(index).cuda()
+    O, lse = grat.grat_selected_attention_fwd(Q, K, V, scale, *lists, return_lse=True, **args)
+    grads = grat.grat_selected_attention_bwd(dO, Q, K, V, O, lse, scale, *lists, **args)
+    mask = orc.attended(count, index, N, M, q_group, block, False)
+    _, _, _, _, want, lim = bounds(*(f64(t) for t in (Q, K, V)), scale, mask, "bf16", f64(dO))
+    for name, g, w, b in zip(("dQ", "dK", "dV"), grads, want, lim):
+        within(f64(g), w, b, name)
+
+
+def test_gradient_against_differences():
+    """Directional differences of sum(O dO) in the kernels' own forward pass, in half.
+
+    A step of 2^-5 along a sign vector: O changes by about 2^-5 of its size, rounded to half (2^-11): the difference of two sums over
+    N d = 40 * 64 outputs scatters by about sqrt(2 * 2560) 2^-11 |dO| |O| / 2^-4, and the third derivative adds the step's square."""
+    shape = (1, 2, 1, 40, 90, 8, 32, 2, None, None, True)
+    B, Hq, Hkv, N, M, q_group, block, top = shape[:8]
+    gen = np.random.default_rng(81)
+    count, index = random_lists(gen, B, Hkv, 5, 3, top, full=True)
+    Q, K, V = tensors(shape, "f16", 64, "heads", 82)
+    dO = normal((B, Hq, N, 64), "f16", 85)
+    args = dict(q_group=q_group, block=block, causal=True)
+    lists = torch.from_numpy(count).cuda(), torch.from_numpy(index).cuda()
+
+    def value(q, k, v):
+        return float((grat.grat_selected_attention_fwd(q, k, v, 0.125, *lists, **args).double() * dO.double()).sum())
+
+    O, lse = grat.grat_selected_attention_fwd(Q, K, V, 0.125, *lists, return_lse=True, **args)
+    grads = grat.grat_selected_attention_bwd(dO, Q, K, V, O, lse, 0.125, *lists, **args)
+    step = 2.0 ** -5
+    for i, (x, g) in enumerate(zip((Q, K, V), grads)):
+        x = torch.round(x * 256) / 256          # (so that x + step is exact in half)
+        base = [Q, K, V]
+        base[i] = x
+        O2, lse2 = grat.grat_selected_attention_fwd(*base, 0.125, *lists, return_lse=True, **args)
+        g = grat.grat_selected_attention_bwd(dO, *base, O2, lse2, 0.125, *lists, **args)[i]
+        sign = torch.from_numpy(gen.choice([-1.0, 1.0], tuple(x.shape))).to(x)
+        lo, hi = list(base), list(base)
+        lo[i], hi[i] = x - step * sign, x + step * sign
+        slope = (value(*hi) - value(*lo)) / (2 * step)
+        want = float((g.double() * sign.double()).sum())
+        size = float(g.double().norm())
+        noise = math.sqrt(2 * O.numel()) * 2.0 ** -11 * float(O.double().square().mean().sqrt()) / (2 * step)
+        assert abs(slope - want) <= 6 * noise + step * size, (i, slope, want, noise, size)
+
+
+def test_offsets_beyond_32_bits():
+    """A cache whose rows lie beyond 4 GiB (and whose element offsets pass 2^31)."""
+    M, d, block = (1 << 24) + 100, 128, 64
+    K = torch.empty((1, 1, M, d), dtype=torch.bfloat16, device="cuda")
+    V = torch.empty((1, 1, M, d), dtype=torch.bfloat16, device="cuda")
+    blocks = -(-M // block)
+    chosen = [0, 5, blocks // 2, blocks - 2, blocks - 1]
+    gen = torch.Generator(device="cuda").manual_seed(91)
+    rows = torch.cat([torch.arange(j * block, min(M, (j + 1) * block)) for j in chosen]).cuda()
+    for t in (K, V):
+        t[0, 0, rows] = torch.randn((len(rows), d), generator=gen, device="cuda").bfloat16()
+    Q = normal((1, 4, 1, d), "bf16", 92)
+    count = torch.tensor([[[len(chosen)]]], dtype=torch.int32, device="cuda")
+    index = torch.tensor([[[chosen]]], dtype=torch.int32, device="cuda")
+    O = grat.grat_selected_attention_fwd(Q, K, V, 0.09, count, index, q_group=1, block=block)
+    mask = np.ones((1, 1, 1, len(rows)), dtype=bool)
+    want, _, bO, _, _, _ = bounds(f64(Q), f64(K[:, :, rows]), f64(V[:, :, rows]), 0.09, mask, "bf16")
+    within(f64(O), want, bO, "O")
+    means = grat.grat_block_means(K[:, :, -200:], 32)   # (a view that begins beyond 4 GiB)
+    assert means.shape == (1, 1, 7, 128)
+
+
+def test_scores_lists_and_attention_together():
+    """The steps in a row, causal, against the oracle on the lists that came out."""
+    B, Hq, Hkv, N, d, q_group, block = 1, 8, 2, 700, 128, 64, 64
+    Q, K, V = tensors((B, Hq, Hkv, N, N), "bf16", d, "tokens", 95)
+    table = grat.grat_rotary_table(N, [d // 2])
+    Q, K = grat.grat_rotary(Q, K, table)
+    scale = 1 / math.sqrt(d)
+    means = grat.grat_block_means(K, block)
+    scores = grat.grat_block_scores(Q, means, scale, q_group, block, N)
+    count, index = grat.grat_select_blocks(scores, 4, 1, 2, n_q=N, n_k=N, q_group=q_group, block=block)
+    want = orc.select_blocks(f64(scores), 4, 1, 2, N, N, q_group, block, True)
+    for h in range(Hkv):
+        for g in range(-(-N // q_group)):
+            assert index[0, h, g, :count[0, h, g]].tolist() == want[0][h][g]
+    O = grat.grat_selected_attention_fwd(Q, K, V, scale, count, index, q_group, block)
+    mask = orc.attended(count.cpu().numpy(), index.cpu().numpy(), N, N, q_group, block, True)
+    assert mask.any(-1).all()               # every row sees itself at least
+    Ow, _, bO, _, _, _ = bounds(f64(Q), f64(K), f64(V), scale, mask, "bf16")
+    within(f64(O), Ow, bO, "O")
+
+
+def test_streams_and_graphs():
+    """A side stream, results allocated for it; a graph of a training step, replayed with new data between other work."""
+    shape = (1, 4, 2, 200, 200, 32, 64, 3, None, None, True)
+    B, Hq, Hkv, N, M, q_group, block, top = shape[:8]
+    count, index = random_lists(np.random.default_rng(97), B, Hkv, 7, 4, top)
+    lists = torch.from_numpy(count).cuda(), torch.from_numpy(index).cuda()
+    args = dict(q_group=q_group, block=block)
+    sets = [tensors(shape, "bf16", 128, "heads", 100 + 10 * i) + (normal((B, Hq, N, 128), "bf16", 105 + 10 * i),) for i in range(3)]
+
+    def step(Q, K, V, dO, stream=None):
+        O, lse = grat.grat_selected_attention_fwd(Q, K, V, 0.1, *lists, return_lse=True, stream=stream, **args)
+        return (O, *grat.grat_selected_attention_bwd(dO, Q, K, V, O, lse, 0.1, *lists, stream=stream, **args))
+
+    eager = [step(*t) for t in sets]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = step(*sets[0], stream=side)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, eager[0]))
+    static = [t.clone() for t in sets[0]]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(*static)
+    for i in (0, 1, 2, 1):
+        for t, x in zip(static, sets[i]):
+            t.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(out, eager[i])), f"replay with data {i}"
+        step(*sets[(i + 1) % 3])
