@@ -159,20 +159,23 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
         g.words = (s.n_groups + 31) / 32;
         g.fd_rows = make_fastdiv((uint32_t)rows);
         g.fd_tiles = make_fastdiv((uint32_t)(s.block / plan.tile_keys));
-        // Parts of twice the rows that a block has on average: entries of all lists times the rows of a group, over all blocks.
+        // Parts of the rows that a block has on average: entries of all lists times the rows of a group, over all blocks.
         const int64_t entries = lists * std::min(max_blocks, s.n_blocks), all_rows = entries * rows;
-        const int64_t part = std::max<int64_t>(1024, (2 * all_rows / blocks + 63) / 64 * 64);
+        const int64_t part = std::max<int64_t>(1024, (all_rows / blocks + 63) / 64 * 64);
         g.part_rows = (int32_t)std::min<int64_t>(part, kMaxRows);
         const int64_t most_parts = blocks + all_rows / g.part_rows, most_slots = 2 * (all_rows / g.part_rows) + 1;
         if (most_parts * (s.block / plan.tile_keys) >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
         g.most_parts = (int32_t)most_parts;
-        g.delta = (float*)(work + take(plan, (int64_t)s.batch * s.q_heads * s.n_q * 4));
+        g.most_joins = (int32_t)std::min<int64_t>(blocks, most_slots / 2);
+        g.stats = (int64_t)s.batch * s.q_heads * s.n_q;
+        g.delta = (float*)(work + take(plan, (g.stats + 1) * 4));
+        g.lse2 = (float*)(work + take(plan, (g.stats + 1) * 4));
         g.bits = (uint32_t*)(work + take(plan, blocks * g.words * 4));
-        g.counters = (int32_t*)(work + take(plan, 3 * 4));
+        g.counters = (int32_t*)(work + take(plan, 4 * 4));
         g.groups = (int32_t*)(work + take(plan, entries * 4));
         g.parts = (int4*)(work + take(plan, most_parts * 16));
         g.part_slot = (int32_t*)(work + take(plan, most_parts * 4));
-        g.joins = (int2*)(work + take(plan, blocks * 8));
+        g.joins = (int4*)(work + take(plan, g.most_joins * 16));
         g.slots = (float*)(work + take(plan, most_slots * s.block * 2 * D * 4));
     }
     *out = plan;

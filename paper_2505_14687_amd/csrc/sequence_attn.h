@@ -32,15 +32,17 @@ struct SelParams {
 // What the gradient needs beside SelParams, in the caller's scratch memory.
 struct GradParams {
     SeqTensor dO, dQ, dK, dV;
-    float* delta;          // [batch][q_heads][n_q]: D
+    float* delta;          // [batch][q_heads][n_q], and one more: D
+    float* lse2;           // as many: lse in base 2
+    int64_t stats;         // batch * q_heads * n_q
     uint32_t* bits;        // [blocks of all heads][words]
-    int32_t* counters;     // entries of `groups` in use, parts, slots in use
+    int32_t* counters;     // entries of `groups` in use, parts, slots in use, blocks of more than one part
     int32_t* groups;       // the groups that list a block, block after block
     int4* parts;           // block (of all heads), first group's place in `groups`, rows from and to
     int32_t* part_slot;    // of every part: its slot, -1: its block has no other
-    int2* joins;           // of every block: first slot, parts
+    int4* joins;           // blocks of more than one part: block, first slot, parts
     float* slots;          // sums of a part: [key tile of the block][dK, dV][key][D]
-    int32_t words, blocks, most_parts, part_rows;
+    int32_t words, blocks, most_parts, most_joins, part_rows;
     FastDiv fd_rows, fd_tiles;   // by rows of a group; by key tiles of a block
 };
 
@@ -68,33 +70,40 @@ __device__ __forceinline__ int tile_swizzle(int row) {
     return D == 128 ? (row & 3) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1) : ((row >> 1) & 1) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1);
 }
 
-// Addresses of a wave's fragments inside a tile (see the two reads above).
+// Where a wave's fragments lie in the current one of two neighbouring tiles.  One register a kind of read: what differs between reads is XORed
+// in (chunks) or a constant offset (tiles, rows).  (Left to itself the compiler keeps an address for every chunk, 16 registers.)
 template <int D>
 struct TileReader {
-    static constexpr int kRow = 2 * D;
-    int row_base, row_x;              // b128: chunk (2 ks + half) ^ swizzle
-    int col_lo, col_hi;               // transpose read: rows 4 half + e and 8 more
-    int col_x;
-    __device__ __forceinline__ explicit TileReader(int lane) {
+    static constexpr int kRow = 2 * D, kTile = 64 * kRow;
+    uint32_t row_at, col_at;
+    // `tiles`: aligned to two tiles; block 0 of this wave is block `first` of a tile
+    __device__ __forceinline__ TileReader(int lane, const uint8_t* tiles, int first) {
+        const uint32_t base = (uint32_t)(uintptr_t)(LDS_PTR(const uint8_t))tiles + 32 * first * kRow;
         const int c = lane & 31, half = lane >> 5;
-        row_base = c * kRow;
-        row_x = tile_swizzle<D>(c) ^ half;
+        row_at = base + c * kRow + ((tile_swizzle<D>(c) ^ half) << 4);
         const int e = (lane & 15) >> 2, cq = lane & 3, dsel = (lane >> 4) & 1, row = 4 * half + e;
-        const int sw = tile_swizzle<D>(row);   // (8 rows on: the lowest bit as well)
-        col_x = sw >> 2;
-        const int low = (2 * dsel + (cq >> 1)) ^ (sw & 3);
-        col_lo = row * kRow + (low << 4) + 8 * (cq & 1);
-        col_hi = (row + 8) * kRow + ((low ^ 1) << 4) + 8 * (cq & 1);
+        col_at = base + row * kRow + (((2 * dsel + (cq >> 1)) ^ tile_swizzle<D>(row)) << 4) + 8 * (cq & 1);
     }
-    // A operand, rows = tile rows 32 block + c, dims 16 ks + 8 half .. + 7
-    __device__ __forceinline__ frag8 rows(const uint8_t* tile, int block, int ks) const {
-        return *(LDS_PTR(const frag8))(tile + 32 * block * kRow + row_base + (((2 * ks) ^ row_x) << 4));
+    __device__ __forceinline__ void flip() {   // to the other tile
+        row_at ^= kTile;
+        col_at ^= kTile;
+        asm volatile("" : "+v"(row_at), "+v"(col_at));
     }
-    // A operand, rows = dims 32 db + c, contracted over 16 tile rows: 32 block + 16 s2 + accumulator order
-    __device__ __forceinline__ frag8 cols(const uint8_t* tile, int block, int s2, int db) const {
-        const uint8_t* src = tile + (32 * block + 16 * s2) * kRow + ((4 * (db ^ col_x)) << 4);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(src + col_lo));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(src + col_hi));
+    __device__ __forceinline__ void other_block() {   // of the same tile
+        row_at ^= 32 * kRow;
+        col_at ^= 32 * kRow;
+        asm volatile("" : "+v"(row_at), "+v"(col_at));
+    }
+    // A operand, rows = tile rows 32 block + c, dims 16 ks + 8 half .. + 7.  pair: tiles 2 pair and 2 pair + 1
+    __device__ __forceinline__ frag8 rows(int pair, int block, int ks) const {
+        return *(LDS_PTR(const frag8))(uintptr_t)((row_at ^ (ks << 5)) + pair * 2 * kTile + 32 * block * kRow);
+    }
+    // A operand, rows = dims 32 db + c, contracted over 16 tile rows: 32 block + 16 s2 + accumulator order.  (8 rows on the swizzle
+    // differs in its lowest bit.)
+    __device__ __forceinline__ frag8 cols(int pair, int block, int s2, int db) const {
+        const uint32_t at = col_at ^ (db << 6), off = pair * 2 * kTile + (32 * block + 16 * s2) * kRow;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(at + off));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)((at ^ 16) + off + 8 * kRow));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
 };
@@ -110,6 +119,12 @@ __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t off, uint
 __device__ __forceinline__ void load_lds(const uint8_t* src, uint8_t* dst) {
     const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_PTR(uint8_t))dst);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+}
+
+// ... 4 bytes a lane, at dst + 4 lane
+__device__ __forceinline__ void load_lds_word(const uint8_t* src, uint8_t* dst) {
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(LDS_PTR(uint8_t))dst);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
 }
 
 // This wave's direct loads have landed, everyone's have, and everyone is done with the buffers that are filled next.

@@ -8,7 +8,7 @@
 // its groups in ascending order.  Blocks that many groups list (the first one: all of them) are cut into parts of about equal length,
 // whose sums are added up in order.
 //
-// Steps: bits and D | lists of every block, parts | dK, dV | joined parts | dQ.
+// Steps: D | bits | lists of every block, parts | dQ | dK, dV | joined parts.
 #pragma once
 #include <type_traits>
 
@@ -16,14 +16,21 @@
 
 namespace grat {
 
-// D of every row, and the scratch memory that has to be 0 (by a kernel: recorded into graphs like any other launch).
+// Half: the weights of long lists fall below its normal numbers (2^-14), so they are taken 2^12 times as large (in lse2) and D and dP
+// as much smaller; dV's product then has 2^12 in it.  (bf16 has fp32's range.)
+constexpr float kWeightBits = 12.f, kWeightScale = 4096.f;
+
+template <bool F16>
+__device__ __forceinline__ float score_grad(float dp, float delta) { return F16 ? fmaf(dp, 1.f / kWeightScale, -delta) : dp - delta; }
+
+// D and lse in base 2 of every row, and the scratch memory that has to be 0 (by a kernel: recorded into graphs like any other launch).
 template <bool F16, int D>
 __global__ __launch_bounds__(256) void grad_delta_kernel(SelParams p, GradParams g, int64_t rows, FastDiv fd_n, FastDiv fd_h) {
     typedef typename Vec16<std::conditional_t<F16, _Float16, __bf16>>::type vec;
     constexpr int L = D / 8;
     const int64_t zeros = (int64_t)g.blocks * g.words;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < zeros; i += (int64_t)gridDim.x * 256) g.bits[i] = 0;
-    if (blockIdx.x == 0 && threadIdx.x < 3) g.counters[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 4) g.counters[threadIdx.x] = 0;
     const int64_t at = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
     if (at >= rows) return;
     uint32_t bh, n, b, h;
@@ -36,27 +43,35 @@ __global__ __launch_bounds__(256) void grad_delta_kernel(SelParams p, GradParams
     for (int e = 0; e < 8; ++e) sum = fmaf((float)x[e], (float)y[e], sum);
 #pragma unroll
     for (int m = 1; m < L; m *= 2) sum += __shfl_xor(sum, m);
-    if (c == 0) g.delta[at] = sum;
+    if (c == 0) {
+        g.delta[at] = F16 ? sum * (1.f / kWeightScale) : sum;
+        const float lse = p.lse[at];   // (a row that attends nothing weighs 0)
+        g.lse2[at] = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f - (F16 ? kWeightBits : 0.f);
+        if (at == 0) {   // what rows that only fill a tile take
+            g.delta[rows] = 0.f;
+            g.lse2[rows] = INFINITY;
+        }
+    }
 }
 
 // ---- dK, dV ------------------------------------------------------------------------------------
 // A workgroup owns 32 KW keys of one block, K and V of a wave's 32 keys in registers, and streams the Q and dO rows of
 // the groups that list the block in tiles of 64 through LDS (TEAMS == 2: a team takes 32 rows of a tile each).
-// What goes with a row - where it lies, lse, D, the keys it sees - is worked out by one wave, three tiles ahead for the loads
-// that depend on each other, and passed on through LDS.
+// What goes with a row - where it lies, lse, D, the keys it sees - is worked out by one wave, a tile ahead of the loads that need it, and
+// passed on through LDS; lse and D go there straight from memory.
 struct alignas(16) RowMeta {
-    const uint8_t* q[64];
-    const uint8_t* d[64];
     float lse2[64], delta[64];
     int32_t limit[64];
-    int32_t least;   // of the 64 limits
+    const uint8_t* q[64];
+    const uint8_t* d[64];
+    int32_t masked;   // some row does not see all keys of the tile
 };
 
 template <int KW, int TEAMS, bool F16, int D>
 __global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad_keys_kernel(SelParams p, GradParams g) {
     using E = Elem<F16>;
     constexpr int NW = KW * TEAMS, kTile = 64 * D * 2, kPieces = kTile / 1024, LPW = kPieces / NW, kRows = 1024 / (2 * D), kChunks = D / 8;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][kTile];   // Q, Q, dO, dO
+    __shared__ __attribute__((aligned(2 * kTile))) uint8_t lds[4][kTile];   // Q, Q, dO, dO
     __shared__ RowMeta meta[4];
     const SeqShape& s = p.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
@@ -89,131 +104,134 @@ __global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) vf[i] = *(const frag8*)(vs + 32 * i);
         }
-        // -- rows: group of row `at` of the walk | its address, limit, lse, D | all of that in LDS
+        // -- rows of the walk
         const int32_t* const groups = g.groups + part.y;
-        auto row_at = [&](int t) { return part.z + 64 * t + lane; };
-        auto find_group = [&](int t) { return groups[fdiv((uint32_t)min(row_at(t), part.w - 1), g.fd_rows)]; };
-        struct Row {
-            const uint8_t *q, *d;
-            float lse, delta;
-            int limit;
-        };
-        auto find_row = [&](int t, int group) {
-            const int at = min(row_at(t), part.w - 1);
-            const GroupRow r(p, h, group, at - (int)(fdiv((uint32_t)at, g.fd_rows) * g.fd_rows.d));
-            const bool there = r.there && row_at(t) < part.w;
-            const int64_t i = ((int64_t)b * s.q_heads + r.head) * s.n_q + r.query;
-            Row x;
-            x.q = row_address(p.Q, b, r.head, r.query);
-            x.d = row_address(g.dO, b, r.head, r.query);
-            x.lse = p.lse[i];
-            x.delta = g.delta[i];
-            x.limit = there ? row_seen(s, len, pos, r.query) : -1;
-            return x;
-        };
-        auto put_row = [&](int t, const Row& x) {
+        auto find_group = [&](int t) { return groups[fdiv((uint32_t)min(part.z + 64 * t + lane, part.w - 1), g.fd_rows)]; };
+        auto put_rows = [&](int t, int group) {
+            const int at = part.z + 64 * t + lane, in_list = min(at, part.w - 1);
+            const GroupRow r(p, h, group, in_list - (int)(fdiv((uint32_t)in_list, g.fd_rows) * g.fd_rows.d));
+            const bool there = r.there && at < part.w;
             RowMeta& m = meta[t & 3];
-            m.q[lane] = x.q;
-            m.d[lane] = x.d;
-            // (rows that attend nothing, and rows that only fill a tile, weigh 0)
-            m.lse2[lane] = x.limit < 0 || x.lse == -INFINITY ? INFINITY : x.lse * 1.4426950408889634f;
-            m.delta[lane] = x.delta;
-            m.limit[lane] = max(x.limit, 0);
-            int least = x.limit < 0 ? 0x7fffffff : x.limit;
-#pragma unroll
-            for (int k = 1; k < 64; k *= 2) least = min(least, __shfl_xor(least, k));
-            if (lane == 0) m.least = least;
+            m.q[lane] = row_address(p.Q, b, r.head, r.query);
+            m.d[lane] = row_address(g.dO, b, r.head, r.query);
+            const int limit = row_seen(s, len, pos, r.query);
+            m.limit[lane] = limit;
+            const bool cut = __builtin_amdgcn_ballot_w64(there && limit < tile_key0 + 32 * KW) != 0;
+            if (lane == 0) m.masked = cut;
+            // (rows that only fill a tile take the entry behind the last row's, which makes them weigh 0)
+            const int64_t i = there ? ((int64_t)b * s.q_heads + r.head) * s.n_q + r.query : g.stats;
+            load_lds_word((const uint8_t*)(g.lse2 + i), (uint8_t*)m.lse2);
+            load_lds_word((const uint8_t*)(g.delta + i), (uint8_t*)m.delta);
         };
         const bool keeper = wave == NW - 1;
-        Row ahead{};
         int group_ahead = 0;
         if (keeper) {
-            put_row(0, find_row(0, find_group(0)));
-            put_row(1, find_row(1, find_group(1)));
-            ahead = find_row(2, find_group(2));
-            group_ahead = find_group(3);
+            put_rows(0, find_group(0));
+            put_rows(1, find_group(1));
+            group_ahead = find_group(2);
         }
-        __syncthreads();
-        int piece_row[LPW], col[LPW];
-#pragma unroll
-        for (int k = 0; k < LPW; ++k) {
-            piece_row[k] = (wave * LPW + k) * kRows + lane / kChunks;
-            col[k] = ((lane % kChunks) ^ tile_swizzle<D>(piece_row[k])) << 4;
-        }
+        tile_barrier();
+        // A wave's pieces of a tile: rows kRows apart; the swizzle of piece k differs from that of piece 0 in bits that all lanes share.
+        static_assert(kRows % 4 == 0, "");
+        const int piece_row = wave * LPW * kRows + lane / kChunks, piece_col = (lane % kChunks) ^ tile_swizzle<D>(lane / kChunks);
         auto issue = [&](int t) {
             const RowMeta& m = meta[t & 3];
             uint8_t *qt = lds[t & 1], *dt = lds[2 + (t & 1)];
+            int chunk = piece_col;
+            asm volatile("" : "+v"(chunk));   // (columns are formed here: kept, they take two registers each)
 #pragma unroll
-            for (int k = 0; k < LPW; ++k) load_lds(m.q[piece_row[k]] + col[k], qt + (wave * LPW + k) * 1024);
-#pragma unroll
-            for (int k = 0; k < LPW; ++k) load_lds(m.d[piece_row[k]] + col[k], dt + (wave * LPW + k) * 1024);
+            for (int k = 0; k < LPW; ++k) {
+                const int col = (chunk ^ tile_swizzle<D>((wave * LPW + k) * kRows)) << 4;
+                load_lds(m.q[piece_row + k * kRows] + col, qt + (wave * LPW + k) * 1024);
+                load_lds(m.d[piece_row + k * kRows] + col, dt + (wave * LPW + k) * 1024);
+            }
         };
-        const TileReader<D> read(lane);
+        TileReader<D> read(lane, lds[0], team);
         const float c = p.scale_log2;
-        auto rows_block = [&](const RowMeta& m, const uint8_t* q_tile, const uint8_t* d_tile, int rb, bool masked) {
-            f32x16 S, T;
+        auto rows_block = [&](const RowMeta& m, int block32, bool masked) {
+            const int row0 = 32 * block32 + 4 * half;   // of this lane in the tile
+            // 4 products, each fragment read kAhead products ahead of its own: the sums of dK and dV, K and V leave 64 registers for
+            // everything else, and the compiler, left to itself, reads further ahead than that allows.
+            constexpr int kAhead = 2, kN = D / 16, kM = 2 * (D / 32);
+            frag8 fr[2 * kN + 2 * kM];
+            auto fetch = [&](int i) {
+                if (i < kN) fr[i] = read.rows(0, 0, i);
+                else if (i < 2 * kN) fr[i] = read.rows(1, 0, i - kN);
+                else if (i < 2 * kN + kM) fr[i] = read.cols(1, 0, (i - 2 * kN) / (D / 32), (i - 2 * kN) % (D / 32));
+                else if (i < 2 * kN + 2 * kM) fr[i] = read.cols(0, 0, (i - 2 * kN - kM) / (D / 32), (i - 2 * kN - kM) % (D / 32));
+            };
+            f32x16 S, T, zero;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) S[i] = T[i] = 0.f;
+            for (int i = 0; i < 16; ++i) zero[i] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(q_tile, rb, ks), kf[ks], S);
+            for (int i = 0; i < kAhead; ++i) fetch(i);
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) T = E::mfma(read.rows(d_tile, rb, ks), vf[ks], T);
-            uint32_t pw[8], dw[8];
+            for (int i = 0; i < 2 * kN; ++i) {
+                if (i + kAhead < 2 * kN) fetch(i + kAhead);
+                if (i < kN) S = E::mfma(fr[i], kf[i], i == 0 ? zero : S);
+                else T = E::mfma(fr[i], vf[i - kN], i == kN ? zero : T);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // (in place: S becomes P, T dS)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float4 l4 = *(const float4*)&m.lse2[32 * rb + 8 * q + 4 * half], d4 = *(const float4*)&m.delta[32 * rb + 8 * q + 4 * half];
+                const float4 l4 = *(const float4*)&m.lse2[row0 + 8 * q], d4 = *(const float4*)&m.delta[row0 + 8 * q];
                 const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
-                float w[4], ds[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    w[i] = __builtin_amdgcn_exp2f(fmaf(S[4 * q + i], c, -l[i]));
-                    ds[i] = w[i] * (T[4 * q + i] - dl[i]);
+                    S[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(S[4 * q + i], c, -l[i]));
+                    T[4 * q + i] = S[4 * q + i] * score_grad<F16>(T[4 * q + i], dl[i]);
                 }
-                if (masked) {
-                    const int4 n4 = *(const int4*)&m.limit[32 * rb + 8 * q + 4 * half];
-                    const int n[4] = {n4.x, n4.y, n4.z, n4.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (key >= n[i]) w[i] = ds[i] = 0.f;
-                }
-                pw[2 * q] = E::pack(w[0], w[1]);
-                pw[2 * q + 1] = E::pack(w[2], w[3]);
-                dw[2 * q] = E::pack(ds[0], ds[1]);
-                dw[2 * q + 1] = E::pack(ds[2], ds[3]);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            if (masked) {
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2) {
-                const frag8 w = __builtin_bit_cast(frag8, make_uint4(pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]));
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db) dv[db] = E::mfma(read.cols(d_tile, rb, s2, db), w, dv[db]);
+                for (int i = 0; i < 16; ++i)
+                    if (key >= m.limit[row0 + 8 * (i >> 2) + (i & 3)]) S[i] = T[i] = 0.f;
             }
+            uint32_t pw[8], dw[8];
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2) {
-                const frag8 w = __builtin_bit_cast(frag8, make_uint4(dw[4 * s2], dw[4 * s2 + 1], dw[4 * s2 + 2], dw[4 * s2 + 3]));
+            for (int i = 0; i < 8; ++i) pw[i] = E::pack(S[2 * i], S[2 * i + 1]);
 #pragma unroll
-                for (int db = 0; db < D / 32; ++db) dk[db] = E::mfma(read.cols(q_tile, rb, s2, db), w, dk[db]);
+            for (int i = 0; i < 8; ++i) dw[i] = E::pack(T[2 * i], T[2 * i + 1]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) fetch(2 * kN + i);
+#pragma unroll
+            for (int i = 0; i < 2 * kM; ++i) {
+                const int s2 = i % kM / (D / 32), db = i % (D / 32);
+                const uint32_t* const x = i < kM ? pw + 4 * s2 : dw + 4 * s2;
+                const frag8 w = __builtin_bit_cast(frag8, make_uint4(x[0], x[1], x[2], x[3]));
+                fetch(2 * kN + i + kAhead);
+                if (i < kM) dv[db] = E::mfma(fr[2 * kN + i], w, dv[db]);
+                else dk[db] = E::mfma(fr[2 * kN + i], w, dk[db]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
         issue(0);
         for (int t = 0; t < n_tiles; ++t) {
             tile_barrier();
             if (t + 1 < n_tiles) issue(t + 1);
-            if (keeper) {   // (past the last tile too: the last row's again, in bounds)
-                put_row(t + 2, ahead);
-                ahead = find_row(t + 3, group_ahead);
-                group_ahead = find_group(t + 4);
+            if (keeper && t + 2 < n_tiles) {
+                put_rows(t + 2, group_ahead);
+                group_ahead = find_group(t + 3);   // (past the last row: the last row's again)
             }
             const RowMeta& m = meta[t & 3];
-            const bool masked = __builtin_amdgcn_readfirstlane(m.least) < tile_key0 + 32 * KW;
+            const bool masked = __builtin_amdgcn_readfirstlane(m.masked) != 0;
             if constexpr (TEAMS == 1) {
-                rows_block(m, lds[t & 1], lds[2 + (t & 1)], 0, masked);
-                rows_block(m, lds[t & 1], lds[2 + (t & 1)], 1, masked);
+#pragma unroll 1
+                for (int i = 0; i < 2; ++i) {   // (one copy: two need more registers than there are)
+                    rows_block(m, i, masked);
+                    read.other_block();
+                }
             } else {
-                rows_block(m, lds[t & 1], lds[2 + (t & 1)], team, masked);
+                rows_block(m, team, masked);
             }
+            read.flip();
         }
     }
-    __syncthreads();   // everyone is done with the tiles
+    // Everyone is done with the tiles.  (The keeper's last loads have to land as well: LDS that is given back is somebody else's.)
+    tile_barrier();
 
     if constexpr (TEAMS == 2) {   // the second team's share, lane by lane: dK, then dV
         float* const mine = (float*)&lds[0][0] + key_wave * 64 * (D / 2) + lane;
@@ -238,6 +256,7 @@ __global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad
         add(dv);
         if (team == 1) return;
     }
+    constexpr float dv_factor = F16 ? 1.f / kWeightScale : 1.f;
     const int slot = g.part_slot[part_id];
     if (slot >= 0) {   // parts are joined by grad_join_kernel
         float* const dst = g.slots + (((int64_t)slot * tiles + tile_in_block) * 2 * (32 * KW) + key_wave * 32 + (lane & 31)) * D + 4 * half;
@@ -257,33 +276,35 @@ __global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad
         return k < s.n_k ? (uint8_t*)row_address(t, b, h, k) : nullptr;
     };
     store_rows<F16, D>(stage, dk, p.scale, lane, [&](int i) { return row_of(g.dK, i); });
-    store_rows<F16, D>(stage, dv, 1.f, lane, [&](int i) { return row_of(g.dV, i); });
+    store_rows<F16, D>(stage, dv, dv_factor, lane, [&](int i) { return row_of(g.dV, i); });
 }
 
-// dK and dV of the blocks that were cut into parts.
+// dK and dV of the blocks that were cut into parts: a thread adds up 4 numbers, kJoinShare workgroups share a key tile.
+constexpr int kJoinShare = 8;
+
 template <bool F16, int D>
 __global__ __launch_bounds__(256) void grad_join_kernel(SelParams p, GradParams g, int tile_keys) {
     const SeqShape& s = p.s;
-    uint32_t block, tile;
-    fdivmod(blockIdx.x, g.fd_tiles, block, tile);
-    const int2 join = g.joins[block];
-    if (join.y <= 1) return;
+    uint32_t at, tile;
+    fdivmod(blockIdx.x / kJoinShare, g.fd_tiles, at, tile);
+    if ((int)at >= g.counters[3]) return;
+    const int4 join = g.joins[at];   // block, first slot, parts
     const int tiles = (int)g.fd_tiles.d;
-    const uint32_t bh = block / (uint32_t)s.n_blocks, j = block - bh * (uint32_t)s.n_blocks;
+    const uint32_t bh = (uint32_t)join.x / (uint32_t)s.n_blocks, j = (uint32_t)join.x - bh * (uint32_t)s.n_blocks;
     const int b = (int)fdiv(bh, p.fd_kv_heads), h = (int)bh - b * s.kv_heads;
     const int64_t pitch = (int64_t)tiles * 2 * tile_keys * D;   // of a slot
-    const float* const src = g.slots + join.x * pitch + (int64_t)tile * 2 * tile_keys * D;
-    for (int i = threadIdx.x; i < 2 * tile_keys * (D / 4); i += 256) {
+    const float* const src = g.slots + join.y * pitch + (int64_t)tile * 2 * tile_keys * D;
+    for (int i = (int)(blockIdx.x % kJoinShare) * 256 + threadIdx.x; i < 2 * tile_keys * (D / 4); i += 256 * kJoinShare) {
         const int which = i / (tile_keys * (D / 4)), row = i / (D / 4) % tile_keys, c = i % (D / 4);
         const int key = (int)j * s.block + (int)tile * tile_keys + row;
         if (key >= s.n_k) continue;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int k = 0; k < join.y; ++k) {
+#pragma unroll 8
+        for (int k = 0; k < join.z; ++k) {
             const float4 v = *(const float4*)(src + k * pitch + 4 * (int64_t)i);
             sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
         }
-        const float f = which == 0 ? p.scale : 1.f;
+        const float f = which == 0 ? p.scale : F16 ? 1.f / kWeightScale : 1.f;
         uint2 v;
         v.x = Elem<F16>::pack(sum.x * f, sum.y * f);
         v.y = Elem<F16>::pack(sum.z * f, sum.w * f);
@@ -293,11 +314,12 @@ __global__ __launch_bounds__(256) void grad_join_kernel(SelParams p, GradParams 
 
 // ---- dQ ----------------------------------------------------------------------------------------
 // The forward walk with dO beside Q in registers: S^T = K Q^T, dP^T = V dO^T, and dQ^T += K^T dS^T with K read both ways from its tile.
+constexpr int kFewUnits = 12;   // lists walked twice
 template <int RW, int TEAMS, bool F16, int D>
 __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad_queries_kernel(SelParams p, GradParams g) {
     using E = Elem<F16>;
     constexpr int NW = RW * TEAMS, kTile = 64 * D * 2;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][kTile];   // K, K, V, V
+    __shared__ __attribute__((aligned(2 * kTile))) uint8_t lds[4][kTile];   // K, K, V, V
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
     const Item it(p);
@@ -314,8 +336,8 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) df[ks] = *(const frag8*)(d_src + 32 * ks);
     const int64_t stat = ((int64_t)it.b * s.q_heads + row.head) * s.n_q + row.query;
-    const float lse = p.lse[stat], delta = g.delta[stat];
-    const float lse2 = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f;   // (a row that attends nothing weighs 0)
+    const float lse2 = g.lse2[stat];
+    float delta = g.delta[stat];
     const int len = seq_len(s, it.b);
     const int64_t pos = seq_pos(s, it.b, len);
     const int seen = group_seen(s, len, pos, it.g);
@@ -334,52 +356,83 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     clear<D>(dq);
     const float c = p.scale_log2;
     const KeyLoader<NW, D> load(p, it, seen, wave, lane);
-    const TileReader<D> read(lane);
+    TileReader<D> read(lane, lds[0], team);
     auto unit_start = [&](int i) { return i < n_units ? __builtin_amdgcn_readfirstlane(s_units[i]) : kNoUnit; };
-    auto block = [&](const uint8_t* k_tile, const uint8_t* v_tile, int hb, int start) {
+    float sum = 0.f;   // over this lane's keys: of P dP while D is being formed, then of dS
+    auto block = [&](auto form_d, int hb, int start) {
+        constexpr bool kFormD = decltype(form_d)::value;
         if (start >= most) return;
         f32x16 S, T;
 #pragma unroll
         for (int i = 0; i < 16; ++i) S[i] = T[i] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(k_tile, hb, ks), qf[ks], S);
+        for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(0, hb, ks), qf[ks], S);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) T = E::mfma(read.rows(v_tile, hb, ks), df[ks], T);
+        for (int ks = 0; ks < D / 16; ++ks) T = E::mfma(read.rows(1, hb, ks), df[ks], T);
         const bool masked = start + kUnit > least;
         uint32_t dw[8];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-            float d0 = __builtin_amdgcn_exp2f(fmaf(S[i], c, -lse2)) * (T[i] - delta);
-            float d1 = __builtin_amdgcn_exp2f(fmaf(S[i + 1], c, -lse2)) * (T[i + 1] - delta);
+            float d0 = __builtin_amdgcn_exp2f(fmaf(S[i], c, -lse2)) * score_grad<F16>(T[i], delta);
+            float d1 = __builtin_amdgcn_exp2f(fmaf(S[i + 1], c, -lse2)) * score_grad<F16>(T[i + 1], delta);
             if (masked) {
                 const int key = start + 8 * (i >> 2) + 4 * half + (i & 3);
                 if (key >= limit) d0 = 0.f;
                 if (key + 1 >= limit) d1 = 0.f;
             }
-            dw[i >> 1] = E::pack(d0, d1);
+            sum += d0 + d1;
+            if constexpr (!kFormD) dw[i >> 1] = E::pack(d0, d1);
         }
+        if constexpr (!kFormD) {
 #pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-            const frag8 w = __builtin_bit_cast(frag8, make_uint4(dw[4 * s2], dw[4 * s2 + 1], dw[4 * s2 + 2], dw[4 * s2 + 3]));
+            for (int s2 = 0; s2 < 2; ++s2) {
+                const frag8 w = __builtin_bit_cast(frag8, make_uint4(dw[4 * s2], dw[4 * s2 + 1], dw[4 * s2 + 2], dw[4 * s2 + 3]));
 #pragma unroll
-            for (int db = 0; db < D / 32; ++db) dq[db] = E::mfma(read.cols(k_tile, hb, s2, db), w, dq[db]);
+                for (int db = 0; db < D / 32; ++db) dq[db] = E::mfma(read.cols(0, hb, s2, db), w, dq[db]);
+            }
         }
     };
-    if (n_tiles > 0) {
+    auto walk = [&](auto form_d) {
         load.issue(unit_start(load.my_unit), lds[0], lds[2], wave);
         for (int t = 0; t < n_tiles; ++t) {
             const int next = unit_start(2 * t + 2 + load.my_unit);
             tile_barrier();
             if (t + 1 < n_tiles) load.issue(next, lds[(t + 1) & 1], lds[2 + ((t + 1) & 1)], wave);
             if constexpr (TEAMS == 1) {
-                block(lds[t & 1], lds[2 + (t & 1)], 0, unit_start(2 * t));
-                block(lds[t & 1], lds[2 + (t & 1)], 1, unit_start(2 * t + 1));
+                block(form_d, 0, unit_start(2 * t));
+                block(form_d, 1, unit_start(2 * t + 1));
             } else {
-                block(lds[t & 1], lds[2 + (t & 1)], team, unit_start(2 * t + team));
+                block(form_d, 0, unit_start(2 * t + team));
             }
+            read.flip();
         }
+        if (n_tiles & 1) read.flip();   // (a walk begins in the first tile)
+        __syncthreads();                // everyone is done with the tiles
+    };
+    // over all keys of this lane's row
+    __shared__ float s_sum[NW][32];
+    auto over_row = [&]() {
+        float all = sum_across_halves(sum);
+        if constexpr (TEAMS == 2) {
+            if (half == 0) s_sum[wave][lane] = all;
+            __syncthreads();
+            all = s_sum[row_wave][lane & 31] + s_sum[RW + row_wave][lane & 31];
+            __syncthreads();
+        }
+        return all;
+    };
+    // dS has to add up to 0 over a row's keys.  With D taken from the rounded O it does not, by sum dO (O's error), which is small
+    // beside dO V^T where many keys are averaged into O, and as large as the rounding of dS where few are: short lists are walked a
+    // first time for what is missing.  What is left over is added to D for the walk over the keys.
+    if (n_tiles > 0) {
+        if (n_units <= kFewUnits) {
+            walk(std::true_type{});
+            delta += F16 ? over_row() * (1.f / kWeightScale) : over_row();
+            sum = 0.f;
+        }
+        walk(std::false_type{});
     }
-    __syncthreads();   // everyone is done with the tiles
+    sum = over_row();
     if constexpr (TEAMS == 2) {
         float* const mine = (float*)&lds[0][0] + row_wave * 64 * (D / 2) + lane;
         if (team == 1) {
@@ -395,6 +448,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
 #pragma unroll
             for (int i = 0; i < 16; ++i) dq[db][i] += mine[(db * 16 + i) * 64];
     }
+    if (half == 0 && row.there) g.delta[stat] = delta + (F16 ? sum * (1.f / kWeightScale) : sum);
     uint8_t* const stage = &lds[0][0] + (TEAMS == 2 ? 2 * kTile : 0) + row_wave * 4096;   // (two teams: behind what team 0 still reads)
     store_rows<F16, D>(stage, dq, p.scale, lane, [&](int i) -> uint8_t* {
         const GroupRow to(p, it.h, it.g, (it.tile * RW + row_wave) * 32 + i);
@@ -406,7 +460,9 @@ template <int KW, int TEAMS, bool F16, int D>
 inline void launch_grad_keys(const SelParams& p, const GradParams& g, hipStream_t stream) {
     const int64_t items = (int64_t)g.most_parts * g.fd_tiles.d;
     hipLaunchKernelGGL((grad_keys_kernel<KW, TEAMS, F16, D>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(KW * TEAMS * 64), 0, stream, p, g);
-    hipLaunchKernelGGL((grad_join_kernel<F16, D>), dim3((unsigned)(g.blocks * g.fd_tiles.d)), dim3(256), 0, stream, p, g, 32 * KW);
+    if (g.most_joins > 0)
+        hipLaunchKernelGGL((grad_join_kernel<F16, D>), dim3((unsigned)(g.most_joins * g.fd_tiles.d * kJoinShare)), dim3(256), 0, stream, p, g,
+                           32 * KW);
 }
 template <int RW, int TEAMS, bool F16, int D>
 inline void launch_grad_queries(const SelParams& p, const GradParams& g, hipStream_t stream) {
@@ -421,12 +477,12 @@ inline hipError_t launch_bwd(const SelParams& p, const GradParams& g, int tile_r
     hipLaunchKernelGGL((grad_delta_kernel<F16, D>), dim3((unsigned)((rows + 2048 / D - 1) / (2048 / D))), dim3(256), 0, stream, p, g, rows,
                        make_fastdiv((uint32_t)p.s.n_q), make_fastdiv((uint32_t)p.s.q_heads));
     launch_grad_lists(p, g, stream);
-    if (tile_keys == 128) launch_grad_keys<4, 1, F16, D>(p, g, stream);
-    else if (tile_keys == 64) launch_grad_keys<2, 2, F16, D>(p, g, stream);
-    else launch_grad_keys<1, 2, F16, D>(p, g, stream);
     if (tile_rows == 128) launch_grad_queries<4, 1, F16, D>(p, g, stream);
     else if (tile_rows == 64) launch_grad_queries<2, 2, F16, D>(p, g, stream);
     else launch_grad_queries<1, 2, F16, D>(p, g, stream);
+    if (tile_keys == 128) launch_grad_keys<4, 1, F16, D>(p, g, stream);
+    else if (tile_keys == 64) launch_grad_keys<2, 2, F16, D>(p, g, stream);
+    else launch_grad_keys<1, 2, F16, D>(p, g, stream);
     return hipGetLastError();
 }
 

@@ -18,49 +18,62 @@ __global__ __launch_bounds__(256) void grad_bits_kernel(SelParams p, GradParams 
     atomicOr(&g.bits[((int64_t)bh * p.s.n_blocks + block) * g.words + group / 32], 1u << (group % 32));
 }
 
-// A block's groups, ascending, and its parts.  One wave a block; where in `groups`, `parts` and `slots` a block's share lies depends on the
-// order of the waves, what is computed from it does not.
+// A block's groups, ascending, and its parts.  A workgroup takes kListBlocks blocks, a wave a block at a time; it asks for its share of `groups`,
+// `parts` and `slots` once.  Where that lies depends on the order of the workgroups, what is computed from it does not.
+constexpr int kListBlocks = 16;
+
 __global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams g) {
-    const int block = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (block >= g.blocks) return;
-    const uint32_t* const words = g.bits + (int64_t)block * g.words;
-    int n = 0;
-    for (int w = lane; w < g.words; w += 64) n += __popc(words[w]);
+    __shared__ int s_n[kListBlocks], s_at[4][kListBlocks + 1], s_base[4];
+    const int block0 = (int)blockIdx.x * kListBlocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int here = min(kListBlocks, g.blocks - block0);
+    for (int i = wave; i < here; i += 4) {
+        const uint32_t* const words = g.bits + (int64_t)(block0 + i) * g.words;
+        int n = 0;
+        for (int w = lane; w < g.words; w += 64) n += __popc(words[w]);
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) n += __shfl_xor(n, m);
-    const int64_t rows = (int64_t)n * p.rows;
-    const int parts = (int)max((int64_t)1, (rows + g.part_rows - 1) / g.part_rows);
-    int first = 0, part0 = 0, slot0 = 0;
-    if (lane == 0) {
-        first = n > 0 ? atomicAdd(&g.counters[0], n) : 0;
-        part0 = atomicAdd(&g.counters[1], parts);
-        if (parts > 1) slot0 = atomicAdd(&g.counters[2], parts);
-        g.joins[block] = make_int2(slot0, parts);
+        for (int m = 1; m < 64; m *= 2) n += __shfl_xor(n, m);
+        if (lane == 0) s_n[i] = n;
     }
-    first = __shfl(first, 0);
-    part0 = __shfl(part0, 0);
-    slot0 = __shfl(slot0, 0);
-    int at = first;
-    for (int w0 = 0; w0 < g.words; w0 += 64) {
-        uint32_t bits = w0 + lane < g.words ? words[w0 + lane] : 0;
-        const int mine = __popc(bits);
-        int before = mine;   // inclusive prefix sum
+    __syncthreads();
+    auto parts_of = [&](int n) { return (int)max((int64_t)1, ((int64_t)n * p.rows + g.part_rows - 1) / g.part_rows); };
+    if (threadIdx.x < 4) {   // groups, parts, slots, joins
+        const int what = threadIdx.x;
+        int sum = 0;
+        for (int i = 0; i < here; ++i) {
+            const int n = s_n[i], parts = parts_of(n);
+            s_at[what][i] = sum;
+            sum += what == 0 ? n : what == 1 ? parts : parts == 1 ? 0 : what == 2 ? parts : 1;
+        }
+        s_base[what] = sum > 0 ? atomicAdd(&g.counters[what], sum) : 0;
+    }
+    __syncthreads();
+    for (int i = wave; i < here; i += 4) {
+        const int block = block0 + i, n = s_n[i], parts = parts_of(n);
+        const int first = s_base[0] + s_at[0][i], part0 = s_base[1] + s_at[1][i], slot0 = s_base[2] + s_at[2][i];
+        const uint32_t* const words = g.bits + (int64_t)block * g.words;
+        int at = first;
+        for (int w0 = 0; w0 < g.words; w0 += 64) {
+            uint32_t bits = w0 + lane < g.words ? words[w0 + lane] : 0;
+            const int mine = __popc(bits);
+            int before = mine;   // inclusive prefix sum
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2) {
-            const int up = __shfl_up(before, m);
-            if (lane >= m) before += up;
+            for (int m = 1; m < 64; m *= 2) {
+                const int up = __shfl_up(before, m);
+                if (lane >= m) before += up;
+            }
+            int to = at + before - mine;
+            while (bits) {
+                g.groups[to++] = (w0 + lane) * 32 + __builtin_ctz(bits);
+                bits &= bits - 1;
+            }
+            at += __shfl(before, 63);
         }
-        int to = at + before - mine;
-        while (bits) {
-            g.groups[to++] = (w0 + lane) * 32 + __builtin_ctz(bits);
-            bits &= bits - 1;
+        const int64_t rows = (int64_t)n * p.rows, per = ((rows + parts - 1) / parts + 63) & ~(int64_t)63;   // whole tiles of 64 rows
+        for (int k = lane; k < parts; k += 64) {
+            g.parts[part0 + k] = make_int4(block, first, (int)min(k * per, rows), (int)min((k + 1) * per, rows));
+            g.part_slot[part0 + k] = parts > 1 ? slot0 + k : -1;
         }
-        at += __shfl(before, 63);
-    }
-    const int64_t per = ((rows + parts - 1) / parts + 63) & ~(int64_t)63;   // whole tiles of 64 rows
-    for (int i = lane; i < parts; i += 64) {
-        g.parts[part0 + i] = make_int4(block, first, (int)min((int64_t)i * per, rows), (int)min((int64_t)(i + 1) * per, rows));
-        g.part_slot[part0 + i] = parts > 1 ? slot0 + i : -1;
+        if (parts > 1 && lane == 0) g.joins[s_base[3] + s_at[3][i]] = make_int4(block, slot0, parts, 0);
     }
 }
 
@@ -68,7 +81,7 @@ void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stre
     const int64_t entries = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.max_blocks;
     hipLaunchKernelGGL(grad_bits_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, stream, p, g, entries,
                        make_fastdiv((uint32_t)p.max_blocks));
-    hipLaunchKernelGGL(grad_lists_kernel, dim3((unsigned)((g.blocks + 3) / 4)), dim3(256), 0, stream, p, g);
+    hipLaunchKernelGGL(grad_lists_kernel, dim3((unsigned)((g.blocks + kListBlocks - 1) / kListBlocks)), dim3(256), 0, stream, p, g);
 }
 
 }  // namespace grat

@@ -13,7 +13,7 @@ template <int RW, int TEAMS, bool F16, int D>
 __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void selected_fwd_kernel(SelParams p) {
     using E = Elem<F16>;
     constexpr int NW = RW * TEAMS, kTile = 64 * D * 2;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][kTile];   // K, K, V, V
+    __shared__ __attribute__((aligned(2 * kTile))) uint8_t lds[4][kTile];   // K, K, V, V
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
     const Item it(p);
@@ -59,17 +59,17 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     float l_run = 0.f;
 
     const KeyLoader<NW, D> load(p, it, seen, wave, lane);
-    const TileReader<D> read(lane);
+    TileReader<D> read(lane, lds[0], team);
     // (a list's last tile may lack its second unit; one of a part that ends inside the list does not)
     auto unit_start = [&](int i) { return i < n_units ? __builtin_amdgcn_readfirstlane(s_units[u_first + i]) : kNoUnit; };
 
-    auto block = [&](const uint8_t* k_tile, const uint8_t* v_tile, int hb, int start) {
+    auto block = [&](int hb, int start) {
         if (start >= most) return;   // nobody in this wave sees the unit
         f32x16 S;
 #pragma unroll
         for (int i = 0; i < 16; ++i) S[i] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(k_tile, hb, ks), qf[ks], S);
+        for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(0, hb, ks), qf[ks], S);
         if (start + kUnit > least) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
         for (int s2 = 0; s2 < 2; ++s2) {
             const frag8 w = __builtin_bit_cast(frag8, make_uint4(pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]));
 #pragma unroll
-            for (int db = 0; db < D / 32; ++db) oacc[db] = E::mfma(read.cols(v_tile, hb, s2, db), w, oacc[db]);
+            for (int db = 0; db < D / 32; ++db) oacc[db] = E::mfma(read.cols(1, hb, s2, db), w, oacc[db]);
         }
     };
 
@@ -119,11 +119,12 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
             tile_barrier();
             if (t + 1 < n_tiles) load.issue(next, lds[(t + 1) & 1], lds[2 + ((t + 1) & 1)], wave);
             if constexpr (TEAMS == 1) {
-                block(lds[t & 1], lds[2 + (t & 1)], 0, unit_start(2 * t));
-                block(lds[t & 1], lds[2 + (t & 1)], 1, unit_start(2 * t + 1));
+                block(0, unit_start(2 * t));
+                block(1, unit_start(2 * t + 1));
             } else {
-                block(lds[t & 1], lds[2 + (t & 1)], team, unit_start(2 * t + team));
+                block(0, unit_start(2 * t + team));
             }
+            read.flip();
         }
     }
     float l = sum_across_halves(l_run);
