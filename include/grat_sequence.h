@@ -141,7 +141,7 @@ grat_status grat_block_scores(const grat_sequence* seq, const grat_tensor* Q, co
  * The list of every query group: of the blocks that it sees the first `first`, the last `local`, and of the others those with
  * the highest scores, `top` blocks in all at most.  Equal scores: the lower block.  A score of NaN or -infinity is never
  * selected (the first and the last blocks are, whatever their scores).
- *   d_scores  as grat_block_scores writes them (or any others of that shape; blocks not seen are not read)
+ *   d_scores  as grat_block_scores writes them (or any others of that shape; those of blocks not seen do not count)
  *   d_count[batch][kv_heads][n_groups]       (out) length of the list, 0 for a group that sees nothing
  *   d_index[batch][kv_heads][n_groups][top]  (out) blocks in ascending order, then -1
  * top >= 1, first >= 0, local >= 0, first + local <= top (GRAT_ERR_BAD_DIMS); `local` of at least ceil(q_group / block) + 1

@@ -138,15 +138,17 @@ __device__ __forceinline__ void tile_barrier() {
 // thread of the workgroup calls it, it ends with a barrier), followed by one kNoUnit.
 __device__ __forceinline__ int list_units(const SelParams& p, int64_t list, int seen, int32_t* s_units, int32_t* s_n) {
     if (threadIdx.x < 64) {
-        const int lane = threadIdx.x;
-        const int n = min(max(p.count[list], 0), p.max_blocks) * (int)p.fd_units.d;
+        // (the count and the first entries are asked for together)
+        const int lane = threadIdx.x, per = (int)p.fd_units.d;
         const int32_t* const entries = p.index + list * p.max_blocks;
+        const int listed = p.count[list], ahead = entries[min((int)fdiv((uint32_t)lane, p.fd_units), p.max_blocks - 1)];
+        const int n = min(max(listed, 0), p.max_blocks) * per;
         int have = 0;
         for (int u0 = 0; u0 < n; u0 += 64) {
             const int u = u0 + lane;
             uint32_t entry, part;
             fdivmod((uint32_t)min(u, n - 1), p.fd_units, entry, part);
-            const int block = entries[entry];
+            const int block = u0 == 0 ? ahead : entries[entry];
             const int start = min(max(block, 0), p.s.n_blocks - 1) * p.s.block + (int)part * kUnit;
             const bool in = u < n && block >= 0 && block < p.s.n_blocks && start < seen;
             const uint64_t all = __ballot(in);

@@ -18,14 +18,14 @@ __global__ __launch_bounds__(256) void grad_bits_kernel(SelParams p, GradParams 
     atomicOr(&g.bits[((int64_t)bh * p.s.n_blocks + block) * g.words + group / 32], 1u << (group % 32));
 }
 
-// A block's groups, ascending, and its parts.  A workgroup takes kListBlocks blocks, a wave a block at a time; it asks for its share of `groups`,
+// A block's groups, ascending, and its parts.  A workgroup takes up to kListBlocks blocks, a wave a block at a time; it asks for its share of `groups`,
 // `parts` and `slots` once.  Where that lies depends on the order of the workgroups, what is computed from it does not.
-constexpr int kListBlocks = 16;
+constexpr int kListBlocks = 16;   // 4 in small launches, for which it is latency that counts
 
-__global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams g) {
+__global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams g, int per_group) {
     __shared__ int s_n[kListBlocks], s_at[4][kListBlocks + 1], s_base[4];
-    const int block0 = (int)blockIdx.x * kListBlocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int here = min(kListBlocks, g.blocks - block0);
+    const int block0 = (int)blockIdx.x * per_group, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int here = min(per_group, g.blocks - block0);
     for (int i = wave; i < here; i += 4) {
         const uint32_t* const words = g.bits + (int64_t)(block0 + i) * g.words;
         int n = 0;
@@ -81,7 +81,8 @@ void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stre
     const int64_t entries = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.max_blocks;
     hipLaunchKernelGGL(grad_bits_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, stream, p, g, entries,
                        make_fastdiv((uint32_t)p.max_blocks));
-    hipLaunchKernelGGL(grad_lists_kernel, dim3((unsigned)((g.blocks + kListBlocks - 1) / kListBlocks)), dim3(256), 0, stream, p, g);
+    const int per_group = g.blocks <= 2048 ? 4 : kListBlocks;
+    hipLaunchKernelGGL(grad_lists_kernel, dim3((unsigned)((g.blocks + per_group - 1) / per_group)), dim3(256), 0, stream, p, g, per_group);
 }
 
 }  // namespace grat

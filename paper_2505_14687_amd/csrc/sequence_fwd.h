@@ -179,45 +179,83 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     });
 }
 
-// Joins the parts of a split list: a row's D / 4 lanes add up its parts, weighted by 2^(c (m - max m)).
-template <bool F16, int D>
+// Joins the parts of a split list, weighted by 2^(c (m - max m)).  D / 4 lanes share a row's dims, SLOTS of them its parts (8 where there
+// are many: then all loads of a row are in flight at once, and the slots' sums are joined through LDS in order).
+template <int SLOTS, bool F16, int D>
 __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int tile_rows, FastDiv fd_rows) {
-    constexpr int L = D / 4;
+    constexpr int L = D / 4, RPB = 256 / (L * SLOTS);   // rows of a workgroup
+    __shared__ float4 s_o[SLOTS > 1 ? 256 : 1];
+    __shared__ float2 s_ml[SLOTS > 1 ? 256 : 1];
     const SeqShape& s = p.s;
-    const int lane = threadIdx.x % L;
+    const int lane = threadIdx.x % L, slot = threadIdx.x / L % SLOTS;
     const int64_t n = (int64_t)s.batch * s.kv_heads * s.n_groups * p.rows;
-    const int64_t at = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    if (at >= n) return;
+    const int64_t at = min((int64_t)blockIdx.x * RPB + threadIdx.x / (L * SLOTS), n - 1);
     uint32_t list, r, bh, g, b, h;
     fdivmod((uint32_t)at, fd_rows, list, r);
     fdivmod(list, p.fd_groups, bh, g);
     fdivmod(bh, p.fd_kv_heads, b, h);
     const GroupRow row(p, (int)h, (int)g, (int)r);
-    if (!row.there) return;
     const int64_t first = (((int64_t)list * p.row_tiles + r / tile_rows) * p.splits) * tile_rows + r % tile_rows;   // + split * tile_rows
     const float2* const ml = (const float2*)p.part_ml + first;
     const float4* const po = (const float4*)p.part_o + first * L + lane;
-    float m = -INFINITY;
-    for (int i = 0; i < p.splits; ++i) m = fmaxf(m, ml[(int64_t)i * tile_rows].x);
-    float l = 0.f, x = 0.f, y = 0.f, z = 0.f, w = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < p.splits; ++i) {
-        const float2 v = ml[(int64_t)i * tile_rows];
-        const float4 o = po[(int64_t)i * tile_rows * L];
-        const float f = __builtin_amdgcn_exp2f((v.x - m) * p.scale_log2);
-        l = fmaf(f, v.y, l);
-        x = fmaf(f, o.x, x);
-        y = fmaf(f, o.y, y);
-        z = fmaf(f, o.z, z);
-        w = fmaf(f, o.w, w);
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = slot; i0 < p.splits; i0 += 8 * SLOTS) {
+        float2 v[8];
+        float4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = min(i0 + k * SLOTS, p.splits - 1);
+            v[k] = ml[(int64_t)i * tile_rows];
+            x[k] = po[(int64_t)i * tile_rows * L];
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, v[k].x);
+        const float old = m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * p.scale_log2);
+        l *= old;
+        o = make_float4(o.x * old, o.y * old, o.z * old, o.w * old);
+        m = top;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float f = i0 + k * SLOTS < p.splits ? __builtin_amdgcn_exp2f((v[k].x - m) * p.scale_log2) : 0.f;
+            l = fmaf(f, v[k].y, l);
+            o = make_float4(fmaf(f, x[k].x, o.x), fmaf(f, x[k].y, o.y), fmaf(f, x[k].z, o.z), fmaf(f, x[k].w, o.w));
+        }
     }
+    if constexpr (SLOTS > 1) {
+        s_o[threadIdx.x] = o;
+        s_ml[threadIdx.x] = make_float2(m, l);
+        __syncthreads();
+        if (slot > 0) return;
+#pragma unroll
+        for (int k = 1; k < SLOTS; ++k) m = fmaxf(m, s_ml[threadIdx.x + k * L].x);
+        l = 0.f;
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) {   // (a slot without a part has m = -infinity: weight 0)
+            const float2 v = s_ml[threadIdx.x + k * L];
+            const float4 x = s_o[threadIdx.x + k * L];
+            const float f = __builtin_amdgcn_exp2f((v.x - m) * p.scale_log2);
+            l = fmaf(f, v.y, l);
+            o = make_float4(fmaf(f, x.x, o.x), fmaf(f, x.y, o.y), fmaf(f, x.z, o.z), fmaf(f, x.w, o.w));
+        }
+    }
+    if ((int64_t)blockIdx.x * RPB + threadIdx.x / (L * SLOTS) >= n || !row.there) return;
     const float inv = l > 0.f ? 1.f / l : l;
     uint2 v;
-    v.x = Elem<F16>::pack(x * inv, y * inv);
-    v.y = Elem<F16>::pack(z * inv, w * inv);
+    v.x = Elem<F16>::pack(o.x * inv, o.y * inv);
+    v.y = Elem<F16>::pack(o.z * inv, o.w * inv);
     *(uint2*)((uint8_t*)row_address(p.O, (int)b, row.head, row.query) + 8 * lane) = v;
     if (p.lse && lane == 0)
         p.lse[((int64_t)b * s.q_heads + row.head) * s.n_q + row.query] = (m * p.scale_log2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int SLOTS, bool F16, int D>
+inline void launch_join(const SelParams& p, int tile_rows, hipStream_t stream) {
+    const int64_t rows = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.rows, per = 1024 / (D * SLOTS);
+    hipLaunchKernelGGL((selected_join_kernel<SLOTS, F16, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p, tile_rows,
+                       make_fastdiv((uint32_t)p.rows));
 }
 
 template <int RW, int TEAMS, bool F16, int D>
@@ -233,11 +271,8 @@ inline hipError_t launch_fwd(const SelParams& p, int tile_rows, hipStream_t stre
     else if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D>(p, stream);
     else if (tile_rows == 64) launch_fwd_tile<2, 2, F16, D>(p, stream);
     else launch_fwd_tile<1, 2, F16, D>(p, stream);
-    if (p.splits > 1) {
-        const int64_t rows = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.rows;
-        hipLaunchKernelGGL((selected_join_kernel<F16, D>), dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, stream, p, tile_rows,
-                           make_fastdiv((uint32_t)p.rows));
-    }
+    if (p.splits > 8) launch_join<8, F16, D>(p, tile_rows, stream);
+    else if (p.splits > 1) launch_join<1, F16, D>(p, tile_rows, stream);
     return hipGetLastError();
 }
 

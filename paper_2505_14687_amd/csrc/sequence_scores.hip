@@ -221,6 +221,11 @@ hipError_t launch_block_scores(const SeqShape& s, const SeqTensor& Q, grat_dtype
 // the scores; 0 is not a candidate.  The smallest selected one is found bit by bit from the highest: the largest T with at least as
 // many keys >= T as are wanted; a count that is met exactly ends the search.  Keys equal to T are taken in ascending order of their
 // blocks.  What is chosen is compacted by ballots, so lists ascend by construction.
+//
+// What bounds it is not the reading but the instructions: R ballots and R scalar counts a bit.  So where few are wanted, the common case,
+// the search runs on the lanes' largest keys only and ends at the first bound that little more than `want` of them reach.  What is not
+// below it (of 500 normal scores about 25 where 13 are wanted) is copied to LDS with its block, and a lane ranks one of those.  With several
+// waves the best of their bounds counts, and one wave ranks.
 struct SelectParams {
     SeqShape s;
     const float* scores;
@@ -229,11 +234,17 @@ struct SelectParams {
     int32_t* index;
     int64_t lists;
     int32_t chunks;   // runs are chunks * 64 blocks long (R = 0)
+    FastDiv fd_groups, fd_kv_heads, fd_block;
 };
+
+constexpr int kFewWanted = 56;   // longest lists that are ranked
 
 template <int WAVES, int R>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_kernel(SelectParams p) {
     __shared__ int s_count[2][WAVES];
+    constexpr int kTwo = WAVES > 1 ? 2 : 1, kFew = 64 * kTwo;   // candidates that a lane ranks, and all of them
+    __shared__ uint2 s_few[WAVES == 1 ? 4 : 1][kFew];            // key, block
+    __shared__ uint32_t s_bound[2][WAVES];
     constexpr int kUnroll = R > 0 ? R : 1;
     const SeqShape& s = p.s;
     const int lane = threadIdx.x & 63;
@@ -241,31 +252,36 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
     // (one wave a list: four lists a workgroup, which then has no barrier)
     const int64_t list = WAVES == 1 ? (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : blockIdx.x;
     if (list >= p.lists) return;
-    const int bh = (int)(list / s.n_groups), g = (int)(list - (int64_t)bh * s.n_groups), b = bh / s.kv_heads;
-    const int len = seq_len(s, b);
-    const int seen = group_seen(s, len, seq_pos(s, b, len), g);
-    const int vis = (seen + s.block - 1) / s.block;
-    const int head_end = min(p.first, vis), tail = max(head_end, vis - p.local);   // [0, head_end) and [tail, vis) are in
-    const int want = min(p.top - head_end - (vis - tail), tail - head_end);        // others, at most
     const float* const row = p.scores + list * s.n_blocks;
-
     const int chunks = R > 0 ? R : p.chunks;
     const int j0 = wave * chunks * 64 + lane;   // this lane's blocks: j0 + 64 r
-    auto read_key = [&](int r) -> uint32_t {
+    float score[R > 0 ? R : 1];   // (asked for ahead of everything that says which of them count)
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) score[r] = row[min(j0 + 64 * r, s.n_blocks - 1)];
+    }
+    uint32_t bh, g;
+    fdivmod((uint32_t)list, p.fd_groups, bh, g);
+    const int b = (int)fdiv(bh, p.fd_kv_heads);
+    const int len = seq_len(s, b);
+    const int seen = group_seen(s, len, seq_pos(s, b, len), (int)g);
+    const int vis = (int)fdiv((uint32_t)(seen + s.block - 1), p.fd_block);
+    const int head_end = min(p.first, vis), tail = max(head_end, vis - p.local);   // [0, head_end) and [tail, vis) are in
+    const int want = min(p.top - head_end - (vis - tail), tail - head_end);        // others, at most
+    auto key_of = [&](int r, float x) -> uint32_t {
         const int j = j0 + 64 * r;
-        if (j < head_end || j >= tail) return 0;
-        const float x = row[j] == 0.f ? 0.f : row[j];   // (-0 and 0 are equal)
-        const uint32_t u = __builtin_bit_cast(uint32_t, x);
-        return x > -INFINITY ? ((u >> 31) ? ~u : u | 0x80000000u) : 0;   // (false for NaN)
+        x = x == 0.f ? 0.f : x;   // (-0 and 0 are equal)
+        const uint32_t u = __builtin_bit_cast(uint32_t, x), order = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+        return j >= head_end && j < tail && x > -INFINITY ? order : 0;   // (false for NaN)
     };
     uint32_t held[R > 0 ? R : 1];
     if constexpr (R > 0) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) held[r] = read_key(r);
+        for (int r = 0; r < R; ++r) held[r] = key_of(r, score[r]);
     }
     auto key = [&](int r) -> uint32_t {
         if constexpr (R > 0) return held[r];
-        else return read_key(r);
+        else return key_of(r, row[min(j0 + 64 * r, s.n_blocks - 1)]);
     };
     int parity = 0;
     // (sum over the waves; of the waves ahead of this one)
@@ -283,7 +299,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
                 all += s_count[parity][w];
             }
             parity ^= 1;
-            return all;
+            before = __builtin_amdgcn_readfirstlane(before);   // (the same in all lanes, which the compiler cannot know of what comes out of LDS)
+            return __builtin_amdgcn_readfirstlane(all);
         }
     };
     auto count_from = [&](uint32_t t) {
@@ -292,13 +309,120 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
         for (int r = 0; r < chunks; ++r) n += __popcll(__ballot(key(r) >= t));
         return everyone(n, before);
     };
+    const uint64_t below = (1ull << lane) - 1ull;
+    int32_t* const out = p.index + list * p.top;
+    if constexpr (R > 1) {
+        if (want > 0 && want <= kFewWanted) {
+            uint32_t best = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) best = max(best, held[r]);
+            auto search = [&](int least, int most) {   // a bound that this many lanes reach, or as few more than `least` as there are
+                uint32_t t = 0;
+#pragma unroll 1   // (unrolled, the code is fetched more slowly than it runs)
+                for (int bit = 31; bit >= 0; --bit) {
+                    const int n = __popcll(__ballot(best >= (t | 1u << bit)));
+                    if (n >= least) t |= 1u << bit;
+                    if (n >= least && n <= most) break;
+                }
+                return t;
+            };
+            uint32_t bound = search(want, want + 8);
+            if constexpr (WAVES > 1) {
+                // `want` keys of one wave reach the highest of the waves' bounds, and an equal share of them in every wave whose run is seen
+                // as a whole the lowest of the bounds for that
+                const int whole = max(1, tail / (R * 64));
+                if (lane == 0) s_bound[0][wave] = bound;
+                const int share = (want + whole - 1) / whole;
+                const uint32_t equal = search(share, share + 1);
+                if (lane == 0) s_bound[1][wave] = equal;
+                __syncthreads();
+                uint32_t lowest = 0xffffffffu;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    bound = max(bound, s_bound[0][w]);
+                    lowest = min(lowest, w < whole ? s_bound[1][w] : lowest);
+                }
+                bound = __builtin_amdgcn_readfirstlane(max(bound, lowest));
+            }
+            int mine = 0, at;
+#pragma unroll
+            for (int r = 0; r < R; ++r) mine += __popcll(__ballot(held[r] >= bound));
+            const int few = everyone(mine, at);
+            if (bound > 0 && few <= kFew) {   // (bound = 0: no wave has `want` lanes with a candidate)
+                uint2* const keys = s_few[WAVES == 1 ? threadIdx.x >> 6 : 0];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const bool in = held[r] >= bound;
+                    const uint64_t all = __ballot(in);
+                    if (in) keys[at + __popcll(all & below)] = make_uint2(held[r], (uint32_t)(j0 + 64 * r));
+                    at += __popcll(all);
+                }
+                if constexpr (WAVES > 1) {
+                    __syncthreads();
+                    if (wave > 0) return;
+                } else {
+                    __builtin_amdgcn_wave_barrier();
+                }
+                // a lane ranks the candidates lane (+ 64): the number of larger ones
+                uint2 k[kTwo];
+                int rank[kTwo];
+                bool in[kTwo];
+                uint64_t all[kTwo];
+                int have = 0;
+                auto with_each = [&](auto&& f) {   // f(candidate, its number)
+#pragma unroll
+                    for (int u = 0; u < kTwo; ++u)
+                        for (int i = 0; i < min(few - 64 * u, 64); ++i) f((uint32_t)__builtin_amdgcn_readlane(k[u].x, i), 64 * u + i);
+                };
+                auto take = [&]() {
+                    have = 0;
+#pragma unroll
+                    for (int u = 0; u < kTwo; ++u) {
+                        in[u] = k[u].x > 0 && rank[u] < want;
+                        all[u] = __ballot(in[u]);
+                        have += __popcll(all[u]);
+                    }
+                };
+#pragma unroll
+                for (int u = 0; u < kTwo; ++u) {
+                    k[u] = 64 * u + lane < few ? keys[64 * u + lane] : make_uint2(0, 0);
+                    rank[u] = 0;
+                }
+                with_each([&](uint32_t x, int) {
+#pragma unroll
+                    for (int u = 0; u < kTwo; ++u) rank[u] += x > k[u].x ? 1 : 0;
+                });
+                take();
+                if (have != want) {   // the last ones taken have equals that are not: the lower blocks
+                    with_each([&](uint32_t x, int i) {
+#pragma unroll
+                        for (int u = 0; u < kTwo; ++u) rank[u] += x == k[u].x && i < 64 * u + lane ? 1 : 0;
+                    });
+                    take();
+                }
+                const int total = head_end + want + (vis - tail);
+                int at_out = head_end;
+#pragma unroll
+                for (int u = 0; u < kTwo; ++u) {
+                    if (in[u]) out[at_out + __popcll(all[u] & below)] = (int)k[u].y;
+                    at_out += __popcll(all[u]);
+                }
+                for (int i = lane; i < head_end; i += 64) out[i] = i;
+                for (int i = lane; i < vis - tail; i += 64) out[head_end + want + i] = tail + i;
+                for (int i = total + lane; i < p.top; i += 64) out[i] = -1;
+                if (lane == 0) p.count[list] = total;
+                return;
+            }
+        }
+    }
     uint32_t T = 1;   // keys >= T are taken, of those equal to T only `ties`
     int ties = 0x7fffffff;
     if (want <= 0) {
         T = 0xffffffffu;   // (no score has this key)
     } else if (count_from(1) > want) {
-        T = 0;
         bool met = false;
+        T = 0;
+#pragma unroll 1
         for (int bit = 31; bit >= 0; --bit) {
             const uint32_t t = T | 1u << bit;
             const int n = count_from(t);
@@ -307,7 +431,6 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
         }
         if (!met) ties = want - count_from(T + 1);
     }
-    const uint64_t below = (1ull << lane) - 1ull;
     int n = 0, tied_before;
 #pragma unroll kUnroll
     for (int r = 0; r < chunks; ++r) n += __popcll(__ballot(key(r) == T));
@@ -327,7 +450,6 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
         for (int r = 0, tied = tied_before; r < chunks; ++r) mine += __popcll(__ballot(taken(r, tied)));
         n = everyone(mine, base);
     }
-    int32_t* const out = p.index + list * p.top;
 #pragma unroll kUnroll
     for (int r = 0, tied = tied_before; r < chunks; ++r) {
         const bool in = taken(r, tied);
@@ -349,7 +471,8 @@ static void launch_select(SelectParams p, hipStream_t stream) {
 
 hipError_t launch_select_blocks(const SeqShape& s, const float* d_scores, int32_t top, int32_t first, int32_t local, int32_t* d_count,
                                 int32_t* d_index, hipStream_t stream) {
-    const SelectParams p{s, d_scores, top, first, local, d_count, d_index, (int64_t)s.batch * s.kv_heads * s.n_groups, 0};
+    const SelectParams p{s, d_scores, top, first, local, d_count, d_index, (int64_t)s.batch * s.kv_heads * s.n_groups, 0,
+                         make_fastdiv((uint32_t)s.n_groups), make_fastdiv((uint32_t)s.kv_heads), make_fastdiv((uint32_t)s.block)};
     const int n = s.n_blocks;
     if (n <= 64) launch_select<1, 1>(p, stream);
     else if (n <= 128) launch_select<1, 2>(p, stream);
