@@ -94,14 +94,15 @@ struct TileReader {
         col_at ^= 32 * kRow;
         asm volatile("" : "+v"(row_at), "+v"(col_at));
     }
-    // A operand, rows = tile rows 32 block + c, dims 16 ks + 8 half .. + 7.  pair: tiles 2 pair and 2 pair + 1
-    __device__ __forceinline__ frag8 rows(int pair, int block, int ks) const {
-        return *(LDS_PTR(const frag8))(uintptr_t)((row_at ^ (ks << 5)) + pair * 2 * kTile + 32 * block * kRow);
+    // A operand, rows = tile rows 32 block + c, dims 16 ks + 8 half .. + 7.  pair: tiles 2 pair and 2 pair + 1; odd: the second of
+    // them, for callers that do not flip
+    __device__ __forceinline__ frag8 rows(int pair, int block, int ks, int odd = 0) const {
+        return *(LDS_PTR(const frag8))(uintptr_t)((row_at ^ (ks << 5)) + (2 * pair + odd) * kTile + 32 * block * kRow);
     }
     // A operand, rows = dims 32 db + c, contracted over 16 tile rows: 32 block + 16 s2 + accumulator order.  (8 rows on the swizzle
     // differs in its lowest bit.)
-    __device__ __forceinline__ frag8 cols(int pair, int block, int s2, int db) const {
-        const uint32_t at = col_at ^ (db << 6), off = pair * 2 * kTile + (32 * block + 16 * s2) * kRow;
+    __device__ __forceinline__ frag8 cols(int pair, int block, int s2, int db, int odd = 0) const {
+        const uint32_t at = col_at ^ (db << 6), off = (2 * pair + odd) * kTile + (32 * block + 16 * s2) * kRow;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(at + off));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)((at ^ 16) + off + 8 * kRow));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -223,13 +224,15 @@ struct KeyLoader {
         }
     }
     // Keys behind the last that some row sees are not read: the last one stands for them, and they are masked.
-    __device__ __forceinline__ void issue(int start, uint8_t* k_tile, uint8_t* v_tile, int wave) const {
+    __device__ __forceinline__ void issue(const uint8_t* head, int64_t pitch, int start, uint8_t* tile, int wave) const {
         const int first = min(start, last), left = last - first;
-        const uint8_t *kb = K + first * pitch_k, *vb = V + first * pitch_v;
+        const uint8_t* const base = head + first * pitch;
 #pragma unroll
-        for (int k = 0; k < LPW; ++k) load_lds(kb, (uint32_t)min(row[k], left) * (uint32_t)pitch_k + col[k], k_tile + (wave * LPW + k) * 1024);
-#pragma unroll
-        for (int k = 0; k < LPW; ++k) load_lds(vb, (uint32_t)min(row[k], left) * (uint32_t)pitch_v + col[k], v_tile + (wave * LPW + k) * 1024);
+        for (int k = 0; k < LPW; ++k) load_lds(base, (uint32_t)min(row[k], left) * (uint32_t)pitch + col[k], tile + (wave * LPW + k) * 1024);
+    }
+    __device__ __forceinline__ void issue(int start, uint8_t* k_tile, uint8_t* v_tile, int wave) const {
+        issue(K, pitch_k, start, k_tile, wave);
+        issue(V, pitch_v, start, v_tile, wave);
     }
 };
 

@@ -5,6 +5,8 @@
 // TEAMS such sets that take the two units of a tile each (few rows), and walks the list, or with `splits` a share of
 // it, in tiles of 64 keys through double-buffered LDS.
 #pragma once
+#include <type_traits>
+
 #include "sequence_attn.h"
 
 namespace grat {
@@ -63,68 +65,175 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     // (a list's last tile may lack its second unit; one of a part that ends inside the list does not)
     auto unit_start = [&](int i) { return i < n_units ? __builtin_amdgcn_readfirstlane(s_units[u_first + i]) : kNoUnit; };
 
-    auto block = [&](int hb, int start) {
-        if (start >= most) return;   // nobody in this wave sees the unit
-        f32x16 S;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(0, hb, ks), qf[ks], S);
+    auto mask = [&](f32x16& S, int start) {
         if (start + kUnit > least) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (start + 8 * (i >> 2) + 4 * half + (i & 3) >= limit) S[i] = -INFINITY;
         }
-        uint32_t pw[8];
+    };
+    auto weigh = [&](const f32x16& S, uint32_t (&w)[8]) {   // weights against the reference; this lane's sum of them
+        const float mc = m_ref * c;
         float ls0 = 0.f, ls1 = 0.f;
-        auto weigh = [&]() {
-            const float mc = m_ref * c;
-            ls0 = ls1 = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float a = __builtin_amdgcn_exp2f(fmaf(S[i], c, -mc)), b = __builtin_amdgcn_exp2f(fmaf(S[i + 1], c, -mc));
-                pw[i >> 1] = E::pack(a, b);
-                ls0 += a;
-                ls1 += b;
+        for (int i = 0; i < 16; i += 2) {
+            const float a = __builtin_amdgcn_exp2f(fmaf(S[i], c, -mc)), b = __builtin_amdgcn_exp2f(fmaf(S[i + 1], c, -mc));
+            w[i >> 1] = E::pack(a, b);
+            ls0 += a;
+            ls1 += b;
+        }
+        return ls0 + ls1;
+    };
+    // The rare path: a block's sum has left the safe range.  The true maximum, and everything against it.
+    auto refresh = [&](const f32x16& S, uint32_t (&w)[8]) {
+        float mx = S[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i]);
+        const float m_new = fmaxf(m_ref, max_across_halves(mx));
+        const float alpha = __builtin_amdgcn_exp2f((m_ref - m_new) * c);
+        m_ref = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
+        return weigh(S, w);
+    };
+    auto outside = [&](float ls) { return __builtin_amdgcn_ballot_w64(!(ls < E::kSumLimit)) != 0; };
+
+    if constexpr (TEAMS == 2) {
+        // few rows: latency is what counts, a block after the other
+        auto block = [&](int start) {
+            if (start >= most) return;   // nobody in this wave sees the unit
+            f32x16 S;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(0, 0, ks), qf[ks], S);
+            mask(S, start);
+            uint32_t pw[8];
+            float ls = weigh(S, pw);
+            if (outside(ls)) ls = refresh(S, pw);
+            l_run += ls;
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2) {
+                const frag8 w = __builtin_bit_cast(frag8, make_uint4(pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]));
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db) oacc[db] = E::mfma(read.cols(1, 0, s2, db), w, oacc[db]);
             }
         };
-        weigh();
-        if (__builtin_amdgcn_ballot_w64(!(ls0 + ls1 < E::kSumLimit)) != 0) {   // the rare path: the true maximum, and everything against it
-            float mx = S[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i]);
-            const float m_new = fmaxf(m_ref, max_across_halves(mx));
-            const float alpha = __builtin_amdgcn_exp2f((m_ref - m_new) * c);
-            m_ref = m_new;
-            l_run *= alpha;
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
-            weigh();
-        }
-        l_run += ls0 + ls1;
-#pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-            const frag8 w = __builtin_bit_cast(frag8, make_uint4(pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]));
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db) oacc[db] = E::mfma(read.cols(1, hb, s2, db), w, oacc[db]);
-        }
-    };
-
-    if (n_tiles > 0) {
-        load.issue(unit_start(load.my_unit), lds[0], lds[2], wave);
+        if (n_tiles > 0) load.issue(unit_start(load.my_unit), lds[0], lds[2], wave);
         for (int t = 0; t < n_tiles; ++t) {
             const int next = unit_start(2 * t + 2 + load.my_unit);
             tile_barrier();
             if (t + 1 < n_tiles) load.issue(next, lds[(t + 1) & 1], lds[2 + ((t + 1) & 1)], wave);
-            if constexpr (TEAMS == 1) {
-                block(0, unit_start(2 * t));
-                block(1, unit_start(2 * t + 1));
-            } else {
-                block(0, unit_start(2 * t + team));
-            }
+            block(unit_start(2 * t + team));
             read.flip();
+        }
+    } else {
+        // Between two barriers one stream of instructions, pipelined by units: while the matrix pipe forms the scores of a unit, the vector
+        // ALU weighs those of the unit before, and the matrix pipe adds the one before that to O.  A step is two such halves: K of
+        // tile t and V of tile t - 1.  The three do not depend on each other, so every product is followed by its share of the vector work
+        // (6 vector instructions fit behind one) and by the read of the fragment for the product kAhead later.
+        constexpr int kAhead = 2, kN = D / 16, kM = 2 * (D / 32);
+        f32x16 S[2];
+        uint32_t pw[2][8];
+        int ahead = unit_start(load.my_unit), here = 0;   // first keys of this wave's pieces of tile t + 1 and t
+        int late = kNoUnit;                               // ... of the second unit of tile t - 1
+        auto step = [&](auto odd_c, auto first_c, auto last_c, int t) {
+            constexpr int kOdd = decltype(odd_c)::value;   // t & 1
+            constexpr bool kScores = !decltype(last_c)::value, kAdds = !decltype(first_c)::value;
+            constexpr int kItems = (kScores ? kN : 0) + (kAdds ? kM : 0);
+            const int start0 = kScores ? unit_start(2 * t) : 0, start1 = kScores ? unit_start(2 * t + 1) : 0;
+            here = ahead;
+            ahead = unit_start(2 * t + 2 + load.my_unit);
+            tile_barrier();
+            if (t + 1 < n_tiles) load.issue(load.K, load.pitch_k, ahead, lds[kOdd ^ 1], wave);
+            if (kScores) load.issue(load.V, load.pitch_v, here, lds[2 + kOdd], wave);
+            frag8 fr[2 * kItems];
+            auto fetch = [&](int i) {
+                const int h = i / kItems, j = i % kItems;
+                if (kScores && j < kN) fr[i] = read.rows(0, h, j, kOdd);
+                else fr[i] = read.cols(1, h, (j - (kScores ? kN : 0)) / (D / 32), (j - (kScores ? kN : 0)) % (D / 32), kOdd ^ 1);
+            };
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) fetch(i);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool weighs = h == 0 ? kAdds : kScores;   // half 0: the second unit of tile t - 1, half 1: the first of tile t
+                f32x16& W = S[h ^ 1];
+                float e0[8], t1[8], ls0 = 0.f, ls1 = 0.f, mc = 0.f;
+                if (weighs) {
+                    mask(W, h == 0 ? late : start0);
+                    mc = m_ref * c;
+                }
+                auto chunk = [&](int i) {   // 16 of them: a pair of scores takes two
+                    const int g = i >> 1;
+                    if ((i & 1) == 0) {
+                        t1[g] = fmaf(W[2 * g + 1], c, -mc);
+                        e0[g] = __builtin_amdgcn_exp2f(fmaf(W[2 * g], c, -mc));
+                    } else {
+                        const float e1 = __builtin_amdgcn_exp2f(t1[g]);
+                        pw[h ^ 1][g] = E::pack(e0[g], e1);
+                        asm volatile("" : "+v"(pw[h ^ 1][g]));   // (keeps the conversion here: its first use is a block later)
+                        ls0 += e0[g];
+                        ls1 += e1;
+                    }
+                };
+#pragma unroll
+                for (int j = 0; j < kItems; ++j) {
+                    const int i = h * kItems + j;
+                    if (i + kAhead < 2 * kItems) fetch(i + kAhead);
+                    if (kScores && j < kN) {
+                        f32x16 zero;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) zero[r] = 0.f;
+                        S[h] = E::mfma(fr[i], qf[j], j == 0 ? zero : S[h]);
+                    } else {
+                        const int a = j - (kScores ? kN : 0), s2 = a / (D / 32), db = a % (D / 32);
+                        const uint32_t* const x = &pw[h][4 * s2];
+                        oacc[db] = E::mfma(fr[i], __builtin_bit_cast(frag8, make_uint4(x[0], x[1], x[2], x[3])), oacc[db]);
+                    }
+                    if (weighs) {
+#pragma unroll
+                        for (int k = 16 * j / kItems; k < 16 * (j + 1) / kItems; ++k) chunk(k);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (weighs) {
+                    float ls = ls0 + ls1;
+                    if (outside(ls)) ls = refresh(W, pw[h ^ 1]);
+                    l_run += ls;
+                }
+            }
+            late = start1;
+        };
+        using std::false_type;
+        using std::true_type;
+        using std::integral_constant;
+        constexpr integral_constant<int, 0> even{};
+        constexpr integral_constant<int, 1> odd{};
+        if (n_tiles > 0) {
+            load.issue(load.K, load.pitch_k, ahead, lds[0], wave);
+            if (most == 0) {   // a wave without a row only fetches
+                for (int t = 0; t <= n_tiles; ++t) {
+                    here = ahead;
+                    ahead = unit_start(2 * t + 2 + load.my_unit);
+                    tile_barrier();
+                    if (t + 1 < n_tiles) load.issue(load.K, load.pitch_k, ahead, lds[(t + 1) & 1], wave);
+                    if (t < n_tiles) load.issue(load.V, load.pitch_v, here, lds[2 + (t & 1)], wave);
+                }
+            } else {
+                step(even, true_type{}, false_type{}, 0);
+                int t = 1;
+                for (; t + 1 < n_tiles; t += 2) {
+                    step(odd, false_type{}, false_type{}, t);
+                    step(even, false_type{}, false_type{}, t + 1);
+                }
+                if (t < n_tiles) step(odd, false_type{}, false_type{}, t);
+                if (n_tiles & 1) step(odd, false_type{}, true_type{}, n_tiles);
+                else step(even, false_type{}, true_type{}, n_tiles);
+            }
         }
     }
     float l = sum_across_halves(l_run);
