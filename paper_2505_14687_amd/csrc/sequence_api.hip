@@ -171,7 +171,7 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
         g.delta = (float*)(work + take(plan, (g.stats + 1) * 4));
         g.lse2 = (float*)(work + take(plan, (g.stats + 1) * 4));
         g.bits = (uint32_t*)(work + take(plan, blocks * g.words * 4));
-        g.counters = (int32_t*)(work + take(plan, 4 * 4));
+        g.counters = (int32_t*)(work + take(plan, 5 * 4));
         g.groups = (int32_t*)(work + take(plan, entries * 4));
         g.parts = (int4*)(work + take(plan, most_parts * 16));
         g.part_slot = (int32_t*)(work + take(plan, most_parts * 4));

@@ -36,7 +36,7 @@ struct GradParams {
     float* lse2;           // as many: lse in base 2
     int64_t stats;         // batch * q_heads * n_q
     uint32_t* bits;        // [blocks of all heads][words]
-    int32_t* counters;     // entries of `groups` in use, parts, slots in use, blocks of more than one part
+    int32_t* counters;     // entries of `groups` in use, long parts, slots in use, blocks of more than one part, short parts
     int32_t* groups;       // the groups that list a block, block after block
     int4* parts;           // block (of all heads), first group's place in `groups`, rows from and to
     int32_t* part_slot;    // of every part: its slot, -1: its block has no other

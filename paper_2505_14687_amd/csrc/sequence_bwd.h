@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void grad_delta_kernel(SelParams p, GradParams
     constexpr int L = D / 8;
     const int64_t zeros = (int64_t)g.blocks * g.words;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < zeros; i += (int64_t)gridDim.x * 256) g.bits[i] = 0;
-    if (blockIdx.x == 0 && threadIdx.x < 4) g.counters[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 5) g.counters[threadIdx.x] = 0;
     const int64_t at = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
     if (at >= rows) return;
     uint32_t bh, n, b, h;
@@ -77,11 +77,15 @@ __global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
     const int team = TEAMS == 1 ? 0 : wave / KW, key_wave = wave % KW;
 
-    const int tiles = (int)g.fd_tiles.d, work = g.counters[1] * tiles, per_xcd = (work + 7) / 8;
-    const int item = ((int)blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per_xcd || item >= work) return;
+    // The XCDs walk the heads together, kChunk items at a time each: Q and dO of one or two K/V heads are in use at a time, which the memory-side
+    // cache holds.
+    constexpr int kChunk = 16;
+    const int tiles = (int)g.fd_tiles.d, longs = g.counters[1], work = (longs + g.counters[4]) * tiles;
+    const int turn = (int)blockIdx.x >> 3, item = ((turn / kChunk) * 8 + ((int)blockIdx.x & 7)) * kChunk + turn % kChunk;
+    if (item >= work) return;
     uint32_t part_id, tile_in_block, b_, h_;
     fdivmod((uint32_t)item, g.fd_tiles, part_id, tile_in_block);
+    if ((int)part_id >= longs) part_id = (uint32_t)(g.most_parts - 1 - ((int)part_id - longs));   // short parts: from the back
     const int4 part = g.parts[part_id];
     const uint32_t bh = (uint32_t)part.x / (uint32_t)s.n_blocks, block = (uint32_t)part.x - bh * (uint32_t)s.n_blocks;
     fdivmod(bh, p.fd_kv_heads, b_, h_);
@@ -139,11 +143,17 @@ __global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad
             uint8_t *qt = lds[t & 1], *dt = lds[2 + (t & 1)];
             int chunk = piece_col;
             asm volatile("" : "+v"(chunk));   // (columns are formed here: kept, they take two registers each)
+            const uint8_t *q[LPW], *d[LPW];
+#pragma unroll
+            for (int k = 0; k < LPW; ++k) {   // (all read ahead of the first load: nothing moves across one)
+                q[k] = m.q[piece_row + k * kRows];
+                d[k] = m.d[piece_row + k * kRows];
+            }
 #pragma unroll
             for (int k = 0; k < LPW; ++k) {
                 const int col = (chunk ^ tile_swizzle<D>((wave * LPW + k) * kRows)) << 4;
-                load_lds(m.q[piece_row + k * kRows] + col, qt + (wave * LPW + k) * 1024);
-                load_lds(m.d[piece_row + k * kRows] + col, dt + (wave * LPW + k) * 1024);
+                load_lds(q[k] + col, qt + (wave * LPW + k) * 1024);
+                load_lds(d[k] + col, dt + (wave * LPW + k) * 1024);
             }
         };
         TileReader<D> read(lane, lds[0], team);
@@ -459,7 +469,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
 template <int KW, int TEAMS, bool F16, int D>
 inline void launch_grad_keys(const SelParams& p, const GradParams& g, hipStream_t stream) {
     const int64_t items = (int64_t)g.most_parts * g.fd_tiles.d;
-    hipLaunchKernelGGL((grad_keys_kernel<KW, TEAMS, F16, D>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(KW * TEAMS * 64), 0, stream, p, g);
+    hipLaunchKernelGGL((grad_keys_kernel<KW, TEAMS, F16, D>), dim3((unsigned)((items + 127) / 128 * 128)), dim3(KW * TEAMS * 64), 0, stream, p, g);
     if (g.most_joins > 0)
         hipLaunchKernelGGL((grad_join_kernel<F16, D>), dim3((unsigned)(g.most_joins * g.fd_tiles.d * kJoinShare)), dim3(256), 0, stream, p, g,
                            32 * KW);

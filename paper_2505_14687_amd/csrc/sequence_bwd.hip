@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256) void grad_bits_kernel(SelParams p, GradParams 
 constexpr int kListBlocks = 16;   // 4 in small launches, for which it is latency that counts
 
 __global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams g, int per_group) {
-    __shared__ int s_n[kListBlocks], s_at[4][kListBlocks + 1], s_base[4];
+    __shared__ int s_n[kListBlocks], s_at[5][kListBlocks], s_base[5];
     const int block0 = (int)blockIdx.x * per_group, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int here = min(per_group, g.blocks - block0);
     for (int i = wave; i < here; i += 4) {
@@ -36,20 +36,23 @@ __global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams
     }
     __syncthreads();
     auto parts_of = [&](int n) { return (int)max((int64_t)1, ((int64_t)n * p.rows + g.part_rows - 1) / g.part_rows); };
-    if (threadIdx.x < 4) {   // groups, parts, slots, joins
+    // Long parts go to the front of `parts`, short ones to its back: the launch ends with these.
+    auto is_long = [&](int n) { return (int64_t)n * p.rows * 2 >= (int64_t)g.part_rows; };
+    if (threadIdx.x < 5) {   // groups, long parts, slots, blocks of several parts, short parts
         const int what = threadIdx.x;
         int sum = 0;
         for (int i = 0; i < here; ++i) {
             const int n = s_n[i], parts = parts_of(n);
             s_at[what][i] = sum;
-            sum += what == 0 ? n : what == 1 ? parts : parts == 1 ? 0 : what == 2 ? parts : 1;
+            sum += what == 0 ? n : what == 1 ? (is_long(n) ? parts : 0) : what == 4 ? (is_long(n) ? 0 : parts) : parts == 1 ? 0 : what == 2 ? parts : 1;
         }
         s_base[what] = sum > 0 ? atomicAdd(&g.counters[what], sum) : 0;
     }
     __syncthreads();
     for (int i = wave; i < here; i += 4) {
         const int block = block0 + i, n = s_n[i], parts = parts_of(n);
-        const int first = s_base[0] + s_at[0][i], part0 = s_base[1] + s_at[1][i], slot0 = s_base[2] + s_at[2][i];
+        const int first = s_base[0] + s_at[0][i], slot0 = s_base[2] + s_at[2][i];
+        const int part0 = is_long(n) ? s_base[1] + s_at[1][i] : g.most_parts - 1 - (s_base[4] + s_at[4][i]);   // (a short part is its block's only one)
         const uint32_t* const words = g.bits + (int64_t)block * g.words;
         int at = first;
         for (int w0 = 0; w0 < g.words; w0 += 64) {
