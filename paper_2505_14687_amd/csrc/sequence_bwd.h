@@ -8,7 +8,7 @@
 // its groups in ascending order.  Blocks that many groups list (the first one: all of them) are cut into parts of about equal length,
 // whose sums are added up in order.
 //
-// Steps: D | bits | lists of every block, parts | dQ | dK, dV | joined parts.
+// Steps: cleared bits | bits | lists of every block, parts | D and dQ | dK, dV | joined parts.
 #pragma once
 #include <type_traits>
 
@@ -22,37 +22,6 @@ constexpr float kWeightBits = 12.f, kWeightScale = 4096.f;
 
 template <bool F16>
 __device__ __forceinline__ float score_grad(float dp, float delta) { return F16 ? fmaf(dp, 1.f / kWeightScale, -delta) : dp - delta; }
-
-// D and lse in base 2 of every row, and the scratch memory that has to be 0 (by a kernel: recorded into graphs like any other launch).
-template <bool F16, int D>
-__global__ __launch_bounds__(256) void grad_delta_kernel(SelParams p, GradParams g, int64_t rows, FastDiv fd_n, FastDiv fd_h) {
-    typedef typename Vec16<std::conditional_t<F16, _Float16, __bf16>>::type vec;
-    constexpr int L = D / 8;
-    const int64_t zeros = (int64_t)g.blocks * g.words;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < zeros; i += (int64_t)gridDim.x * 256) g.bits[i] = 0;
-    if (blockIdx.x == 0 && threadIdx.x < 5) g.counters[threadIdx.x] = 0;
-    const int64_t at = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    if (at >= rows) return;
-    uint32_t bh, n, b, h;
-    fdivmod((uint32_t)at, fd_n, bh, n);
-    fdivmod(bh, fd_h, b, h);
-    const int c = threadIdx.x % L;
-    const vec x = *(const vec*)(row_address(g.dO, (int)b, (int)h, (int)n) + 16 * c), y = *(const vec*)(row_address(p.O, (int)b, (int)h, (int)n) + 16 * c);
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf((float)x[e], (float)y[e], sum);
-#pragma unroll
-    for (int m = 1; m < L; m *= 2) sum += __shfl_xor(sum, m);
-    if (c == 0) {
-        g.delta[at] = F16 ? sum * (1.f / kWeightScale) : sum;
-        const float lse = p.lse[at];   // (a row that attends nothing weighs 0)
-        g.lse2[at] = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f - (F16 ? kWeightBits : 0.f);
-        if (at == 0) {   // what rows that only fill a tile take
-            g.delta[rows] = 0.f;
-            g.lse2[rows] = INFINITY;
-        }
-    }
-}
 
 // ---- dK, dV ------------------------------------------------------------------------------------
 // A workgroup owns 32 KW keys of one block, K and V of a wave's 32 keys in registers, and streams the Q and dO rows of
@@ -345,9 +314,24 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const frag8*)(q_src + 32 * ks);
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) df[ks] = *(const frag8*)(d_src + 32 * ks);
+    // D, and lse in base 2 (a row that attends nothing weighs 0); the walk over the keys takes both from memory
     const int64_t stat = ((int64_t)it.b * s.q_heads + row.head) * s.n_q + row.query;
-    const float lse2 = g.lse2[stat];
-    float delta = g.delta[stat];
+    const float lse = p.lse[stat], lse2 = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f - (F16 ? kWeightBits : 0.f);
+    float delta = 0.f;
+    {
+        typedef typename Vec16<std::conditional_t<F16, _Float16, __bf16>>::type vec;
+        const uint8_t* const o_src = row_address(p.O, it.b, row.head, row.query) + 16 * half;
+        vec o[D / 16];
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) o[ks] = *(const vec*)(o_src + 32 * ks);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            const vec d = __builtin_bit_cast(vec, df[ks]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)o[ks][e], (float)d[e], delta);
+        }
+        delta = sum_across_halves(delta) * (F16 ? 1.f / kWeightScale : 1.f);
+    }
     const int len = seq_len(s, it.b);
     const int64_t pos = seq_pos(s, it.b, len);
     const int seen = group_seen(s, len, pos, it.g);
@@ -458,7 +442,10 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
 #pragma unroll
             for (int i = 0; i < 16; ++i) dq[db][i] += mine[(db * 16 + i) * 64];
     }
-    if (half == 0 && row.there) g.delta[stat] = delta + (F16 ? sum * (1.f / kWeightScale) : sum);
+    if (half == 0 && row.there) {
+        g.delta[stat] = delta + (F16 ? sum * (1.f / kWeightScale) : sum);
+        g.lse2[stat] = lse2;
+    }
     uint8_t* const stage = &lds[0][0] + (TEAMS == 2 ? 2 * kTile : 0) + row_wave * 4096;   // (two teams: behind what team 0 still reads)
     store_rows<F16, D>(stage, dq, p.scale, lane, [&](int i) -> uint8_t* {
         const GroupRow to(p, it.h, it.g, (it.tile * RW + row_wave) * 32 + i);
@@ -483,9 +470,6 @@ inline void launch_grad_queries(const SelParams& p, const GradParams& g, hipStre
 // tile_rows: 128, 64 or 32; key tiles of 128, 64 or 32 keys
 template <bool F16, int D>
 inline hipError_t launch_bwd(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream) {
-    const int64_t rows = (int64_t)p.s.batch * p.s.q_heads * p.s.n_q;
-    hipLaunchKernelGGL((grad_delta_kernel<F16, D>), dim3((unsigned)((rows + 2048 / D - 1) / (2048 / D))), dim3(256), 0, stream, p, g, rows,
-                       make_fastdiv((uint32_t)p.s.n_q), make_fastdiv((uint32_t)p.s.q_heads));
     launch_grad_lists(p, g, stream);
     if (tile_rows == 128) launch_grad_queries<4, 1, F16, D>(p, g, stream);
     else if (tile_rows == 64) launch_grad_queries<2, 2, F16, D>(p, g, stream);

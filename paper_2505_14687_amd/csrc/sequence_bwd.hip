@@ -3,6 +3,18 @@
 
 namespace grat {
 
+// The scratch memory that has to be 0 (by a kernel: recorded into graphs like any other launch), and what rows that only fill a tile take.
+__global__ __launch_bounds__(256) void grad_clear_kernel(GradParams g) {
+    const int64_t n = (int64_t)g.blocks * g.words;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) g.bits[i] = 0;
+    if (blockIdx.x > 0) return;
+    if (threadIdx.x < 5) g.counters[threadIdx.x] = 0;
+    if (threadIdx.x == 0) {
+        g.delta[g.stats] = 0.f;
+        g.lse2[g.stats] = INFINITY;
+    }
+}
+
 // A bit for every listed block with a key that the group sees.
 __global__ __launch_bounds__(256) void grad_bits_kernel(SelParams p, GradParams g, int64_t entries, FastDiv fd_top) {
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -81,6 +93,8 @@ __global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams
 }
 
 void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stream) {
+    const int64_t clears = ((int64_t)g.blocks * g.words + 1023) / 1024;
+    hipLaunchKernelGGL(grad_clear_kernel, dim3((unsigned)(clears < 2048 ? clears : 2048)), dim3(256), 0, stream, g);
     const int64_t entries = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.max_blocks;
     hipLaunchKernelGGL(grad_bits_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, stream, p, g, entries,
                        make_fastdiv((uint32_t)p.max_blocks));
