@@ -1,7 +1,7 @@
 """Token sequences: rotary positions, and attention over key blocks that a score selects (include/grat_sequence.h).
 
-Marshalling only, like grat.py: every step runs in the library's kernels, on the current stream or the one that is given.
-Results and scratch memory are allocated for the stream that the call runs on.
+Marshalling only, like grat.py (ordinary calls on the current stream in csrc/binding.cpp, all others here): every step runs in the
+library's kernels, on the current stream or the one that is given.  Results and scratch memory are allocated for the stream that the call runs on.
 
     table = grat_rotary_table(n_pos, [head_dim // 2])                      # once
     Q, K = grat_rotary(Q, K, table)
@@ -21,7 +21,8 @@ from typing import Optional, Sequence
 
 import torch
 
-from .grat import DTYPES, GRAT_OK, GratError, _i32, _i64, _f32, _vp, lib
+from . import grat
+from .grat import DTYPES, GRAT_OK, GratError, _i32, _i64, _f32, _result, _vp, lib
 
 SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
 LAYOUTS = {"half": 0, "interleaved": 1}
@@ -60,15 +61,27 @@ _SIGNATURES = {
     "grat_selected_attention_bwd": (_i32, [_ps] + [_pt] * 5 + [_vp] + [_pt] * 3 + [_f32, _vp, _vp, _i32, _vp, _vp]),
 }
 _lib = None
+_native = None   # csrc/binding.cpp, as in grat.py; not None once _lib is not
+
+
+class _NoNative:
+    """In the place of _binding where that is not there: it takes no call."""
+    rotary = append = means = scores = select = selected_fwd = selected_bwd = staticmethod(lambda *args: None)
 
 
 def _library() -> ctypes.CDLL:
-    global _lib
+    global _lib, _native
     if _lib is None:
         L = lib()
         for name, (result, arguments) in _SIGNATURES.items():
             getattr(L, name).restype = result
             getattr(L, name).argtypes = arguments
+        native = grat._native
+        if hasattr(native, "set_sequence_library"):
+            native.set_sequence_library(*(ctypes.cast(getattr(L, name), _vp).value for name in _SIGNATURES if name != "grat_rotary_table"))
+        else:
+            native = _NoNative
+        _native = native   # (ahead of _lib: another thread that finds _lib set uses both)
         _lib = L
     return _lib
 
@@ -191,6 +204,10 @@ def grat_rotary(Q, K, table, positions=None, start=None, layout: str = "half", a
 
     positions int32 [B or 1, N, axes], or start int32 [B] (token i is at start + i), or neither (token i is at i).  inverse: the
     gradient.  out: a pair of tensors to write to; Q and K themselves for a rotation in place."""
+    _library()
+    r = _native.rotary(Q, K, table, positions, start, LAYOUTS.get(layout), axis_pairs, inverse, out, stream)
+    if r is not None:
+        return _result(r, "grat_rotary")
     _check("Q", Q)
     if K is not None:
         _check("K", K, (Q.shape[0], K.shape[1] if isinstance(K, torch.Tensor) and K.dim() == 4 else 0, Q.shape[2], Q.shape[3]), Q)
@@ -210,6 +227,10 @@ def grat_rotary(Q, K, table, positions=None, start=None, layout: str = "half", a
 
 def grat_rotary_append(Q, K, V, table, K_cache, V_cache, start, layout: str = "half", out=None, stream=None):
     """Serving: returns Q turned, and writes K turned and V to rows start[b] + i of the caches.  Rows outside of them are dropped."""
+    _library()
+    r = _native.append(Q, K, V, table, K_cache, V_cache, start, LAYOUTS.get(layout), out, stream)
+    if r is not None:
+        return _result(r, "grat_rotary_append")
     _check("Q", Q)
     _check("K", K, None, Q)
     B, _, N, d = Q.shape
@@ -236,6 +257,10 @@ def grat_rotary_append(Q, K, V, table, K_cache, V_cache, start, layout: str = "h
 def grat_block_means(K, block: int, k_len=None, new: int = 0, out=None, stream=None):
     """Mean of the valid keys of every block, fp32 [B, Hkv, blocks, d].  new > 0: only the blocks with one of the last `new` valid
     keys are written, to `out`, which holds the others."""
+    _library()
+    r = _native.means(K, block, k_len, new, out, stream)
+    if r is not None:
+        return _result(r, "grat_block_means")
     _check("K", K)
     _positive(block=block)
     B, H, M, d = K.shape
@@ -254,6 +279,10 @@ def grat_block_means(K, block: int, k_len=None, new: int = 0, out=None, stream=N
 def grat_block_scores(Q, means, scale: float, q_group: int, block: int, n_k: int, causal: bool = True, k_len=None, q_pos=None,
                       out=None, stream=None):
     """Score of every query group for every key block, fp32 [B, Hkv, groups, blocks]; -inf for blocks that a group does not see."""
+    _library()
+    r = _native.scores(Q, means, scale, q_group, block, n_k, causal, k_len, q_pos, out, stream)
+    if r is not None:
+        return _result(r, "grat_block_scores")
     _check("Q", Q)
     _positive(q_group=q_group, block=block, n_k=n_k)
     B, Hq, N, d = Q.shape
@@ -264,7 +293,7 @@ def grat_block_scores(Q, means, scale: float, q_group: int, block: int, n_k: int
     where = _flat("means", means, torch.float32, (B, Hkv, blocks, d), Q.device)
     seq = _Sequence(DTYPES[Q.dtype], B, Hq, Hkv, d, N, int(n_k), int(q_group), int(block), int(bool(causal)),
                     _ints("k_len", k_len, B, Q.device), _ints("q_pos", q_pos, B, Q.device))
-    need = _library().grat_block_scores_work(ctypes.byref(seq))
+    need = _lib.grat_block_scores_work(ctypes.byref(seq))
     context, s = _on(stream, Q.device)
     with context:
         work = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
@@ -278,6 +307,10 @@ def grat_block_scores(Q, means, scale: float, q_group: int, block: int, n_k: int
 def grat_select_blocks(scores, top: int, first: int, local: int, n_q: int, n_k: int, q_group: int, block: int, causal: bool = True,
                        k_len=None, q_pos=None, stream=None):
     """The lists: (count int32 [B, Hkv, groups], index int32 [B, Hkv, groups, top]), ascending, -1 behind a list's end."""
+    _library()
+    r = _native.select(scores, top, first, local, n_q, n_k, q_group, block, causal, k_len, q_pos, stream)
+    if r is not None:
+        return _result(r, "grat_select_blocks")
     _positive(top=top, n_q=n_q, n_k=n_k, q_group=q_group, block=block)
     if not isinstance(scores, torch.Tensor) or scores.dim() != 4:
         raise ValueError("scores must have shape [B, Hkv, groups, blocks]")
@@ -315,13 +348,17 @@ def _attention_args(Q, K, V, count, index, q_group, block, causal, k_len, q_pos)
 
 
 def _work(seq: _Sequence, top: int, backward: int, device):
-    need = _library().grat_selected_attention_work(ctypes.byref(seq), top, backward)
+    need = _lib.grat_selected_attention_work(ctypes.byref(seq), top, backward)
     return torch.empty(need, dtype=torch.uint8, device=device) if need else None
 
 
 def grat_selected_attention_fwd(Q, K, V, scale: float, count, index, q_group: int, block: int, causal: bool = True, k_len=None,
                                 q_pos=None, return_lse: bool = False, out=None, stream=None):
     """O = softmax(scale * Q K^T over the listed keys that a row sees) V; with return_lse also the rows' log-sum-exp, fp32 [B, Hq, N]."""
+    _library()
+    r = _native.selected_fwd(Q, K, V, scale, count, index, q_group, block, causal, k_len, q_pos, return_lse, out, stream)
+    if r is not None:
+        return _result(r, "grat_selected_attention_fwd")
     seq, lists = _attention_args(Q, K, V, count, index, q_group, block, causal, k_len, q_pos)
     context, s = _on(stream, Q.device)
     with context:
@@ -337,6 +374,10 @@ def grat_selected_attention_fwd(Q, K, V, scale: float, count, index, q_group: in
 def grat_selected_attention_bwd(dO, Q, K, V, O, lse, scale: float, count, index, q_group: int, block: int, causal: bool = True,
                                 k_len=None, q_pos=None, out=None, stream=None):
     """(dQ, dK, dV) of grat_selected_attention_fwd for dO; O and lse as it returned them.  out: three tensors to write to."""
+    _library()
+    r = _native.selected_bwd(Q, K, V, scale, count, index, q_group, block, causal, k_len, q_pos, dO, O, lse, out, stream)
+    if r is not None:
+        return _result(r, "grat_selected_attention_bwd")
     seq, lists = _attention_args(Q, K, V, count, index, q_group, block, causal, k_len, q_pos)
     _check("dO", dO, Q.shape, Q)
     _check("O", O, Q.shape, Q)
