@@ -158,6 +158,7 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
         g.blocks = (int32_t)blocks;
         g.words = (s.n_groups + 31) / 32;
         g.fd_rows = make_fastdiv((uint32_t)rows);
+        g.fd_top = make_fastdiv((uint32_t)max_blocks);
         g.fd_tiles = make_fastdiv((uint32_t)(s.block / plan.tile_keys));
         // Parts of the rows that a block has on average: entries of all lists times the rows of a group, over all blocks.
         const int64_t entries = lists * std::min(max_blocks, s.n_blocks), all_rows = entries * rows;

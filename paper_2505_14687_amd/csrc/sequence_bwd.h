@@ -8,7 +8,7 @@
 // its groups in ascending order.  Blocks that many groups list (the first one: all of them) are cut into parts of about equal length,
 // whose sums are added up in order.
 //
-// Steps: cleared bits | bits | lists of every block, parts | D and dQ | dK, dV | joined parts.
+// Steps: D and dQ | lists of every block, parts | dK, dV | joined parts.
 #pragma once
 #include <type_traits>
 
@@ -302,6 +302,11 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
     const Item it(p);
+    if (blockIdx.x == 0 && threadIdx.x < 5) {   // for the launches that follow: what they count, and what rows that only fill a tile take
+        g.counters[threadIdx.x] = 0;
+        g.delta[g.stats] = 0.f;
+        g.lse2[g.stats] = INFINITY;
+    }
     if (it.idle(p)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int team = TEAMS == 1 ? 0 : wave / RW, row_wave = wave % RW, half = lane >> 5;
@@ -470,10 +475,10 @@ inline void launch_grad_queries(const SelParams& p, const GradParams& g, hipStre
 // tile_rows: 128, 64 or 32; key tiles of 128, 64 or 32 keys
 template <bool F16, int D>
 inline hipError_t launch_bwd(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream) {
-    launch_grad_lists(p, g, stream);
     if (tile_rows == 128) launch_grad_queries<4, 1, F16, D>(p, g, stream);
     else if (tile_rows == 64) launch_grad_queries<2, 2, F16, D>(p, g, stream);
     else launch_grad_queries<1, 2, F16, D>(p, g, stream);
+    launch_grad_lists(p, g, stream);
     if (tile_keys == 128) launch_grad_keys<4, 1, F16, D>(p, g, stream);
     else if (tile_keys == 64) launch_grad_keys<2, 2, F16, D>(p, g, stream);
     else launch_grad_keys<1, 2, F16, D>(p, g, stream);
