@@ -128,7 +128,7 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
     const int64_t rows = (int64_t)s.q_group * s.share, lists = (int64_t)s.batch * s.kv_heads * s.n_groups;
     const int64_t blocks = (int64_t)s.batch * s.kv_heads * s.n_blocks, D = seq->head_dim;
     if ((int64_t)max_blocks * s.block > (1 << 18) || lists * max_blocks >= kMaxRows || blocks >= (1 << 24)) return GRAT_ERR_UNSUPPORTED;
-    if ((int64_t)s.batch * s.q_heads * s.n_q >= kMaxRows || lists * rows >= 2 * kMaxRows || lists * ((rows + 31) / 32) >= (1 << 23))
+    if ((int64_t)s.batch * s.q_heads * s.n_q >= kMaxRows / 2 || lists * rows >= kMaxRows || lists * ((rows + 31) / 32) >= (1 << 23))
         return GRAT_ERR_UNSUPPORTED;
     p.max_blocks = max_blocks;
     p.scale = scale;
@@ -163,7 +163,8 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
         // Parts of the rows that a block has on average: entries of all lists times the rows of a group, over all blocks.
         const int64_t entries = lists * std::min(max_blocks, s.n_blocks), all_rows = entries * rows;
         const int64_t part = std::max<int64_t>(512, (all_rows / blocks + 63) / 64 * 64);
-        g.part_rows = (int32_t)std::min<int64_t>(part, kMaxRows);
+        g.part_rows = (int32_t)std::min<int64_t>(part, kMaxRows / 2);
+        g.fd_part = make_fastdiv((uint32_t)g.part_rows);
         const int64_t most_parts = blocks + all_rows / g.part_rows, most_slots = 2 * (all_rows / g.part_rows) + 1;
         if (most_parts * (s.block / plan.tile_keys) >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
         g.most_parts = (int32_t)most_parts;

@@ -43,7 +43,7 @@ struct GradParams {
     int4* joins;           // blocks of more than one part: block, first slot, parts
     float* slots;          // sums of a part: [key tile of the block][dK, dV][key][D]
     int32_t words, blocks, most_parts, most_joins, part_rows;
-    FastDiv fd_rows, fd_tiles, fd_top;   // by rows of a group; by key tiles of a block; by max_blocks
+    FastDiv fd_rows, fd_tiles, fd_top, fd_part;   // by rows of a group; key tiles of a block; max_blocks; part_rows
 };
 
 // Dispatch by element type and head_dim (sequence_fwd_*.hip, sequence_bwd_*.hip).

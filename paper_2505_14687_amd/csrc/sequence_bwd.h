@@ -391,17 +391,86 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
             }
         }
     };
+    // A tile of two units as one stream of instructions.  Every product is followed by its share of the vector work: P of a unit behind its
+    // dO V^T, its dS behind the next unit's scores (unit 0) or unit 0's dS K (unit 1); and by the read of the fragment for the
+    // product kAhead later.  Keys that a row does not see get their -infinity as what their scores are added to.
+    auto tile = [&](int start0, int start1) {
+        constexpr int kAhead = 2, kN = D / 16, kM = 2 * (D / 32), kAll = 4 * kN + 2 * kM;
+        if (start0 >= most && start1 >= most) return;   // nobody in this wave sees the units
+        frag8 fr[kAll];
+        auto fetch = [&](int i) {   // S T of unit 0, S T of unit 1, dS K of both
+            if (i < 4 * kN) fr[i] = read.rows(i / kN % 2, i / (2 * kN), i % kN);
+            else fr[i] = read.cols(0, (i - 4 * kN) / kM, (i - 4 * kN) % kM / (D / 32), (i - 4 * kN) % (D / 32));
+        };
+        f32x16 S[2], T[2], zero;
+        uint32_t dw[2][8];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[0][i] = S[1][i] = zero[i] = 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int start = u == 0 ? start0 : start1;
+            if (start + kUnit > least) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) S[u][i] = start + 8 * (i >> 2) + 4 * half + (i & 3) < limit ? 0.f : -INFINITY;
+            }
+        }
+        auto weigh = [&](int u, int j) {   // pair j
+            S[u][2 * j] = __builtin_amdgcn_exp2f(fmaf(S[u][2 * j], c, -lse2));
+            S[u][2 * j + 1] = __builtin_amdgcn_exp2f(fmaf(S[u][2 * j + 1], c, -lse2));
+        };
+        auto grad = [&](int u, int j) {
+            const float d0 = S[u][2 * j] * score_grad<F16>(T[u][2 * j], delta), d1 = S[u][2 * j + 1] * score_grad<F16>(T[u][2 * j + 1], delta);
+            sum += d0 + d1;
+            dw[u][j] = E::pack(d0, d1);
+            asm volatile("" : "+v"(dw[u][j]));   // (keeps the conversion here: its first use is later)
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fetch(i);
+        auto products = [&](auto u_c, auto what_c, auto&& work) {   // what: 0 scores, 1 dO V^T, 2 dS K; work(j): vector work of pair j
+            constexpr int u = decltype(u_c)::value, what = decltype(what_c)::value;
+            constexpr int first = what == 2 ? 4 * kN + u * kM : (2 * u + what) * kN, n = what == 2 ? kM : kN;
+#pragma unroll
+            for (int k = 0; k < n; ++k) {
+                const int i = first + k;
+                if (i + kAhead < kAll) fetch(i + kAhead);
+                if constexpr (what == 0) {
+                    S[u] = E::mfma(fr[i], qf[k], S[u]);
+                } else if constexpr (what == 1) {
+                    T[u] = E::mfma(fr[i], df[k], k == 0 ? zero : T[u]);
+                } else {
+                    const uint32_t* const x = &dw[u][4 * (k / (D / 32))];
+                    dq[k % (D / 32)] = E::mfma(fr[i], __builtin_bit_cast(frag8, make_uint4(x[0], x[1], x[2], x[3])), dq[k % (D / 32)]);
+                }
+#pragma unroll
+                for (int j = 8 * k / n; j < 8 * (k + 1) / n; ++j) work(j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        using std::integral_constant;
+        constexpr integral_constant<int, 0> c0{};
+        constexpr integral_constant<int, 1> c1{};
+        constexpr integral_constant<int, 2> c2{};
+        products(c0, c0, [](int) {});
+        products(c0, c1, [&](int j) { weigh(0, j); });
+        products(c1, c0, [&](int j) { grad(0, j); });
+        products(c1, c1, [&](int j) { weigh(1, j); });
+        products(c0, c2, [&](int j) { grad(1, j); });
+        products(c1, c2, [](int) {});
+    };
     auto walk = [&](auto form_d) {
         load.issue(unit_start(load.my_unit), lds[0], lds[2], wave);
         for (int t = 0; t < n_tiles; ++t) {
-            const int next = unit_start(2 * t + 2 + load.my_unit);
+            const int next = unit_start(2 * t + 2 + load.my_unit), start0 = unit_start(2 * t + (TEAMS == 1 ? 0 : team));
+            const int start1 = TEAMS == 1 ? unit_start(2 * t + 1) : kNoUnit;
             tile_barrier();
             if (t + 1 < n_tiles) load.issue(next, lds[(t + 1) & 1], lds[2 + ((t + 1) & 1)], wave);
-            if constexpr (TEAMS == 1) {
-                block(form_d, 0, unit_start(2 * t));
-                block(form_d, 1, unit_start(2 * t + 1));
+            if constexpr (TEAMS == 2) {
+                block(form_d, 0, start0);
+            } else if constexpr (decltype(form_d)::value) {
+                block(form_d, 0, start0);
+                block(form_d, 1, start1);
             } else {
-                block(form_d, 0, unit_start(2 * t + team));
+                tile(start0, start1);
             }
             read.flip();
         }

@@ -26,9 +26,9 @@ __global__ __launch_bounds__(256) void grad_bits_kernel(SelParams p, GradParams 
 
 // Rows of a block are cut into parts of about p.part_rows.  Long ones go to the front of `parts`, short ones to its back: the launch ends with these.
 __device__ __forceinline__ int parts_of(const SelParams& p, const GradParams& g, int n) {
-    return (int)max((int64_t)1, ((int64_t)n * p.rows + g.part_rows - 1) / g.part_rows);
+    return max(1, (int)fdiv((uint32_t)(n * p.rows) + (uint32_t)g.part_rows - 1u, g.fd_part));   // (a block's rows and a part's are below 2^30)
 }
-__device__ __forceinline__ bool is_long(const SelParams& p, const GradParams& g, int n) { return (int64_t)n * p.rows * 2 >= (int64_t)g.part_rows; }
+__device__ __forceinline__ bool is_long(const SelParams& p, const GradParams& g, int n) { return 2u * (uint32_t)(n * p.rows) >= (uint32_t)g.part_rows; }
 // What a block of n groups takes: groups, long parts, slots, places in `joins`, short parts.
 __device__ __forceinline__ int takes(const SelParams& p, const GradParams& g, int n, int what) {
     const int parts = parts_of(p, g, n);
@@ -36,27 +36,16 @@ __device__ __forceinline__ int takes(const SelParams& p, const GradParams& g, in
 }
 // Writes a block's groups, ascending, and its parts to the places `at` (one wave).
 __device__ __forceinline__ void put_block(const SelParams& p, const GradParams& g, int block, int n, const uint32_t* words, const int (&at)[5], int lane) {
-    int to_group = at[0];
-    for (int w0 = 0; w0 < g.words; w0 += 64) {
-        uint32_t bits = w0 + lane < g.words ? words[w0 + lane] : 0;
-        const int mine = __popc(bits);
-        int before = mine;   // inclusive prefix sum
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2) {
-            const int up = __shfl_up(before, m);
-            if (lane >= m) before += up;
-        }
-        int to = to_group + before - mine;
-        while (bits) {
-            g.groups[to++] = (w0 + lane) * 32 + __builtin_ctz(bits);
-            bits &= bits - 1;
-        }
-        to_group += __shfl(before, 63);
+    int to = at[0];
+    for (int w = 0; w < g.words; w += 2) {   // a group a lane
+        const uint64_t bits = words[w] | (uint64_t)(w + 1 < g.words ? words[w + 1] : 0) << 32;
+        if (bits >> lane & 1) g.groups[to + __popcll(bits & ((1ull << lane) - 1ull))] = 32 * w + lane;
+        to += __popcll(bits);
     }
     const int parts = parts_of(p, g, n), part0 = is_long(p, g, n) ? at[1] : g.most_parts - 1 - at[4];   // (a short part is its block's only one)
-    const int64_t rows = (int64_t)n * p.rows, per = ((rows + parts - 1) / parts + 63) & ~(int64_t)63;     // whole tiles of 64 rows
+    const uint32_t rows = (uint32_t)(n * p.rows), per = ((rows + parts - 1) / (uint32_t)parts + 63u) & ~63u;   // whole tiles of 64 rows
     for (int k = lane; k < parts; k += 64) {
-        g.parts[part0 + k] = make_int4(block, at[0], (int)min(k * per, rows), (int)min((k + 1) * per, rows));
+        g.parts[part0 + k] = make_int4(block, at[0], (int)min((uint32_t)k * per, rows), (int)min((uint32_t)(k + 1) * per, rows));
         g.part_slot[part0 + k] = parts > 1 ? at[2] + k : -1;
     }
     if (parts > 1 && lane == 0) g.joins[at[3]] = make_int4(block, at[2], parts, 0);
@@ -96,16 +85,17 @@ __global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams
     }
 }
 
-// The same, bits included, where a head's bitmap fits LDS: one workgroup a head, one launch instead of three.  LDS: [n_blocks * words] bits,
-// [5][n_blocks] places, [n_blocks] groups.
+// The same, bits included, where a head's lists are few enough that every workgroup can read all of them: one launch instead of three.  A
+// workgroup takes kHeadBlocks blocks of a head, their bits in LDS.
+constexpr int kHeadBlocks = 64;
+
 __global__ __launch_bounds__(1024) void grad_head_lists_kernel(SelParams p, GradParams g) {
-    extern __shared__ int32_t s_all[];
+    extern __shared__ uint32_t s_bits[];   // [kHeadBlocks][words]
+    __shared__ int s_at[5][kHeadBlocks], s_n[kHeadBlocks];
     const SeqShape& s = p.s;
-    const int blocks = s.n_blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bh = (int)blockIdx.x;
-    uint32_t* const bits = (uint32_t*)s_all;
-    int32_t* const s_at = s_all + blocks * g.words;
-    int32_t* const s_n = s_at + 5 * blocks;
-    for (int i = threadIdx.x; i < blocks * g.words; i += 1024) bits[i] = 0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bh = (int)blockIdx.y, block0 = (int)blockIdx.x * kHeadBlocks;
+    const int blocks = min(kHeadBlocks, s.n_blocks - block0);
+    for (int i = threadIdx.x; i < blocks * g.words; i += 1024) s_bits[i] = 0;
     const int b = (int)fdiv((uint32_t)bh, p.fd_kv_heads), len = seq_len(s, b);
     const int64_t pos = seq_pos(s, b, len);
     __syncthreads();
@@ -113,47 +103,45 @@ __global__ __launch_bounds__(1024) void grad_head_lists_kernel(SelParams p, Grad
     for (int i = threadIdx.x; i < s.n_groups * p.max_blocks; i += 1024) {
         uint32_t group, t;
         fdivmod((uint32_t)i, g.fd_top, group, t);
-        const int block = p.index[list0 * p.max_blocks + i];
-        if ((int)t < p.count[list0 + group] && block >= 0 && block < blocks && block * s.block < group_seen(s, len, pos, (int)group))
-            atomicOr(&bits[block * g.words + group / 32], 1u << (group % 32));
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < blocks; i += 1024) {
-        int n = 0;
-        for (int w = 0; w < g.words; ++w) n += __popc(bits[i * g.words + w]);
-        s_n[i] = n;
-    }
-    __syncthreads();
-    if (wave < 5) {   // places within the head, then the head's place
-        int sum = 0;
-        for (int i0 = 0; i0 < blocks; i0 += 64) {
-            const int mine = i0 + lane < blocks ? takes(p, g, s_n[i0 + lane], wave) : 0;
-            int before = mine;
-#pragma unroll
-            for (int m = 1; m < 64; m *= 2) {
-                const int up = __shfl_up(before, m);
-                if (lane >= m) before += up;
-            }
-            if (i0 + lane < blocks) s_at[wave * blocks + i0 + lane] = sum + before - mine;
-            sum += __shfl(before, 63);
-        }
-        int base = 0;
-        if (lane == 0 && sum > 0) base = atomicAdd(&g.counters[wave], sum);
-        base = __shfl(base, 0);
-        for (int i = lane; i < blocks; i += 64) s_at[wave * blocks + i] += base;
+        const int block = p.index[list0 * p.max_blocks + i], at = block - block0;
+        if ((int)t < p.count[list0 + group] && block >= block0 && at < blocks && block * s.block < group_seen(s, len, pos, (int)group))
+            atomicOr(&s_bits[at * g.words + group / 32], 1u << (group % 32));
     }
     __syncthreads();
     for (int i = wave; i < blocks; i += 16) {
-        const int at[5] = {s_at[i], s_at[blocks + i], s_at[2 * blocks + i], s_at[3 * blocks + i], s_at[4 * blocks + i]};
-        put_block(p, g, bh * blocks + i, s_n[i], bits + i * g.words, at, lane);
+        int n = 0;
+        for (int w = lane; w < g.words; w += 64) n += __popc(s_bits[i * g.words + w]);
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) n += __shfl_xor(n, m);
+        if (lane == 0) s_n[i] = n;
+    }
+    __syncthreads();
+    if (wave < 5) {   // places: within the workgroup, then the workgroup's
+        static_assert(kHeadBlocks == 64, "a block a lane");
+        const int mine = lane < blocks ? takes(p, g, s_n[lane], wave) : 0;
+        int before = mine;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const int up = __shfl_up(before, m);
+            if (lane >= m) before += up;
+        }
+        const int sum = __shfl(before, 63);
+        int base = 0;
+        if (lane == 0 && sum > 0) base = atomicAdd(&g.counters[wave], sum);
+        s_at[wave][lane] = __shfl(base, 0) + before - mine;
+    }
+    __syncthreads();
+    for (int i = wave; i < blocks; i += 16) {
+        const int at[5] = {s_at[0][i], s_at[1][i], s_at[2][i], s_at[3][i], s_at[4][i]};
+        put_block(p, g, bh * s.n_blocks + block0 + i, s_n[i], s_bits + i * g.words, at, lane);
     }
 }
 
 void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stream) {
-    // (a head's bits, places and counts in LDS; n_groups * max_blocks of them are walked by one workgroup)
-    const int64_t lds = 4 * ((int64_t)p.s.n_blocks * g.words + 6 * (int64_t)p.s.n_blocks);
-    if (lds <= 64 * 1024 && (int64_t)p.s.n_groups * p.max_blocks <= 65536) {
-        hipLaunchKernelGGL(grad_head_lists_kernel, dim3((unsigned)(p.s.batch * p.s.kv_heads)), dim3(1024), (size_t)lds, stream, p, g);
+    const int64_t lds = 4 * (int64_t)kHeadBlocks * g.words;
+    if (lds <= 64 * 1024 && (int64_t)p.s.n_groups * p.max_blocks <= 32768) {
+        hipLaunchKernelGGL(grad_head_lists_kernel, dim3((unsigned)((p.s.n_blocks + kHeadBlocks - 1) / kHeadBlocks), (unsigned)(p.s.batch * p.s.kv_heads)),
+                           dim3(1024), (size_t)lds, stream, p, g);
         return;
     }
     const int64_t clears = ((int64_t)g.blocks * g.words + 1023) / 1024;

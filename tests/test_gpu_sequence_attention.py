@@ -180,6 +180,11 @@ def test_larger(shape, pick):
     run_case(shape, "bf16", 128, backward=True, seed=61, full=True, pick=pick)
 
 
+def test_lists_too_many_for_one_workgroup():
+    """20 000 lists of a head, turned round through a bitmap in memory."""
+    run_case((1, 1, 1, 20000, 600, 1, 32, 3, None, None, False), "f16", 64, backward=True, seed=63, full=True)
+
+
 def test_a_block_that_every_group_lists_is_cut_into_parts():
     B, Hq, Hkv, N, M, q_group, block, top = 1, 4, 1, 1500, 1500, 16, 64, 3
     groups, blocks = -(-N // q_group), -(-M // block)
