@@ -160,9 +160,10 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
         g.fd_rows = make_fastdiv((uint32_t)rows);
         g.fd_top = make_fastdiv((uint32_t)max_blocks);
         g.fd_tiles = make_fastdiv((uint32_t)(s.block / plan.tile_keys));
-        // Parts of the rows that a block has on average: entries of all lists times the rows of a group, over all blocks.
+        // Parts of the rows that a block has on average (entries of all lists times the rows of a group, over all blocks), or of fewer where
+        // that leaves compute units idle: a launch takes as long as its longest part.
         const int64_t entries = lists * std::min(max_blocks, s.n_blocks), all_rows = entries * rows;
-        const int64_t part = std::max<int64_t>(512, (all_rows / blocks + 63) / 64 * 64);
+        const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(all_rows / blocks, 512), all_rows / 768) + 63) / 64 * 64);
         g.part_rows = (int32_t)std::min<int64_t>(part, kMaxRows / 2);
         g.fd_part = make_fastdiv((uint32_t)g.part_rows);
         const int64_t most_parts = blocks + all_rows / g.part_rows, most_slots = 2 * (all_rows / g.part_rows) + 1;

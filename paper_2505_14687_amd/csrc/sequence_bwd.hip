@@ -139,7 +139,7 @@ __global__ __launch_bounds__(1024) void grad_head_lists_kernel(SelParams p, Grad
 
 void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stream) {
     const int64_t lds = 4 * (int64_t)kHeadBlocks * g.words;
-    if (lds <= 64 * 1024 && (int64_t)p.s.n_groups * p.max_blocks <= 32768) {
+    if (lds <= 64 * 1024 && (int64_t)p.s.n_groups * p.max_blocks <= 8192) {
         hipLaunchKernelGGL(grad_head_lists_kernel, dim3((unsigned)((p.s.n_blocks + kHeadBlocks - 1) / kHeadBlocks), (unsigned)(p.s.batch * p.s.kv_heads)),
                            dim3(1024), (size_t)lds, stream, p, g);
         return;
