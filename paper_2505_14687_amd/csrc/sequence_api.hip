@@ -92,6 +92,7 @@ grat_status make_rotary(const grat_rotary_args* a, bool with_k, RotaryParams* ou
 // ---- attention over lists --------------------------------------------------------------------
 // Rows of a forward workgroup.  (rows = those of a group)
 int fwd_tile_rows(const SeqShape& s, int head_dim, int64_t rows) {
+    if (rows <= 16) return 16;
     if (rows <= 32) return 32;
     if (rows <= 64) return 64;
     const int64_t lists = (int64_t)s.batch * s.kv_heads * s.n_groups;
@@ -136,9 +137,10 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
     p.rows = (int32_t)rows;
     plan.tile_rows = backward ? bwd_tile_rows(rows) : fwd_tile_rows(s, (int)D, rows);
     p.row_tiles = (int32_t)((rows + plan.tile_rows - 1) / plan.tile_rows);
-    const int64_t items = lists * p.row_tiles, key_tiles = ((int64_t)max_blocks * (s.block / kUnit) + 1) / 2;
+    const int64_t items = lists * p.row_tiles, units = (int64_t)max_blocks * (s.block / kUnit);
+    const int64_t shares = plan.tile_rows == 16 ? (units + 3) / 4 : (units + 1) / 2;   // what a workgroup takes at a time
     // A forward launch that leaves compute units idle (each takes two workgroups) has lists shared by several workgroups.
-    p.splits = backward || items >= 512 ? 1 : (int32_t)std::min<int64_t>(std::min<int64_t>((512 + items - 1) / items, key_tiles), 64);
+    p.splits = backward || items >= 512 ? 1 : (int32_t)std::min<int64_t>(std::min<int64_t>((512 + items - 1) / items, shares), 64);
     p.items = (int32_t)(items * p.splits);
     p.per_xcd = (p.items + 7) / 8;
     p.fd_splits = make_fastdiv((uint32_t)p.splits);

@@ -128,6 +128,12 @@ __device__ __forceinline__ void load_lds_word(const uint8_t* src, uint8_t* dst) 
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
 }
 
+// This wave's loads have landed, and what it read from LDS is in registers.
+__device__ __forceinline__ void wave_wait() {
+    __builtin_amdgcn_s_waitcnt(0);
+    asm volatile("" ::: "memory");   // (no LDS read moves up past the wait)
+}
+
 // This wave's direct loads have landed, everyone's have, and everyone is done with the buffers that are filled next.
 __device__ __forceinline__ void tile_barrier() {
     __builtin_amdgcn_s_waitcnt(0);
