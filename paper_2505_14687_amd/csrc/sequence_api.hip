@@ -99,7 +99,7 @@ int fwd_tile_rows(const SeqShape& s, int head_dim, int64_t rows) {
     if (head_dim == 128 && (rows % 256 == 0 || rows % 256 > 128) && lists * ((rows + 255) / 256) >= 256) return 256;
     return 128;
 }
-int bwd_tile_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+int bwd_tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
 int bwd_tile_keys(int block) { return block % 128 == 0 ? 128 : block % 64 == 0 ? 64 : 32; }
 
 // A checked call on lists, with everything that is decided about its launches.

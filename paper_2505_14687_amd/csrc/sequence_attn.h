@@ -242,6 +242,121 @@ struct KeyLoader {
     }
 };
 
+// ---- groups of at most 16 rows ------------------------------------------------------------------
+// Single tokens, lists of single queries: bound by fetching K and V, which no other rows share.  A workgroup is four waves that take every fourth
+// unit of the list and wait for nothing but their own loads.  The 16x16x32 instruction wastes no columns: with Y the group's
+// rows, T^T (32 keys x 16 rows, two instructions a step) leaves lane (row r = lane % 16, g = lane / 16) with keys 16 m + 4 g + i, and
+// Z^T[16 dims, row] += X'^T T is contracted in that order: elements 0 .. 3 keys 4 g + i, 4 .. 7 keys 16 + 4 g + i.
+// Of K and V the one that is only read by rows goes straight from memory to registers as the A operand (lane: key lane % 16, 16 bytes of
+// the 64 that four lanes read of its row), the other through LDS; both a unit ahead, so that a wave has 16 KiB on their way with
+// 16 KiB of LDS.
+template <int D>
+struct NarrowWave {
+    static constexpr int kRow = 2 * D, kTile = kUnit * kRow, kChunks = D / 8, kRows = 1024 / kRow, kPieces = kTile / 1024, kN = D / 32, kM = D / 16;
+    const uint8_t *regs, *tiles;         // what goes to registers (this lane's bytes of it), what through LDS
+    int64_t pitch_regs, pitch_tiles;     // bytes
+    uint8_t* lds;                        // two tiles
+    int last;                            // last key that may be read: it stands for those behind it, which are masked
+    int lane;
+    uint32_t row_at, col_at;
+    __device__ __forceinline__ NarrowWave(const SelParams& p, const Item& it, const SeqTensor& to_regs, const SeqTensor& to_tiles, uint8_t* lds_, int seen,
+                                          int lane_)
+        : lds(lds_), last(seen - 1), lane(lane_) {
+        const int r = lane & 15, g = lane >> 4, cq = r & 3, row = 4 * g + (r >> 2);
+        regs = row_address(to_regs, it.b, it.h, 0) + 16 * g;
+        tiles = row_address(to_tiles, it.b, it.h, 0);
+        pitch_regs = 2 * to_regs.stride_n;
+        pitch_tiles = 2 * to_tiles.stride_n;
+        const uint32_t base = (uint32_t)(uintptr_t)(LDS_PTR(uint8_t))lds;
+        row_at = base + r * kRow + ((tile_swizzle<D>(r) ^ g) << 4);
+        col_at = base + row * kRow + (((cq >> 1) ^ tile_swizzle<D>(row)) << 4) + 8 * (cq & 1);
+    }
+    __device__ __forceinline__ void fetch(int start, frag8 (&f)[2][kN], int odd) const {
+        const int first = min(start, last), left = last - first;
+        const uint8_t *const rb = regs + first * pitch_regs, *const tb = tiles + first * pitch_tiles;
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            const int row = k * kRows + lane / kChunks;
+            load_lds(tb, (uint32_t)min(row, left) * (uint32_t)pitch_tiles + (((lane % kChunks) ^ tile_swizzle<D>(row)) << 4), lds + odd * kTile + k * 1024);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const uint8_t* const src = rb + (uint32_t)min(16 * m + (lane & 15), left) * (uint32_t)pitch_regs;
+#pragma unroll
+            for (int ks = 0; ks < kN; ++ks) f[m][ks] = *(const frag8*)(src + 64 * ks);
+        }
+    }
+    // A operand, rows = keys 16 m + lane % 16, dims 32 ks + 8 g .. + 7
+    __device__ __forceinline__ frag8 rows(int m, int ks, int odd) const {
+        return *(LDS_PTR(const frag8))(uintptr_t)((row_at ^ (ks << 6)) + odd * kTile + 16 * m * kRow);
+    }
+    // A operand, rows = dims 16 dt + lane % 16, contracted over the unit's keys
+    __device__ __forceinline__ frag8 cols(int dt, int odd) const {   // (16 rows on the swizzle is the same)
+        const uint32_t at = (col_at ^ (dt << 5)) + odd * kTile;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(at + 16 * kRow));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    // unit(parity, registers, first key) for every unit of this wave, with the next one's loads on their way
+    template <typename F>
+    __device__ __forceinline__ void walk(const int32_t* units, int n_units, int wave, F&& unit) const {
+        const int mine = max((n_units - wave + 3) / 4, 0);
+        if (mine == 0) return;
+        auto start = [&](int i) { return __builtin_amdgcn_readfirstlane(units[wave + 4 * i]); };
+        frag8 f[2][2][kN];
+        fetch(start(0), f[0], 0);
+        int i = 0;
+        for (; i + 1 < mine; i += 2) {
+            const int a = start(i), b = start(i + 1), ahead = start(min(i + 2, mine - 1));
+            wave_wait();
+            fetch(b, f[1], 1);
+            unit(0, f[0], a);
+            wave_wait();
+            if (i + 2 < mine) fetch(ahead, f[0], 0);
+            unit(1, f[1], b);
+        }
+        if (i < mine) {
+            wave_wait();
+            unit(0, f[0], start(i));
+        }
+    }
+    // The waves' sums go through LDS: [wave][row][16-byte chunks of 4 dims, XORed with the row].  Then thread (row tid / 16) has D / 16
+    // dims from (tid % 16) D / 16 on.
+    static constexpr int kOwn = D / 16;
+    static __device__ __forceinline__ void put(float* sums, int wave, int lane, const f32x4* acc) {
+        const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int dt = 0; dt < kM; ++dt)
+            *(float4*)(sums + (wave * 16 + r) * D + 4 * ((4 * dt + g) ^ r)) = make_float4(acc[dt][0], acc[dt][1], acc[dt][2], acc[dt][3]);
+    }
+    static __device__ __forceinline__ void get(const float* sums, const float (&factor)[4], float (&x)[kOwn]) {
+        const int r = threadIdx.x >> 4, sub = threadIdx.x & 15;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) x[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+            for (int u = 0; u < kOwn / 4; ++u) {
+                const float4 v = *(const float4*)(sums + (w * 16 + r) * D + 4 * ((sub * (kOwn / 4) + u) ^ r));
+                x[4 * u] = fmaf(factor[w], v.x, x[4 * u]);
+                x[4 * u + 1] = fmaf(factor[w], v.y, x[4 * u + 1]);
+                x[4 * u + 2] = fmaf(factor[w], v.z, x[4 * u + 2]);
+                x[4 * u + 3] = fmaf(factor[w], v.w, x[4 * u + 3]);
+            }
+    }
+    template <bool F16>
+    static __device__ __forceinline__ void store(uint8_t* row, const float (&x)[kOwn], float factor) {
+        uint8_t* const dst = row + 2 * kOwn * (threadIdx.x & 15);
+#pragma unroll
+        for (int u = 0; u < kOwn / 4; ++u) {
+            uint2 v;
+            v.x = Elem<F16>::pack(x[4 * u] * factor, x[4 * u + 1] * factor);
+            v.y = Elem<F16>::pack(x[4 * u + 2] * factor, x[4 * u + 3] * factor);
+            *(uint2*)(dst + 8 * u) = v;
+        }
+    }
+};
+
 // Rows from accumulators: a lane holds 4 consecutive dims at a time of its row (dims 32 db + 8 q + 4 half ..).  A wave turns its 32 rows
 // through 4 KiB of LDS, 64 dims at a time, so that a store instruction covers 8 rows of 128 bytes.  row_of(i): address of row i of
 // the 32, or null.  Only the wave itself uses `stage`.

@@ -294,6 +294,16 @@ __global__ __launch_bounds__(256) void grad_join_kernel(SelParams p, GradParams 
 // ---- dQ ----------------------------------------------------------------------------------------
 // The forward walk with dO beside Q in registers: S^T = K Q^T, dP^T = V dO^T, and dQ^T += K^T dS^T with K read both ways from its tile.
 constexpr int kFewUnits = 12;   // lists walked twice
+
+// For the launches that follow: what they count, and what rows that only fill a tile take.
+__device__ __forceinline__ void start_lists(const GradParams& g) {
+    if (blockIdx.x == 0 && threadIdx.x < 5) {
+        g.counters[threadIdx.x] = 0;
+        g.delta[g.stats] = 0.f;
+        g.lse2[g.stats] = INFINITY;
+    }
+}
+
 template <int RW, int TEAMS, bool F16, int D>
 __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad_queries_kernel(SelParams p, GradParams g) {
     using E = Elem<F16>;
@@ -302,11 +312,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
     const Item it(p);
-    if (blockIdx.x == 0 && threadIdx.x < 5) {   // for the launches that follow: what they count, and what rows that only fill a tile take
-        g.counters[threadIdx.x] = 0;
-        g.delta[g.stats] = 0.f;
-        g.lse2[g.stats] = INFINITY;
-    }
+    start_lists(g);
     if (it.idle(p)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int team = TEAMS == 1 ? 0 : wave / RW, row_wave = wave % RW, half = lane >> 5;
@@ -527,6 +533,127 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     });
 }
 
+// ... of groups of at most 16 rows: V in registers, K through LDS, where it is read by rows and by columns.
+template <bool F16, int D>
+__global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p, GradParams g) {
+    using E = Elem<F16>;
+    using W = NarrowWave<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2 * W::kTile];   // K, of every wave
+    __shared__ float s_sum[2][4][16];
+    __shared__ int32_t s_n;
+    extern __shared__ int32_t s_units[];
+    const Item it(p);
+    start_lists(g);
+    if (it.idle(p)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r = lane & 15, quad = lane >> 4;
+    const SeqShape& s = p.s;
+    const GroupRow row(p, it.h, it.g, it.tile * 16 + r);
+    const uint8_t* const q_src = row_address(p.Q, it.b, row.head, row.query) + 16 * quad;
+    const uint8_t* const d_src = row_address(g.dO, it.b, row.head, row.query) + 16 * quad;
+    const uint8_t* const o_src = row_address(p.O, it.b, row.head, row.query) + 16 * quad;
+    typedef typename Vec16<std::conditional_t<F16, _Float16, __bf16>>::type vec;
+    frag8 qf[W::kN], df[W::kN];
+    vec o[W::kN];
+#pragma unroll
+    for (int ks = 0; ks < W::kN; ++ks) {
+        qf[ks] = *(const frag8*)(q_src + 64 * ks);
+        df[ks] = *(const frag8*)(d_src + 64 * ks);
+        o[ks] = *(const vec*)(o_src + 64 * ks);
+    }
+    const int64_t stat = ((int64_t)it.b * s.q_heads + row.head) * s.n_q + row.query;
+    const float lse = p.lse[stat], lse2 = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f - (F16 ? kWeightBits : 0.f);
+    auto over_quads = [](float x) {
+        x += __shfl_xor(x, 16);
+        return x + __shfl_xor(x, 32);
+    };
+    float delta = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < W::kN; ++ks) {
+        const vec d = __builtin_bit_cast(vec, df[ks]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf((float)o[ks][e], (float)d[e], delta);
+    }
+    delta = over_quads(delta) * (F16 ? 1.f / kWeightScale : 1.f);
+    const int len = seq_len(s, it.b);
+    const int64_t pos = seq_pos(s, it.b, len);
+    const int seen = group_seen(s, len, pos, it.g);
+    const int limit = row.there ? row_seen(s, len, pos, row.query) : 0;
+    int least = row.there ? limit : 0x7fffffff;
+#pragma unroll
+    for (int m = 1; m < 16; m *= 2) least = min(least, __shfl_xor(least, m));
+    least = __builtin_amdgcn_readfirstlane(least);
+    const int n_units = seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
+
+    f32x4 dq[W::kM];
+#pragma unroll
+    for (int i = 0; i < W::kM; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float c = p.scale_log2;
+    float sum = 0.f;   // over this lane's keys: of P dP while D is being formed, then of dS
+    const W w(p, it, p.V, p.K, lds[wave], seen, lane);
+    auto walk = [&](auto form_d) {
+        constexpr bool kFormD = decltype(form_d)::value;
+        w.walk(s_units, n_units, wave, [&](int odd, const frag8 (&vf)[2][W::kN], int start) {
+            f32x4 S[2], T[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                S[m] = T[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < W::kN; ++ks) S[m] = E::mfma16(w.rows(m, ks, odd), qf[ks], S[m]);
+#pragma unroll
+                for (int ks = 0; ks < W::kN; ++ks) T[m] = E::mfma16(vf[m][ks], df[ks], T[m]);
+            }
+            const bool masked = start + kUnit > least;
+            uint32_t dw[4];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const f32x4 &x = S[i >> 2], &t = T[i >> 2];
+                float d0 = __builtin_amdgcn_exp2f(fmaf(x[i & 3], c, -lse2)) * score_grad<F16>(t[i & 3], delta);
+                float d1 = __builtin_amdgcn_exp2f(fmaf(x[(i & 3) + 1], c, -lse2)) * score_grad<F16>(t[(i & 3) + 1], delta);
+                if (masked) {
+                    const int key = start + 16 * (i >> 2) + 4 * quad + (i & 3);
+                    if (key >= limit) d0 = 0.f;
+                    if (key + 1 >= limit) d1 = 0.f;
+                }
+                sum += d0 + d1;
+                if constexpr (!kFormD) dw[i >> 1] = E::pack(d0, d1);
+            }
+            if constexpr (!kFormD) {
+                const frag8 x = __builtin_bit_cast(frag8, make_uint4(dw[0], dw[1], dw[2], dw[3]));
+#pragma unroll
+                for (int dt = 0; dt < W::kM; ++dt) dq[dt] = E::mfma16(w.cols(dt, odd), x, dq[dt]);
+            }
+        });
+    };
+    auto over_row = [&](int which) {   // over all keys of row `r`
+        const float all = over_quads(sum);
+        if (quad == 0) s_sum[which][wave][r] = all;
+        __syncthreads();
+        return (s_sum[which][0][r] + s_sum[which][1][r] + s_sum[which][2][r] + s_sum[which][3][r]) * (F16 ? 1.f / kWeightScale : 1.f);
+    };
+    if (n_units > 0) {
+        if (n_units <= kFewUnits) {   // short lists: a first walk for the exact D
+            walk(std::true_type{});
+            delta += over_row(0);
+            sum = 0.f;
+        }
+        walk(std::false_type{});
+    }
+    const float left = over_row(1);   // (its barrier: everyone is done with the tiles)
+    if (wave == 0 && quad == 0 && row.there) {
+        g.delta[stat] = delta + left;
+        g.lse2[stat] = lse2;
+    }
+    float* const sums = (float*)&lds[0][0];
+    static_assert(4 * 16 * D * 4 <= (int)sizeof(lds), "the results fit the tiles");
+    W::put(sums, wave, lane, dq);
+    __syncthreads();
+    float x[W::kOwn];
+    const float ones[4] = {1.f, 1.f, 1.f, 1.f};
+    W::get(sums, ones, x);
+    const GroupRow to(p, it.h, it.g, it.tile * 16 + (int)(threadIdx.x >> 4));
+    if (to.there) W::template store<F16>((uint8_t*)row_address(g.dQ, it.b, to.head, to.query), x, p.scale);
+}
+
 template <int KW, int TEAMS, bool F16, int D>
 inline void launch_grad_keys(const SelParams& p, const GradParams& g, hipStream_t stream) {
     const int64_t items = (int64_t)g.most_parts * g.fd_tiles.d;
@@ -541,12 +668,15 @@ inline void launch_grad_queries(const SelParams& p, const GradParams& g, hipStre
     hipLaunchKernelGGL((grad_queries_kernel<RW, TEAMS, F16, D>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p, g);
 }
 
-// tile_rows: 128, 64 or 32; key tiles of 128, 64 or 32 keys
+// tile_rows: 128, 64, 32 or 16; key tiles of 128, 64 or 32 keys
 template <bool F16, int D>
 inline hipError_t launch_bwd(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream) {
     if (tile_rows == 128) launch_grad_queries<4, 1, F16, D>(p, g, stream);
     else if (tile_rows == 64) launch_grad_queries<2, 2, F16, D>(p, g, stream);
-    else launch_grad_queries<1, 2, F16, D>(p, g, stream);
+    else if (tile_rows == 32) launch_grad_queries<1, 2, F16, D>(p, g, stream);
+    else
+        hipLaunchKernelGGL((grad_queries_narrow_kernel<F16, D>), dim3(8 * p.per_xcd), dim3(256), sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1),
+                           stream, p, g);
     launch_grad_lists(p, g, stream);
     if (tile_keys == 128) launch_grad_keys<4, 1, F16, D>(p, g, stream);
     else if (tile_keys == 64) launch_grad_keys<2, 2, F16, D>(p, g, stream);

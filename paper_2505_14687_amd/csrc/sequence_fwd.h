@@ -288,22 +288,14 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     });
 }
 
-// Groups of at most 16 rows (single tokens, lists of single queries): bound by fetching K and V, which no other rows share.  A
-// workgroup is four waves that take every fourth unit of 32 keys and wait for nothing but their own loads; their results are joined
-// through LDS.  The 16x16x32 instruction wastes no columns.  K goes straight from memory to registers as the A operand (lane: key
-// lane % 16, 16 bytes of the 64 that four lanes read of its row), V through LDS, from where the transpose read takes it; both a unit
-// ahead, so that a wave has 16 KiB on their way with 16 KiB of LDS.  Against 32 rows with K and V in tiles that the workgroup shares: 32
-// tokens of half over 1 024 keys 29.5 -> 26.7 us (with the join; 134 MB, 5.0 TB/s), 6 218 lists of 16 rows 580 -> 450 us.
-//   S^T (32 keys x 16 rows, two instructions a step): lane (row r = lane % 16, g = lane / 16) holds keys 16 m + 4 g + i;
-//   O^T[16 dims, row] += V^T P^T with the contraction in that order: elements 0 .. 3 keys 4 g + i, 4 .. 7 keys 16 + 4 g + i.
-template <int D>
-__device__ __forceinline__ int narrow_swizzle(int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
-
+// Groups of at most 16 rows: K in registers, V through LDS, the four waves' results joined through LDS.  Against 32 rows on two waves with K
+// and V in tiles that they share: 64 tokens of half over 2 048 keys 29.5 -> 26.7 us (134 MB, 5.0 TB/s, with the join of the parts),
+// 6 218 lists of 16 rows 580 -> 450 us.
 template <bool F16, int D>
 __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p) {
     using E = Elem<F16>;
-    constexpr int kRow = 2 * D, kTile = kUnit * kRow, kChunks = D / 8, kRows = 1024 / kRow, kPieces = kTile / 1024, kN = D / 32, kM = D / 16;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2][kTile];   // V, of every wave
+    using W = NarrowWave<D>;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2 * W::kTile];   // V, of every wave
     __shared__ float s_m[4][16], s_l[4][16];
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
@@ -313,9 +305,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p
     const SeqShape& s = p.s;
     const GroupRow row(p, it.h, it.g, it.tile * 16 + r);
     const uint8_t* const q_src = row_address(p.Q, it.b, row.head, row.query) + 16 * g;
-    frag8 qf[kN];
+    frag8 qf[W::kN];
 #pragma unroll
-    for (int ks = 0; ks < kN; ++ks) qf[ks] = *(const frag8*)(q_src + 64 * ks);
+    for (int ks = 0; ks < W::kN; ++ks) qf[ks] = *(const frag8*)(q_src + 64 * ks);
     const int len = seq_len(s, it.b);
     const int64_t pos = seq_pos(s, it.b, len);
     const int seen = group_seen(s, len, pos, it.g);
@@ -331,47 +323,20 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p
         u_first = min(it.split * per, all_units);
         n_units = min(per, all_units - u_first);
     }
-    const int mine = max((n_units - wave + 3) / 4, 0);
-    auto unit_start = [&](int i) { return __builtin_amdgcn_readfirstlane(s_units[u_first + wave + 4 * i]); };
 
-    f32x4 oacc[kM];
+    f32x4 oacc[W::kM];
 #pragma unroll
-    for (int i = 0; i < kM; ++i) oacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < W::kM; ++i) oacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float c = p.scale_log2;
     float m_ref = -1e38f / fmaxf(c, 1.f), l_run = 0.f;   // (finite, so that a unit without a seen key weighs 0)
-
-    const uint8_t *const K = row_address(p.K, it.b, it.h, 0) + 16 * g, *const V = row_address(p.V, it.b, it.h, 0);
-    const int64_t pitch_k = 2 * p.K.stride_n, pitch_v = 2 * p.V.stride_n;
-    const int last = seen - 1;   // keys behind it are not read: it stands for them, and they are masked
-    const int piece_row = lane / kChunks;
-    // the transpose read: row 4 g + e (16 on: the same swizzle), 8 bytes of dims 16 dt + 4 cq
-    const int e = r >> 2, cq = r & 3, tr_row = 4 * g + e, tr_sw = narrow_swizzle<D>(tr_row);
-    const uint32_t v_at = (uint32_t)(uintptr_t)(LDS_PTR(uint8_t))&lds[wave][0][0] + tr_row * kRow + 8 * (cq & 1);
-    frag8 kf[2][2][kN];   // K of the unit at hand and of the next: [parity][16 keys][dims]
-    auto fetch = [&](auto odd_c, int start) {
-        constexpr int kOdd = decltype(odd_c)::value;
-        const int first = min(start, last), left = last - first;
-        const uint8_t *const kb = K + first * pitch_k, *const vb = V + first * pitch_v;
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-            const int vr = k * kRows + piece_row;
-            load_lds(vb, (uint32_t)min(vr, left) * (uint32_t)pitch_v + (((lane % kChunks) ^ narrow_swizzle<D>(vr)) << 4), lds[wave][kOdd] + k * 1024);
-        }
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const uint8_t* const src = kb + (uint32_t)min(16 * m + r, left) * (uint32_t)pitch_k;
-#pragma unroll
-            for (int ks = 0; ks < kN; ++ks) kf[kOdd][m][ks] = *(const frag8*)(src + 64 * ks);
-        }
-    };
-    auto unit = [&](auto odd_c, int start) {
-        constexpr int kOdd = decltype(odd_c)::value;
+    const W w(p, it, p.K, p.V, lds[wave], seen, lane);
+    w.walk(s_units + u_first, n_units, wave, [&](int odd, const frag8 (&kf)[2][W::kN], int start) {
         f32x4 S[2];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             S[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int ks = 0; ks < kN; ++ks) S[m] = E::mfma16(kf[kOdd][m][ks], qf[ks], S[m]);
+            for (int ks = 0; ks < W::kN; ++ks) S[m] = E::mfma16(kf[m][ks], qf[ks], S[m]);
         }
         if (start + kUnit > least) {
 #pragma unroll
@@ -384,7 +349,8 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p
             float ls = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float a = __builtin_amdgcn_exp2f(fmaf(S[i >> 1][2 * (i & 1)], c, -mc)), b = __builtin_amdgcn_exp2f(fmaf(S[i >> 1][2 * (i & 1) + 1], c, -mc));
+                const float x = S[i >> 1][2 * (i & 1)], y = S[i >> 1][2 * (i & 1) + 1];
+                const float a = __builtin_amdgcn_exp2f(fmaf(x, c, -mc)), b = __builtin_amdgcn_exp2f(fmaf(y, c, -mc));
                 pw[i] = E::pack(a, b);
                 ls += a + b;
             }
@@ -399,93 +365,47 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p
             m_ref = m_new;
             l_run *= alpha;
 #pragma unroll
-            for (int i = 0; i < kM; ++i) oacc[i] *= alpha;
+            for (int i = 0; i < W::kM; ++i) oacc[i] *= alpha;
             ls = weigh();
         }
         l_run += ls;
-        const frag8 w = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        const frag8 x = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
 #pragma unroll
-        for (int dt = 0; dt < kM; ++dt) {
-            const uint32_t at = v_at + kOdd * kTile + (((2 * dt + (cq >> 1)) ^ tr_sw) << 4);
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(at + 16 * kRow));
-            oacc[dt] = E::mfma16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), w, oacc[dt]);
-        }
-    };
-    constexpr std::integral_constant<int, 0> even{};
-    constexpr std::integral_constant<int, 1> odd{};
-    if (mine > 0) {
-        fetch(even, unit_start(0));
-        int i = 0;
-        for (; i + 1 < mine; i += 2) {
-            const int a = unit_start(i), b = unit_start(i + 1), ahead = unit_start(min(i + 2, mine - 1));
-            wave_wait();   // this unit's K and V
-            fetch(odd, b);
-            unit(even, a);
-            wave_wait();
-            if (i + 2 < mine) fetch(even, ahead);
-            unit(odd, b);
-        }
-        if (i < mine) {
-            wave_wait();
-            unit(even, unit_start(i));
-        }
-    }
+        for (int dt = 0; dt < W::kM; ++dt) oacc[dt] = E::mfma16(w.cols(dt, odd), x, oacc[dt]);
+    });
 
-    // The four waves' results: [wave][row][16-byte chunks of 4 dims, XORed with the row]
     float l = l_run + __shfl_xor(l_run, 16);
     l += __shfl_xor(l, 32);
-    float* const sums = (float*)&lds[0][0][0];
+    float* const sums = (float*)&lds[0][0];
     static_assert(4 * 16 * D * 4 <= (int)sizeof(lds), "the results fit the tiles");
     __syncthreads();   // everyone is done with the tiles
-#pragma unroll
-    for (int dt = 0; dt < kM; ++dt)
-        *(float4*)(sums + (wave * 16 + r) * D + 4 * ((4 * dt + g) ^ r)) = make_float4(oacc[dt][0], oacc[dt][1], oacc[dt][2], oacc[dt][3]);
+    W::put(sums, wave, lane, oacc);
     if (g == 0) {
         s_m[wave][r] = m_ref;
         s_l[wave][r] = l;
     }
     __syncthreads();
-    constexpr int kOwn = D / 16;   // dims of a thread: row tid / 16
-    const int or_ = threadIdx.x >> 4, sub = threadIdx.x & 15;
-    float M = s_m[0][or_], f[4], total = 0.f, x[kOwn];
+    const int mine = threadIdx.x >> 4, sub = threadIdx.x & 15;
+    float M = s_m[0][mine], f[4], total = 0.f, x[W::kOwn];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) M = fmaxf(M, s_m[w][or_]);
+    for (int k = 1; k < 4; ++k) M = fmaxf(M, s_m[k][mine]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        f[w] = __builtin_amdgcn_exp2f((s_m[w][or_] - M) * c);
-        total = fmaf(f[w], s_l[w][or_], total);
+    for (int k = 0; k < 4; ++k) {
+        f[k] = __builtin_amdgcn_exp2f((s_m[k][mine] - M) * c);
+        total = fmaf(f[k], s_l[k][mine], total);
     }
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) x[i] = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-#pragma unroll
-        for (int u = 0; u < kOwn / 4; ++u) {
-            const float4 v = *(const float4*)(sums + (w * 16 + or_) * D + 4 * ((sub * (kOwn / 4) + u) ^ or_));
-            x[4 * u] = fmaf(f[w], v.x, x[4 * u]);
-            x[4 * u + 1] = fmaf(f[w], v.y, x[4 * u + 1]);
-            x[4 * u + 2] = fmaf(f[w], v.z, x[4 * u + 2]);
-            x[4 * u + 3] = fmaf(f[w], v.w, x[4 * u + 3]);
-        }
+    W::get(sums, f, x);
     if (p.splits > 1) {   // parts are joined by selected_join_kernel
-        const int64_t at = (int64_t)it.item * 16 + or_;
+        const int64_t at = (int64_t)it.item * 16 + mine;
 #pragma unroll
-        for (int u = 0; u < kOwn / 4; ++u) *(float4*)(p.part_o + at * D + kOwn * sub + 4 * u) = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
+        for (int u = 0; u < W::kOwn / 4; ++u)
+            *(float4*)(p.part_o + at * D + W::kOwn * sub + 4 * u) = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
         if (sub == 0) *(float2*)(p.part_ml + 2 * at) = make_float2(M, total);
         return;
     }
-    const GroupRow to(p, it.h, it.g, it.tile * 16 + or_);
+    const GroupRow to(p, it.h, it.g, it.tile * 16 + mine);
     if (!to.there) return;
-    const float inv = total > 0.f ? 1.f / total : total;   // (a row that attends nothing: 0; NaN stays)
-    uint8_t* const dst = (uint8_t*)row_address(p.O, it.b, to.head, to.query) + 2 * kOwn * sub;
-#pragma unroll
-    for (int u = 0; u < kOwn / 4; ++u) {
-        uint2 v;
-        v.x = E::pack(x[4 * u] * inv, x[4 * u + 1] * inv);
-        v.y = E::pack(x[4 * u + 2] * inv, x[4 * u + 3] * inv);
-        *(uint2*)(dst + 8 * u) = v;
-    }
+    W::template store<F16>((uint8_t*)row_address(p.O, it.b, to.head, to.query), x, total > 0.f ? 1.f / total : total);   // (a row that attends nothing: 0; NaN stays)
     if (p.lse && sub == 0)
         p.lse[((int64_t)it.b * s.q_heads + to.head) * s.n_q + to.query] = (M * c + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
