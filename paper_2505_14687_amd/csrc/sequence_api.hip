@@ -90,7 +90,8 @@ grat_status make_rotary(const grat_rotary_args* a, bool with_k, RotaryParams* ou
 }
 
 // ---- attention over lists --------------------------------------------------------------------
-// Rows of a forward workgroup.  (rows = those of a group)
+// Rows of a forward workgroup, of the `rows` of a group: one tile where they fit, else 256 if that fills the chip and wastes no half tile, else 128
+// (32 768 tokens in groups of 64 x 4 heads: 580 us in tiles of 256, 590 in tiles of 128).
 int fwd_tile_rows(const SeqShape& s, int head_dim, int64_t rows) {
     if (rows <= 16) return 16;
     if (rows <= 32) return 32;
@@ -100,7 +101,9 @@ int fwd_tile_rows(const SeqShape& s, int head_dim, int64_t rows) {
     return 128;
 }
 int bwd_tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
-int bwd_tile_keys(int block) { return block % 128 == 0 ? 128 : block % 64 == 0 ? 64 : 32; }
+// Keys of a workgroup of the walk over keys.  (128, four waves that each take all rows of a tile, spill: blocks of 128 keys, 2 048 tokens 187 us against 154,
+// 8 192 tokens of half at head_dim 64 440 against 420; blocks of 256 in groups of 128 2 310 against 2 395.)
+int bwd_tile_keys(int block) { return block % 64 == 0 ? 64 : 32; }
 
 // A checked call on lists, with everything that is decided about its launches.
 struct SelPlan {
@@ -137,10 +140,14 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
     p.rows = (int32_t)rows;
     plan.tile_rows = backward ? bwd_tile_rows(rows) : fwd_tile_rows(s, (int)D, rows);
     p.row_tiles = (int32_t)((rows + plan.tile_rows - 1) / plan.tile_rows);
-    const int64_t items = lists * p.row_tiles, units = (int64_t)max_blocks * (s.block / kUnit);
-    const int64_t shares = plan.tile_rows == 16 ? (units + 3) / 4 : (units + 1) / 2;   // what a workgroup takes at a time
-    // A forward launch that leaves compute units idle (each takes two workgroups) has lists shared by several workgroups.
-    p.splits = backward || items >= 512 ? 1 : (int32_t)std::min<int64_t>(std::min<int64_t>((512 + items - 1) / items, shares), 64);
+    const int64_t items = lists * p.row_tiles, units = (int64_t)std::min(max_blocks, s.n_blocks) * (s.block / kUnit);
+    const int64_t shares = plan.tile_rows == 16 ? (units + 3) / 4 : (units + 1) / 2;   // steps of a workgroup
+    // A forward launch that leaves compute units idle has lists shared by several workgroups: two a compute unit where a part's results are few
+    // rows, one where they are many (1 000 queries, 20 blocks of 64 keys, 256 workgroups of 128 rows: 30 us, shared by two each 42).  A part is
+    // two steps or more, and a list of fewer than 8 is not split: the launch that joins costs as much (one token, us, not split and split: 4 steps 8.6 and
+    // 9.5, 8 steps 13.0 and 9.2, 16 steps 21.7 and 9.2; 64 queries, 16 steps 23.5, in 8 parts 15.4, in 16 parts 21.1).
+    const int64_t wanted = plan.tile_rows <= 32 ? (512 + items - 1) / items : 256 / items;
+    p.splits = backward || shares < 8 ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(wanted, shares / 2), 64));
     p.items = (int32_t)(items * p.splits);
     p.per_xcd = (p.items + 7) / 8;
     p.fd_splits = make_fastdiv((uint32_t)p.splits);

@@ -89,11 +89,6 @@ struct TileReader {
         col_at ^= kTile;
         asm volatile("" : "+v"(row_at), "+v"(col_at));
     }
-    __device__ __forceinline__ void other_block() {   // of the same tile
-        row_at ^= 32 * kRow;
-        col_at ^= 32 * kRow;
-        asm volatile("" : "+v"(row_at), "+v"(col_at));
-    }
     // A operand, rows = tile rows 32 block + c, dims 16 ks + 8 half .. + 7.  pair: tiles 2 pair and 2 pair + 1; odd: the second of
     // them, for callers that do not flip
     __device__ __forceinline__ frag8 rows(int pair, int block, int ks, int odd = 0) const {

@@ -25,7 +25,7 @@ __device__ __forceinline__ float score_grad(float dp, float delta) { return F16 
 
 // ---- dK, dV ------------------------------------------------------------------------------------
 // A workgroup owns 32 KW keys of one block, K and V of a wave's 32 keys in registers, and streams the Q and dO rows of
-// the groups that list the block in tiles of 64 through LDS (TEAMS == 2: a team takes 32 rows of a tile each).
+// the groups that list the block in tiles of 64 through LDS; two teams of KW waves take 32 rows of a tile each.
 // What goes with a row - where it lies, lse, D, the keys it sees - is worked out by one wave, a tile ahead of the loads that need it, and
 // passed on through LDS; lse and D go there straight from memory.
 struct alignas(16) RowMeta {
@@ -36,15 +36,15 @@ struct alignas(16) RowMeta {
     int32_t masked;   // some row does not see all keys of the tile
 };
 
-template <int KW, int TEAMS, bool F16, int D>
-__global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad_keys_kernel(SelParams p, GradParams g) {
+template <int KW, bool F16, int D>
+__global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, GradParams g) {
     using E = Elem<F16>;
-    constexpr int NW = KW * TEAMS, kTile = 64 * D * 2, kPieces = kTile / 1024, LPW = kPieces / NW, kRows = 1024 / (2 * D), kChunks = D / 8;
+    constexpr int NW = 2 * KW, kTile = 64 * D * 2, kPieces = kTile / 1024, LPW = kPieces / NW, kRows = 1024 / (2 * D), kChunks = D / 8;
     __shared__ __attribute__((aligned(2 * kTile))) uint8_t lds[4][kTile];   // Q, Q, dO, dO
     __shared__ RowMeta meta[4];
     const SeqShape& s = p.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
-    const int team = TEAMS == 1 ? 0 : wave / KW, key_wave = wave % KW;
+    const int team = wave / KW, key_wave = wave % KW;
 
     // The XCDs walk the heads together, kChunk items at a time each: Q and dO of one or two K/V heads are in use at a time, which the memory-side
     // cache holds.
@@ -127,8 +127,8 @@ __global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad
         };
         TileReader<D> read(lane, lds[0], team);
         const float c = p.scale_log2;
-        auto rows_block = [&](const RowMeta& m, int block32, bool masked) {
-            const int row0 = 32 * block32 + 4 * half;   // of this lane in the tile
+        auto rows_block = [&](const RowMeta& m, bool masked) {
+            const int row0 = 32 * team + 4 * half;   // of this lane in the tile
             // 4 products, each fragment read kAhead products ahead of its own: the sums of dK and dV, K and V leave 64 registers for
             // everything else, and the compiler, left to itself, reads further ahead than that allows.
             constexpr int kAhead = 2, kN = D / 16, kM = 2 * (D / 32);
@@ -196,45 +196,35 @@ __global__ __launch_bounds__(KW * TEAMS * 64, KW * TEAMS == 2 ? 1 : 2) void grad
                 group_ahead = find_group(t + 3);   // (past the last row: the last row's again)
             }
             const RowMeta& m = meta[t & 3];
-            const bool masked = __builtin_amdgcn_readfirstlane(m.masked) != 0;
-            if constexpr (TEAMS == 1) {
-#pragma unroll 1
-                for (int i = 0; i < 2; ++i) {   // (one copy: two need more registers than there are)
-                    rows_block(m, i, masked);
-                    read.other_block();
-                }
-            } else {
-                rows_block(m, team, masked);
-            }
+            rows_block(m, __builtin_amdgcn_readfirstlane(m.masked) != 0);
             read.flip();
         }
     }
     // Everyone is done with the tiles.  (The keeper's last loads have to land as well: LDS that is given back is somebody else's.)
     tile_barrier();
 
-    if constexpr (TEAMS == 2) {   // the second team's share, lane by lane: dK, then dV
-        float* const mine = (float*)&lds[0][0] + key_wave * 64 * (D / 2) + lane;
-        static_assert(KW * 64 * (D / 2) * 4 <= 2 * kTile, "one sum of the second team fits two tiles");
-        auto add = [&](f32x16 (&acc)[D / 32]) {
-            if (team == 1) {
+    // the second team's share, lane by lane: dK, then dV
+    float* const mine = (float*)&lds[0][0] + key_wave * 64 * (D / 2) + lane;
+    static_assert(KW * 64 * (D / 2) * 4 <= 2 * kTile, "one sum of the second team fits two tiles");
+    auto add = [&](f32x16 (&acc)[D / 32]) {
+        if (team == 1) {
 #pragma unroll
-                for (int db = 0; db < D / 32; ++db)
+            for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) mine[(db * 16 + i) * 64] = acc[db][i];
-            }
-            __syncthreads();
-            if (team == 0) {
+                for (int i = 0; i < 16; ++i) mine[(db * 16 + i) * 64] = acc[db][i];
+        }
+        __syncthreads();
+        if (team == 0) {
 #pragma unroll
-                for (int db = 0; db < D / 32; ++db)
+            for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[db][i] += mine[(db * 16 + i) * 64];
-            }
-            __syncthreads();
-        };
-        add(dk);
-        add(dv);
-        if (team == 1) return;
-    }
+                for (int i = 0; i < 16; ++i) acc[db][i] += mine[(db * 16 + i) * 64];
+        }
+        __syncthreads();
+    };
+    add(dk);
+    add(dv);
+    if (team == 1) return;
     constexpr float dv_factor = F16 ? 1.f / kWeightScale : 1.f;
     const int slot = g.part_slot[part_id];
     if (slot >= 0) {   // parts are joined by grad_join_kernel
@@ -654,10 +644,10 @@ __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p
     if (to.there) W::template store<F16>((uint8_t*)row_address(g.dQ, it.b, to.head, to.query), x, p.scale);
 }
 
-template <int KW, int TEAMS, bool F16, int D>
+template <int KW, bool F16, int D>
 inline void launch_grad_keys(const SelParams& p, const GradParams& g, hipStream_t stream) {
     const int64_t items = (int64_t)g.most_parts * g.fd_tiles.d;
-    hipLaunchKernelGGL((grad_keys_kernel<KW, TEAMS, F16, D>), dim3((unsigned)((items + 127) / 128 * 128)), dim3(KW * TEAMS * 64), 0, stream, p, g);
+    hipLaunchKernelGGL((grad_keys_kernel<KW, F16, D>), dim3((unsigned)((items + 127) / 128 * 128)), dim3(KW * 128), 0, stream, p, g);
     if (g.most_joins > 0)
         hipLaunchKernelGGL((grad_join_kernel<F16, D>), dim3((unsigned)(g.most_joins * g.fd_tiles.d * kJoinShare)), dim3(256), 0, stream, p, g,
                            32 * KW);
@@ -668,7 +658,7 @@ inline void launch_grad_queries(const SelParams& p, const GradParams& g, hipStre
     hipLaunchKernelGGL((grad_queries_kernel<RW, TEAMS, F16, D>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p, g);
 }
 
-// tile_rows: 128, 64, 32 or 16; key tiles of 128, 64 or 32 keys
+// tile_rows: 128, 64, 32 or 16; key tiles of 64 or 32 keys
 template <bool F16, int D>
 inline hipError_t launch_bwd(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream) {
     if (tile_rows == 128) launch_grad_queries<4, 1, F16, D>(p, g, stream);
@@ -678,9 +668,8 @@ inline hipError_t launch_bwd(const SelParams& p, const GradParams& g, int tile_r
         hipLaunchKernelGGL((grad_queries_narrow_kernel<F16, D>), dim3(8 * p.per_xcd), dim3(256), sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1),
                            stream, p, g);
     launch_grad_lists(p, g, stream);
-    if (tile_keys == 128) launch_grad_keys<4, 1, F16, D>(p, g, stream);
-    else if (tile_keys == 64) launch_grad_keys<2, 2, F16, D>(p, g, stream);
-    else launch_grad_keys<1, 2, F16, D>(p, g, stream);
+    if (tile_keys == 64) launch_grad_keys<2, F16, D>(p, g, stream);
+    else launch_grad_keys<1, F16, D>(p, g, stream);
     return hipGetLastError();
 }
 

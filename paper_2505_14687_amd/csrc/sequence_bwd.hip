@@ -51,14 +51,14 @@ __device__ __forceinline__ void put_block(const SelParams& p, const GradParams& 
     if (parts > 1 && lane == 0) g.joins[at[3]] = make_int4(block, at[2], parts, 0);
 }
 
-// A workgroup takes up to kListBlocks blocks, a wave a block at a time; it asks for its share of `groups`, `parts`, `slots` and `joins` once.
+// A workgroup takes kListBlocks blocks, a wave a block at a time; it asks for its share of `groups`, `parts`, `slots` and `joins` once.
 // Where that lies depends on the order of the workgroups, what is computed from it does not.
-constexpr int kListBlocks = 16;   // 4 in small launches, for which it is latency that counts
+constexpr int kListBlocks = 4;   // (a block a wave: 226 blocks of 7 223 groups in 16s step 375 us, in 4s 318; 4 096 blocks 1 600 and 1 591)
 
-__global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams g, int per_group) {
+__global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams g) {
     __shared__ int s_n[kListBlocks], s_at[5][kListBlocks];
-    const int block0 = (int)blockIdx.x * per_group, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int here = min(per_group, g.blocks - block0);
+    const int block0 = (int)blockIdx.x * kListBlocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int here = min(kListBlocks, g.blocks - block0);
     for (int i = wave; i < here; i += 4) {
         const uint32_t* const words = g.bits + (int64_t)(block0 + i) * g.words;
         int n = 0;
@@ -148,8 +148,7 @@ void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stre
     hipLaunchKernelGGL(grad_clear_kernel, dim3((unsigned)(clears < 2048 ? clears : 2048)), dim3(256), 0, stream, g);
     const int64_t entries = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.max_blocks;
     hipLaunchKernelGGL(grad_bits_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, stream, p, g, entries);
-    const int per_group = g.blocks <= 2048 ? 4 : kListBlocks;
-    hipLaunchKernelGGL(grad_lists_kernel, dim3((unsigned)((g.blocks + per_group - 1) / per_group)), dim3(256), 0, stream, p, g, per_group);
+    hipLaunchKernelGGL(grad_lists_kernel, dim3((unsigned)((g.blocks + kListBlocks - 1) / kListBlocks)), dim3(256), 0, stream, p, g);
 }
 
 }  // namespace grat

@@ -410,17 +410,13 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p
         p.lse[((int64_t)it.b * s.q_heads + to.head) * s.n_q + to.query] = (M * c + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
 
-// Joins the parts of a split list, weighted by 2^(c (m - max m)).  D / 4 lanes share a row's dims, SLOTS of them its parts (8 where there
-// are many: then all loads of a row are in flight at once, and the slots' sums are joined through LDS in order).
-template <int SLOTS, bool F16, int D>
+// Joins the parts of a split list, weighted by 2^(c (m - max m)).  D / 4 lanes share a row's dims; eight parts are in flight at a time.
+template <bool F16, int D>
 __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int tile_rows, FastDiv fd_rows) {
-    constexpr int L = D / 4, RPB = 256 / (L * SLOTS);   // rows of a workgroup
-    __shared__ float4 s_o[SLOTS > 1 ? 256 : 1];
-    __shared__ float2 s_ml[SLOTS > 1 ? 256 : 1];
+    constexpr int L = D / 4, RPB = 256 / L;   // lanes of a row, rows of a workgroup
     const SeqShape& s = p.s;
-    const int lane = threadIdx.x % L, slot = threadIdx.x / L % SLOTS;
-    const int64_t n = (int64_t)s.batch * s.kv_heads * s.n_groups * p.rows;
-    const int64_t at = min((int64_t)blockIdx.x * RPB + threadIdx.x / (L * SLOTS), n - 1);
+    const int lane = threadIdx.x % L;
+    const int64_t n = (int64_t)s.batch * s.kv_heads * s.n_groups * p.rows, at = min((int64_t)blockIdx.x * RPB + threadIdx.x / L, n - 1);
     uint32_t list, r, bh, g, b, h;
     fdivmod((uint32_t)at, fd_rows, list, r);
     fdivmod(list, p.fd_groups, bh, g);
@@ -431,12 +427,12 @@ __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int til
     const float4* const po = (const float4*)p.part_o + first * L + lane;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = slot; i0 < p.splits; i0 += 8 * SLOTS) {
+    for (int i0 = 0; i0 < p.splits; i0 += 8) {
         float2 v[8];
         float4 x[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int i = min(i0 + k * SLOTS, p.splits - 1);
+            const int i = min(i0 + k, p.splits - 1);
             v[k] = ml[(int64_t)i * tile_rows];
             x[k] = po[(int64_t)i * tile_rows * L];
         }
@@ -449,30 +445,12 @@ __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int til
         m = top;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float f = i0 + k * SLOTS < p.splits ? __builtin_amdgcn_exp2f((v[k].x - m) * p.scale_log2) : 0.f;
+            const float f = i0 + k < p.splits ? __builtin_amdgcn_exp2f((v[k].x - m) * p.scale_log2) : 0.f;
             l = fmaf(f, v[k].y, l);
             o = make_float4(fmaf(f, x[k].x, o.x), fmaf(f, x[k].y, o.y), fmaf(f, x[k].z, o.z), fmaf(f, x[k].w, o.w));
         }
     }
-    if constexpr (SLOTS > 1) {
-        s_o[threadIdx.x] = o;
-        s_ml[threadIdx.x] = make_float2(m, l);
-        __syncthreads();
-        if (slot > 0) return;
-#pragma unroll
-        for (int k = 1; k < SLOTS; ++k) m = fmaxf(m, s_ml[threadIdx.x + k * L].x);
-        l = 0.f;
-        o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < SLOTS; ++k) {   // (a slot without a part has m = -infinity: weight 0)
-            const float2 v = s_ml[threadIdx.x + k * L];
-            const float4 x = s_o[threadIdx.x + k * L];
-            const float f = __builtin_amdgcn_exp2f((v.x - m) * p.scale_log2);
-            l = fmaf(f, v.y, l);
-            o = make_float4(fmaf(f, x.x, o.x), fmaf(f, x.y, o.y), fmaf(f, x.z, o.z), fmaf(f, x.w, o.w));
-        }
-    }
-    if ((int64_t)blockIdx.x * RPB + threadIdx.x / (L * SLOTS) >= n || !row.there) return;
+    if ((int64_t)blockIdx.x * RPB + threadIdx.x / L >= n || !row.there) return;
     const float inv = l > 0.f ? 1.f / l : l;
     uint2 v;
     v.x = Elem<F16>::pack(o.x * inv, o.y * inv);
@@ -482,10 +460,10 @@ __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int til
         p.lse[((int64_t)b * s.q_heads + row.head) * s.n_q + row.query] = (m * p.scale_log2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-template <int SLOTS, bool F16, int D>
+template <bool F16, int D>
 inline void launch_join(const SelParams& p, int tile_rows, hipStream_t stream) {
-    const int64_t rows = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.rows, per = 1024 / (D * SLOTS);
-    hipLaunchKernelGGL((selected_join_kernel<SLOTS, F16, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p, tile_rows,
+    const int64_t rows = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.rows, per = 1024 / D;
+    hipLaunchKernelGGL((selected_join_kernel<F16, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p, tile_rows,
                        make_fastdiv((uint32_t)p.rows));
 }
 
@@ -507,8 +485,7 @@ inline hipError_t launch_fwd(const SelParams& p, int tile_rows, hipStream_t stre
     else if (tile_rows == 16)
         hipLaunchKernelGGL((selected_fwd_narrow_kernel<F16, D>), dim3(8 * p.per_xcd), dim3(256), sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1),
                            stream, p);
-    if (p.splits > 8) launch_join<8, F16, D>(p, tile_rows, stream);
-    else if (p.splits > 1) launch_join<1, F16, D>(p, tile_rows, stream);
+    if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
     return hipGetLastError();
 }
 
