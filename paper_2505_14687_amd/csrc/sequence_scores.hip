@@ -56,9 +56,54 @@ __global__ __launch_bounds__(256) void run_means_kernel(MeanParams p) {
     }
 }
 
+// Groups of few queries: C lanes a run, each all of its rows, so that a workgroup takes 256 / C runs and nothing is joined.  (Key blocks stay with the
+// other kernel, also short ones: means of some blocks have the bits that all blocks' have.)
+constexpr int kShortRun = 16;   // rows; 4: 8 192 lists x 8 heads 118 -> 59 us with the scores, 16: 73 -> 27 (x 2 heads), 32: 20 -> 22
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void short_run_means_kernel(MeanParams p) {
+    typedef typename Vec16<T>::type vec;
+    constexpr int V = Vec16<T>::n, C = D / V;
+    const int col = threadIdx.x % C, run = (int)blockIdx.x * (256 / C) + threadIdx.x / C;
+    if (run >= p.runs) return;
+    const int bh = blockIdx.y, b = bh / p.s.kv_heads, h = bh - b * p.s.kv_heads;
+    const int row0 = run * p.run_rows, n = min(p.run_rows, p.s.n_q - row0);
+    const T* const src = (const T*)p.x.data + b * p.x.stride_b + (int64_t)h * p.share * p.x.stride_h + (int64_t)row0 * p.x.stride_n + col * V;
+    float sum[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = 0.f;
+    int i = 0, r = 0;   // head and row
+    for (int left = n * p.share; left > 0; left -= 8) {
+        vec v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {   // (behind the last row: it again, and not added)
+            v[k] = *(const vec*)(src + (int64_t)i * p.x.stride_h + (int64_t)r * p.x.stride_n);
+            if (k + 1 < left && ++r == n) {
+                r = 0;
+                ++i;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += k < left ? (float)v[k][e] : 0.f;
+    }
+    float* const out = p.out + ((int64_t)bh * p.runs + run) * D + col * V;
+    const float all = (float)(n * p.share);
+#pragma unroll
+    for (int e = 0; e < V; e += 4) *(float4*)(out + e) = make_float4(sum[e] / all, sum[e + 1] / all, sum[e + 2] / all, sum[e + 3] / all);
+}
+
 template <typename T>
 static hipError_t launch_means_type(const MeanParams& p, int head_dim, int runs, hipStream_t stream) {
     const int heads = p.s.batch * p.s.kv_heads;
+    if (!p.of_keys && (int64_t)p.run_rows * p.share <= kShortRun) {
+        const int per = 256 * Vec16<T>::n / head_dim;
+        const dim3 grid((unsigned)((runs + per - 1) / per), (unsigned)heads);
+        if (head_dim == 128) hipLaunchKernelGGL((short_run_means_kernel<T, 128>), grid, dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((short_run_means_kernel<T, 64>), grid, dim3(256), 0, stream, p);
+        return hipGetLastError();
+    }
     const dim3 grid((unsigned)runs, (unsigned)heads);
     if (head_dim == 128) hipLaunchKernelGGL((run_means_kernel<T, 128>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((run_means_kernel<T, 64>), grid, dim3(256), 0, stream, p);

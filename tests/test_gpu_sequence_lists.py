@@ -75,6 +75,19 @@ def test_scores(dtype, d, shape):
     assert (np.abs(got[fin] - want[fin]) <= (d + n + 4) * EPS * mag[fin]).all()
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 128), ("f32", 128)])
+@pytest.mark.parametrize("share,q_group", [(1, 1), (3, 5), (2, 8), (16, 1), (1, 16), (17, 1)])
+def test_scores_of_few_queries_a_group(dtype, d, share, q_group):
+    """Mean queries of up to 16 rows, and one more; the last group is short."""
+    N, M, block = 67 + 4 * q_group, 200, 32
+    Q, K = normal((2, 2 * share, N, d), dtype, 26, "heads"), normal((2, 2, M, d), dtype, 27)
+    means = grat.grat_block_means(K, block)
+    got = f64(grat.grat_block_scores(Q, means, 0.3, q_group, block, M, causal=False))
+    want = orc.block_scores(f64(Q), f64(means), 0.3, q_group, block, M, False)
+    mag = orc.block_scores(np.abs(f64(Q)), np.abs(f64(means)), 0.3, q_group, block, M, False)
+    assert (np.abs(got - want) <= (d + q_group * share + 4) * EPS * mag).all()
+
+
 def expect_lists(scores, top, first, local, *where):
     want = orc.select_blocks(scores, top, first, local, *where)
     B, H, G = len(want), len(want[0]), len(want[0][0])
