@@ -142,12 +142,11 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
     p.row_tiles = (int32_t)((rows + plan.tile_rows - 1) / plan.tile_rows);
     const int64_t items = lists * p.row_tiles, units = (int64_t)std::min(max_blocks, s.n_blocks) * (s.block / kUnit);
     const int64_t shares = plan.tile_rows == 16 ? (units + 3) / 4 : (units + 1) / 2;   // steps of a workgroup
-    // A forward launch that leaves compute units idle has lists shared by several workgroups: two a compute unit where a part's results are few
-    // rows, one where they are many (1 000 queries, 20 blocks of 64 keys, 256 workgroups of 128 rows: 30 us, shared by two each 42).  A part is
+    // A forward launch that leaves compute units idle has lists shared by several workgroups, one a compute unit (two cost more than they hide, 64 tokens of
+    // half over 2 048 keys 28.0 us against 26.9, and with many rows their parts' results: 1 000 queries, 20 blocks of 64 keys, 42 against 30).  A part is
     // two steps or more, and a list of fewer than 8 is not split: the launch that joins costs as much (one token, us, not split and split: 4 steps 8.6 and
-    // 9.5, 8 steps 13.0 and 9.2, 16 steps 21.7 and 9.2; 64 queries, 16 steps 23.5, in 8 parts 15.4, in 16 parts 21.1).
-    const int64_t wanted = plan.tile_rows <= 32 ? (512 + items - 1) / items : 256 / items;
-    p.splits = backward || shares < 8 ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(wanted, shares / 2), 64));
+    // 9.5, 8 steps 13.0 and 8.7, 16 steps 21.7 and 8.9; 64 queries, 16 steps 23.5, in 8 parts 15.4, in 16 parts 21.1).
+    p.splits = backward || shares < 8 ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min(256 / items, shares / 2), 64));
     p.items = (int32_t)(items * p.splits);
     p.per_xcd = (p.items + 7) / 8;
     p.fd_splits = make_fastdiv((uint32_t)p.splits);

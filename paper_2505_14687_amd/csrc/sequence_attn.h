@@ -242,77 +242,77 @@ struct KeyLoader {
 // unit of the list and wait for nothing but their own loads.  The 16x16x32 instruction wastes no columns: with Y the group's
 // rows, T^T (32 keys x 16 rows, two instructions a step) leaves lane (row r = lane % 16, g = lane / 16) with keys 16 m + 4 g + i, and
 // Z^T[16 dims, row] += X'^T T is contracted in that order: elements 0 .. 3 keys 4 g + i, 4 .. 7 keys 16 + 4 g + i.
-// Of K and V the one that is only read by rows goes straight from memory to registers as the A operand (lane: key lane % 16, 16 bytes of
-// the 64 that four lanes read of its row), the other through LDS; both a unit ahead, so that a wave has 16 KiB on their way with
-// 16 KiB of LDS.
+// A wave has one unit of K and one of V in LDS, 16 KiB (head_dim 128): as soon as either has landed it is read into fragments, and the next one's
+// loads go out into the same place.  So one of the two is on its way at any time.  (Straight from memory into fragments the 64 bytes
+// of a row belong to lanes 16 apart, and a load takes four times the cycles: 5 227 queries x 8 lists of 4 rows over 512 keys 739 us.)
 template <int D>
 struct NarrowWave {
     static constexpr int kRow = 2 * D, kTile = kUnit * kRow, kChunks = D / 8, kRows = 1024 / kRow, kPieces = kTile / 1024, kN = D / 32, kM = D / 16;
-    const uint8_t *regs, *tiles;         // what goes to registers (this lane's bytes of it), what through LDS
-    int64_t pitch_regs, pitch_tiles;     // bytes
-    uint8_t* lds;                        // two tiles
-    int last;                            // last key that may be read: it stands for those behind it, which are masked
+    const uint8_t *K, *V;        // of the head
+    int64_t pitch_k, pitch_v;    // bytes
+    uint8_t* lds;                // K, V
+    int last;                    // last key that may be read: it stands for those behind it, which are masked
     int lane;
     uint32_t row_at, col_at;
-    __device__ __forceinline__ NarrowWave(const SelParams& p, const Item& it, const SeqTensor& to_regs, const SeqTensor& to_tiles, uint8_t* lds_, int seen,
-                                          int lane_)
-        : lds(lds_), last(seen - 1), lane(lane_) {
+    __device__ __forceinline__ NarrowWave(const SelParams& p, const Item& it, uint8_t* lds_, int seen, int lane_) : lds(lds_), last(seen - 1), lane(lane_) {
         const int r = lane & 15, g = lane >> 4, cq = r & 3, row = 4 * g + (r >> 2);
-        regs = row_address(to_regs, it.b, it.h, 0) + 16 * g;
-        tiles = row_address(to_tiles, it.b, it.h, 0);
-        pitch_regs = 2 * to_regs.stride_n;
-        pitch_tiles = 2 * to_tiles.stride_n;
+        K = row_address(p.K, it.b, it.h, 0);
+        V = row_address(p.V, it.b, it.h, 0);
+        pitch_k = 2 * p.K.stride_n;
+        pitch_v = 2 * p.V.stride_n;
         const uint32_t base = (uint32_t)(uintptr_t)(LDS_PTR(uint8_t))lds;
         row_at = base + r * kRow + ((tile_swizzle<D>(r) ^ g) << 4);
         col_at = base + row * kRow + (((cq >> 1) ^ tile_swizzle<D>(row)) << 4) + 8 * (cq & 1);
     }
-    __device__ __forceinline__ void fetch(int start, frag8 (&f)[2][kN], int odd) const {
+    __device__ __forceinline__ void fetch(const uint8_t* head, int64_t pitch, int start, uint8_t* tile) const {
         const int first = min(start, last), left = last - first;
-        const uint8_t *const rb = regs + first * pitch_regs, *const tb = tiles + first * pitch_tiles;
+        const uint8_t* const base = head + first * pitch;
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) {
             const int row = k * kRows + lane / kChunks;
-            load_lds(tb, (uint32_t)min(row, left) * (uint32_t)pitch_tiles + (((lane % kChunks) ^ tile_swizzle<D>(row)) << 4), lds + odd * kTile + k * 1024);
-        }
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const uint8_t* const src = rb + (uint32_t)min(16 * m + (lane & 15), left) * (uint32_t)pitch_regs;
-#pragma unroll
-            for (int ks = 0; ks < kN; ++ks) f[m][ks] = *(const frag8*)(src + 64 * ks);
+            load_lds(base, (uint32_t)min(row, left) * (uint32_t)pitch + (((lane % kChunks) ^ tile_swizzle<D>(row)) << 4), tile + k * 1024);
         }
     }
-    // A operand, rows = keys 16 m + lane % 16, dims 32 ks + 8 g .. + 7
-    __device__ __forceinline__ frag8 rows(int m, int ks, int odd) const {
-        return *(LDS_PTR(const frag8))(uintptr_t)((row_at ^ (ks << 6)) + odd * kTile + 16 * m * kRow);
+    // A operand, rows = keys 16 m + lane % 16 of K (tile 0) or V (1), dims 32 ks + 8 g .. + 7
+    __device__ __forceinline__ frag8 rows(int tile, int m, int ks) const {
+        return *(LDS_PTR(const frag8))(uintptr_t)((row_at ^ (ks << 6)) + tile * kTile + 16 * m * kRow);
     }
     // A operand, rows = dims 16 dt + lane % 16, contracted over the unit's keys
-    __device__ __forceinline__ frag8 cols(int dt, int odd) const {   // (16 rows on the swizzle is the same)
-        const uint32_t at = (col_at ^ (dt << 5)) + odd * kTile;
+    __device__ __forceinline__ frag8 cols(int tile, int dt) const {   // (16 rows on the swizzle is the same)
+        const uint32_t at = (col_at ^ (dt << 5)) + tile * kTile;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)at);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)(at + 16 * kRow));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    // unit(parity, registers, first key) for every unit of this wave, with the next one's loads on their way
-    template <typename F>
-    __device__ __forceinline__ void walk(const int32_t* units, int n_units, int wave, F&& unit) const {
-        const int mine = max((n_units - wave + 3) / 4, 0);
-        if (mine == 0) return;
-        auto start = [&](int i) { return __builtin_amdgcn_readfirstlane(units[wave + 4 * i]); };
-        frag8 f[2][2][kN];
-        fetch(start(0), f[0], 0);
-        int i = 0;
-        for (; i + 1 < mine; i += 2) {
-            const int a = start(i), b = start(i + 1), ahead = start(min(i + 2, mine - 1));
-            wave_wait();
-            fetch(b, f[1], 1);
-            unit(0, f[0], a);
-            wave_wait();
-            if (i + 2 < mine) fetch(ahead, f[0], 0);
-            unit(1, f[1], b);
-        }
-        if (i < mine) {
-            wave_wait();
-            unit(0, f[0], start(i));
+    // Everything but the last tile's loads, or everything, has landed.  (Loads return in order; what was read from LDS is in registers too.)
+    static __device__ __forceinline__ void wait_but_last() {
+        __builtin_amdgcn_s_waitcnt(kPieces | 7 << 4);
+        asm volatile("" ::: "memory");
+    }
+    // For every unit of this wave: take_k() and take_v() read what they need of K and V from LDS into registers; scores(first key) works
+    // on the former, products(first key) on both.
+    template <typename TK, typename S, typename TV, typename P>
+    __device__ __forceinline__ void walk(const int32_t* units, int n_units, int wave, TK&& take_k, S&& scores, TV&& take_v, P&& products) const {
+        if (wave >= n_units) return;
+        int next = __builtin_amdgcn_readfirstlane(units[wave]);
+        fetch(K, pitch_k, next, lds);
+        fetch(V, pitch_v, next, lds + kTile);
+        for (int i = wave; i < n_units; i += 4) {
+            const int start = next;
+            const bool more = i + 4 < n_units;
+            next = __builtin_amdgcn_readfirstlane(units[min(i + 4, n_units - 1)]);
+            wait_but_last();   // K has landed
+            take_k();
+            wait_but_last();   // and is in registers
+            if (more) fetch(K, pitch_k, next, lds);
+            scores(start);
+            if (more) wait_but_last();   // V has landed
+            else wave_wait();
+            take_v();
+            if (more) wait_but_last();
+            else wave_wait();
+            if (more) fetch(V, pitch_v, next, lds + kTile);
+            products(start);
         }
     }
     // The waves' sums go through LDS: [wave][row][16-byte chunks of 4 dims, XORed with the row].  Then thread (row tid / 16) has D / 16

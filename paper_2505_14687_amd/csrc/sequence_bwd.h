@@ -523,12 +523,12 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     });
 }
 
-// ... of groups of at most 16 rows: V in registers, K through LDS, where it is read by rows and by columns.
+// ... of groups of at most 16 rows.
 template <bool F16, int D>
 __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p, GradParams g) {
     using E = Elem<F16>;
     using W = NarrowWave<D>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2 * W::kTile];   // K, of every wave
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2 * W::kTile];   // K, V of every wave
     __shared__ float s_sum[2][4][16];
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
@@ -579,16 +579,40 @@ __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p
     for (int i = 0; i < W::kM; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float c = p.scale_log2;
     float sum = 0.f;   // over this lane's keys: of P dP while D is being formed, then of dS
-    const W w(p, it, p.V, p.K, lds[wave], seen, lane);
+    const W w(p, it, lds[wave], seen, lane);
+    frag8 kf[2][W::kN], vf[2][W::kN], kt[W::kM];   // K, V by rows, K by columns
     auto walk = [&](auto form_d) {
         constexpr bool kFormD = decltype(form_d)::value;
-        w.walk(s_units, n_units, wave, [&](int odd, const frag8 (&vf)[2][W::kN], int start) {
-            f32x4 S[2], T[2];
+        f32x4 S[2];
+        auto take_k = [&]() {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int ks = 0; ks < W::kN; ++ks) kf[m][ks] = w.rows(0, m, ks);
+            if constexpr (!kFormD) {
+#pragma unroll
+                for (int dt = 0; dt < W::kM; ++dt) kt[dt] = w.cols(0, dt);
+            }
+        };
+        auto take_v = [&]() {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int ks = 0; ks < W::kN; ++ks) vf[m][ks] = w.rows(1, m, ks);
+        };
+        auto scores = [&](int) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                S[m] = T[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                S[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int ks = 0; ks < W::kN; ++ks) S[m] = E::mfma16(w.rows(m, ks, odd), qf[ks], S[m]);
+                for (int ks = 0; ks < W::kN; ++ks) S[m] = E::mfma16(kf[m][ks], qf[ks], S[m]);
+            }
+        };
+        w.walk(s_units, n_units, wave, take_k, scores, take_v, [&](int start) {
+            f32x4 T[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                T[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < W::kN; ++ks) T[m] = E::mfma16(vf[m][ks], df[ks], T[m]);
             }
@@ -610,7 +634,7 @@ __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p
             if constexpr (!kFormD) {
                 const frag8 x = __builtin_bit_cast(frag8, make_uint4(dw[0], dw[1], dw[2], dw[3]));
 #pragma unroll
-                for (int dt = 0; dt < W::kM; ++dt) dq[dt] = E::mfma16(w.cols(dt, odd), x, dq[dt]);
+                for (int dt = 0; dt < W::kM; ++dt) dq[dt] = E::mfma16(kt[dt], x, dq[dt]);
             }
         });
     };

@@ -288,14 +288,12 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     });
 }
 
-// Groups of at most 16 rows: K in registers, V through LDS, the four waves' results joined through LDS.  Against 32 rows on two waves with K
-// and V in tiles that they share: 64 tokens of half over 2 048 keys 29.5 -> 26.7 us (134 MB, 5.0 TB/s, with the join of the parts),
-// 6 218 lists of 16 rows 580 -> 450 us.
+// Groups of at most 16 rows; the four waves' results are joined through LDS.
 template <bool F16, int D>
 __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p) {
     using E = Elem<F16>;
     using W = NarrowWave<D>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2 * W::kTile];   // V, of every wave
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2 * W::kTile];   // K, V of every wave
     __shared__ float s_m[4][16], s_l[4][16];
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
@@ -329,8 +327,19 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p
     for (int i = 0; i < W::kM; ++i) oacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float c = p.scale_log2;
     float m_ref = -1e38f / fmaxf(c, 1.f), l_run = 0.f;   // (finite, so that a unit without a seen key weighs 0)
-    const W w(p, it, p.K, p.V, lds[wave], seen, lane);
-    w.walk(s_units + u_first, n_units, wave, [&](int odd, const frag8 (&kf)[2][W::kN], int start) {
+    const W w(p, it, lds[wave], seen, lane);
+    frag8 kf[2][W::kN], vf[W::kM], weights;
+    auto take_k = [&]() {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int ks = 0; ks < W::kN; ++ks) kf[m][ks] = w.rows(0, m, ks);
+    };
+    auto take_v = [&]() {
+#pragma unroll
+        for (int dt = 0; dt < W::kM; ++dt) vf[dt] = w.cols(1, dt);
+    };
+    auto scores = [&](int start) {
         f32x4 S[2];
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -369,9 +378,11 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p
             ls = weigh();
         }
         l_run += ls;
-        const frag8 x = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        weights = __builtin_bit_cast(frag8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+    };
+    w.walk(s_units + u_first, n_units, wave, take_k, scores, take_v, [&](int) {
 #pragma unroll
-        for (int dt = 0; dt < W::kM; ++dt) oacc[dt] = E::mfma16(w.cols(dt, odd), x, oacc[dt]);
+        for (int dt = 0; dt < W::kM; ++dt) oacc[dt] = E::mfma16(vf[dt], weights, oacc[dt]);
     });
 
     float l = l_run + __shfl_xor(l_run, 16);

@@ -164,6 +164,22 @@ def test_gradient(dtype, d, shape):
     run_case(shape, dtype, d, where="wide" if d == 128 else "tokens", junk=True, backward=True, seed=41)
 
 
+FEW_ROWS = [
+    (1, 1, 1, 1, 1400, 1, 32, 40, [1399], None, True),        # one row; 40 units, dealt to parts and their waves
+    (2, 6, 2, 71, 700, 5, 32, 20, [700, 90], None, True),     # 15 rows a group, the last group 3
+    (1, 48, 2, 3, 1100, 1, 64, 16, None, None, True),         # 24 rows, shared by several workgroups
+    (1, 8, 2, 64, 1200, 64, 64, 16, None, None, True),        # 256 rows, shared by several workgroups
+    (3, 4, 1, 2, 2000, 2, 32, 32, [2000, 40, 0], None, True),  # parts that a short sequence leaves empty
+    (1, 16, 1, 90, 90, 1, 32, 3, None, None, False),          # 16 rows, a unit or less a wave
+]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("shape", FEW_ROWS)
+def test_few_rows(dtype, d, shape):
+    run_case(shape, dtype, d, where="tokens", junk=True, backward=True, seed=61)
+
+
 @pytest.mark.parametrize("dtype,gain", [("bf16", 16.0), ("f16", 8.0)])
 @pytest.mark.parametrize("shape", [TOKENS[1], GROUPS[1], GROUPS[2]])
 def test_peaked_weights(dtype, gain, shape):
@@ -173,7 +189,7 @@ def test_peaked_weights(dtype, gain, shape):
 
 @pytest.mark.parametrize("shape,pick", [
     ((4, 32, 8, 512, 512, 64, 64, 5, None, None, True), [(0, 0), (3, 7)]),              # 256-row workgroups
-    ((1, 8, 2, 1000, 1000, 125, 128, 4, None, None, True), [(0, 1)]),                   # 500 rows a group, 128-key tiles
+    ((1, 8, 2, 1000, 1000, 125, 128, 4, None, None, True), [(0, 1)]),                   # 500 rows a group, blocks of two key tiles
     ((1, 2, 1, 2100, 2100, 1, 32, 4, None, None, True), None),                          # lists of many groups, turned round
 ])
 def test_larger(shape, pick):
