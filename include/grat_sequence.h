@@ -162,7 +162,9 @@ grat_status grat_select_blocks(const grat_sequence* seq, const float* d_scores, 
  *   d_work     scratch memory of grat_selected_attention_work(seq, max_blocks, 0) bytes (NULL where that is 0), 16-byte
  *              aligned
  * Supported: GRAT_BF16, GRAT_F16; head_dim 64 or 128; block a multiple of 32; max_blocks * block <= 2^18; stride_n
- * < 2^24; every other stride as in grat.h.  scale > 0.
+ * < 2^24; every other stride as in grat.h.  scale > 0.  With L = batch * kv_heads * n_groups lists and R = q_group *
+ * (q_heads / kv_heads) rows a list: L * max_blocks, L * R < 2^30, L * ceil(R / 32) < 2^23, batch * q_heads * n_q < 2^29,
+ * batch * kv_heads * n_blocks < 2^24.
  * Scores, reference maximum, sum and output accumulate in fp32; the weights are rounded to the element type (nearest-even)
  * for the product with V, their sum is not.  A NaN or infinite V of a key that some row of a query group sees reaches
  * all rows of that group (0 * NaN); keys that no row of the group sees are never read.
@@ -178,6 +180,8 @@ grat_status grat_selected_attention_fwd(const grat_sequence* seq, const grat_ten
  * no query attends, also those behind the valid keys, get 0.  Every output is written once, nothing is added
  * atomically: the same inputs give the same bits.
  *   d_work     grat_selected_attention_work(seq, max_blocks, 1) bytes, 16-byte aligned
+ * Supported: as the forward call; in addition the parts that the walk over keys is cut into, at most batch * kv_heads *
+ * n_blocks + L * min(max_blocks, n_blocks) * R / 256, times the key tiles of 64 (or 32) of a block, stay below 2^23.
  * The softmax weights and the score gradients are rounded to the element type for the products; all sums in fp32.
  */
 grat_status grat_selected_attention_bwd(const grat_sequence* seq, const grat_tensor* dO, const grat_tensor* Q, const grat_tensor* K,

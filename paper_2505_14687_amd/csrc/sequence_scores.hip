@@ -8,7 +8,8 @@ namespace grat {
 // ---- means -----------------------------------------------------------------------------------
 // Means of runs of rows: key blocks (one head, rows of the tensor up to the sequence's valid keys) and query groups (the heads
 // that share a K/V head, rows up to n_q).  Bound by reading the rows once.  A workgroup per run: a thread owns a 16-byte
-// column and every RL-th row, sums in fp32, and the row lanes are added up through LDS in a fixed order.
+// column and every RL-th row, sums in fp32, and the row lanes are added up through LDS in a fixed order.  Measured: Q of 32 768 tokens, 32 heads,
+// bf16, in groups of 64: 268 MB in 50 us, 5.4 TB/s.
 struct MeanParams {
     SeqShape s;
     SeqTensor x;
@@ -133,7 +134,8 @@ struct ScoreParams {
 };
 
 // Few queries: a matrix-vector product, bound by reading the means once.  A workgroup takes 64 blocks of one K/V head; it forms the
-// groups' mean queries itself, from few rows, and D / 4 lanes share a block.
+// groups' mean queries itself, from few rows, and D / 4 lanes share a block.  Measured: 16 sequences of 1 024 blocks, 8 heads: 68 MB in
+// 16 us, 4.2 TB/s.  (As a matrix product, with a launch for the mean queries, the call takes 38 us against 19.)
 constexpr int kThinRows = 64;     // query rows of a K/V head up to which launches are thin
 constexpr int kThinBlocks = 64;
 
@@ -181,7 +183,8 @@ __global__ __launch_bounds__(256) void thin_scores_kernel(ScoreParams p) {
 // Many queries: a matrix product in fp32 on the fp32 matrix instruction (32x32x2), 64 groups x 64 blocks a workgroup, each of its
 // four waves a quarter.  Both operands lie in LDS as rows of D floats whose 16-byte chunks are XORed with the row, so that a wave's
 // b128 reads (lane = row, half of the lanes each of two chunks) spread over the banks; which k an instruction takes is free as
-// long as both operands agree: element e of chunk 2 i + half.
+// long as both operands agree: element e of chunk 2 i + half.  Measured: 8 heads of 512 groups x 512 blocks 13 us, 41 TFLOP/s of the 154 that
+// a large fp32 product reaches: two workgroups a compute unit, each of which waits for its tiles once.  The means before it take three times as long.
 typedef __attribute__((ext_vector_type(16))) float score16;
 
 template <int D>
@@ -270,7 +273,8 @@ hipError_t launch_block_scores(const SeqShape& s, const SeqTensor& Q, grat_dtype
 // What bounds it is not the reading but the instructions: R ballots and R scalar counts a bit.  So where few are wanted, the common case,
 // the search runs on the lanes' largest keys only and ends at the first bound that little more than `want` of them reach.  What is not
 // below it (of 500 normal scores about 25 where 13 are wanted) is copied to LDS with its block, and a lane ranks one of those.  With several
-// waves the best of their bounds counts, and one wave ranks.
+// waves the best of their bounds counts, and one wave ranks.  Measured: 32 768 lists of 16 from 512 blocks 28 us (46 by bits alone; reading the
+// scores takes 14), 128 lists of 32 from 2 048 blocks 9.4 us a call (four waves a list; 12.5 with sixteen).
 struct SelectParams {
     SeqShape s;
     const float* scores;

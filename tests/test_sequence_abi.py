@@ -107,10 +107,11 @@ def test_attention_refusals():
         assert call(top=(1 << 18) // 64 + 1) == UNSUPPORTED and call(work=FAKE + 4) == UNSUPPORTED
         assert call(s=seq(q_heads=65534, n_q=1 << 16, q_group=1 << 16)) == UNSUPPORTED
     assert fwd(k=tensor(n=132)) == UNSUPPORTED and fwd(v=tensor(n=1 << 24)) == UNSUPPORTED and fwd(q=tensor(b=-8)) == DIMS
-    # few workgroups share their lists, and need room for the parts; many do not
-    assert fwd(work=None) == NULL
-    assert L.grat_selected_attention_work(ref(seq(batch=64, n_q=512)), 4, 0) == 0
-    assert L.grat_selected_attention_work(ref(seq()), 4, 0) > 0 and L.grat_selected_attention_work(ref(seq()), 4, 1) > 0
+    # few workgroups share lists that are long, and need room for the parts; many workgroups and short lists do not
+    assert fwd(s=seq(n_k=4096), top=32, work=None) == NULL
+    assert L.grat_selected_attention_work(ref(seq(batch=64, n_q=512, n_k=4096)), 32, 0) == 0
+    assert L.grat_selected_attention_work(ref(seq()), 4, 0) == 0 and L.grat_selected_attention_work(ref(seq(n_k=4096)), 4, 0) == 0
+    assert L.grat_selected_attention_work(ref(seq(n_k=4096)), 32, 0) > 0 and L.grat_selected_attention_work(ref(seq()), 4, 1) > 0
     assert L.grat_selected_attention_work(ref(seq(d=96)), 4, 1) == 0 and L.grat_selected_attention_work(None, 4, 0) == 0
 
 
