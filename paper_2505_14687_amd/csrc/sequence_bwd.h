@@ -11,7 +11,7 @@
 // Steps: D and dQ | lists of every block, parts | dK, dV | joined parts.
 //
 // Bound by the matrix pipe: 16 384 tokens, 32 heads on 8, 16 blocks of 64 keys, bf16: dQ 420 us (6 d operations a pair, 950 TFLOP/s), lists 12, dK and dV
-// 670 (8 d, 790 TFLOP/s; the pipe busy for 40 % of the cycles, rows gathered from 1.9 GB), join 28.
+// 670 (8 d, 790 TFLOP/s; the pipe busy for 40 % of the cycles, 3.9 GB of rows gathered through the L2, five of six from beyond it), join 28.
 #pragma once
 #include <type_traits>
 
