@@ -264,9 +264,8 @@ hipError_t launch_block_scores(const SeqShape& s, const SeqTensor& Q, grat_dtype
 }
 
 // ---- selection -------------------------------------------------------------------------------
-// A list is chosen by WAVES waves.  Each owns a run of consecutive blocks, 64 at a time, and holds their scores in R registers
-// (R = 0: reads them again from memory whenever they are asked for, for lists too long for that) as integers that order like
-// the scores; 0 is not a candidate.  The smallest selected one is found bit by bit from the highest: the largest T with at least as
+// A list is chosen by WAVES waves.  Each owns a run of 64 R consecutive blocks and holds their scores in R registers as integers that order
+// like the scores; 0 is not a candidate.  The smallest selected one is found bit by bit from the highest: the largest T with at least as
 // many keys >= T as are wanted; a count that is met exactly ends the search.  Keys equal to T are taken in ascending order of their
 // blocks.  What is chosen is compacted by ballots, so lists ascend by construction.
 //
@@ -274,7 +273,7 @@ hipError_t launch_block_scores(const SeqShape& s, const SeqTensor& Q, grat_dtype
 // the search runs on the lanes' largest keys only and ends at the first bound that little more than `want` of them reach.  What is not
 // below it (of 500 normal scores about 25 where 13 are wanted) is copied to LDS with its block, and a lane ranks one of those.  With several
 // waves the best of their bounds counts, and one wave ranks.  Measured: 32 768 lists of 16 from 512 blocks 28 us (46 by bits alone; reading the
-// scores takes 14), 128 lists of 32 from 2 048 blocks 9.4 us a call (four waves a list; 12.5 with sixteen).
+// scores takes 14), 128 lists of 32 from 2 048 blocks 8.9 us a call.
 struct SelectParams {
     SeqShape s;
     const float* scores;
@@ -282,7 +281,6 @@ struct SelectParams {
     int32_t* count;
     int32_t* index;
     int64_t lists;
-    int32_t chunks;   // runs are chunks * 64 blocks long (R = 0)
     FastDiv fd_groups, fd_kv_heads, fd_block;
 };
 
@@ -294,7 +292,6 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
     constexpr int kTwo = WAVES > 1 ? 2 : 1, kFew = 64 * kTwo;   // candidates that a lane ranks, and all of them
     __shared__ uint2 s_few[WAVES == 1 ? 4 : 1][kFew];            // key, block
     __shared__ uint32_t s_bound[2][WAVES];
-    constexpr int kUnroll = R > 0 ? R : 1;
     const SeqShape& s = p.s;
     const int lane = threadIdx.x & 63;
     const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -302,13 +299,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
     const int64_t list = WAVES == 1 ? (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : blockIdx.x;
     if (list >= p.lists) return;
     const float* const row = p.scores + list * s.n_blocks;
-    const int chunks = R > 0 ? R : p.chunks;
-    const int j0 = wave * chunks * 64 + lane;   // this lane's blocks: j0 + 64 r
-    float score[R > 0 ? R : 1];   // (asked for ahead of everything that says which of them count)
-    if constexpr (R > 0) {
+    const int j0 = wave * R * 64 + lane;   // this lane's blocks: j0 + 64 r
+    float score[R];   // (asked for ahead of everything that says which of them count)
 #pragma unroll
-        for (int r = 0; r < R; ++r) score[r] = row[min(j0 + 64 * r, s.n_blocks - 1)];
-    }
+    for (int r = 0; r < R; ++r) score[r] = row[min(j0 + 64 * r, s.n_blocks - 1)];
     uint32_t bh, g;
     fdivmod((uint32_t)list, p.fd_groups, bh, g);
     const int b = (int)fdiv(bh, p.fd_kv_heads);
@@ -323,15 +317,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
         const uint32_t u = __builtin_bit_cast(uint32_t, x), order = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
         return j >= head_end && j < tail && x > -INFINITY ? order : 0;   // (false for NaN)
     };
-    uint32_t held[R > 0 ? R : 1];
-    if constexpr (R > 0) {
+    uint32_t held[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) held[r] = key_of(r, score[r]);
-    }
-    auto key = [&](int r) -> uint32_t {
-        if constexpr (R > 0) return held[r];
-        else return key_of(r, row[min(j0 + 64 * r, s.n_blocks - 1)]);
-    };
+    for (int r = 0; r < R; ++r) held[r] = key_of(r, score[r]);
     int parity = 0;
     // (sum over the waves; of the waves ahead of this one)
     auto everyone = [&](int mine, int& before) {
@@ -354,8 +342,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
     };
     auto count_from = [&](uint32_t t) {
         int n = 0, before;
-#pragma unroll kUnroll
-        for (int r = 0; r < chunks; ++r) n += __popcll(__ballot(key(r) >= t));
+#pragma unroll
+        for (int r = 0; r < R; ++r) n += __popcll(__ballot(held[r] >= t));
         return everyone(n, before);
     };
     const uint64_t below = (1ull << lane) - 1ull;
@@ -481,12 +469,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
         if (!met) ties = want - count_from(T + 1);
     }
     int n = 0, tied_before;
-#pragma unroll kUnroll
-    for (int r = 0; r < chunks; ++r) n += __popcll(__ballot(key(r) == T));
+#pragma unroll
+    for (int r = 0; r < R; ++r) n += __popcll(__ballot(held[r] == T));
     everyone(n, tied_before);
     auto taken = [&](int r, int& tied) {   // tied: keys equal to T ahead of this chunk
         const int j = j0 + 64 * r;
-        const uint32_t k = key(r);
+        const uint32_t k = held[r];
         const uint64_t same = __ballot(k == T);
         const bool in = j < vis && (j < head_end || j >= tail || k > T || (k == T && tied + __popcll(same & below) < ties));
         tied += __popcll(same);
@@ -495,12 +483,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
     int base = 0;
     if constexpr (WAVES > 1) {   // where this wave's part of the list begins
         int mine = 0;
-#pragma unroll kUnroll
-        for (int r = 0, tied = tied_before; r < chunks; ++r) mine += __popcll(__ballot(taken(r, tied)));
+#pragma unroll
+        for (int r = 0, tied = tied_before; r < R; ++r) mine += __popcll(__ballot(taken(r, tied)));
         n = everyone(mine, base);
     }
-#pragma unroll kUnroll
-    for (int r = 0, tied = tied_before; r < chunks; ++r) {
+#pragma unroll
+    for (int r = 0, tied = tied_before; r < R; ++r) {
         const bool in = taken(r, tied);
         const uint64_t all = __ballot(in);
         if (in) out[base + __popcll(all & below)] = j0 + 64 * r;
@@ -512,24 +500,30 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
 }
 
 template <int WAVES, int R>
-static void launch_select(SelectParams p, hipStream_t stream) {
+static void launch_select(const SelectParams& p, hipStream_t stream) {
     const int64_t blocks = WAVES == 1 ? (p.lists + 3) / 4 : p.lists;
-    p.chunks = (p.s.n_blocks + WAVES * 64 - 1) / (WAVES * 64);
     hipLaunchKernelGGL((select_blocks_kernel<WAVES, R>), dim3((unsigned)blocks), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, stream, p);
 }
 
 hipError_t launch_select_blocks(const SeqShape& s, const float* d_scores, int32_t top, int32_t first, int32_t local, int32_t* d_count,
                                 int32_t* d_index, hipStream_t stream) {
-    const SelectParams p{s, d_scores, top, first, local, d_count, d_index, (int64_t)s.batch * s.kv_heads * s.n_groups, 0,
+    const SelectParams p{s, d_scores, top, first, local, d_count, d_index, (int64_t)s.batch * s.kv_heads * s.n_groups,
                          make_fastdiv((uint32_t)s.n_groups), make_fastdiv((uint32_t)s.kv_heads), make_fastdiv((uint32_t)s.block)};
+    // As few waves a list as hold its scores: waves that share a list wait for each other, which costs more than the longer code of one that has
+    // more registers to go through (8 192 lists of 1 024 blocks: one wave 12 us, four 44; of 4 096: four 45, sixteen 247; 512 lists of 16 384: four 15, sixteen
+    // 27).  Two waves for 2 048 blocks where lists are few (128 lists of 32: 8.9 us; one wave 13.8, four 9.7; 1 024 lists: one 8.2, four 8.7).
     const int n = s.n_blocks;
     if (n <= 64) launch_select<1, 1>(p, stream);
     else if (n <= 128) launch_select<1, 2>(p, stream);
     else if (n <= 256) launch_select<1, 4>(p, stream);
     else if (n <= 512) launch_select<1, 8>(p, stream);
-    else if (n <= 2048) launch_select<4, 8>(p, stream);
-    else if (n <= 8192) launch_select<16, 8>(p, stream);
-    else launch_select<16, 0>(p, stream);
+    else if (n <= 1024) launch_select<1, 16>(p, stream);
+    else if (n <= 2048 && p.lists >= 1024) launch_select<1, 32>(p, stream);
+    else if (n <= 2048) launch_select<2, 16>(p, stream);
+    else if (n <= 4096) launch_select<4, 16>(p, stream);
+    else if (n <= 8192) launch_select<4, 32>(p, stream);
+    else if (n <= 16384) launch_select<4, 64>(p, stream);
+    else launch_select<8, 64>(p, stream);
     return hipGetLastError();
 }
 

@@ -142,3 +142,17 @@ def test_selection_of_every_length(blocks):
         want = np.sort(order[:, :top], axis=-1)
         got = index.cpu().numpy()[0, 0][:, :want.shape[1]]
         assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("blocks", [1024, 1025, 1500, 2048, 4096, 4097, 16384, 16385])
+@pytest.mark.parametrize("lists", [3, 1030])
+def test_selection_of_few_and_many_lists(blocks, lists):
+    if blocks > 2048 and lists > 3:
+        lists = 40
+    gen = np.random.default_rng(blocks + lists)
+    scores = np.round(20 * gen.standard_normal((1, 1, lists, blocks))).astype(np.float32)
+    order = np.argsort(-scores[0, 0], axis=-1, kind="stable")
+    for top in (2, 29, 57, 300):
+        count, index = grat.grat_select_blocks(torch.from_numpy(scores).cuda(), top, 0, 0, n_q=lists, n_k=32 * blocks, q_group=1, block=32, causal=False)
+        assert (count == top).all()
+        assert np.array_equal(index.cpu().numpy()[0, 0], np.sort(order[:, :top], axis=-1))
