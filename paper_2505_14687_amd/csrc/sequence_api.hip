@@ -90,14 +90,15 @@ grat_status make_rotary(const grat_rotary_args* a, bool with_k, RotaryParams* ou
 }
 
 // ---- attention over lists --------------------------------------------------------------------
-// Rows of a forward workgroup, of the `rows` of a group: one tile where they fit, else 256 if that fills the chip and wastes no half tile, else 128
-// (32 768 tokens in groups of 64 x 4 heads: 580 us in tiles of 256, 590 in tiles of 128).
+// Rows of a forward workgroup, of the `rows` of a group: one tile where they fit, else 256 if that makes four rounds of the chip and wastes no half tile, else 128
+// (groups of 64 x 4 heads, 16 blocks of 64 keys, us in tiles of 256 and of 128: 512 groups x 8 heads 580 and 590, 100 x 8 109 and 109, 82 x 8 93 and 91, 47 x 8
+// 60 and 55).
 int fwd_tile_rows(const SeqShape& s, int head_dim, int64_t rows) {
     if (rows <= 16) return 16;
     if (rows <= 32) return 32;
     if (rows <= 64) return 64;
     const int64_t lists = (int64_t)s.batch * s.kv_heads * s.n_groups;
-    if (head_dim == 128 && (rows % 256 == 0 || rows % 256 > 128) && lists * ((rows + 255) / 256) >= 256) return 256;
+    if (head_dim == 128 && (rows % 256 == 0 || rows % 256 > 128) && lists * ((rows + 255) / 256) >= 1024) return 256;
     return 128;
 }
 int bwd_tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }

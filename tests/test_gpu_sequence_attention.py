@@ -188,12 +188,21 @@ def test_peaked_weights(dtype, gain, shape):
 
 
 @pytest.mark.parametrize("shape,pick", [
-    ((4, 32, 8, 512, 512, 64, 64, 5, None, None, True), [(0, 0), (3, 7)]),              # 256-row workgroups
+    ((4, 32, 8, 512, 512, 64, 64, 5, None, None, True), [(0, 0), (3, 7)]),              # 256 rows a group
     ((1, 8, 2, 1000, 1000, 125, 128, 4, None, None, True), [(0, 1)]),                   # 500 rows a group, blocks of two key tiles
     ((1, 2, 1, 2100, 2100, 1, 32, 4, None, None, True), None),                          # lists of many groups, turned round
 ])
 def test_larger(shape, pick):
     run_case(shape, "bf16", 128, backward=True, seed=61, full=True, pick=pick)
+
+
+@pytest.mark.parametrize("shape,dtype,pick", [
+    ((4, 32, 8, 2047, 2047, 64, 64, 4, [2047, 1500, 70, 0], None, True), "bf16", [(0, 0), (1, 6), (2, 7)]),   # 256 rows a group
+    ((4, 32, 4, 2000, 2000, 64, 32, 5, None, None, False), "f16", [(0, 1), (3, 3)]),                          # 512
+    ((2, 12, 4, 11000, 600, 80, 64, 5, None, [0, 30], True), "bf16", [(1, 2)]),                               # 240, more queries than keys
+])
+def test_workgroups_of_256_rows(shape, dtype, pick):
+    run_case(shape, dtype, 128, where="tokens", seed=67, full=True, pick=pick)
 
 
 def test_lists_too_many_for_one_workgroup():
