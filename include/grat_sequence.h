@@ -182,7 +182,9 @@ grat_status grat_selected_attention_fwd(const grat_sequence* seq, const grat_ten
  *   d_work     grat_selected_attention_work(seq, max_blocks, 1) bytes, 16-byte aligned
  * Supported: as the forward call; in addition the parts that the walk over keys is cut into, at most batch * kv_heads *
  * n_blocks + L * min(max_blocks, n_blocks) * R / 256, times the key tiles of 64 (or 32) of a block, stay below 2^23.
- * The softmax weights and the score gradients are rounded to the element type for the products; all sums in fp32.
+ * The softmax weights and the score gradients are rounded to the element type for the products; all sums in fp32.  GRAT_F16: both are
+ * taken times powers of two that keep them within half's normal numbers - weights from 2^-26 on; score gradients by the size of
+ * dO, of the row for dQ and of the K/V head's largest row for dK - so dO and V of any size lose nothing that half's results could hold.
  */
 grat_status grat_selected_attention_bwd(const grat_sequence* seq, const grat_tensor* dO, const grat_tensor* Q, const grat_tensor* K,
                                         const grat_tensor* V, const grat_tensor* O, const float* d_lse, const grat_tensor* dQ,

@@ -191,6 +191,12 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
         g.part_slot = (int32_t*)(work + take(plan, most_parts * 4));
         g.joins = (int4*)(work + take(plan, g.most_joins * 16));
         g.slots = (float*)(work + take(plan, most_slots * s.block * 2 * D * 4));
+        g.heads = s.batch * s.kv_heads;
+        if (seq->dtype == GRAT_F16) {
+            g.head_runs = s.n_groups * p.row_tiles * std::max(plan.tile_rows / 32, 1);   // (below 2^30: rows of a head)
+            g.row_bits = (int32_t*)(work + take(plan, (int64_t)g.heads * g.head_runs * 4));
+            g.head_bits = (int32_t*)(work + take(plan, (int64_t)g.heads * 4));
+        }
     }
     *out = plan;
     return GRAT_OK;

@@ -42,6 +42,9 @@ struct GradParams {
     int32_t* part_slot;    // of every part: its slot, -1: its block has no other
     int4* joins;           // blocks of more than one part: block, first slot, parts
     float* slots;          // sums of a part: [key tile of the block][dK, dV][key][D]
+    int32_t* row_bits;     // half: exponents that dS is formed with, the smallest of each run of (at most 32) rows, head after head; else null
+    int32_t* head_bits;    // half: the exponent of a K/V head
+    int32_t heads, head_runs;   // K/V heads of the batch, runs of each
     int32_t words, blocks, most_parts, most_joins, part_rows;
     FastDiv fd_rows, fd_tiles, fd_top, fd_part;   // by rows of a group; key tiles of a block; max_blocks; part_rows
 };

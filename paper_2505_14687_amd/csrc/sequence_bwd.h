@@ -19,12 +19,20 @@
 
 namespace grat {
 
-// Half: the weights of long lists fall below its normal numbers (2^-14), so they are taken 2^12 times as large (in lse2) and D and dP
-// as much smaller; dV's product then has 2^12 in it.  (bf16 has fp32's range.)
-constexpr float kWeightBits = 12.f, kWeightScale = 4096.f;
+// Half ends at 65 504, and below 2^-14 it loses bits; what is rounded to it for a product is taken times a power of two that the fp32 sum is
+// divided by (bf16 has fp32's range):
+//   P in dV's product   2^12, in the lse2 of the walk over keys: weights down to 2^-26 keep all bits
+//   dS in dQ's          a row's own 2^row_bits, in the row's lse2, so that |dO| 2^row_bits is 2^9 to 2^10.  |dS| < |dO| |V| may still be too large
+//                       where V is: an infinite dS leaves no element of the row's sums finite, and such a row is walked again with 2^kBitsBack less, which
+//                       is enough for any V (|V| < 2^19.5 at head_dim 128)
+//   dS in dK's          one power for all rows of a K/V head: the smallest that the rows took (a row that another one outweighs by 2^10 has weights down
+//                       to 2^-14 in full), and one bit less: dS is formed there once more and may come out a little larger
+constexpr int kWeightBits = 12, kRowBits = 10, kBitsBack = 16, kMostBits = 64;
 
-template <bool F16>
-__device__ __forceinline__ float score_grad(float dp, float delta) { return F16 ? fmaf(dp, 1.f / kWeightScale, -delta) : dp - delta; }
+// Exponent for a row whose dO has the sum of squares n2; a row of zeros (or NaN, infinities) has no say in the head's.
+__device__ __forceinline__ int row_bits(float n2) { return kRowBits - ((__builtin_amdgcn_frexp_expf(n2) + 1) >> 1); }
+__device__ __forceinline__ int head_say(float n2, int bits) { return n2 > 0.f && n2 < INFINITY ? bits : kMostBits; }
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
 // ---- dK, dV ------------------------------------------------------------------------------------
 // A workgroup owns 32 KW keys of one block, K and V of a wave's 32 keys in registers, and streams the Q and dO rows of
@@ -70,6 +78,8 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
     f32x16 dk[D / 32], dv[D / 32];
     clear<D>(dk);
     clear<D>(dv);
+    const int bits = F16 ? __builtin_amdgcn_readfirstlane(g.head_bits[bh]) : 0;
+    const float grad_factor = ldexpf(1.f, bits - kWeightBits);   // (half: dS from the P that dV takes)
     if (n_tiles > 0 && tile_key0 < len) {
         frag8 kf[D / 16], vf[D / 16];
         {
@@ -162,7 +172,7 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     S[4 * q + i] = __builtin_amdgcn_exp2f(fmaf(S[4 * q + i], c, -l[i]));
-                    T[4 * q + i] = S[4 * q + i] * score_grad<F16>(T[4 * q + i], dl[i]);
+                    T[4 * q + i] = (F16 ? S[4 * q + i] * grad_factor : S[4 * q + i]) * (T[4 * q + i] - dl[i]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -228,7 +238,7 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
     add(dk);
     add(dv);
     if (team == 1) return;
-    constexpr float dv_factor = F16 ? 1.f / kWeightScale : 1.f;
+    const float dk_factor = F16 ? ldexpf(p.scale, -bits) : p.scale, dv_factor = F16 ? ldexpf(1.f, -kWeightBits) : 1.f;
     const int slot = g.part_slot[part_id];
     if (slot >= 0) {   // parts are joined by grad_join_kernel
         float* const dst = g.slots + (((int64_t)slot * tiles + tile_in_block) * 2 * (32 * KW) + key_wave * 32 + (lane & 31)) * D + 4 * half;
@@ -247,7 +257,7 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
         const int k = tile_key0 + key_wave * 32 + i;
         return k < s.n_k ? (uint8_t*)row_address(t, b, h, k) : nullptr;
     };
-    store_rows<F16, D>(stage, dk, p.scale, lane, [&](int i) { return row_of(g.dK, i); });
+    store_rows<F16, D>(stage, dk, dk_factor, lane, [&](int i) { return row_of(g.dK, i); });
     store_rows<F16, D>(stage, dv, dv_factor, lane, [&](int i) { return row_of(g.dV, i); });
 }
 
@@ -276,7 +286,7 @@ __global__ __launch_bounds__(256) void grad_join_kernel(SelParams p, GradParams 
             const float4 v = *(const float4*)(src + k * pitch + 4 * (int64_t)i);
             sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
         }
-        const float f = which == 0 ? p.scale : F16 ? 1.f / kWeightScale : 1.f;
+        const float f = which == 0 ? (F16 ? ldexpf(p.scale, -g.head_bits[bh]) : p.scale) : F16 ? ldexpf(1.f, -kWeightBits) : 1.f;
         uint2 v;
         v.x = Elem<F16>::pack(sum.x * f, sum.y * f);
         v.y = Elem<F16>::pack(sum.z * f, sum.w * f);
@@ -320,8 +330,8 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     for (int ks = 0; ks < D / 16; ++ks) df[ks] = *(const frag8*)(d_src + 32 * ks);
     // D, and lse in base 2 (a row that attends nothing weighs 0); the walk over the keys takes both from memory
     const int64_t stat = ((int64_t)it.b * s.q_heads + row.head) * s.n_q + row.query;
-    const float lse = p.lse[stat], lse2 = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f - (F16 ? kWeightBits : 0.f);
-    float delta = 0.f;
+    const float lse = p.lse[stat];
+    float lse2 = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f, delta = 0.f, n2 = 0.f;
     {
         typedef typename Vec16<std::conditional_t<F16, _Float16, __bf16>>::type vec;
         const uint8_t* const o_src = row_address(p.O, it.b, row.head, row.query) + 16 * half;
@@ -332,10 +342,24 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
         for (int ks = 0; ks < D / 16; ++ks) {
             const vec d = __builtin_bit_cast(vec, df[ks]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) delta = fmaf((float)o[ks][e], (float)d[e], delta);
+            for (int e = 0; e < 8; ++e) {
+                delta = fmaf((float)o[ks][e], (float)d[e], delta);
+                if constexpr (F16) n2 = fmaf((float)d[e], (float)d[e], n2);
+            }
         }
-        delta = sum_across_halves(delta) * (F16 ? 1.f / kWeightScale : 1.f);
+        delta = sum_across_halves(delta);
     }
+    // half: the exponent of this lane's row (in lse2 as well), and what counts for the head's; kept in LDS for want of registers
+    __shared__ int32_t s_bits[F16 ? 2 : 1][F16 ? NW * 64 : 1];
+    int32_t &bits = s_bits[0][F16 ? threadIdx.x : 0], &say = s_bits[F16][F16 ? threadIdx.x : 0];
+    if constexpr (F16) {
+        n2 = sum_across_halves(n2);
+        const int mine = row_bits(n2);
+        lse2 -= (float)mine;
+        bits = mine;
+        say = head_say(n2, mine);
+    }
+    auto unscaled = [&](float x) { return F16 ? ldexpf(x, -bits) : x; };
     const int len = seq_len(s, it.b);
     const int64_t pos = seq_pos(s, it.b, len);
     const int seen = group_seen(s, len, pos, it.g);
@@ -371,8 +395,8 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
         uint32_t dw[8];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-            float d0 = __builtin_amdgcn_exp2f(fmaf(S[i], c, -lse2)) * score_grad<F16>(T[i], delta);
-            float d1 = __builtin_amdgcn_exp2f(fmaf(S[i + 1], c, -lse2)) * score_grad<F16>(T[i + 1], delta);
+            float d0 = __builtin_amdgcn_exp2f(fmaf(S[i], c, -lse2)) * (T[i] - delta);
+            float d1 = __builtin_amdgcn_exp2f(fmaf(S[i + 1], c, -lse2)) * (T[i + 1] - delta);
             if (masked) {
                 const int key = start + 8 * (i >> 2) + 4 * half + (i & 3);
                 if (key >= limit) d0 = 0.f;
@@ -418,7 +442,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
             S[u][2 * j + 1] = __builtin_amdgcn_exp2f(fmaf(S[u][2 * j + 1], c, -lse2));
         };
         auto grad = [&](int u, int j) {
-            const float d0 = S[u][2 * j] * score_grad<F16>(T[u][2 * j], delta), d1 = S[u][2 * j + 1] * score_grad<F16>(T[u][2 * j + 1], delta);
+            const float d0 = S[u][2 * j] * (T[u][2 * j] - delta), d1 = S[u][2 * j + 1] * (T[u][2 * j + 1] - delta);
             sum += d0 + d1;
             dw[u][j] = E::pack(d0, d1);
             asm volatile("" : "+v"(dw[u][j]));   // (keeps the conversion here: its first use is later)
@@ -478,8 +502,8 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     };
     // over all keys of this lane's row
     __shared__ float s_sum[NW][32];
-    auto over_row = [&]() {
-        float all = sum_across_halves(sum);
+    auto over_row = [&](float mine) {
+        float all = sum_across_halves(mine);
         if constexpr (TEAMS == 2) {
             if (half == 0) s_sum[wave][lane] = all;
             __syncthreads();
@@ -494,12 +518,31 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     if (n_tiles > 0) {
         if (n_units <= kFewUnits) {
             walk(std::true_type{});
-            delta += F16 ? over_row() * (1.f / kWeightScale) : over_row();
+            delta += unscaled(over_row(sum));
             sum = 0.f;
         }
         walk(std::false_type{});
+        if constexpr (F16) {
+            const bool over = over_row(finite(dq[0][0]) ? 0.f : 1.f) > 0.f;
+            if (__syncthreads_or(over)) {
+                if (over) {
+                    bits -= kBitsBack;
+                    say -= kBitsBack;
+                    lse2 += (float)kBitsBack;
+                }
+                clear<D>(dq);
+                sum = 0.f;
+                walk(std::false_type{});
+            }
+        }
     }
-    sum = over_row();
+    sum = unscaled(over_row(sum));
+    if constexpr (F16) {
+        int least = limit > 0 ? say : kMostBits;
+#pragma unroll
+        for (int m = 1; m < 32; m *= 2) least = min(least, __shfl_xor(least, m));
+        if (team == 0 && lane == 0) g.row_bits[it.item * RW + row_wave] = least;
+    }
     if constexpr (TEAMS == 2) {
         float* const mine = (float*)&lds[0][0] + row_wave * 64 * (D / 2) + lane;
         if (team == 1) {
@@ -516,11 +559,11 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
             for (int i = 0; i < 16; ++i) dq[db][i] += mine[(db * 16 + i) * 64];
     }
     if (half == 0 && row.there) {
-        g.delta[stat] = delta + (F16 ? sum * (1.f / kWeightScale) : sum);
-        g.lse2[stat] = lse2;
+        g.delta[stat] = delta + sum;
+        g.lse2[stat] = F16 ? lse2 + (float)(bits - kWeightBits) : lse2;
     }
     uint8_t* const stage = &lds[0][0] + (TEAMS == 2 ? 2 * kTile : 0) + row_wave * 4096;   // (two teams: behind what team 0 still reads)
-    store_rows<F16, D>(stage, dq, p.scale, lane, [&](int i) -> uint8_t* {
+    store_rows<F16, D>(stage, dq, unscaled(p.scale), lane, [&](int i) -> uint8_t* {
         const GroupRow to(p, it.h, it.g, (it.tile * RW + row_wave) * 32 + i);
         return to.there ? (uint8_t*)row_address(g.dQ, it.b, to.head, to.query) : nullptr;
     });
@@ -533,7 +576,7 @@ __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p
     using W = NarrowWave<D>;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[4][2 * W::kTile];   // K, V of every wave
     __shared__ float s_sum[2][4][16];
-    __shared__ int32_t s_n;
+    __shared__ int32_t s_n, s_bits[16];
     extern __shared__ int32_t s_units[];
     const Item it(p);
     start_lists(g);
@@ -554,19 +597,28 @@ __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p
         o[ks] = *(const vec*)(o_src + 64 * ks);
     }
     const int64_t stat = ((int64_t)it.b * s.q_heads + row.head) * s.n_q + row.query;
-    const float lse = p.lse[stat], lse2 = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f - (F16 ? kWeightBits : 0.f);
+    const float lse = p.lse[stat];
+    float lse2 = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f, delta = 0.f, n2 = 0.f;
     auto over_quads = [](float x) {
         x += __shfl_xor(x, 16);
         return x + __shfl_xor(x, 32);
     };
-    float delta = 0.f;
 #pragma unroll
     for (int ks = 0; ks < W::kN; ++ks) {
         const vec d = __builtin_bit_cast(vec, df[ks]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) delta = fmaf((float)o[ks][e], (float)d[e], delta);
+        for (int e = 0; e < 8; ++e) {
+            delta = fmaf((float)o[ks][e], (float)d[e], delta);
+            if constexpr (F16) n2 = fmaf((float)d[e], (float)d[e], n2);
+        }
     }
-    delta = over_quads(delta) * (F16 ? 1.f / kWeightScale : 1.f);
+    delta = over_quads(delta);
+    int bits = 0;   // (as in grad_queries_kernel)
+    if constexpr (F16) {
+        n2 = over_quads(n2);
+        bits = row_bits(n2);
+        lse2 -= (float)bits;
+    }
     const int len = seq_len(s, it.b);
     const int64_t pos = seq_pos(s, it.b, len);
     const int seen = group_seen(s, len, pos, it.g);
@@ -624,8 +676,8 @@ __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 const f32x4 &x = S[i >> 2], &t = T[i >> 2];
-                float d0 = __builtin_amdgcn_exp2f(fmaf(x[i & 3], c, -lse2)) * score_grad<F16>(t[i & 3], delta);
-                float d1 = __builtin_amdgcn_exp2f(fmaf(x[(i & 3) + 1], c, -lse2)) * score_grad<F16>(t[(i & 3) + 1], delta);
+                float d0 = __builtin_amdgcn_exp2f(fmaf(x[i & 3], c, -lse2)) * (t[i & 3] - delta);
+                float d1 = __builtin_amdgcn_exp2f(fmaf(x[(i & 3) + 1], c, -lse2)) * (t[(i & 3) + 1] - delta);
                 if (masked) {
                     const int key = start + 16 * (i >> 2) + 4 * quad + (i & 3);
                     if (key >= limit) d0 = 0.f;
@@ -641,34 +693,57 @@ __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p
             }
         });
     };
-    auto over_row = [&](int which) {   // over all keys of row `r`
-        const float all = over_quads(sum);
-        if (quad == 0) s_sum[which][wave][r] = all;
+    int turn = 0;
+    auto over_row = [&](float mine) {   // over all keys of row `r`
+        const float all = over_quads(mine);
+        turn ^= 1;   // (a barrier lies between what is read here and the next but one's writes)
+        if (quad == 0) s_sum[turn][wave][r] = all;
         __syncthreads();
-        return (s_sum[which][0][r] + s_sum[which][1][r] + s_sum[which][2][r] + s_sum[which][3][r]) * (F16 ? 1.f / kWeightScale : 1.f);
+        return s_sum[turn][0][r] + s_sum[turn][1][r] + s_sum[turn][2][r] + s_sum[turn][3][r];
     };
     if (n_units > 0) {
         if (n_units <= kFewUnits) {   // short lists: a first walk for the exact D
             walk(std::true_type{});
-            delta += over_row(0);
+            delta += ldexpf(over_row(sum), -bits);
             sum = 0.f;
         }
-        walk(std::false_type{});
+#pragma unroll 1
+        for (bool again = false;; again = true) {
+            walk(std::false_type{});
+            if (!F16 || again) break;
+            const bool over = over_row(finite(dq[0][0]) ? 0.f : 1.f) > 0.f;   // (the same in all four waves)
+            if (__builtin_amdgcn_ballot_w64(over) == 0) break;
+            if (over) {
+                bits -= kBitsBack;
+                lse2 += (float)kBitsBack;
+            }
+#pragma unroll
+            for (int i = 0; i < W::kM; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            sum = 0.f;
+        }
     }
-    const float left = over_row(1);   // (its barrier: everyone is done with the tiles)
+    const float left = ldexpf(over_row(sum), -bits);   // (its barrier: everyone is done with the tiles)
+    if constexpr (F16) {
+        int say = limit > 0 ? head_say(n2, bits) : kMostBits;
+#pragma unroll
+        for (int m = 1; m < 16; m *= 2) say = min(say, __shfl_xor(say, m));
+        if (threadIdx.x == 0) g.row_bits[it.item] = say;
+    }
     if (wave == 0 && quad == 0 && row.there) {
         g.delta[stat] = delta + left;
-        g.lse2[stat] = lse2;
+        g.lse2[stat] = F16 ? lse2 + (float)(bits - kWeightBits) : lse2;
     }
     float* const sums = (float*)&lds[0][0];
     static_assert(4 * 16 * D * 4 <= (int)sizeof(lds), "the results fit the tiles");
     W::put(sums, wave, lane, dq);
+    if (threadIdx.x < 16) s_bits[threadIdx.x] = bits;
     __syncthreads();
     float x[W::kOwn];
     const float ones[4] = {1.f, 1.f, 1.f, 1.f};
     W::get(sums, ones, x);
     const GroupRow to(p, it.h, it.g, it.tile * 16 + (int)(threadIdx.x >> 4));
-    if (to.there) W::template store<F16>((uint8_t*)row_address(g.dQ, it.b, to.head, to.query), x, p.scale);
+    const float factor = F16 ? ldexpf(p.scale, -s_bits[threadIdx.x >> 4]) : p.scale;
+    if (to.there) W::template store<F16>((uint8_t*)row_address(g.dQ, it.b, to.head, to.query), x, factor);
 }
 
 template <int KW, bool F16, int D>

@@ -3,8 +3,29 @@
 
 namespace grat {
 
-// The bitmap, cleared (by a kernel: recorded into graphs like any other launch).
+// Half: the exponent that dS of a K/V head is formed with (see sequence_bwd.h), by a workgroup of THREADS.
+template <int THREADS>
+__device__ __forceinline__ void put_head_bits(const GradParams& g, int bh) {
+    __shared__ int s_least[THREADS / 64];
+    const int32_t* const runs = g.row_bits + (int64_t)bh * g.head_runs;
+    int least = 0x7fffffff;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < g.head_runs; i += THREADS) least = min(least, runs[i]);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) least = min(least, __shfl_xor(least, m));
+    if ((threadIdx.x & 63) == 0) s_least[threadIdx.x >> 6] = least;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < THREADS / 64; ++w) least = min(least, s_least[w]);
+        g.head_bits[bh] = least - 1;
+    }
+    __syncthreads();
+}
+
+// The bitmap, cleared (by a kernel: recorded into graphs like any other launch), and half's exponents.
 __global__ __launch_bounds__(256) void grad_clear_kernel(GradParams g) {
+    if (g.row_bits)
+        for (int bh = (int)blockIdx.x; bh < g.heads; bh += (int)gridDim.x) put_head_bits<256>(g, bh);
     const int64_t n = (int64_t)g.blocks * g.words;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) g.bits[i] = 0;
 }
@@ -96,6 +117,7 @@ __global__ __launch_bounds__(1024) void grad_head_lists_kernel(SelParams p, Grad
     const SeqShape& s = p.s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bh = (int)blockIdx.y, block0 = (int)blockIdx.x * kHeadBlocks;
     const int blocks = min(kHeadBlocks, s.n_blocks - block0);
+    if (g.row_bits && blockIdx.x == 0) put_head_bits<1024>(g, bh);
     for (int i = threadIdx.x; i < blocks * g.words; i += 1024) s_bits[i] = 0;
     const int b = (int)fdiv((uint32_t)bh, p.fd_kv_heads), len = seq_len(s, b);
     const int64_t pos = seq_pos(s, b, len);
