@@ -179,7 +179,11 @@ grat_status grat_selected_attention_fwd(const grat_sequence* seq, const grat_ten
  * d_lse as the forward call wrote them.  Heads that share a K/V head add up in its dK and dV.  Rows of dK and dV that
  * no query attends, also those behind the valid keys, get 0.  Every output is written once, nothing is added
  * atomically: the same inputs give the same bits.
- *   d_work     grat_selected_attention_work(seq, max_blocks, 1) bytes, 16-byte aligned
+ *   d_work     grat_selected_attention_work(seq, max_blocks, 1) bytes, 16-byte aligned.  About four times the bytes of dK and dV (100 MB
+ *              at least possible where these are small) for sums of parts, 8 bytes a query row, 4 an entry of a list, and a bit for
+ *              every group and block of a K/V head, n_groups * n_blocks / 8 bytes: with a list per query (q_group = 1) that grows with
+ *              the square of the length - 131 072 tokens in blocks of 64 keys: 34 MB a K/V head, 524 288 tokens 537 MB - and is
+ *              cleared and read once a call
  * Supported: as the forward call; in addition the parts that the walk over keys is cut into, at most batch * kv_heads *
  * n_blocks + L * min(max_blocks, n_blocks) * R / 256, times the key tiles of 64 (or 32) of a block, stay below 2^23.
  * The softmax weights and the score gradients are rounded to the element type for the products; all sums in fp32.  GRAT_F16: both are

@@ -171,10 +171,12 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t max_blocks,
         g.fd_tiles = make_fastdiv((uint32_t)(s.block / plan.tile_keys));
         // Parts of the rows that a block has on average (entries of all lists times the rows of a group, over all blocks), or of fewer where
         // that leaves compute units idle: a launch takes as long as its longest part.  (Against parts of the average length, 512 rows or more, a training
-        // step: 201 queries with a list each 127 -> 60 us, 6 218 of them 2 024 -> 1 550.  More parts, 1 024 or 1 536 for 768: 2 626 tokens 262 -> 252 and 260,
-        // 2 048 in blocks of 128 keys 151 -> 166, 2 047 of half at head_dim 64 67.8 -> 69.3.)
+        // step: 201 queries with a list each 127 -> 60 us, 6 218 of them 2 024 -> 1 550.  More workgroups, 1 024 or 1 536 for 768: 2 626 tokens 262 -> 252 and
+        // 260, 2 047 of half at head_dim 64 67.8 -> 69.3.)  A part is a workgroup a key tile of its block and holds whole blocks in fp32, so it is key tiles
+        // that are counted: with parts counted, 16 384 tokens in blocks of 4 096 keys took 5 960 MiB of scratch memory, not 264, and a step of 1 024 queries on 8 192
+        // keys 1 170 us, not 636; 2 048 tokens in blocks of 128 keys 155, not 136, of 256 keys 163, not 139.
         const int64_t entries = lists * std::min(max_blocks, s.n_blocks), all_rows = entries * rows;
-        const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(all_rows / blocks, 512), all_rows / 768) + 63) / 64 * 64);
+        const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(all_rows / blocks, 512), all_rows * (s.block / plan.tile_keys) / 768) + 63) / 64 * 64);
         g.part_rows = (int32_t)std::min<int64_t>(part, kMaxRows / 2);
         g.fd_part = make_fastdiv((uint32_t)g.part_rows);
         const int64_t most_parts = blocks + all_rows / g.part_rows, most_slots = 2 * (all_rows / g.part_rows) + 1;

@@ -115,6 +115,17 @@ def test_attention_refusals():
     assert L.grat_selected_attention_work(ref(seq(d=96)), 4, 1) == 0 and L.grat_selected_attention_work(None, 4, 0) == 0
 
 
+@pytest.mark.parametrize("block,top", [(32, 32), (64, 16), (128, 8), (256, 8), (1024, 4), (4096, 2), (4096, 4)])
+@pytest.mark.parametrize("n_q,n_k", [(16384, 16384), (1024, 8192), (131072, 131072)])
+def test_scratch_of_the_gradient_goes_with_its_results(block, top, n_q, n_k):
+    """Parts of the walk over keys hold whole blocks in fp32: twice dK and dV, and as much again for the parts' uneven ends; or, in small launches, 2 * 768 + 1
+    parts of 64 keys.  The rest: statistics, lists and bits."""
+    s = seq(q_heads=32, kv_heads=8, n_q=n_q, n_k=n_k, q_group=64, block=block)
+    results = 2 * 2 * 8 * n_k * 128
+    work = sq._library().grat_selected_attention_work(ref(s), top, 1)
+    assert work <= 4.25 * results + (2 * 768 + 1) * 64 * 2 * 128 * 4
+
+
 def test_binding_refusals():
     Q, K = torch.zeros(1, 4, 100, 128, dtype=torch.bfloat16), torch.zeros(1, 2, 100, 128, dtype=torch.bfloat16)
     count, index = torch.zeros(1, 2, 4, dtype=torch.int32), torch.zeros(1, 2, 4, 3, dtype=torch.int32)
