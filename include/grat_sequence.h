@@ -166,8 +166,8 @@ grat_status grat_select_blocks(const grat_sequence* seq, const float* d_scores, 
  * (q_heads / kv_heads) rows a list: L * max_blocks, L * R < 2^30, L * ceil(R / 32) < 2^23, batch * q_heads * n_q < 2^29,
  * batch * kv_heads * n_blocks < 2^24.
  * Scores, reference maximum, sum and output accumulate in fp32; the weights are rounded to the element type (nearest-even)
- * for the product with V, their sum is not.  A NaN or infinite V of a key that some row of a query group sees reaches
- * all rows of that group (0 * NaN); keys that no row of the group sees are never read.
+ * for the product with V, their sum is not.  A NaN or infinite V of a listed key that some row of a query group sees
+ * reaches all rows of that group (0 * NaN); keys that the group does not list, or that none of its rows sees, are never read.
  */
 int64_t grat_selected_attention_work(const grat_sequence* seq, int32_t max_blocks, int32_t backward);
 grat_status grat_selected_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K, const grat_tensor* V,
@@ -179,8 +179,8 @@ grat_status grat_selected_attention_fwd(const grat_sequence* seq, const grat_ten
  * d_lse as the forward call wrote them.  Heads that share a K/V head add up in its dK and dV.  Rows of dK and dV that
  * no query attends, also those behind the valid keys, get 0.  Every output is written once, nothing is added
  * atomically: the same inputs give the same bits.
- *   d_work     grat_selected_attention_work(seq, max_blocks, 1) bytes, 16-byte aligned.  About four times the bytes of dK and dV (100 MB
- *              at least possible where these are small) for sums of parts, 8 bytes a query row, 4 an entry of a list, and a bit for
+ *   d_work     grat_selected_attention_work(seq, max_blocks, 1) bytes, 16-byte aligned.  About four times the bytes of dK and dV (up to
+ *              100 MB where that is less) for sums of parts, 8 bytes a query row, 4 an entry of a list, and a bit for
  *              every group and block of a K/V head, n_groups * n_blocks / 8 bytes: with a list per query (q_group = 1) that grows with
  *              the square of the length - 131 072 tokens in blocks of 64 keys: 34 MB a K/V head, 524 288 tokens 537 MB - and is
  *              cleared and read once a call

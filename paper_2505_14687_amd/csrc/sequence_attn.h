@@ -227,10 +227,11 @@ struct KeyLoader {
             col[k] = ((lane % kChunks) ^ tile_swizzle<D>(r)) << 4;
         }
     }
-    // Keys behind the last that some row sees are not read: the last one stands for them, and they are masked.
+    // start: of a listed unit, which begins with a key that some row sees.  Keys behind the last of these are not read: it stands for them, and they are
+    // masked.
     __device__ __forceinline__ void issue(const uint8_t* head, int64_t pitch, int start, uint8_t* tile, int wave) const {
-        const int first = min(start, last), left = last - first;
-        const uint8_t* const base = head + first * pitch;
+        const int left = last - start;
+        const uint8_t* const base = head + start * pitch;
 #pragma unroll
         for (int k = 0; k < LPW; ++k) load_lds(base, (uint32_t)min(row[k], left) * (uint32_t)pitch + col[k], tile + (wave * LPW + k) * 1024);
     }

@@ -380,6 +380,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     const KeyLoader<NW, D> load(p, it, seen, wave, lane);
     TileReader<D> read(lane, lds[0], team);
     auto unit_start = [&](int i) { return i < n_units ? __builtin_amdgcn_readfirstlane(s_units[i]) : kNoUnit; };
+    auto unit_load = [&](int i) { return __builtin_amdgcn_readfirstlane(s_units[min(i, n_units - 1)]); };   // (as in the forward walk)
     float sum = 0.f;   // over this lane's keys: of P dP while D is being formed, then of dS
     auto block = [&](auto form_d, int hb, int start) {
         constexpr bool kFormD = decltype(form_d)::value;
@@ -481,9 +482,9 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
         products(c1, c2, [](int) {});
     };
     auto walk = [&](auto form_d) {
-        load.issue(unit_start(load.my_unit), lds[0], lds[2], wave);
+        load.issue(unit_load(load.my_unit), lds[0], lds[2], wave);
         for (int t = 0; t < n_tiles; ++t) {
-            const int next = unit_start(2 * t + 2 + load.my_unit), start0 = unit_start(2 * t + (TEAMS == 1 ? 0 : team));
+            const int next = unit_load(2 * t + 2 + load.my_unit), start0 = unit_start(2 * t + (TEAMS == 1 ? 0 : team));
             const int start1 = TEAMS == 1 ? unit_start(2 * t + 1) : kNoUnit;
             tile_barrier();
             if (t + 1 < n_tiles) load.issue(next, lds[(t + 1) & 1], lds[2 + ((t + 1) & 1)], wave);

@@ -67,6 +67,8 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     TileReader<D> read(lane, lds[0], team);
     // (a list's last tile may lack its second unit; one of a part that ends inside the list does not)
     auto unit_start = [&](int i) { return i < n_units ? __builtin_amdgcn_readfirstlane(s_units[u_first + i]) : kNoUnit; };
+    // (what fills a tile in its place is the list's last unit again: a key that is not listed may hold anything, and 0 * NaN is NaN)
+    auto unit_load = [&](int i) { return __builtin_amdgcn_readfirstlane(s_units[u_first + max(min(i, n_units - 1), 0)]); };
 
     auto mask = [&](f32x16& S, int start) {
         if (start + kUnit > least) {
@@ -125,9 +127,9 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
                 for (int db = 0; db < D / 32; ++db) oacc[db] = E::mfma(read.cols(1, 0, s2, db), w, oacc[db]);
             }
         };
-        if (n_tiles > 0) load.issue(unit_start(load.my_unit), lds[0], lds[2], wave);
+        if (n_tiles > 0) load.issue(unit_load(load.my_unit), lds[0], lds[2], wave);
         for (int t = 0; t < n_tiles; ++t) {
-            const int next = unit_start(2 * t + 2 + load.my_unit);
+            const int next = unit_load(2 * t + 2 + load.my_unit);
             tile_barrier();
             if (t + 1 < n_tiles) load.issue(next, lds[(t + 1) & 1], lds[2 + ((t + 1) & 1)], wave);
             block(unit_start(2 * t + team));
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
         constexpr int kAhead = 2, kN = D / 16, kM = 2 * (D / 32);
         f32x16 S[2];
         uint32_t pw[2][8];
-        int ahead = unit_start(load.my_unit), here = 0;   // first keys of this wave's pieces of tile t + 1 and t
+        int ahead = unit_load(load.my_unit), here = 0;   // first keys of this wave's pieces of tile t + 1 and t
         int late = kNoUnit;                               // ... of the second unit of tile t - 1
         auto step = [&](auto odd_c, auto first_c, auto last_c, int t) {
             constexpr int kOdd = decltype(odd_c)::value;   // t & 1
@@ -149,7 +151,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
             constexpr int kItems = (kScores ? kN : 0) + (kAdds ? kM : 0);
             const int start0 = kScores ? unit_start(2 * t) : 0, start1 = kScores ? unit_start(2 * t + 1) : 0;
             here = ahead;
-            ahead = unit_start(2 * t + 2 + load.my_unit);
+            ahead = unit_load(2 * t + 2 + load.my_unit);
             tile_barrier();
             if (t + 1 < n_tiles) load.issue(load.K, load.pitch_k, ahead, lds[kOdd ^ 1], wave);
             if (kScores) load.issue(load.V, load.pitch_v, here, lds[2 + kOdd], wave);
@@ -221,7 +223,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
             if (most == 0) {   // a wave without a row only fetches
                 for (int t = 0; t <= n_tiles; ++t) {
                     here = ahead;
-                    ahead = unit_start(2 * t + 2 + load.my_unit);
+                    ahead = unit_load(2 * t + 2 + load.my_unit);
                     tile_barrier();
                     if (t + 1 < n_tiles) load.issue(load.K, load.pitch_k, ahead, lds[(t + 1) & 1], wave);
                     if (t < n_tiles) load.issue(load.V, load.pitch_v, here, lds[2 + (t & 1)], wave);
