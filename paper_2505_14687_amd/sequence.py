@@ -26,6 +26,7 @@ from .grat import DTYPES, GRAT_OK, GratError, _i32, _i64, _f32, _result, _vp, li
 
 SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
 LAYOUTS = {"half": 0, "interleaved": 1}
+INT32_MAX = 2 ** 31 - 1   # the library's sizes; what is beyond would be cut off on the way
 
 
 class _Tensor(ctypes.Structure):
@@ -111,6 +112,8 @@ def _check(name: str, t, shape=None, like=None):
         raise ValueError(f"{name}: expected a [B, H, N, d] tensor (any strides with d contiguous)")
     if t.stride(3) != 1:
         raise ValueError(f"{name}: the head_dim axis must be contiguous")
+    if max(t.shape) > INT32_MAX:
+        raise ValueError(f"{name}: an axis is longer than {INT32_MAX}")
     if t.dtype not in DTYPES:
         raise ValueError(f"{name}: unsupported dtype {t.dtype}")
     if shape is not None and tuple(t.shape) != tuple(shape):
@@ -136,8 +139,14 @@ def _ints(name: str, t, batch: int, device) -> Optional[int]:
 
 def _positive(**values) -> None:
     for name, v in values.items():
-        if int(v) < 1:
-            raise ValueError(f"{name} must be positive")
+        if not 1 <= int(v) <= INT32_MAX:
+            raise ValueError(f"{name} must be positive and at most {INT32_MAX}")
+
+
+def _int32(**values) -> None:   # (the library refuses what is negative)
+    for name, v in values.items():
+        if abs(int(v)) > INT32_MAX:
+            raise ValueError(f"{name} must be at most {INT32_MAX}")
 
 
 def _shared(q_heads: int, kv_heads: int) -> None:
@@ -158,7 +167,7 @@ def grat_rotary_table(n_pos: int, axis_pairs: Sequence[int], base: float = 10000
     if scaling not in SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(SCALINGS)}")
     _positive(n_pos=n_pos)
-    if not 1 <= len(pairs) <= 3 or min(pairs) < 1:
+    if not 1 <= len(pairs) <= 3 or min(pairs) < 1 or max(pairs) > INT32_MAX:
         raise ValueError("axis_pairs must hold 1 to 3 positive numbers")
     device = torch.device(device)
     context, s = _on(stream, device)
@@ -181,6 +190,8 @@ def _rotary_args(Q, kv_heads: int, table, positions, start, layout: str, axis_pa
         raise ValueError("axis_pairs must hold 1 to 3 positive numbers that add up to the table's pairs")
     if 2 * table.shape[1] > d:
         raise ValueError("the table has more pairs than a head")
+    if table.shape[0] > INT32_MAX:
+        raise ValueError(f"the table has more than {INT32_MAX} positions")
     if positions is not None and start is not None:
         raise ValueError("positions and start exclude each other")
     at, stride = None, 0
@@ -263,6 +274,7 @@ def grat_block_means(K, block: int, k_len=None, new: int = 0, out=None, stream=N
         return _result(r, "grat_block_means")
     _check("K", K)
     _positive(block=block)
+    _int32(new=new)
     B, H, M, d = K.shape
     if int(new) < 0 or (int(new) > 0 and out is None):
         raise ValueError("new keys are added to means that are given as out")
@@ -312,6 +324,7 @@ def grat_select_blocks(scores, top: int, first: int, local: int, n_q: int, n_k: 
     if r is not None:
         return _result(r, "grat_select_blocks")
     _positive(top=top, n_q=n_q, n_k=n_k, q_group=q_group, block=block)
+    _int32(first=first, local=local)
     if not isinstance(scores, torch.Tensor) or scores.dim() != 4:
         raise ValueError("scores must have shape [B, Hkv, groups, blocks]")
     B, Hkv, groups, blocks = scores.shape

@@ -165,6 +165,33 @@ def test_binding_refusals():
         grat.grat_rotary_append(Q, K, K, table, K, K, None)
 
 
+def test_sizes_that_do_not_fit_32_bits_are_refused():
+    """Cut off on the way, 2^32 + 64 keys a block would be 64 with results allocated for one block."""
+    Q, K = torch.zeros(1, 4, 100, 128, dtype=torch.bfloat16), torch.zeros(1, 2, 100, 128, dtype=torch.bfloat16)
+    much = 2 ** 32 + 64
+    count, index = torch.zeros(1, 2, 1, dtype=torch.int32), torch.zeros(1, 2, 1, 3, dtype=torch.int32)
+    scores, lse = torch.zeros(1, 2, 4, 2), torch.zeros(1, 4, 100)
+    lists = dict(n_q=100, n_k=100, q_group=32, block=64)
+    for name, call in [
+        ("block", lambda: grat.grat_block_means(K, much)),
+        ("new", lambda: grat.grat_block_means(K, 64, new=2 ** 32, out=torch.zeros(1, 2, 2, 128))),
+        ("q_group", lambda: grat.grat_block_scores(Q, torch.zeros(1, 2, 2, 128), 0.1, much, 64, 100)),
+        ("n_k", lambda: grat.grat_block_scores(Q, torch.zeros(1, 2, 2, 128), 0.1, 32, 64, 2 ** 32 + 100)),
+        ("q_group", lambda: grat.grat_select_blocks(scores, 2, 0, 1, **{**lists, "q_group": much})),
+        ("block", lambda: grat.grat_select_blocks(scores, 2, 0, 1, **{**lists, "block": much})),
+        ("top", lambda: grat.grat_select_blocks(scores, much, 0, 1, **lists)),
+        ("first", lambda: grat.grat_select_blocks(scores, 2, 2 ** 32, 1, **lists)),
+        ("local", lambda: grat.grat_select_blocks(scores, 2, 0, -2 ** 32, **lists)),
+        ("q_group", lambda: grat.grat_selected_attention_fwd(Q, K, K, 0.1, count, index, much, 64)),
+        ("block", lambda: grat.grat_selected_attention_fwd(Q, K, K, 0.1, count, index, 100, much)),
+        ("q_group", lambda: grat.grat_selected_attention_bwd(Q, Q, K, K, Q, lse, 0.1, count, index, much, 64)),
+        ("n_pos", lambda: grat.grat_rotary_table(2 ** 32 + 1, [8])),
+        ("Q", lambda: grat.grat_rotary(Q.expand(2 ** 32 + 1, -1, -1, -1), None, torch.zeros(100, 64, 2))),
+    ]:
+        with pytest.raises(ValueError, match=rf"^{name}\b"):
+            call()
+
+
 def test_the_native_part_leaves_alone_what_is_not_ordinary():
     sq._library()
     n = sq._native
