@@ -112,7 +112,10 @@ def _result(r, where: str):
 def _ivec(values: Optional[Sequence[int]]):
     if values is None:
         return None
-    return (ctypes.c_int32 * len(values))(*[int(v) for v in values])
+    values = [int(v) for v in values]
+    if any(not -2 ** 31 <= v < 2 ** 31 for v in values):   # (ctypes would cut them off)
+        raise ValueError("extents of grids, groups and radii must fit 32 bits")
+    return (ctypes.c_int32 * len(values))(*values)
 
 
 def _pattern_id(pattern) -> int:

@@ -150,6 +150,16 @@ def test_binding_checks_sequence_length_and_lists():
         grat.grat_attention_packed_fwd(qkv, 0.1, grid, group, cnt, idx)
 
 
+def test_extents_that_do_not_fit_32_bits_are_refused():
+    """Cut off, a group of 2^32 + 2 would be one of 2, with lists for fewer groups than the kernels walk."""
+    with pytest.raises(ValueError, match="32 bits"):
+        grat.grat_block_list_shape([8, 8], [2 ** 32 + 2, 2], "block", [1, 1])
+    with pytest.raises(ValueError, match="32 bits"):
+        grat.grat_block_list_shape([8, 2 ** 32 + 8], [2, 2], "block", [1, 1])
+    with pytest.raises(ValueError, match="32 bits"):
+        grat.grat_block_list_shape([8, 8], [2, 2], "block", [1, -2 ** 32 + 1])
+
+
 def test_validate_block_lists_argument_errors():
     L = grat.lib()
     i32x2 = ctypes.c_int32 * 2
