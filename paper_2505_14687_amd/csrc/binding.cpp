@@ -113,12 +113,8 @@ struct Extents {   // of a grid, a group or a radius
     }
 };
 
-// The device is set up as it is ahead of every tensor that Python makes there, and nothing is done in a forked child.
-hipStream_t stream_of(PyObject* o) {
-    need(!torch::utils::is_device_in_bad_fork(at::kCUDA));
-    torch::utils::device_lazy_init(at::kCUDA);
-    if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
-    PyObject* p = PyObject_GetAttrString(o, "cuda_stream");
+unsigned long long attribute(PyObject* o, const char* name) {   // a whole number
+    PyObject* p = PyObject_GetAttrString(o, name);
     const bool ok = p && PyLong_Check(p);
     const unsigned long long v = ok ? PyLong_AsUnsignedLongLong(p) : 0;
     Py_XDECREF(p);
@@ -126,7 +122,19 @@ hipStream_t stream_of(PyObject* o) {
         PyErr_Clear();
         throw Unusual{};
     }
-    return (hipStream_t)(uintptr_t)v;
+    return v;
+}
+
+// The device is set up as it is ahead of every tensor that Python makes there, and nothing is done in a forked child.  The device is the current one, which
+// the library works on, and the stream one of it.
+hipStream_t stream_of(PyObject* o, const at::Tensor* t) {
+    need(!torch::utils::is_device_in_bad_fork(at::kCUDA));
+    torch::utils::device_lazy_init(at::kCUDA);
+    const c10::hip::HIPStream current = c10::hip::getCurrentHIPStream();
+    need(!t || t->device().index() == current.device_index());
+    if (o == Py_None) return current.stream();
+    need(attribute(o, "device_index") == (unsigned long long)current.device_index());
+    return (hipStream_t)(uintptr_t)attribute(o, "cuda_stream");
 }
 
 grat_dtype dtype_of(const at::Tensor& t) {
@@ -218,7 +226,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Lists lists(a[8], a[9], grid, group, q);
         check_sequence(q.size(2), grid, n_global);
         need(q.size(0) <= INT32_MAX && q.size(1) <= INT32_MAX && q.size(3) <= INT32_MAX);
-        const hipStream_t stream = stream_of(a[11]);
+        const hipStream_t stream = stream_of(a[11], &q);
         const at::Tensor o = a[10] == Py_None ? at::empty_like(q) : tensor_of(a[10]);
         check_like(q, o);
         void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr(), *op = o.data_ptr();
@@ -247,7 +255,7 @@ PyObject* packed(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Lists lists(a[6], a[7], grid, group, x);
         check_sequence(x.size(1), grid, n_global);
         need(x.size(0) <= INT32_MAX && x.size(3) <= INT32_MAX && x.size(4) <= INT32_MAX);
-        const hipStream_t stream = stream_of(a[9]);
+        const hipStream_t stream = stream_of(a[9], &x);
         const std::array<int64_t, 4> shape = {x.size(0), x.size(1), x.size(3), x.size(4)};
         const at::Tensor o = a[8] == Py_None ? at::empty(shape, x.options()) : tensor_of(a[8]);
         need(o.sizes() == at::IntArrayRef(shape) && o.scalar_type() == x.scalar_type() && o.is_contiguous() && o.device() == x.device());
@@ -270,7 +278,7 @@ PyObject* dense(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const grat_dtype dt = dtype_of(q);
         const float scale = scale_of(a[3]);
         need(q.size(0) <= INT32_MAX && q.size(1) <= INT32_MAX && q.size(3) <= INT32_MAX);
-        const hipStream_t stream = stream_of(a[5]);
+        const hipStream_t stream = stream_of(a[5], &q);
         const at::Tensor o = a[4] == Py_None ? at::empty_like(q) : tensor_of(a[4]);
         check_like(q, o);
         void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr(), *op = o.data_ptr();
@@ -299,7 +307,7 @@ PyObject* block_lists(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int32_t* rp = has_radius ? radius : nullptr;
         int32_t groups = 0, max_kv = 0;
         need(g_lib.list_shape(grid.n, grid.v, group.v, pattern, rp, &groups, &max_kv) == GRAT_OK && max_kv >= 1);
-        const hipStream_t stream = stream_of(a[4]);
+        const hipStream_t stream = stream_of(a[4], nullptr);
         const at::TensorOptions opt = at::TensorOptions().dtype(at::kInt).device(at::kCUDA);
         const at::Tensor count = at::empty({groups}, opt), index = at::empty({groups, max_kv}, opt);
         int32_t *cp = (int32_t*)count.data_ptr(), *ip = (int32_t*)index.data_ptr();
@@ -318,10 +326,8 @@ PyObject* block_lists(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // The current stream of the tensors' device, which has to be the current one.
 hipStream_t current_stream(const at::Tensor& t, PyObject* given) {
-    need(given == Py_None);
-    const hipStream_t s = stream_of(given);
-    need(t.is_cuda() && t.device().index() == c10::hip::getCurrentHIPStream().device_index());
-    return s;
+    need(given == Py_None && t.is_cuda());
+    return stream_of(given, &t);
 }
 
 // A [B, H, N, d] tensor like the others.

@@ -10,6 +10,7 @@ torch it was built against; where it cannot be loaded every call takes the ctype
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib
 import os
@@ -127,6 +128,19 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
+@contextlib.contextmanager
+def _on(stream, device):
+    """Where a call runs: on the tensors' device, which is the current one inside (the library works on that, and the handle of a default
+    stream does not say whose it is), and on the stream that is given or the device's current one.  Yields the handle to enqueue on."""
+    if device.type != "cuda":
+        raise ValueError("libgrat works on device memory only")
+    given = getattr(stream, "device", None)
+    if given is not None and device.index is not None and given.index != device.index:
+        raise ValueError(f"the stream must be one of the tensors' device ({device}), not of {given}")
+    with torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else torch.cuda.device(device):
+        yield int((torch.cuda.current_stream(device) if stream is None else stream).cuda_stream)
+
+
 def grat_block_list_shape(grid: Sequence[int], group: Sequence[int], pattern,
                           radius: Optional[Sequence[int]] = None) -> Tuple[int, int]:
     """(num_groups, max_kv) for a pattern; host only."""
@@ -151,9 +165,10 @@ def grat_build_block_lists(grid: Sequence[int], group: Sequence[int], pattern,
     max_kv = need if max_kv is None else int(max_kv)
     kv_count = torch.empty(G, dtype=torch.int32, device=device)
     kv_index = torch.empty((G, max(max_kv, 1)), dtype=torch.int32, device=device)
-    st = lib().grat_build_block_lists(len(grid), _ivec(grid), _ivec(group), _pattern_id(pattern),
-                                      _ivec(radius), kv_count.data_ptr(), kv_index.data_ptr(),
-                                      max_kv, _stream_ptr(stream))
+    with _on(stream, kv_count.device) as s:
+        st = lib().grat_build_block_lists(len(grid), _ivec(grid), _ivec(group), _pattern_id(pattern),
+                                          _ivec(radius), kv_count.data_ptr(), kv_index.data_ptr(),
+                                          max_kv, s)
     if st != GRAT_OK:
         raise GratError(st, "grat_build_block_lists")
     return kv_count, kv_index
@@ -169,9 +184,10 @@ def grat_validate_block_lists(grid: Sequence[int], group: Sequence[int], kv_coun
     if not kv_count.is_cuda:
         raise ValueError("libgrat works on device memory only")
     status = torch.empty(1, dtype=torch.int32, device=kv_count.device)
-    st = lib().grat_validate_block_lists(len(grid), _ivec(grid), _ivec(group), kv_count.data_ptr(),
-                                         kv_index.data_ptr(), int(kv_index.shape[1]), status.data_ptr(),
-                                         _stream_ptr(stream))
+    with _on(stream, kv_count.device) as s:
+        st = lib().grat_validate_block_lists(len(grid), _ivec(grid), _ivec(group), kv_count.data_ptr(),
+                                             kv_index.data_ptr(), int(kv_index.shape[1]), status.data_ptr(),
+                                             s)
     if st != GRAT_OK:
         raise GratError(st, "grat_validate_block_lists")
     return status
@@ -238,11 +254,12 @@ def grat_attention_fwd(Q, K, V, scale: float, grid: Sequence[int], group: Sequen
         _check_lists(kv_count, kv_index, _num_groups(grid, group), Q.device)
     _check_qkvo(Q, K, V, O)
     B, H, N, d = Q.shape
-    st = lib().grat_attention_fwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
-                                  DTYPES[Q.dtype], B, H, d, Q.stride(0), Q.stride(1), Q.stride(2),
-                                  float(scale), len(grid), _ivec(grid), _ivec(group),
-                                  kv_count.data_ptr(), kv_index.data_ptr(), int(kv_index.shape[1]),
-                                  _stream_ptr(stream))
+    with _on(stream, Q.device) as s:
+        st = lib().grat_attention_fwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
+                                      DTYPES[Q.dtype], B, H, d, Q.stride(0), Q.stride(1), Q.stride(2),
+                                      float(scale), len(grid), _ivec(grid), _ivec(group),
+                                      kv_count.data_ptr(), kv_index.data_ptr(), int(kv_index.shape[1]),
+                                      s)
     if st != GRAT_OK:
         raise GratError(st, "grat_attention_fwd")
     return O
@@ -262,12 +279,13 @@ def grat_attention_global_fwd(Q, K, V, scale: float, n_global: int, global_first
         _check_lists(kv_count, kv_index, _num_groups(grid, group), Q.device)
     _check_qkvo(Q, K, V, O)
     B, H, L, d = Q.shape
-    st = lib().grat_attention_global_fwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
-                                         DTYPES[Q.dtype], B, H, d, Q.stride(0), Q.stride(1),
-                                         Q.stride(2), float(scale), int(n_global), int(bool(global_first)),
-                                         len(grid), _ivec(grid), _ivec(group), kv_count.data_ptr(),
-                                         kv_index.data_ptr(), int(kv_index.shape[1]),
-                                         _stream_ptr(stream))
+    with _on(stream, Q.device) as s:
+        st = lib().grat_attention_global_fwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
+                                             DTYPES[Q.dtype], B, H, d, Q.stride(0), Q.stride(1),
+                                             Q.stride(2), float(scale), int(n_global), int(bool(global_first)),
+                                             len(grid), _ivec(grid), _ivec(group), kv_count.data_ptr(),
+                                             kv_index.data_ptr(), int(kv_index.shape[1]),
+                                             s)
     if st != GRAT_OK:
         raise GratError(st, "grat_attention_global_fwd")
     return O
@@ -291,11 +309,12 @@ def grat_attention_packed_fwd(QKV, scale: float, grid: Sequence[int], group: Seq
     O = torch.empty((B, L, H, d), dtype=QKV.dtype, device=QKV.device) if out is None else out
     if O.shape != (B, L, H, d) or O.dtype != QKV.dtype or not O.is_contiguous() or O.device != QKV.device:
         raise ValueError("out must be a contiguous [B, L, H, d] tensor of QKV's dtype and device")
-    st = lib().grat_attention_packed_fwd(QKV.data_ptr(), O.data_ptr(), DTYPES[QKV.dtype], B, H, d,
-                                         float(scale), int(n_global), int(bool(global_first)),
-                                         len(grid), _ivec(grid), _ivec(group), kv_count.data_ptr(),
-                                         kv_index.data_ptr(), int(kv_index.shape[1]),
-                                         _stream_ptr(stream))
+    with _on(stream, QKV.device) as s:
+        st = lib().grat_attention_packed_fwd(QKV.data_ptr(), O.data_ptr(), DTYPES[QKV.dtype], B, H, d,
+                                             float(scale), int(n_global), int(bool(global_first)),
+                                             len(grid), _ivec(grid), _ivec(group), kv_count.data_ptr(),
+                                             kv_index.data_ptr(), int(kv_index.shape[1]),
+                                             s)
     if st != GRAT_OK:
         raise GratError(st, "grat_attention_packed_fwd")
     return O
@@ -310,9 +329,10 @@ def grat_dense_attention_fwd(Q, K, V, scale: float, out=None, stream=None):
     O = torch.empty_like(Q) if out is None else out
     _check_qkvo(Q, K, V, O)
     B, H, N, d = Q.shape
-    st = lib().grat_dense_attention_fwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
-                                        DTYPES[Q.dtype], B, H, N, d, Q.stride(0), Q.stride(1),
-                                        Q.stride(2), float(scale), _stream_ptr(stream))
+    with _on(stream, Q.device) as s:
+        st = lib().grat_dense_attention_fwd(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
+                                            DTYPES[Q.dtype], B, H, N, d, Q.stride(0), Q.stride(1),
+                                            Q.stride(2), float(scale), s)
     if st != GRAT_OK:
         raise GratError(st, "grat_dense_attention_fwd")
     return O

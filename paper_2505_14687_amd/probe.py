@@ -8,7 +8,7 @@ from typing import Optional, Sequence
 import numpy as np
 import torch
 
-from .grat import DTYPES, GRAT_OK, GratError, _ivec, _stream_ptr, lib
+from .grat import DTYPES, GRAT_OK, GratError, _ivec, _on, lib
 
 PROBE_DATA = {"ones": 0, "small_ints": 1, "normal_like": 2}
 
@@ -21,7 +21,8 @@ def grat_probe_mfma(dtype, data, blocks: int, iters: int, sink=None, stream=None
     if sink.dtype != torch.int64 or not sink.is_contiguous() or sink.numel() < int(blocks) * 256:
         raise ValueError("sink: contiguous int64, at least blocks * 256 elements")
     kind = PROBE_DATA[data] if isinstance(data, str) else int(data)
-    st = lib().grat_probe_mfma(DTYPES[dtype], kind, sink.data_ptr(), int(blocks), int(iters), _stream_ptr(stream))
+    with _on(stream, sink.device) as s:
+        st = lib().grat_probe_mfma(DTYPES[dtype], kind, sink.data_ptr(), int(blocks), int(iters), s)
     if st != GRAT_OK:
         raise GratError(st, "grat_probe_mfma")
     return sink

@@ -1,7 +1,7 @@
 """Token sequences: rotary positions, and attention over key blocks that a score selects (include/grat_sequence.h).
 
 Marshalling only, like grat.py (ordinary calls on the current stream in csrc/binding.cpp, all others here): every step runs in the
-library's kernels, on the current stream or the one that is given.  Results and scratch memory are allocated for the stream that the call runs on.
+library's kernels, on the tensors' device, on its current stream or the one that is given.  Results and scratch memory are allocated for the stream that the call runs on.
 
     table = grat_rotary_table(n_pos, [head_dim // 2])                      # once
     Q, K = grat_rotary(Q, K, table)
@@ -15,14 +15,13 @@ each sequence; q_pos (int32 [B]): position of its first query, by default the qu
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 from typing import Optional, Sequence
 
 import torch
 
 from . import grat
-from .grat import DTYPES, GRAT_OK, GratError, _i32, _i64, _f32, _result, _vp, lib
+from .grat import DTYPES, GRAT_OK, GratError, _i32, _i64, _f32, _on, _result, _vp, lib
 
 SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
 LAYOUTS = {"half": 0, "interleaved": 1}
@@ -93,15 +92,6 @@ def _call(name: str, *args):
         raise GratError(st, name)
 
 
-def _on(stream, device):
-    """Context in which results are allocated, and the stream to enqueue on."""
-    if device.type != "cuda":
-        raise ValueError("libgrat works on device memory only")
-    if stream is None:
-        return contextlib.nullcontext(), int(torch.cuda.current_stream(device).cuda_stream)
-    return torch.cuda.stream(stream), int(stream.cuda_stream)
-
-
 def _tensor(t: torch.Tensor) -> _Tensor:
     return _Tensor(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
 
@@ -170,11 +160,10 @@ def grat_rotary_table(n_pos: int, axis_pairs: Sequence[int], base: float = 10000
     if not 1 <= len(pairs) <= 3 or min(pairs) < 1 or max(pairs) > INT32_MAX:
         raise ValueError("axis_pairs must hold 1 to 3 positive numbers")
     device = torch.device(device)
-    context, s = _on(stream, device)
-    with context:
-        table = torch.empty((int(n_pos), sum(pairs), 2), dtype=torch.float32, device=device)
     spec = _Spec(SCALINGS[scaling], float(base), float(factor), float(magnitude), float(trained), float(low), float(high))
-    _call("grat_rotary_table", ctypes.byref(spec), int(n_pos), len(pairs), (_i32 * len(pairs))(*pairs), table.data_ptr(), s)
+    with _on(stream, device) as s:
+        table = torch.empty((int(n_pos), sum(pairs), 2), dtype=torch.float32, device=device)
+        _call("grat_rotary_table", ctypes.byref(spec), int(n_pos), len(pairs), (_i32 * len(pairs))(*pairs), table.data_ptr(), s)
     return table
 
 
@@ -223,16 +212,15 @@ def grat_rotary(Q, K, table, positions=None, start=None, layout: str = "half", a
     if K is not None:
         _check("K", K, (Q.shape[0], K.shape[1] if isinstance(K, torch.Tensor) and K.dim() == 4 else 0, Q.shape[2], Q.shape[3]), Q)
     args = _rotary_args(Q, 0 if K is None else K.shape[1], table, positions, start, layout, axis_pairs, inverse)
-    context, s = _on(stream, Q.device)
-    if out is None:
-        with context:
+    with _on(stream, Q.device) as s:
+        if out is None:
             out = torch.empty_like(Q), None if K is None else torch.empty_like(K)
-    Qo, Ko = out
-    _check("out[0]", Qo, Q.shape, Q)
-    if K is not None:
-        _check("out[1]", Ko, K.shape, Q)
-    k = (None, None) if K is None else (ctypes.byref(_tensor(K)), ctypes.byref(_tensor(Ko)))
-    _call("grat_rotary", ctypes.byref(args), ctypes.byref(_tensor(Q)), ctypes.byref(_tensor(Qo)), *k, s)
+        Qo, Ko = out
+        _check("out[0]", Qo, Q.shape, Q)
+        if K is not None:
+            _check("out[1]", Ko, K.shape, Q)
+        k = (None, None) if K is None else (ctypes.byref(_tensor(K)), ctypes.byref(_tensor(Ko)))
+        _call("grat_rotary", ctypes.byref(args), ctypes.byref(_tensor(Q)), ctypes.byref(_tensor(Qo)), *k, s)
     return Qo, Ko
 
 
@@ -253,13 +241,12 @@ def grat_rotary_append(Q, K, V, table, K_cache, V_cache, start, layout: str = "h
     if start is None:
         raise ValueError("start must be given: tokens that each cache holds")
     args = _rotary_args(Q, K.shape[1], table, None, start, layout, None, False)
-    context, s = _on(stream, Q.device)
-    if out is None:
-        with context:
+    with _on(stream, Q.device) as s:
+        if out is None:
             out = torch.empty_like(Q)
-    _check("out", out, Q.shape, Q)
-    _call("grat_rotary_append", ctypes.byref(args), *(ctypes.byref(_tensor(t)) for t in (Q, out, K, V, K_cache, V_cache)),
-          int(K_cache.shape[2]), s)
+        _check("out", out, Q.shape, Q)
+        _call("grat_rotary_append", ctypes.byref(args), *(ctypes.byref(_tensor(t)) for t in (Q, out, K, V, K_cache, V_cache)),
+              int(K_cache.shape[2]), s)
     return out
 
 
@@ -280,11 +267,10 @@ def grat_block_means(K, block: int, k_len=None, new: int = 0, out=None, stream=N
         raise ValueError("new keys are added to means that are given as out")
     shape = (B, H, _ceil(M, int(block)), d)
     seq = _Sequence(DTYPES[K.dtype], B, H, H, d, 1, M, 1, int(block), 0, _ints("k_len", k_len, B, K.device), None)
-    context, s = _on(stream, K.device)
-    if out is None:
-        with context:
+    with _on(stream, K.device) as s:
+        if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=K.device)
-    _call("grat_block_means", ctypes.byref(seq), ctypes.byref(_tensor(K)), int(new), _flat("out", out, torch.float32, shape, K.device), s)
+        _call("grat_block_means", ctypes.byref(seq), ctypes.byref(_tensor(K)), int(new), _flat("out", out, torch.float32, shape, K.device), s)
     return out
 
 
@@ -306,13 +292,12 @@ def grat_block_scores(Q, means, scale: float, q_group: int, block: int, n_k: int
     seq = _Sequence(DTYPES[Q.dtype], B, Hq, Hkv, d, N, int(n_k), int(q_group), int(block), int(bool(causal)),
                     _ints("k_len", k_len, B, Q.device), _ints("q_pos", q_pos, B, Q.device))
     need = _lib.grat_block_scores_work(ctypes.byref(seq))
-    context, s = _on(stream, Q.device)
-    with context:
+    with _on(stream, Q.device) as s:
         work = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
         if out is None:
             out = torch.empty((B, Hkv, groups, blocks), dtype=torch.float32, device=Q.device)
-    _call("grat_block_scores", ctypes.byref(seq), ctypes.byref(_tensor(Q)), where, float(scale),
-          _flat("out", out, torch.float32, (B, Hkv, groups, blocks), Q.device), work.data_ptr() if need else None, s)
+        _call("grat_block_scores", ctypes.byref(seq), ctypes.byref(_tensor(Q)), where, float(scale),
+              _flat("out", out, torch.float32, (B, Hkv, groups, blocks), Q.device), work.data_ptr() if need else None, s)
     return out
 
 
@@ -331,11 +316,10 @@ def grat_select_blocks(scores, top: int, first: int, local: int, n_q: int, n_k: 
     where = _flat("scores", scores, torch.float32, (B, Hkv, _ceil(int(n_q), int(q_group)), _ceil(int(n_k), int(block))), scores.device)
     seq = _Sequence(0, B, Hkv, Hkv, 0, int(n_q), int(n_k), int(q_group), int(block), int(bool(causal)),
                     _ints("k_len", k_len, B, scores.device), _ints("q_pos", q_pos, B, scores.device))
-    context, s = _on(stream, scores.device)
-    with context:
+    with _on(stream, scores.device) as s:
         count = torch.empty((B, Hkv, groups), dtype=torch.int32, device=scores.device)
         index = torch.empty((B, Hkv, groups, int(top)), dtype=torch.int32, device=scores.device)
-    _call("grat_select_blocks", ctypes.byref(seq), where, int(top), int(first), int(local), count.data_ptr(), index.data_ptr(), s)
+        _call("grat_select_blocks", ctypes.byref(seq), where, int(top), int(first), int(local), count.data_ptr(), index.data_ptr(), s)
     return count, index
 
 
@@ -373,14 +357,13 @@ def grat_selected_attention_fwd(Q, K, V, scale: float, count, index, q_group: in
     if r is not None:
         return _result(r, "grat_selected_attention_fwd")
     seq, lists = _attention_args(Q, K, V, count, index, q_group, block, causal, k_len, q_pos)
-    context, s = _on(stream, Q.device)
-    with context:
+    with _on(stream, Q.device) as s:
         work = _work(seq, lists[2], 0, Q.device)
         O = torch.empty_like(Q) if out is None else out
         lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if return_lse else None
-    _check("out", O, Q.shape, Q)
-    _call("grat_selected_attention_fwd", ctypes.byref(seq), *(ctypes.byref(_tensor(t)) for t in (Q, K, V, O)),
-          lse.data_ptr() if return_lse else None, float(scale), *lists, work.data_ptr() if work is not None else None, s)
+        _check("out", O, Q.shape, Q)
+        _call("grat_selected_attention_fwd", ctypes.byref(seq), *(ctypes.byref(_tensor(t)) for t in (Q, K, V, O)),
+              lse.data_ptr() if return_lse else None, float(scale), *lists, work.data_ptr() if work is not None else None, s)
     return (O, lse) if return_lse else O
 
 
@@ -395,13 +378,11 @@ def grat_selected_attention_bwd(dO, Q, K, V, O, lse, scale: float, count, index,
     _check("dO", dO, Q.shape, Q)
     _check("O", O, Q.shape, Q)
     where = _flat("lse", lse, torch.float32, Q.shape[:3], Q.device)
-    context, s = _on(stream, Q.device)
-    with context:
+    with _on(stream, Q.device) as s:
         work = _work(seq, lists[2], 1, Q.device)
-        grads = (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)) if out is None else tuple(out)
-    for name, t, like in zip(("out[0]", "out[1]", "out[2]"), grads, (Q, K, V)):
-        _check(name, t, like.shape, Q)
-    dQ, dK, dV = grads
-    _call("grat_selected_attention_bwd", ctypes.byref(seq), *(ctypes.byref(_tensor(t)) for t in (dO, Q, K, V, O)), where,
-          *(ctypes.byref(_tensor(t)) for t in (dQ, dK, dV)), float(scale), *lists, work.data_ptr() if work is not None else None, s)
+        dQ, dK, dV = grads = (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)) if out is None else tuple(out)
+        for name, t, like in zip(("out[0]", "out[1]", "out[2]"), grads, (Q, K, V)):
+            _check(name, t, like.shape, Q)
+        _call("grat_selected_attention_bwd", ctypes.byref(seq), *(ctypes.byref(_tensor(t)) for t in (dO, Q, K, V, O)), where,
+              *(ctypes.byref(_tensor(t)) for t in (dQ, dK, dV)), float(scale), *lists, work.data_ptr() if work is not None else None, s)
     return dQ, dK, dV
