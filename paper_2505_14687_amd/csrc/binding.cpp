@@ -9,6 +9,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -330,12 +331,16 @@ hipStream_t current_stream(const at::Tensor& t, PyObject* given) {
     return stream_of(given, &t);
 }
 
+// Nothing is recorded by autograd: a tensor that asks for a gradient is not an ordinary one (and is refused).
+void no_gradient(const at::Tensor& t) { need(!(t.requires_grad() && c10::GradMode::is_enabled()) && !t._fw_grad(0).defined()); }
+
 // A [B, H, N, d] tensor like the others.
 const at::Tensor& rows_of(PyObject* o, const at::Tensor* like = nullptr) {
     const at::Tensor& t = tensor_of(o);
     need(t.dim() == 4 && t.stride(3) == 1 && t.is_cuda());
     if (like) need(t.scalar_type() == like->scalar_type() && t.device() == like->device());
     for (int i = 0; i < 4; ++i) need(t.size(i) >= 1 && t.size(i) <= INT32_MAX);
+    no_gradient(t);
     return t;
 }
 void same_shape(const at::Tensor& a, const at::Tensor& b) { need(a.sizes() == b.sizes()); }
@@ -345,6 +350,7 @@ grat_tensor tensor4(const at::Tensor& t) { return {t.data_ptr(), t.stride(0), t.
 void* flat(PyObject* o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor& like, bool optional = false) {
     if (optional && o == Py_None) return nullptr;
     const at::Tensor& t = tensor_of(o);
+    no_gradient(t);
     need(t.scalar_type() == type && t.sizes() == shape && t.is_contiguous() && t.device() == like.device());
     return t.data_ptr();
 }
@@ -385,6 +391,7 @@ struct RotaryCall {
         const at::Tensor& t = tensor_of(table);
         need(t.dim() == 3 && t.size(2) == 2 && t.size(0) >= 1 && t.size(0) <= INT32_MAX && 2 * t.size(1) <= q.size(3) && t.size(1) >= 1);
         need(t.scalar_type() == at::kFloat && t.is_contiguous() && t.device() == q.device());
+        no_gradient(t);
         args.dtype = dtype_of(q);
         args.batch = (int32_t)q.size(0);
         args.q_heads = (int32_t)q.size(1);
@@ -489,6 +496,7 @@ PyObject* means(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const hipStream_t stream = current_stream(k, a[5]);
         const at::Tensor out = a[4] == Py_None ? at::empty({B, H, blocks, d}, k.options().dtype(at::kFloat)) : tensor_of(a[4]);
         need(out.scalar_type() == at::kFloat && out.sizes() == at::IntArrayRef({B, H, blocks, d}) && out.is_contiguous() && out.device() == k.device());
+        no_gradient(out);
         const grat_tensor t = tensor4(k);
         float* const o = (float*)out.data_ptr();
         return result(without_gil([&] { return g_seq.means(&s, &t, (int32_t)fresh, o, stream); }), a[4], out);
@@ -512,6 +520,7 @@ PyObject* scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor work = bytes ? scratch(bytes, q) : at::Tensor();
         const at::Tensor out = a[9] == Py_None ? at::empty({B, Hkv, groups, blocks}, q.options().dtype(at::kFloat)) : tensor_of(a[9]);
         need(out.scalar_type() == at::kFloat && out.sizes() == at::IntArrayRef({B, Hkv, groups, blocks}) && out.is_contiguous() && out.device() == q.device());
+        no_gradient(out);
         const grat_tensor t = tensor4(q);
         float* const o = (float*)out.data_ptr();
         void* const w = bytes ? work.data_ptr() : nullptr;

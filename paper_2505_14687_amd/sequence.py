@@ -12,6 +12,9 @@ library's kernels, on the tensors' device, on its current stream or the one that
 
 Q is [B, Hq, N, d], K and V are [B, Hkv, M, d] views (any strides with d contiguous); Hkv divides Hq.  k_len (int32 [B]): valid keys of
 each sequence; q_pos (int32 [B]): position of its first query, by default the queries are the newest tokens.
+
+Nothing is recorded by autograd, and tensors that require a gradient are refused while it records: make the calls in a torch.autograd.Function
+(examples/selected_attention.py), with grat_rotary(inverse=True) and grat_selected_attention_bwd in its backward, or under torch.no_grad().
 """
 from __future__ import annotations
 
@@ -19,6 +22,7 @@ import ctypes
 from typing import Optional, Sequence
 
 import torch
+from torch.autograd import forward_ad
 
 from . import grat
 from .grat import DTYPES, GRAT_OK, GratError, _i32, _i64, _f32, _on, _result, _vp, lib
@@ -96,6 +100,13 @@ def _tensor(t: torch.Tensor) -> _Tensor:
     return _Tensor(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
 
 
+def _no_gradient(name: str, t) -> None:
+    """What the library computes is not recorded by autograd: the gradient of such a tensor would be lost without a word."""
+    if torch.is_grad_enabled() and t.requires_grad or forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} requires a gradient, which these calls do not record: make them in a torch.autograd.Function whose backward "
+                         "calls the gradients' entry points, or under torch.no_grad()")
+
+
 def _check(name: str, t, shape=None, like=None):
     """A [B, H, N, d] tensor as the library reads it."""
     if not isinstance(t, torch.Tensor) or t.dim() != 4:
@@ -110,9 +121,10 @@ def _check(name: str, t, shape=None, like=None):
         raise ValueError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
     if like is not None and (t.dtype != like.dtype or t.device != like.device):
         raise ValueError(f"{name} must have the dtype and the device of the other tensors")
+    _no_gradient(name, t)
 
 
-def _flat(name: str, t, dtype, shape, device) -> int:
+def _flat(name: str, t, dtype, shape, device, differentiable: bool = True) -> int:
     """A contiguous tensor of one shape; its address."""
     if not isinstance(t, torch.Tensor) or t.dtype != dtype:
         raise ValueError(f"{name} must be a tensor of {dtype}")
@@ -120,6 +132,8 @@ def _flat(name: str, t, dtype, shape, device) -> int:
         raise ValueError(f"{name} must be contiguous and have shape {list(shape)}, not {list(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} must live on the tensors' device ({device})")
+    if differentiable:
+        _no_gradient(name, t)
     return t.data_ptr()
 
 
@@ -313,7 +327,8 @@ def grat_select_blocks(scores, top: int, first: int, local: int, n_q: int, n_k: 
     if not isinstance(scores, torch.Tensor) or scores.dim() != 4:
         raise ValueError("scores must have shape [B, Hkv, groups, blocks]")
     B, Hkv, groups, blocks = scores.shape
-    where = _flat("scores", scores, torch.float32, (B, Hkv, _ceil(int(n_q), int(q_group)), _ceil(int(n_k), int(block))), scores.device)
+    where = _flat("scores", scores, torch.float32, (B, Hkv, _ceil(int(n_q), int(q_group)), _ceil(int(n_k), int(block))), scores.device,
+                  differentiable=False)   # (the lists are whole numbers)
     seq = _Sequence(0, B, Hkv, Hkv, 0, int(n_q), int(n_k), int(q_group), int(block), int(bool(causal)),
                     _ints("k_len", k_len, B, scores.device), _ints("q_pos", q_pos, B, scores.device))
     with _on(stream, scores.device) as s:

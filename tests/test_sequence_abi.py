@@ -192,6 +192,60 @@ def test_sizes_that_do_not_fit_32_bits_are_refused():
             call()
 
 
+def calls_on(device, dtype=torch.bfloat16):
+    """name -> (call(tensors), the tensors whose gradient it would lose)"""
+    def floats(*shape):
+        return torch.zeros(shape, device=device)
+    t = dict(Q=floats(1, 4, 100, 128).to(dtype), K=floats(1, 2, 100, 128).to(dtype), V=floats(1, 2, 100, 128).to(dtype),
+             dO=floats(1, 4, 100, 128).to(dtype), O=floats(1, 4, 100, 128).to(dtype), table=floats(100, 64, 2), means=floats(1, 2, 2, 128),
+             lse=floats(1, 4, 100), cache=floats(1, 2, 100, 128).to(dtype), out=floats(1, 4, 100, 128).to(dtype), kept=floats(1, 2, 2, 128),
+             written=floats(1, 2, 4, 2))
+    lists = torch.zeros(1, 2, 4, dtype=torch.int32, device=device), torch.full((1, 2, 4, 2), -1, dtype=torch.int32, device=device)
+    start = torch.zeros(1, dtype=torch.int32, device=device)
+    return t, {
+        "rotary": (lambda x: grat.grat_rotary(x["Q"], x["K"], x["table"], out=(x["out"], torch.empty_like(x["K"]))), ("Q", "K", "table", "out")),
+        "append": (lambda x: grat.grat_rotary_append(x["Q"], x["K"], x["V"], x["table"], x["cache"], torch.empty_like(x["cache"]), start),
+                   ("Q", "K", "V", "table", "cache")),
+        "means": (lambda x: grat.grat_block_means(x["K"], 64, out=x["kept"]), ("K", "kept")),
+        "scores": (lambda x: grat.grat_block_scores(x["Q"], x["means"], 0.1, 32, 64, 100, out=x["written"]), ("Q", "means", "written")),
+        "fwd": (lambda x: grat.grat_selected_attention_fwd(x["Q"], x["K"], x["V"], 0.1, *lists, 32, 64, out=x["out"]), ("Q", "K", "V", "out")),
+        "bwd": (lambda x: grat.grat_selected_attention_bwd(x["dO"], x["Q"], x["K"], x["V"], x["O"], x["lse"], 0.1, *lists, 32, 64),
+                ("dO", "Q", "K", "V", "O", "lse")),
+    }
+
+
+def check_gradients_are_not_lost(device):
+    tensors, entries = calls_on(device)
+    for call, names in entries.values():
+        for name in names:
+            if device == "cpu" and name in ("out", "kept", "written"):   # (results are looked at when the device is known to be right)
+                continue
+            x = {k: v.clone().requires_grad_(k == name) for k, v in tensors.items()}
+            with pytest.raises(ValueError, match="requires a gradient"):
+                call(x)
+            if device == "cuda":
+                with torch.no_grad():
+                    call(x)
+            with torch.autograd.forward_ad.dual_level():
+                x = {k: torch.autograd.forward_ad.make_dual(v, torch.ones_like(v)) if k == name else v for k, v in tensors.items()}
+                with pytest.raises(ValueError, match="requires a gradient"):
+                    call(x)
+        if device == "cuda":
+            call(tensors)
+
+
+def test_gradients_are_not_lost():
+    check_gradients_are_not_lost("cpu")
+
+
+@pytest.mark.gpu
+def test_gradients_are_not_lost_on_the_gpu():
+    check_gradients_are_not_lost("cuda")
+    scores = torch.zeros(1, 2, 4, 2, device="cuda", requires_grad=True)   # lists have no gradient to lose
+    count, _ = grat.grat_select_blocks(scores, 1, 0, 0, n_q=100, n_k=100, q_group=32, block=64)
+    assert (count == 1).all()
+
+
 def test_the_native_part_leaves_alone_what_is_not_ordinary():
     sq._library()
     n = sq._native
