@@ -377,10 +377,18 @@ PyObject* tuple_of(std::initializer_list<PyObject*> items) {
     if (!ok) Py_CLEAR(t);
     return t;
 }
+// A tensor of the caller's has been written to: autograd then notices where it had saved it.  (Inference tensors have no version.)
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 PyObject* given_or(PyObject* given, const at::Tensor& t) {
     if (given == Py_None) return THPVariable_Wrap(t);
+    written(t);
     Py_INCREF(given);
     return given;
+}
+PyObject* sequence_result(grat_status st, PyObject* given, const at::Tensor& t) {
+    return st != GRAT_OK ? PyLong_FromLong((long)st) : given_or(given, t);
 }
 
 struct RotaryCall {
@@ -479,7 +487,12 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         same_shape(q, qo);
         const grat_tensor t[6] = {tensor4(q), tensor4(qo), tensor4(k), tensor4(v), tensor4(kc), tensor4(vc)};
         const int32_t rows = (int32_t)kc.size(2);
-        return result(without_gil([&] { return g_seq.append(&call.args, t, t + 1, t + 2, t + 3, t + 4, t + 5, rows, stream); }), a[8], qo);
+        const grat_status st = without_gil([&] { return g_seq.append(&call.args, t, t + 1, t + 2, t + 3, t + 4, t + 5, rows, stream); });
+        if (st == GRAT_OK) {
+            written(kc);
+            written(vc);
+        }
+        return sequence_result(st, a[8], qo);
     });
 }
 
@@ -499,7 +512,7 @@ PyObject* means(PyObject*, PyObject* const* a, Py_ssize_t n) {
         no_gradient(out);
         const grat_tensor t = tensor4(k);
         float* const o = (float*)out.data_ptr();
-        return result(without_gil([&] { return g_seq.means(&s, &t, (int32_t)fresh, o, stream); }), a[4], out);
+        return sequence_result(without_gil([&] { return g_seq.means(&s, &t, (int32_t)fresh, o, stream); }), a[4], out);
     });
 }
 
@@ -524,7 +537,7 @@ PyObject* scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const grat_tensor t = tensor4(q);
         float* const o = (float*)out.data_ptr();
         void* const w = bytes ? work.data_ptr() : nullptr;
-        return result(without_gil([&] { return g_seq.scores(&s, &t, mp, scale, o, w, stream); }), a[9], out);
+        return sequence_result(without_gil([&] { return g_seq.scores(&s, &t, mp, scale, o, w, stream); }), a[9], out);
     });
 }
 
@@ -589,7 +602,7 @@ PyObject* selected_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const grat_status st = without_gil([&] {
             return g_seq.attention_fwd(&c.s, t, t + 1, t + 2, t + 3, lp, c.scale, c.count, c.index, c.top, w, stream);
         });
-        if (st != GRAT_OK || !with_lse) return result(st, a[12], o);
+        if (st != GRAT_OK || !with_lse) return sequence_result(st, a[12], o);
         return tuple_of({given_or(a[12], o), THPVariable_Wrap(lse)});
     });
 }

@@ -90,10 +90,14 @@ def _library() -> ctypes.CDLL:
     return _lib
 
 
-def _call(name: str, *args):
+def _call(name: str, *args, written=()):
+    """written: the caller's tensors that it writes to; autograd then notices where it had saved one of them."""
     st = getattr(_library(), name)(*args)
     if st != GRAT_OK:
         raise GratError(st, name)
+    for t in written:
+        if t is not None and not t.is_inference():   # (these have no version)
+            torch.autograd.graph.increment_version(t)
 
 
 def _tensor(t: torch.Tensor) -> _Tensor:
@@ -227,6 +231,7 @@ def grat_rotary(Q, K, table, positions=None, start=None, layout: str = "half", a
         _check("K", K, (Q.shape[0], K.shape[1] if isinstance(K, torch.Tensor) and K.dim() == 4 else 0, Q.shape[2], Q.shape[3]), Q)
     args = _rotary_args(Q, 0 if K is None else K.shape[1], table, positions, start, layout, axis_pairs, inverse)
     with _on(stream, Q.device) as s:
+        written = () if out is None else tuple(out)
         if out is None:
             out = torch.empty_like(Q), None if K is None else torch.empty_like(K)
         Qo, Ko = out
@@ -234,7 +239,7 @@ def grat_rotary(Q, K, table, positions=None, start=None, layout: str = "half", a
         if K is not None:
             _check("out[1]", Ko, K.shape, Q)
         k = (None, None) if K is None else (ctypes.byref(_tensor(K)), ctypes.byref(_tensor(Ko)))
-        _call("grat_rotary", ctypes.byref(args), ctypes.byref(_tensor(Q)), ctypes.byref(_tensor(Qo)), *k, s)
+        _call("grat_rotary", ctypes.byref(args), ctypes.byref(_tensor(Q)), ctypes.byref(_tensor(Qo)), *k, s, written=written[:1 if K is None else 2])
     return Qo, Ko
 
 
@@ -256,11 +261,12 @@ def grat_rotary_append(Q, K, V, table, K_cache, V_cache, start, layout: str = "h
         raise ValueError("start must be given: tokens that each cache holds")
     args = _rotary_args(Q, K.shape[1], table, None, start, layout, None, False)
     with _on(stream, Q.device) as s:
+        written = (K_cache, V_cache, out)
         if out is None:
             out = torch.empty_like(Q)
         _check("out", out, Q.shape, Q)
         _call("grat_rotary_append", ctypes.byref(args), *(ctypes.byref(_tensor(t)) for t in (Q, out, K, V, K_cache, V_cache)),
-              int(K_cache.shape[2]), s)
+              int(K_cache.shape[2]), s, written=written)
     return out
 
 
@@ -282,9 +288,11 @@ def grat_block_means(K, block: int, k_len=None, new: int = 0, out=None, stream=N
     shape = (B, H, _ceil(M, int(block)), d)
     seq = _Sequence(DTYPES[K.dtype], B, H, H, d, 1, M, 1, int(block), 0, _ints("k_len", k_len, B, K.device), None)
     with _on(stream, K.device) as s:
+        written = (out,)
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=K.device)
-        _call("grat_block_means", ctypes.byref(seq), ctypes.byref(_tensor(K)), int(new), _flat("out", out, torch.float32, shape, K.device), s)
+        _call("grat_block_means", ctypes.byref(seq), ctypes.byref(_tensor(K)), int(new), _flat("out", out, torch.float32, shape, K.device), s,
+              written=written)
     return out
 
 
@@ -307,11 +315,11 @@ def grat_block_scores(Q, means, scale: float, q_group: int, block: int, n_k: int
                     _ints("k_len", k_len, B, Q.device), _ints("q_pos", q_pos, B, Q.device))
     need = _lib.grat_block_scores_work(ctypes.byref(seq))
     with _on(stream, Q.device) as s:
-        work = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
+        work, written = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None, (out,)
         if out is None:
             out = torch.empty((B, Hkv, groups, blocks), dtype=torch.float32, device=Q.device)
         _call("grat_block_scores", ctypes.byref(seq), ctypes.byref(_tensor(Q)), where, float(scale),
-              _flat("out", out, torch.float32, (B, Hkv, groups, blocks), Q.device), work.data_ptr() if need else None, s)
+              _flat("out", out, torch.float32, (B, Hkv, groups, blocks), Q.device), work.data_ptr() if need else None, s, written=written)
     return out
 
 
@@ -378,7 +386,8 @@ def grat_selected_attention_fwd(Q, K, V, scale: float, count, index, q_group: in
         lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if return_lse else None
         _check("out", O, Q.shape, Q)
         _call("grat_selected_attention_fwd", ctypes.byref(seq), *(ctypes.byref(_tensor(t)) for t in (Q, K, V, O)),
-              lse.data_ptr() if return_lse else None, float(scale), *lists, work.data_ptr() if work is not None else None, s)
+              lse.data_ptr() if return_lse else None, float(scale), *lists, work.data_ptr() if work is not None else None, s,
+              written=(out,))
     return (O, lse) if return_lse else O
 
 
@@ -399,5 +408,6 @@ def grat_selected_attention_bwd(dO, Q, K, V, O, lse, scale: float, count, index,
         for name, t, like in zip(("out[0]", "out[1]", "out[2]"), grads, (Q, K, V)):
             _check(name, t, like.shape, Q)
         _call("grat_selected_attention_bwd", ctypes.byref(seq), *(ctypes.byref(_tensor(t)) for t in (dO, Q, K, V, O)), where,
-              *(ctypes.byref(_tensor(t)) for t in (dQ, dK, dV)), float(scale), *lists, work.data_ptr() if work is not None else None, s)
+              *(ctypes.byref(_tensor(t)) for t in (dQ, dK, dV)), float(scale), *lists, work.data_ptr() if work is not None else None, s,
+              written=() if out is None else grads)
     return dQ, dK, dV

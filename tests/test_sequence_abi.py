@@ -246,6 +246,41 @@ def test_gradients_are_not_lost_on_the_gpu():
     assert (count == 1).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("given", [False, True])
+def test_autograd_notices_what_is_written(given):
+    """Tensors of the caller's that a call writes to have a new version afterwards; in both ways of marshalling."""
+    t, _ = calls_on("cuda")
+    Q, K, V = t["Q"], t["K"], t["V"]
+    lists = torch.zeros(1, 2, 4, dtype=torch.int32, device="cuda"), torch.full((1, 2, 4, 2), -1, dtype=torch.int32, device="cuda")
+    start, s = torch.zeros(1, dtype=torch.int32, device="cuda"), dict(stream=torch.cuda.current_stream() if given else None)
+    Qo, Ko, Vo = (torch.empty_like(x) for x in (Q, K, V))
+    for call, written in [
+        (lambda: grat.grat_rotary(Q, K, t["table"], out=(Qo, Ko), **s), (Qo, Ko)),
+        (lambda: grat.grat_rotary(Q, None, t["table"], out=(Qo, None), **s), (Qo,)),
+        (lambda: grat.grat_rotary_append(Q, K, V, t["table"], t["cache"], Vo, start, out=Qo, **s), (t["cache"], Vo, Qo)),
+        (lambda: grat.grat_block_means(K, 64, out=t["kept"], **s), (t["kept"],)),
+        (lambda: grat.grat_block_scores(Q, t["means"], 0.1, 32, 64, 100, out=t["written"], **s), (t["written"],)),
+        (lambda: grat.grat_selected_attention_fwd(Q, K, V, 0.1, *lists, 32, 64, out=t["out"], **s), (t["out"],)),
+        (lambda: grat.grat_selected_attention_fwd(Q, K, V, 0.1, *lists, 32, 64, out=t["out"], return_lse=True, **s), (t["out"],)),
+        (lambda: grat.grat_selected_attention_bwd(t["dO"], Q, K, V, t["O"], t["lse"], 0.1, *lists, 32, 64, out=(Qo, Ko, Vo), **s), (Qo, Ko, Vo)),
+    ]:
+        before = {id(x): x._version for x in (*t.values(), Qo, Ko, Vo)}
+        call()
+        for x in (*t.values(), Qo, Ko, Vo):
+            assert x._version - before[id(x)] == any(x is w for w in written)
+        with torch.inference_mode():
+            call()
+    w = torch.ones(1, 4, 100, 128, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    y = (w * Qo).sum()                       # (saves Qo)
+    grat.grat_rotary(Q, None, t["table"], out=(Qo, None), **s)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    with torch.inference_mode():             # these have no version
+        a, b = torch.zeros_like(Q), torch.zeros_like(Q)
+    grat.grat_rotary(a, None, t["table"], out=(b, None), **s)
+
+
 def test_the_native_part_leaves_alone_what_is_not_ordinary():
     sq._library()
     n = sq._native
