@@ -66,7 +66,7 @@ typedef struct {
  *                           are forced into it.
  * Products and sums in fp32 (pairs of bf16 / half are exact there), rounded once.
  * Supported: all three dtypes; head_dim and rot multiples of 16, rot <= head_dim <= 1024; strides and pointers in 16
- * bytes as in grat.h.
+ * bytes as in grat.h; batch * n_tokens < 2^24 floor(w / head_dim), w = 2048 (fp32) or 4096 (16 bits), and < 2^30.
  */
 typedef struct {
     grat_dtype dtype;
@@ -121,7 +121,7 @@ grat_status grat_rotary_append(const grat_rotary_args* args, const grat_tensor* 
  *   n_new = 0: all blocks.  n_new > 0: only the blocks that hold one of the last n_new valid keys of their sequence
  *   (means kept with a cache); the others are not touched.
  * Of `seq` dtype, batch, kv_heads, head_dim, n_k, block and d_k_len are read.
- * Supported: all three dtypes; head_dim 64 or 128; block a multiple of 32, <= 4096.
+ * Supported: all three dtypes; head_dim 64 or 128; block a multiple of 32, <= 4096; n_blocks < 2^24.
  */
 grat_status grat_block_means(const grat_sequence* seq, const grat_tensor* K, int32_t n_new, float* d_means, void* hip_stream);
 
@@ -131,7 +131,7 @@ grat_status grat_block_means(const grat_sequence* seq, const grat_tensor* K, int
  * Sums and products in fp32.
  *   d_means as grat_block_means writes them
  *   d_work  scratch memory of grat_block_scores_work(seq) bytes (NULL where that is 0), 16-byte aligned
- * Supported: as grat_block_means; scale any finite number.
+ * Supported: as grat_block_means; n_groups <= 64 * 65535; scale any finite number.
  */
 int64_t grat_block_scores_work(const grat_sequence* seq);
 grat_status grat_block_scores(const grat_sequence* seq, const grat_tensor* Q, const float* d_means, float scale, float* d_scores,
@@ -146,7 +146,7 @@ grat_status grat_block_scores(const grat_sequence* seq, const grat_tensor* Q, co
  *   d_index[batch][kv_heads][n_groups][top]  (out) blocks in ascending order, then -1
  * top >= 1, first >= 0, local >= 0, first + local <= top (GRAT_ERR_BAD_DIMS); `local` of at least ceil(q_group / block) + 1
  * lets every row of a causal group see itself.
- * Supported: n_blocks <= 32768, top <= 8192, fewer than 2^26 lists.  Of `seq` dtype and q_heads are not read, head_dim neither.
+ * Supported: n_blocks <= 32768, top <= 8192, at most 2^26 - 4 lists, below 2^24 where n_blocks > 2048, below 2^23 where it is > 16384.  Of `seq` dtype and q_heads are not read, head_dim neither.
  */
 grat_status grat_select_blocks(const grat_sequence* seq, const float* d_scores, int32_t top, int32_t first, int32_t local,
                                int32_t* d_count, int32_t* d_index, void* hip_stream);

@@ -26,6 +26,7 @@ grat_status check_tensor(const grat_tensor* t, grat_dtype dtype, int32_t head_di
 SeqTensor of(const grat_tensor* t) { return {(uint8_t*)t->data, t->stride_b, t->stride_h, t->stride_n}; }
 
 constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxThreads = (int64_t)1 << 32;   // of an axis of a launch; fewer
 
 // The parts of a grat_sequence that every operator on lists reads.
 grat_status make_shape(const grat_sequence* s, SeqShape* out) {
@@ -70,7 +71,10 @@ grat_status make_rotary(const grat_rotary_args* a, bool with_k, RotaryParams* ou
     if (a->positions_stride_b < 0) return GRAT_ERR_BAD_DIMS;
     if (!known(a->dtype)) return GRAT_ERR_UNSUPPORTED;
     if (a->head_dim % 16 || a->rot % 16 || a->head_dim > 1024 || !aligned16(a->d_table)) return GRAT_ERR_UNSUPPORTED;
-    if ((int64_t)a->batch * a->n_tokens >= kMaxRows || (int64_t)a->q_heads + 2 * (int64_t)(with_k ? a->kv_heads : 0) > 65535) return GRAT_ERR_UNSUPPORTED;
+    // (a workgroup of 256 threads takes at least 256 / pieces tokens, rounded down)
+    const int64_t tokens = (int64_t)a->batch * a->n_tokens, per = 256 / (a->head_dim / (is16(a->dtype) ? 16 : 8));
+    if (tokens >= kMaxRows || (tokens + per - 1) / per * 256 >= kMaxThreads) return GRAT_ERR_UNSUPPORTED;
+    if ((int64_t)a->q_heads + 2 * (int64_t)(with_k ? a->kv_heads : 0) > 65535) return GRAT_ERR_UNSUPPORTED;
     p.heads[0] = a->q_heads;
     p.heads[1] = with_k ? a->kv_heads : 0;
     p.batch = a->batch;
@@ -275,6 +279,7 @@ extern "C" grat_status grat_block_means(const grat_sequence* seq, const grat_ten
     if (st != GRAT_OK) return st;
     if (n_new < 0) return GRAT_ERR_BAD_DIMS;
     if (!known(seq->dtype) || (seq->head_dim != 64 && seq->head_dim != 128)) return GRAT_ERR_UNSUPPORTED;
+    if ((int64_t)s.n_blocks * 256 >= kMaxThreads) return GRAT_ERR_UNSUPPORTED;
     st = check_tensor(K, seq->dtype, seq->head_dim);
     if (st != GRAT_OK) return st;
     return status_of(launch_block_means(s, of(K), seq->dtype, seq->head_dim, n_new, d_means, (hipStream_t)hip_stream));
@@ -309,6 +314,7 @@ extern "C" grat_status grat_select_blocks(const grat_sequence* seq, const float*
     if (st != GRAT_OK) return st;
     if (top < 1 || first < 0 || local < 0 || (int64_t)first + local > top) return GRAT_ERR_BAD_DIMS;
     if (s.n_blocks > 32768 || top > 8192 || (int64_t)s.batch * s.kv_heads * s.n_groups >= (1 << 26)) return GRAT_ERR_UNSUPPORTED;
+    if (select_blocks_threads(s) >= kMaxThreads) return GRAT_ERR_UNSUPPORTED;
     return status_of(launch_select_blocks(s, d_scores, top, first, local, d_count, d_index, (hipStream_t)hip_stream));
 }
 

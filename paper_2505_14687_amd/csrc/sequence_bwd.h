@@ -268,7 +268,7 @@ template <bool F16, int D>
 __global__ __launch_bounds__(256) void grad_join_kernel(SelParams p, GradParams g, int tile_keys) {
     const SeqShape& s = p.s;
     uint32_t at, tile;
-    fdivmod(blockIdx.x / kJoinShare, g.fd_tiles, at, tile);
+    fdivmod(blockIdx.x, g.fd_tiles, at, tile);
     if ((int)at >= g.counters[3]) return;
     const int4 join = g.joins[at];   // block, first slot, parts
     const int tiles = (int)g.fd_tiles.d;
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(256) void grad_join_kernel(SelParams p, GradParams 
     const int b = (int)fdiv(bh, p.fd_kv_heads), h = (int)bh - b * s.kv_heads;
     const int64_t pitch = (int64_t)tiles * 2 * tile_keys * D;   // of a slot
     const float* const src = g.slots + join.y * pitch + (int64_t)tile * 2 * tile_keys * D;
-    for (int i = (int)(blockIdx.x % kJoinShare) * 256 + threadIdx.x; i < 2 * tile_keys * (D / 4); i += 256 * kJoinShare) {
+    for (int i = (int)blockIdx.y * 256 + threadIdx.x; i < 2 * tile_keys * (D / 4); i += 256 * kJoinShare) {
         const int which = i / (tile_keys * (D / 4)), row = i / (D / 4) % tile_keys, c = i % (D / 4);
         const int key = (int)j * s.block + (int)tile * tile_keys + row;
         if (key >= s.n_k) continue;
@@ -752,7 +752,7 @@ inline void launch_grad_keys(const SelParams& p, const GradParams& g, hipStream_
     const int64_t items = (int64_t)g.most_parts * g.fd_tiles.d;
     hipLaunchKernelGGL((grad_keys_kernel<KW, F16, D>), dim3((unsigned)((items + 127) / 128 * 128)), dim3(KW * 128), 0, stream, p, g);
     if (g.most_joins > 0)
-        hipLaunchKernelGGL((grad_join_kernel<F16, D>), dim3((unsigned)(g.most_joins * g.fd_tiles.d * kJoinShare)), dim3(256), 0, stream, p, g,
+        hipLaunchKernelGGL((grad_join_kernel<F16, D>), dim3((unsigned)(g.most_joins * g.fd_tiles.d), kJoinShare), dim3(256), 0, stream, p, g,
                            32 * KW);
 }
 template <int RW, int TEAMS, bool F16, int D>

@@ -499,31 +499,48 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * 64) void select_blocks_k
     if (lane == 0 && wave == 0) p.count[list] = total;
 }
 
+static int64_t lists_of(const SeqShape& s) { return (int64_t)s.batch * s.kv_heads * s.n_groups; }
+
 template <int WAVES, int R>
 static void launch_select(const SelectParams& p, hipStream_t stream) {
     const int64_t blocks = WAVES == 1 ? (p.lists + 3) / 4 : p.lists;
     hipLaunchKernelGGL((select_blocks_kernel<WAVES, R>), dim3((unsigned)blocks), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, stream, p);
 }
 
+// Waves that share a list.
+static int select_waves(int n_blocks, int64_t lists) {
+    return n_blocks <= 1024 || (n_blocks <= 2048 && lists >= 1024) ? 1 : n_blocks <= 2048 ? 2 : n_blocks <= 16384 ? 4 : 8;
+}
+int64_t select_blocks_threads(const SeqShape& s) {
+    const int64_t lists = lists_of(s);
+    const int waves = select_waves(s.n_blocks, lists);
+    return waves == 1 ? (lists + 3) / 4 * 256 : lists * waves * 64;
+}
+
 hipError_t launch_select_blocks(const SeqShape& s, const float* d_scores, int32_t top, int32_t first, int32_t local, int32_t* d_count,
                                 int32_t* d_index, hipStream_t stream) {
-    const SelectParams p{s, d_scores, top, first, local, d_count, d_index, (int64_t)s.batch * s.kv_heads * s.n_groups,
+    const SelectParams p{s, d_scores, top, first, local, d_count, d_index, lists_of(s),
                          make_fastdiv((uint32_t)s.n_groups), make_fastdiv((uint32_t)s.kv_heads), make_fastdiv((uint32_t)s.block)};
     // As few waves a list as hold its scores: waves that share a list wait for each other, which costs more than the longer code of one that has
     // more registers to go through (8 192 lists of 1 024 blocks: one wave 12 us, four 44; of 4 096: four 45, sixteen 247; 512 lists of 16 384: four 15, sixteen
     // 27).  Two waves for 2 048 blocks where lists are few (128 lists of 32: 8.9 us; one wave 13.8, four 9.7; 1 024 lists: one 8.2, four 8.7).
-    const int n = s.n_blocks;
-    if (n <= 64) launch_select<1, 1>(p, stream);
-    else if (n <= 128) launch_select<1, 2>(p, stream);
-    else if (n <= 256) launch_select<1, 4>(p, stream);
-    else if (n <= 512) launch_select<1, 8>(p, stream);
-    else if (n <= 1024) launch_select<1, 16>(p, stream);
-    else if (n <= 2048 && p.lists >= 1024) launch_select<1, 32>(p, stream);
-    else if (n <= 2048) launch_select<2, 16>(p, stream);
-    else if (n <= 4096) launch_select<4, 16>(p, stream);
-    else if (n <= 8192) launch_select<4, 32>(p, stream);
-    else if (n <= 16384) launch_select<4, 64>(p, stream);
-    else launch_select<8, 64>(p, stream);
+    const int n = s.n_blocks, waves = select_waves(n, p.lists);
+    if (waves == 1) {
+        if (n <= 64) launch_select<1, 1>(p, stream);
+        else if (n <= 128) launch_select<1, 2>(p, stream);
+        else if (n <= 256) launch_select<1, 4>(p, stream);
+        else if (n <= 512) launch_select<1, 8>(p, stream);
+        else if (n <= 1024) launch_select<1, 16>(p, stream);
+        else launch_select<1, 32>(p, stream);
+    } else if (waves == 2) {
+        launch_select<2, 16>(p, stream);
+    } else if (waves == 4) {
+        if (n <= 4096) launch_select<4, 16>(p, stream);
+        else if (n <= 8192) launch_select<4, 32>(p, stream);
+        else launch_select<4, 64>(p, stream);
+    } else {
+        launch_select<8, 64>(p, stream);
+    }
     return hipGetLastError();
 }
 

@@ -165,6 +165,25 @@ def test_binding_refusals():
         grat.grat_rotary_append(Q, K, K, table, K, K, None)
 
 
+def test_launches_of_2_to_the_32_threads_are_refused():
+    """An axis of a launch ends there: the call says so ahead of it."""
+    L = sq._library()
+    t = tensor()
+
+    def select(n_k, lists, block=32):
+        s = seq(batch=1 << 10, kv_heads=1, q_heads=1, n_q=lists >> 10, n_k=n_k, q_group=1, block=block)
+        return L.grat_select_blocks(ref(s), FAKE, 4, 1, 2, FAKE, FAKE, None)
+    assert select(32 * 2049, 1 << 24) == UNSUPPORTED and select(32 * 16384, 1 << 24) == UNSUPPORTED      # four waves a list
+    assert select(32 * 16385, 1 << 23) == UNSUPPORTED and select(32 * 32768, 1 << 23) == UNSUPPORTED     # eight
+    s = seq(batch=1, kv_heads=1, q_heads=1, n_q=(1 << 26) - 3, n_k=64, q_group=1, block=32)              # one, four lists a workgroup
+    assert L.grat_select_blocks(ref(s), FAKE, 1, 0, 1, FAKE, FAKE, None) == UNSUPPORTED
+    assert L.grat_block_means(ref(seq(n_k=1 << 29, block=32)), ref(t), 0, FAKE, None) == UNSUPPORTED
+    for dtype, d, tokens in ((0, 128, 1 << 29), (1, 128, 1 << 28), (0, 1024, 1 << 26), (1, 96, 21 << 24)):
+        a = rotary(dtype=dtype, d=d, rot=16, pairs=(8, 0, 0), n=tokens)
+        q = tensor(n=d)
+        assert L.grat_rotary(ref(a), ref(q), ref(q), None, None, None) == UNSUPPORTED
+
+
 def test_sizes_that_do_not_fit_32_bits_are_refused():
     """Cut off on the way, 2^32 + 64 keys a block would be 64 with results allocated for one block."""
     Q, K = torch.zeros(1, 4, 100, 128, dtype=torch.bfloat16), torch.zeros(1, 2, 100, 128, dtype=torch.bfloat16)
