@@ -344,7 +344,10 @@ const at::Tensor& rows_of(PyObject* o, const at::Tensor* like = nullptr) {
     return t;
 }
 void same_shape(const at::Tensor& a, const at::Tensor& b) { need(a.sizes() == b.sizes()); }
-grat_tensor tensor4(const at::Tensor& t) { return {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)}; }
+// (The stride of an axis of one element counts for nothing and may be any number.)
+grat_tensor tensor4(const at::Tensor& t) {
+    return {t.data_ptr(), t.size(0) > 1 ? t.stride(0) : 0, t.size(1) > 1 ? t.stride(1) : 0, t.size(2) > 1 ? t.stride(2) : t.size(3)};
+}
 
 // A contiguous tensor of one type and shape; null where None is given and allowed.
 void* flat(PyObject* o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor& like, bool optional = false) {

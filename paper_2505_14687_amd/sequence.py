@@ -101,7 +101,8 @@ def _call(name: str, *args, written=()):
 
 
 def _tensor(t: torch.Tensor) -> _Tensor:
-    return _Tensor(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    B, H, N, d = t.shape   # (the stride of an axis of one element counts for nothing and may be any number)
+    return _Tensor(t.data_ptr(), t.stride(0) if B > 1 else 0, t.stride(1) if H > 1 else 0, t.stride(2) if N > 1 else d)
 
 
 def _no_gradient(name: str, t) -> None:
