@@ -37,7 +37,8 @@
 extern "C" {
 #endif
 
-/* Element (b, h, n, c) at data + b*stride_b + h*stride_h + n*stride_n + c, strides in elements. */
+/* Element (b, h, n, c) at data + b*stride_b + h*stride_h + n*stride_n + c, strides in elements.  Inputs may repeat (stride_b, stride_h 0);
+ * tensors that are written to may not (GRAT_ERR_BAD_DIMS where that axis has more than one element). */
 typedef struct {
     void* data;
     int64_t stride_b, stride_h, stride_n;

@@ -23,6 +23,12 @@ grat_status check_tensor(const grat_tensor* t, grat_dtype dtype, int32_t head_di
     return GRAT_OK;
 }
 
+// ... and one that is written to: its rows may not lie on each other.
+grat_status check_output(const grat_tensor* t, grat_dtype dtype, int32_t head_dim, int32_t batch, int32_t heads) {
+    const grat_status st = check_tensor(t, dtype, head_dim);
+    return st == GRAT_OK && ((batch > 1 && t->stride_b == 0) || (heads > 1 && t->stride_h == 0)) ? GRAT_ERR_BAD_DIMS : st;
+}
+
 SeqTensor of(const grat_tensor* t) { return {(uint8_t*)t->data, t->stride_b, t->stride_h, t->stride_n}; }
 
 constexpr int64_t kMaxRows = (int64_t)1 << 30;
@@ -240,7 +246,8 @@ extern "C" grat_status grat_rotary(const grat_rotary_args* args, const grat_tens
     const bool with_k = K || K_out;
     grat_status st = make_rotary(args, with_k, &p);
     const grat_tensor* const tensors[4] = {Q, Q_out, K, K_out};
-    for (int i = 0; st == GRAT_OK && i < (with_k ? 4 : 2); ++i) st = check_tensor(tensors[i], args->dtype, args->head_dim);
+    for (int i = 0; st == GRAT_OK && i < (with_k ? 4 : 2); ++i)
+        st = i % 2 ? check_output(tensors[i], args->dtype, args->head_dim, args->batch, p.heads[i / 2]) : check_tensor(tensors[i], args->dtype, args->head_dim);
     if (st != GRAT_OK) return st;
     p.in[0] = of(Q);
     p.out[0] = of(Q_out);
@@ -257,7 +264,8 @@ extern "C" grat_status grat_rotary_append(const grat_rotary_args* args, const gr
     RotaryParams p;
     grat_status st = make_rotary(args, true, &p);
     const grat_tensor* const tensors[6] = {Q, Q_out, K, K_cache, V, V_cache};
-    for (int i = 0; st == GRAT_OK && i < 6; ++i) st = check_tensor(tensors[i], args->dtype, args->head_dim);
+    for (int i = 0; st == GRAT_OK && i < 6; ++i)
+        st = i % 2 ? check_output(tensors[i], args->dtype, args->head_dim, args->batch, p.heads[i < 2 ? 0 : 1]) : check_tensor(tensors[i], args->dtype, args->head_dim);
     if (st != GRAT_OK) return st;
     if (!args->d_start) return GRAT_ERR_NULL;
     if (n_cache < 1 || args->axes != 1 || args->d_positions || args->inverse) return GRAT_ERR_BAD_DIMS;
@@ -329,8 +337,9 @@ extern "C" grat_status grat_selected_attention_fwd(const grat_sequence* seq, con
     if (!d_count || !d_index) return GRAT_ERR_NULL;
     SelPlan plan;
     grat_status st = make_plan(seq, scale, max_blocks, false, (uint8_t*)d_work, &plan);
-    for (const grat_tensor* t : {Q, K, V, O})
+    for (const grat_tensor* t : {Q, K, V})
         if (st == GRAT_OK) st = check_tensor(t, seq->dtype, seq->head_dim);
+    if (st == GRAT_OK) st = check_output(O, seq->dtype, seq->head_dim, seq->batch, seq->q_heads);
     if (st != GRAT_OK) return st;
     if (plan.work > 0 && !d_work) return GRAT_ERR_NULL;
     if (!aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;
@@ -355,8 +364,11 @@ extern "C" grat_status grat_selected_attention_bwd(const grat_sequence* seq, con
     if (!d_lse || !d_count || !d_index) return GRAT_ERR_NULL;
     SelPlan plan;
     grat_status st = make_plan(seq, scale, max_blocks, true, (uint8_t*)d_work, &plan);
-    for (const grat_tensor* t : {dO, Q, K, V, O, dQ, dK, dV})
+    for (const grat_tensor* t : {dO, Q, K, V, O})
         if (st == GRAT_OK) st = check_tensor(t, seq->dtype, seq->head_dim);
+    if (st == GRAT_OK) st = check_output(dQ, seq->dtype, seq->head_dim, seq->batch, seq->q_heads);
+    for (const grat_tensor* t : {dK, dV})
+        if (st == GRAT_OK) st = check_output(t, seq->dtype, seq->head_dim, seq->batch, seq->kv_heads);
     if (st != GRAT_OK) return st;
     if (!d_work) return GRAT_ERR_NULL;
     if (!aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;

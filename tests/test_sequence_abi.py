@@ -165,6 +165,22 @@ def test_binding_refusals():
         grat.grat_rotary_append(Q, K, K, table, K, K, None)
 
 
+def test_outputs_whose_rows_lie_on_each_other_are_refused():
+    L = sq._library()
+    t = tensor(b=4 * 4096 * 128)
+    for flat in (tensor(b=0), tensor(b=4 * 4096 * 128, h=0)):
+        a, s = rotary(batch=2, start=FAKE), seq(batch=2)
+        assert L.grat_rotary(ref(a), ref(t), ref(flat), ref(t), ref(t), None) == DIMS
+        assert L.grat_rotary(ref(a), ref(t), ref(t), ref(t), ref(flat), None) == DIMS
+        for k in (1, 4, 5):   # Q_out, K_cache, V_cache
+            x = [ref(flat if i == k else t) for i in range(6)]
+            assert L.grat_rotary_append(ref(a), *x, 5, None) == DIMS
+        assert L.grat_selected_attention_fwd(ref(s), ref(t), ref(t), ref(t), ref(flat), None, 0.1, FAKE, FAKE, 4, FAKE, None) == DIMS
+        for k in range(3):
+            grads = [ref(flat if i == k else t) for i in range(3)]
+            assert L.grat_selected_attention_bwd(ref(s), *[ref(t)] * 5, FAKE, *grads, 0.1, FAKE, FAKE, 4, FAKE, None) == DIMS
+
+
 def test_launches_of_2_to_the_32_threads_are_refused():
     """An axis of a launch ends there: the call says so ahead of it."""
     L = sq._library()
