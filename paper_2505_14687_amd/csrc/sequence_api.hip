@@ -322,7 +322,7 @@ extern "C" grat_status grat_select_blocks(const grat_sequence* seq, const float*
     if (st != GRAT_OK) return st;
     if (top < 1 || first < 0 || local < 0 || (int64_t)first + local > top) return GRAT_ERR_BAD_DIMS;
     if (s.n_blocks > 32768 || top > 8192 || (int64_t)s.batch * s.kv_heads * s.n_groups >= (1 << 26)) return GRAT_ERR_UNSUPPORTED;
-    if (select_blocks_threads(s) >= kMaxThreads) return GRAT_ERR_UNSUPPORTED;
+    if (select_blocks_threads(s, top) >= kMaxThreads) return GRAT_ERR_UNSUPPORTED;
     return status_of(launch_select_blocks(s, d_scores, top, first, local, d_count, d_index, (hipStream_t)hip_stream));
 }
 

@@ -67,7 +67,7 @@ hipError_t launch_block_means(const SeqShape& s, const SeqTensor& K, grat_dtype 
 int64_t block_scores_work(const SeqShape& s, int32_t head_dim);
 hipError_t launch_block_scores(const SeqShape& s, const SeqTensor& Q, grat_dtype dtype, int32_t head_dim, const float* d_means, float scale,
                                float* d_scores, float* d_work, hipStream_t stream);
-int64_t select_blocks_threads(const SeqShape& s);   // of a launch
+int64_t select_blocks_threads(const SeqShape& s, int32_t top);   // of a launch
 hipError_t launch_select_blocks(const SeqShape& s, const float* d_scores, int32_t top, int32_t first, int32_t local, int32_t* d_count,
                                 int32_t* d_index, hipStream_t stream);
 

@@ -507,13 +507,19 @@ static void launch_select(const SelectParams& p, hipStream_t stream) {
     hipLaunchKernelGGL((select_blocks_kernel<WAVES, R>), dim3((unsigned)blocks), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, stream, p);
 }
 
-// Waves that share a list.
-static int select_waves(int n_blocks, int64_t lists) {
-    return n_blocks <= 1024 || (n_blocks <= 2048 && lists >= 1024) ? 1 : n_blocks <= 2048 ? 2 : n_blocks <= 16384 ? 4 : 8;
+// Waves that share a list: as few as hold its scores.  Waves that share one wait for each other, which costs more than the longer code of one that has more registers
+// to go through (8 192 lists of 1 024 blocks: one wave 12 us, four 44; of 4 096: four 45, sixteen 247; 512 lists of 16 384: four 15, sixteen 27).  1 025 to 2 048
+// blocks are the exception: two waves where there are few lists, and where a list is long enough that one wave mostly ends in the search by bits and two do
+// not, unless the chip is full many times over.  2 048 blocks, us of one and of two waves: 1 024 lists of 16 8.2 and 7.7, 2 048 8.7 and 9.4, 16 384 31 and 43; lists of
+// 32: 1 024 17.9 and 9.7, 2 048 18.4 and 11.7, 4 096 23 and 19, 16 384 43 and 52; lists of 48: 1 024 23 and 17, 2 048 23 and 24, 4 096 32 and 39.
+static int select_waves(int n_blocks, int64_t lists, int top) {
+    if (n_blocks <= 1024) return 1;
+    if (n_blocks <= 2048) return lists >= 2048 && (top < 30 || top > 40 || lists >= 16384) ? 1 : 2;
+    return n_blocks <= 16384 ? 4 : 8;
 }
-int64_t select_blocks_threads(const SeqShape& s) {
+int64_t select_blocks_threads(const SeqShape& s, int32_t top) {
     const int64_t lists = lists_of(s);
-    const int waves = select_waves(s.n_blocks, lists);
+    const int waves = select_waves(s.n_blocks, lists, top);
     return waves == 1 ? (lists + 3) / 4 * 256 : lists * waves * 64;
 }
 
@@ -521,10 +527,7 @@ hipError_t launch_select_blocks(const SeqShape& s, const float* d_scores, int32_
                                 int32_t* d_index, hipStream_t stream) {
     const SelectParams p{s, d_scores, top, first, local, d_count, d_index, lists_of(s),
                          make_fastdiv((uint32_t)s.n_groups), make_fastdiv((uint32_t)s.kv_heads), make_fastdiv((uint32_t)s.block)};
-    // As few waves a list as hold its scores: waves that share a list wait for each other, which costs more than the longer code of one that has
-    // more registers to go through (8 192 lists of 1 024 blocks: one wave 12 us, four 44; of 4 096: four 45, sixteen 247; 512 lists of 16 384: four 15, sixteen
-    // 27).  Two waves for 2 048 blocks where lists are few (128 lists of 32: 8.9 us; one wave 13.8, four 9.7; 1 024 lists: one 8.2, four 8.7).
-    const int n = s.n_blocks, waves = select_waves(n, p.lists);
+    const int n = s.n_blocks, waves = select_waves(n, p.lists, top);
     if (waves == 1) {
         if (n <= 64) launch_select<1, 1>(p, stream);
         else if (n <= 128) launch_select<1, 2>(p, stream);
