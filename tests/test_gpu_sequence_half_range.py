@@ -111,3 +111,29 @@ def test_rows_of_different_sizes(d, shape):
 def test_no_gradient_at_all():
     shape = SHAPES[3]
     run(shape, 128, (1, 1, 1, 1), 320, lambda gen, s: torch.zeros(s, device="cuda"))
+
+
+def test_a_graph_follows_the_size_of_dO():
+    """Replays of a recorded step with dO of other sizes, between other work: the exponents belong to the replay."""
+    B, Hq, Hkv, N, M, q_group, block, top, k_len = SHAPES[4]
+    count, index = random_lists(np.random.default_rng(330), B, Hkv, -(-N // q_group), -(-M // block), top, full=True)
+    lists = torch.from_numpy(count).cuda(), torch.from_numpy(index).cuda()
+    args, scale = dict(q_group=q_group, block=block, k_len=ints(k_len)), 0.125
+    Q, K, V = (normal((B, h, n, 64), "f16", 331 + i) for i, (h, n) in enumerate(((Hq, N), (Hkv, M), (Hkv, M))))
+    sizes = [normal((B, Hq, N, 64), "f16", 340 + i, gain=gain) for i, gain in enumerate((1.0, 2.0 ** -13, 2.0 ** 9))]
+    O, lse = grat.grat_selected_attention_fwd(Q, K, V, scale, *lists, return_lse=True, **args)
+
+    def step(dO):
+        return grat.grat_selected_attention_bwd(dO, Q, K, V, O, lse, scale, *lists, **args)
+    eager = [step(dO) for dO in sizes]
+    static = sizes[0].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(static)
+    for i in (0, 1, 2, 1, 0):
+        static.copy_(sizes[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(out, eager[i])), f"replay with dO {i}"
+        step(sizes[(i + 1) % 3])
