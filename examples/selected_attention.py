@@ -5,7 +5,9 @@
 Training: Q, K, V are projected, turned by their positions, key blocks are scored by their means, every group of 64 queries attends the blocks
 selected for it, and the gradient goes back through attention and rotation (the selection is not differentiated).  Serving: a
 prompt and then single tokens are appended to a cache, the means of the blocks that they touch are brought up to date, and each new token
-attends the blocks that are selected for it alone.
+attends the blocks that are selected for it alone.  The blocks of a group of 64 come from all of its queries, the later ones too, which a token
+that is served alone has not got: where lists do not hold every block, what is served differs from the whole sequence by that choice.  A model
+that has to be served as it was trained takes groups of one query (Q_GROUP = 1) throughout.
 """
 import math
 import os

@@ -26,6 +26,10 @@
  *   q_group consecutive rows, [g q_group, (g + 1) q_group), of all heads that share a K/V head are query group g and
  *   have one list; n_groups = ceil(n_q / q_group).  Key block j is the keys [j block, (j + 1) block), n_blocks =
  *   ceil(n_k / block).  The blocks that group g SEES are those with a key that one of its rows sees, blocks [0, s).
+ *   A list is common to its group, and so is what it is made of: scores take the mean of all of the group's queries, and of all valid keys of a
+ *   block.  With q_group > 1 the CHOICE of a causal row's blocks thus depends on up to q_group - 1 later tokens (the values that it attends
+ *   do not), and single tokens that are served later cannot make the same choice.  With q_group = 1 and local >= 1 (grat_select_blocks) it
+ *   depends on no later token: the one block whose mean reaches beyond the row is selected whatever its score.
  * Everywhere batch * kv_heads <= 65535, n_q, n_k < 2^30 (GRAT_ERR_UNSUPPORTED).
  */
 #ifndef GRAT_SEQUENCE_H

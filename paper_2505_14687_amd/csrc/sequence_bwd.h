@@ -10,8 +10,10 @@
 //
 // Steps: D and dQ | lists of every block, parts | dK, dV | joined parts.
 //
-// Bound by the matrix pipe: 16 384 tokens, 32 heads on 8, 16 blocks of 64 keys, bf16: dQ 420 us (6 d operations a pair, 950 TFLOP/s), lists 12, dK and dV
-// 670 (8 d, 790 TFLOP/s; the pipe busy for 40 % of the cycles, 3.9 GB of rows gathered through the L2, five of six from beyond it), join 28.
+// 16 384 tokens, 32 heads on 8, 16 blocks of 64 keys, bf16: dQ 420 us (6 d operations a pair, 950 TFLOP/s, the matrix pipe busy for 48 % of the cycles), lists 12,
+// dK and dV 670 (8 d, 790 TFLOP/s, 40 %), join 28.  dQ is held back as the forward walk is; the walk over keys by its order - weights and dS of 32 rows are
+// worked out while the wave issues no product - and by rows that are gathered through the L2, 3.9 GB, five of six from beyond it (with all of them in it a step
+// takes 7 % less).
 #pragma once
 #include <type_traits>
 

@@ -5,8 +5,10 @@
 // TEAMS such sets that take the two units of a tile each (few rows), and walks the list, or with `splits` a share of
 // it, in tiles of 64 keys through double-buffered LDS.
 //
-// Bound by the matrix pipe and the clock that it runs at: 32 768 tokens, 32 heads on 8, 16 blocks of 64 keys, bf16: 570 us, 950 TFLOP/s (a library
-// product of 16 384^3 reaches 1 375), the pipe busy for 47 % of the cycles.  Few rows: by fetching K and V, see NarrowWave.
+// 32 768 tokens, 32 heads on 8, 16 blocks of 64 keys, bf16: 570 to 606 us from card to card, 950 to 900 TFLOP/s (a library product of 16 384^3 reaches 1 375),
+// the matrix pipe busy for 47 % of the cycles.  What holds it back: a block more takes 29 us (8 to 64 blocks: 363, 606, 1 080, 2 008), 1 185 TFLOP/s, and 140 us go
+// by without the walk: 225 registers leave one workgroup of 8 waves to a compute unit, so nothing covers its start (count, list, Q, first K tile, one after the
+// other) and its end (O through LDS), 9 us each time.  Few rows: bound by fetching K and V, see NarrowWave.
 #pragma once
 #include <type_traits>
 

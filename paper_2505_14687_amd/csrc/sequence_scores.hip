@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void run_means_kernel(MeanParams p) {
 
 // Groups of few queries: C lanes a run, each all of its rows, so that a workgroup takes 256 / C runs and nothing is joined.  (Key blocks stay with the
 // other kernel, also short ones: means of some blocks have the bits that all blocks' have.)
-constexpr int kShortRun = 16;   // rows; 4: 8 192 lists x 8 heads 118 -> 59 us with the scores, 16: 73 -> 27 (x 2 heads), 32: 20 -> 22
+constexpr int kShortRun = 16;   // rows; 4: 8 192 lists x 8 heads 118 -> 59 us with the scores (118 MB: 18), 16: 73 -> 27 (x 2 heads), 32: 20 -> 22
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void short_run_means_kernel(MeanParams p) {
@@ -272,7 +272,8 @@ hipError_t launch_block_scores(const SeqShape& s, const SeqTensor& Q, grat_dtype
 // What bounds it is not the reading but the instructions: R ballots and R scalar counts a bit.  So where few are wanted, the common case,
 // the search runs on the lanes' largest keys only and ends at the first bound that little more than `want` of them reach.  What is not
 // below it (of 500 normal scores about 25 where 13 are wanted) is copied to LDS with its block, and a lane ranks one of those.  With several
-// waves the best of their bounds counts, and one wave ranks.  Measured: 32 768 lists of 16 from 512 blocks 28 us (46 by bits alone; reading the
+// waves the best of their bounds counts, and one wave ranks.  From 4 097 blocks on (32 registers a lane and four waves, and more) the compiler keeps 132 to 482 scalar registers
+// - masks of the unrolled ballots - in lanes of vector registers.  Measured: 32 768 lists of 16 from 512 blocks 28 us (46 by bits alone; reading the
 // scores takes 14), 128 lists of 32 from 2 048 blocks 8.9 us a call.
 struct SelectParams {
     SeqShape s;

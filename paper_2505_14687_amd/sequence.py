@@ -326,7 +326,10 @@ def grat_block_scores(Q, means, scale: float, q_group: int, block: int, n_k: int
 
 def grat_select_blocks(scores, top: int, first: int, local: int, n_q: int, n_k: int, q_group: int, block: int, causal: bool = True,
                        k_len=None, q_pos=None, stream=None):
-    """The lists: (count int32 [B, Hkv, groups], index int32 [B, Hkv, groups, top]), ascending, -1 behind a list's end."""
+    """The lists: (count int32 [B, Hkv, groups], index int32 [B, Hkv, groups, top]), ascending, -1 behind a list's end.
+
+    The choice of a group's blocks depends on all of its queries, up to q_group - 1 of them later than a row's own; with q_group 1 and
+    local >= 1 on no later token."""
     _library()
     r = _native.select(scores, top, first, local, n_q, n_k, q_group, block, causal, k_len, q_pos, stream)
     if r is not None:
