@@ -108,7 +108,8 @@ __global__ __launch_bounds__(256) void grad_lists_kernel(SelParams p, GradParams
 
 // The same, bits included, where a head's lists have so few entries (8 192) that every workgroup can read all of them: one launch instead of three.  A
 // workgroup takes kHeadBlocks blocks of a head, their bits in LDS.  (One against three, a training step: 2 047 tokens 67.5 and 72.3 us, 16 384 in groups
-// of 64 1 406 and 1 427; 7 223 queries with 28 892 entries 419 and 387.)
+// of 64 1 406 and 1 427.  On 30 shapes of 512 to 16 384 entries, 2, 8 and 16 heads, one is 1 to 4 % ahead up to 8 192 - behind by 1 % once, 8 heads of 256
+// groups x 32 - and -0.4 to 2 % at 16 384; at 28 892, 7 223 queries, 419 and 387.)
 constexpr int kHeadBlocks = 64;
 
 __global__ __launch_bounds__(1024) void grad_head_lists_kernel(SelParams p, GradParams g) {
