@@ -17,6 +17,7 @@
 
 #include "grat.h"
 #include "grat_sequence.h"
+#include "grat_window.h"
 
 namespace {
 
@@ -58,6 +59,20 @@ PyObject* set_sequence_library(PyObject*, PyObject* args) {
     g_seq = {(decltype(g_seq.rotary))a[0],         (decltype(g_seq.append))a[1],        (decltype(g_seq.means))a[2],
              (decltype(g_seq.scores_work))a[3],    (decltype(g_seq.scores))a[4],        (decltype(g_seq.select))a[5],
              (decltype(g_seq.attention_work))a[6], (decltype(g_seq.attention_fwd))a[7], (decltype(g_seq.attention_bwd))a[8]};
+    Py_RETURN_NONE;
+}
+
+struct WindowLibrary {   // ... and those of grat_window.h
+    decltype(&grat_window_attention_work) attention_work;
+    decltype(&grat_window_attention_fwd) attention_fwd;
+    decltype(&grat_window_attention_bwd) attention_bwd;
+} g_win;
+
+// set_window_library(addresses): in the order above
+PyObject* set_window_library(PyObject*, PyObject* args) {
+    unsigned long long a[3];
+    if (!PyArg_ParseTuple(args, "KKK", a, a + 1, a + 2)) return nullptr;
+    g_win = {(decltype(g_win.attention_work))a[0], (decltype(g_win.attention_fwd))a[1], (decltype(g_win.attention_bwd))a[2]};
     Py_RETURN_NONE;
 }
 
@@ -394,6 +409,26 @@ PyObject* sequence_result(grat_status st, PyObject* given, const at::Tensor& t) 
     return st != GRAT_OK ? PyLong_FromLong((long)st) : given_or(given, t);
 }
 
+struct Gradients {   // dQ, dK, dV: new ones, or a tuple of the caller's
+    PyObject* given[3] = {Py_None, Py_None, Py_None};
+    at::Tensor t[3];
+    Gradients(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, PyObject* out) {
+        if (out != Py_None) {
+            need(PyTuple_CheckExact(out) && PyTuple_GET_SIZE(out) == 3);
+            for (int i = 0; i < 3; ++i) need((given[i] = PyTuple_GET_ITEM(out, i)) != Py_None);
+        }
+        const at::Tensor* like[3] = {&q, &k, &v};
+        for (int i = 0; i < 3; ++i) {
+            t[i] = given[i] == Py_None ? at::empty_like(*like[i]) : rows_of(given[i], &q);
+            same_shape(t[i], *like[i]);
+        }
+    }
+    PyObject* result(grat_status st) const {
+        if (st != GRAT_OK) return PyLong_FromLong((long)st);
+        return tuple_of({given_or(given[0], t[0]), given_or(given[1], t[1]), given_or(given[2], t[2])});
+    }
+};
+
 struct RotaryCall {
     grat_rotary_args args{};
     // table, positions, start, layout (0 half, 1 interleaved), axis_pairs, inverse
@@ -619,25 +654,76 @@ PyObject* selected_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         same_shape(c.q, o);
         const float* const lse = (const float*)flat(a[13], at::kFloat, {c.q.size(0), c.q.size(1), c.q.size(2)}, c.q);
         const hipStream_t stream = current_stream(c.q, a[15]);
-        PyObject* given[3] = {Py_None, Py_None, Py_None};
-        if (a[14] != Py_None) {
-            need(PyTuple_CheckExact(a[14]) && PyTuple_GET_SIZE(a[14]) == 3);
-            for (int i = 0; i < 3; ++i) need((given[i] = PyTuple_GET_ITEM(a[14], i)) != Py_None);
-        }
-        const at::Tensor* like[3] = {&c.q, &c.k, &c.v};
-        at::Tensor d[3];
-        for (int i = 0; i < 3; ++i) {
-            d[i] = given[i] == Py_None ? at::empty_like(*like[i]) : rows_of(given[i], &c.q);
-            same_shape(d[i], *like[i]);
-        }
+        Gradients d(c.q, c.k, c.v, a[14]);
         const at::Tensor work = scratch(g_seq.attention_work(&c.s, c.top, 1), c.q);
-        const grat_tensor t[8] = {tensor4(g), tensor4(c.q), tensor4(c.k), tensor4(c.v), tensor4(o), tensor4(d[0]), tensor4(d[1]), tensor4(d[2])};
+        const grat_tensor t[8] = {tensor4(g), tensor4(c.q), tensor4(c.k), tensor4(c.v), tensor4(o), tensor4(d.t[0]), tensor4(d.t[1]), tensor4(d.t[2])};
         void* const w = work.data_ptr();
-        const grat_status st = without_gil([&] {
+        return d.result(without_gil([&] {
             return g_seq.attention_bwd(&c.s, t, t + 1, t + 2, t + 3, t + 4, lse, t + 5, t + 6, t + 7, c.scale, c.count, c.index, c.top, w, stream);
+        }));
+    });
+}
+
+// ---- attention within a window (grat_window.h) -----------------------------------------------------
+
+struct Limits {   // window (None: no limit) and sinks
+    int32_t window, sinks;
+    Limits(PyObject* w, PyObject* f) : window(w == Py_None ? 0 : positive(w)), sinks((int32_t)int_of(f)) { need(sinks >= 0); }
+};
+
+struct WindowCall {   // Q, K, V, scale, window, sinks, causal, k_len, q_pos
+    const at::Tensor &q, &k, &v;
+    float scale;
+    Limits limits;
+    grat_sequence s{};
+    explicit WindowCall(PyObject* const* a)
+        : q(rows_of(a[0])), k(rows_of(a[1], &q)), v(rows_of(a[2], &q)), scale(scale_of(a[3])), limits(a[4], a[5]) {
+        const int64_t B = q.size(0), Hkv = k.size(1);
+        need(k.size(0) == B && k.size(3) == q.size(3) && q.size(1) % Hkv == 0);
+        same_shape(k, v);
+        s = grat_sequence{dtype_of(q), (int32_t)B, (int32_t)q.size(1), (int32_t)Hkv, (int32_t)q.size(3), (int32_t)q.size(2), (int32_t)k.size(2),
+                          0, 0, bool_of(a[6]), (const int32_t*)flat(a[7], at::kInt, {B}, q, true), (const int32_t*)flat(a[8], at::kInt, {B}, q, true)};
+    }
+};
+
+// window_fwd(Q, K, V, scale, window, sinks, causal, k_len, q_pos, return_lse, out, stream): O or (O, lse)
+PyObject* window_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return ordinary(n, 12, [&]() -> PyObject* {
+        const WindowCall c(a);
+        const bool with_lse = bool_of(a[9]);
+        const hipStream_t stream = current_stream(c.q, a[11]);
+        const int64_t bytes = g_win.attention_work(&c.s, c.limits.window, c.limits.sinks, 0);
+        const at::Tensor work = bytes ? scratch(bytes, c.q) : at::Tensor();
+        const at::Tensor o = a[10] == Py_None ? at::empty_like(c.q) : rows_of(a[10], &c.q);
+        same_shape(c.q, o);
+        const at::Tensor lse = with_lse ? at::empty({c.q.size(0), c.q.size(1), c.q.size(2)}, c.q.options().dtype(at::kFloat)) : at::Tensor();
+        const grat_tensor t[4] = {tensor4(c.q), tensor4(c.k), tensor4(c.v), tensor4(o)};
+        float* const lp = with_lse ? (float*)lse.data_ptr() : nullptr;
+        void* const w = bytes ? work.data_ptr() : nullptr;
+        const grat_status st = without_gil([&] {
+            return g_win.attention_fwd(&c.s, t, t + 1, t + 2, t + 3, lp, c.scale, c.limits.window, c.limits.sinks, w, stream);
         });
-        if (st != GRAT_OK) return PyLong_FromLong((long)st);
-        return tuple_of({given_or(given[0], d[0]), given_or(given[1], d[1]), given_or(given[2], d[2])});
+        if (st != GRAT_OK || !with_lse) return sequence_result(st, a[10], o);
+        return tuple_of({given_or(a[10], o), THPVariable_Wrap(lse)});
+    });
+}
+
+// window_bwd(Q, K, V, scale, window, sinks, causal, k_len, q_pos, dO, O, lse, out or None, stream): (dQ, dK, dV)
+PyObject* window_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return ordinary(n, 14, [&]() -> PyObject* {
+        const WindowCall c(a);
+        const at::Tensor &g = rows_of(a[9], &c.q), &o = rows_of(a[10], &c.q);
+        same_shape(c.q, g);
+        same_shape(c.q, o);
+        const float* const lse = (const float*)flat(a[11], at::kFloat, {c.q.size(0), c.q.size(1), c.q.size(2)}, c.q);
+        const hipStream_t stream = current_stream(c.q, a[13]);
+        Gradients d(c.q, c.k, c.v, a[12]);
+        const at::Tensor work = scratch(g_win.attention_work(&c.s, c.limits.window, c.limits.sinks, 1), c.q);
+        const grat_tensor t[8] = {tensor4(g), tensor4(c.q), tensor4(c.k), tensor4(c.v), tensor4(o), tensor4(d.t[0]), tensor4(d.t[1]), tensor4(d.t[2])};
+        void* const w = work.data_ptr();
+        return d.result(without_gil([&] {
+            return g_win.attention_bwd(&c.s, t, t + 1, t + 2, t + 3, t + 4, lse, t + 5, t + 6, t + 7, c.scale, c.limits.window, c.limits.sinks, w, stream);
+        }));
     });
 }
 
@@ -655,6 +741,9 @@ PyMethodDef kMethods[] = {
     {"select", (PyCFunction)(void (*)())select, METH_FASTCALL, nullptr},
     {"selected_fwd", (PyCFunction)(void (*)())selected_fwd, METH_FASTCALL, nullptr},
     {"selected_bwd", (PyCFunction)(void (*)())selected_bwd, METH_FASTCALL, nullptr},
+    {"set_window_library", set_window_library, METH_VARARGS, nullptr},
+    {"window_fwd", (PyCFunction)(void (*)())window_fwd, METH_FASTCALL, nullptr},
+    {"window_bwd", (PyCFunction)(void (*)())window_bwd, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

@@ -4,58 +4,9 @@
 #include <cstdint>
 
 #include "sequence_attn.h"
+#include "sequence_checks.h"
 
 namespace grat {
-namespace {
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-bool is16(grat_dtype t) { return t == GRAT_BF16 || t == GRAT_F16; }
-bool known(grat_dtype t) { return is16(t) || t == GRAT_F32; }
-
-// A tensor whose rows are read or written as 16-byte vectors.
-grat_status check_tensor(const grat_tensor* t, grat_dtype dtype, int32_t head_dim) {
-    if (!t || !t->data) return GRAT_ERR_NULL;
-    if (t->stride_n < head_dim || t->stride_b < 0 || t->stride_h < 0) return GRAT_ERR_BAD_DIMS;
-    const int vec = is16(dtype) ? 8 : 4;
-    if (t->stride_n % vec || t->stride_b % vec || t->stride_h % vec || !aligned16(t->data)) return GRAT_ERR_UNSUPPORTED;
-    if (t->stride_n >= ((int64_t)1 << 24) || t->stride_b >= ((int64_t)1 << 46) || t->stride_h >= ((int64_t)1 << 46))
-        return GRAT_ERR_UNSUPPORTED;
-    return GRAT_OK;
-}
-
-// ... and one that is written to: its rows may not lie on each other.
-grat_status check_output(const grat_tensor* t, grat_dtype dtype, int32_t head_dim, int32_t batch, int32_t heads) {
-    const grat_status st = check_tensor(t, dtype, head_dim);
-    return st == GRAT_OK && ((batch > 1 && t->stride_b == 0) || (heads > 1 && t->stride_h == 0)) ? GRAT_ERR_BAD_DIMS : st;
-}
-
-SeqTensor of(const grat_tensor* t) { return {(uint8_t*)t->data, t->stride_b, t->stride_h, t->stride_n}; }
-
-constexpr int64_t kMaxRows = (int64_t)1 << 30;
-constexpr int64_t kMaxThreads = (int64_t)1 << 32;   // of an axis of a launch; fewer
-
-// The parts of a grat_sequence that every operator on lists reads.
-grat_status make_shape(const grat_sequence* s, SeqShape* out) {
-    if (!s) return GRAT_ERR_NULL;
-    if (s->batch < 1 || s->kv_heads < 1 || s->q_heads < 1 || s->n_q < 1 || s->n_k < 1 || s->q_group < 1 || s->block < 1) return GRAT_ERR_BAD_DIMS;
-    if (s->q_heads % s->kv_heads) return GRAT_ERR_BAD_DIMS;
-    if (s->block % 32 || s->block > 4096) return GRAT_ERR_UNSUPPORTED;
-    if (s->n_q >= kMaxRows || s->n_k >= kMaxRows || (int64_t)s->batch * s->kv_heads > 65535 || s->q_heads > 65535) return GRAT_ERR_UNSUPPORTED;
-    *out = SeqShape{s->batch, s->q_heads, s->kv_heads, s->q_heads / s->kv_heads, s->n_q, s->n_k,
-                    s->q_group < s->n_q ? s->q_group : s->n_q, s->block, 0, 0, s->causal ? 1 : 0, s->d_k_len, s->d_q_pos};
-    out->n_groups = (out->n_q + out->q_group - 1) / out->q_group;
-    out->n_blocks = (out->n_k + out->block - 1) / out->block;
-    return GRAT_OK;
-}
-
-// For the operators that do not read all of it.
-grat_sequence with_heads(const grat_sequence& s) {
-    grat_sequence t = s;
-    t.q_heads = t.kv_heads;
-    return t;
-}
-
-grat_status status_of(hipError_t e) { return e == hipSuccess ? GRAT_OK : GRAT_ERR_HIP; }
 
 grat_status make_rotary(const grat_rotary_args* a, bool with_k, RotaryParams* out) {
     if (!a || !a->d_table) return GRAT_ERR_NULL;
@@ -97,6 +48,29 @@ grat_status make_rotary(const grat_rotary_args* a, bool with_k, RotaryParams* ou
     p.start = a->d_start;
     *out = p;
     return GRAT_OK;
+}
+
+namespace {
+
+// The parts of a grat_sequence that every operator on lists reads.
+grat_status make_shape(const grat_sequence* s, SeqShape* out) {
+    if (!s) return GRAT_ERR_NULL;
+    if (s->batch < 1 || s->kv_heads < 1 || s->q_heads < 1 || s->n_q < 1 || s->n_k < 1 || s->q_group < 1 || s->block < 1) return GRAT_ERR_BAD_DIMS;
+    if (s->q_heads % s->kv_heads) return GRAT_ERR_BAD_DIMS;
+    if (s->block % 32 || s->block > 4096) return GRAT_ERR_UNSUPPORTED;
+    if (s->n_q >= kMaxRows || s->n_k >= kMaxRows || (int64_t)s->batch * s->kv_heads > 65535 || s->q_heads > 65535) return GRAT_ERR_UNSUPPORTED;
+    *out = SeqShape{s->batch, s->q_heads, s->kv_heads, s->q_heads / s->kv_heads, s->n_q, s->n_k,
+                    s->q_group < s->n_q ? s->q_group : s->n_q, s->block, 0, 0, s->causal ? 1 : 0, s->d_k_len, s->d_q_pos};
+    out->n_groups = (out->n_q + out->q_group - 1) / out->q_group;
+    out->n_blocks = (out->n_k + out->block - 1) / out->block;
+    return GRAT_OK;
+}
+
+// For the operators that do not read all of it.
+grat_sequence with_heads(const grat_sequence& s) {
+    grat_sequence t = s;
+    t.q_heads = t.kv_heads;
+    return t;
 }
 
 // ---- attention over lists --------------------------------------------------------------------

@@ -27,6 +27,17 @@ struct SelParams {
     FastDiv fd_splits, fd_row_tiles, fd_groups, fd_kv_heads, fd_q_group, fd_units;   // fd_units: by block / 32
     float* part_o;                // splits > 1: [items][rows of a tile][D], with part_ml [items][rows of a tile][2]
     float* part_ml;
+    int32_t window, sinks;        // attention within a window: no lists, q_group is the launch's own
+};
+constexpr int32_t kNoWindow = 0x7fffffff;
+
+// The walk over keys of attention within a window: key tiles of 64 keys, the rows that see a tile cut into parts of about equal length.  Rows that see
+// one of the first keys are as many as there are, of others at most a window's.
+struct WindowGradParams {
+    int32_t tiles, first_tiles;         // of a K/V head; those that hold first keys
+    int32_t first_parts, near_parts;    // parts of either kind of tile
+    int32_t items, per_xcd;             // of the launch
+    int32_t head_items, head_slots;     // items and places in `slots` of a K/V head
 };
 
 // What the gradient needs beside SelParams, in the caller's scratch memory.
@@ -47,6 +58,7 @@ struct GradParams {
     int32_t heads, head_runs;   // K/V heads of the batch, runs of each
     int32_t words, blocks, most_parts, most_joins, part_rows;
     FastDiv fd_rows, fd_tiles, fd_top, fd_part;   // by rows of a group; key tiles of a block; max_blocks; part_rows
+    WindowGradParams window;   // attention within a window: in the place of bits .. joins
 };
 
 // Dispatch by element type and head_dim (sequence_fwd_*.hip, sequence_bwd_*.hip).
@@ -59,6 +71,16 @@ hipError_t launch_selected_bwd_bf16_d64(const SelParams& p, const GradParams& g,
 hipError_t launch_selected_bwd_f16_d128(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream);
 hipError_t launch_selected_bwd_f16_d64(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream);
 void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stream);
+void launch_grad_head_bits(const GradParams& g, hipStream_t stream);
+// ... of attention within a window (window_fwd_*.hip, window_bwd_*.hip)
+hipError_t launch_window_fwd_bf16_d128(const SelParams& p, int tile_rows, hipStream_t stream);
+hipError_t launch_window_fwd_bf16_d64(const SelParams& p, int tile_rows, hipStream_t stream);
+hipError_t launch_window_fwd_f16_d128(const SelParams& p, int tile_rows, hipStream_t stream);
+hipError_t launch_window_fwd_f16_d64(const SelParams& p, int tile_rows, hipStream_t stream);
+hipError_t launch_window_bwd_bf16_d128(const SelParams& p, const GradParams& g, int tile_rows, hipStream_t stream);
+hipError_t launch_window_bwd_bf16_d64(const SelParams& p, const GradParams& g, int tile_rows, hipStream_t stream);
+hipError_t launch_window_bwd_f16_d128(const SelParams& p, const GradParams& g, int tile_rows, hipStream_t stream);
+hipError_t launch_window_bwd_f16_d64(const SelParams& p, const GradParams& g, int tile_rows, hipStream_t stream);
 
 constexpr int kUnit = 32;         // keys that are looked up, masked and skipped together
 constexpr int kNoUnit = 0x7fffff00;   // start of a unit that only fills a tile: behind every key
@@ -203,17 +225,111 @@ __device__ __forceinline__ const uint8_t* row_address(const SeqTensor& t, int b,
     return t.data + 2 * (b * t.stride_b + head * t.stride_h + row * t.stride_n);
 }
 
+// ---- windows --------------------------------------------------------------------------------------
+// The query in row i, at position pos + i, sees the keys [0, first) and [lo, hi): the first keys and its window.  All three grow with i.
+struct RowSpan {
+    int first, lo, hi;
+};
+__device__ __forceinline__ int64_t window_pos(const SeqShape& s, int b, int len) { return s.q_pos ? (int64_t)s.q_pos[b] : (int64_t)len - s.n_q; }
+__device__ __forceinline__ RowSpan row_span(const SelParams& p, int len, int64_t pos, int i) {
+    const int64_t at = pos + i;
+    RowSpan r;
+    const bool all = p.window == kNoWindow;
+    r.hi = (int)max((int64_t)0, min((int64_t)len, p.s.causal ? at + 1 : all ? (int64_t)len : at + p.window));
+    r.lo = all ? 0 : (int)max((int64_t)0, min((int64_t)r.hi, at - p.window + 1));
+    r.first = min(p.sinks, p.s.causal ? r.hi : len);
+    return r;
+}
+// The keys that the rows [i0, i1] see, as units of 32 keys: of the first keys from key 0 on, then from the first key of row i0's window on that is
+// not among these.  A unit's keys that no row sees are not read: the last one that some row sees stands for them.
+struct WindowUnits {
+    int first_end, first_units, near, near_end, n;
+    __device__ __forceinline__ WindowUnits(const SelParams& p, int len, int64_t pos, int i0, int i1) {
+        const RowSpan a = row_span(p, len, pos, i0), z = row_span(p, len, pos, i1);
+        first_end = z.first;
+        first_units = (first_end + kUnit - 1) / kUnit;
+        near = max(a.lo, first_end);
+        near_end = z.hi;
+        n = first_units + (max(near_end - near, 0) + kUnit - 1) / kUnit;
+    }
+    __device__ __forceinline__ int start(int i) const { return i < first_units ? i * kUnit : near + (i - first_units) * kUnit; }
+};
+
+// What a lane's row does not see of a unit, of 32 rows a wave.
+template <bool WINDOW>
+struct RowMask;
+template <>
+struct RowMask<false> {   // keys behind the row's own
+    int limit, least, most;   // keys below it are seen; of the wave's rows
+    __device__ __forceinline__ RowMask(const SelParams& p, const GroupRow& row, const WindowUnits*, int len, int64_t pos) {
+        limit = row.there ? row_seen(p.s, len, pos, row.query) : 0;
+        least = row.there ? limit : 0x7fffffff;
+        most = limit;
+#pragma unroll
+        for (int m = 1; m < 32; m *= 2) {
+            least = min(least, __shfl_xor(least, m));
+            most = max(most, __shfl_xor(most, m));
+        }
+        least = __builtin_amdgcn_readfirstlane(least);
+        most = __builtin_amdgcn_readfirstlane(most);
+    }
+    __device__ __forceinline__ bool nothing() const { return most == 0; }
+    __device__ __forceinline__ bool sees() const { return limit > 0; }   // this lane's row
+    __device__ __forceinline__ bool idle(int start) const { return start >= most; }   // nobody in this wave sees the unit
+    __device__ __forceinline__ bool cuts(int start) const { return start + kUnit > least; }
+    __device__ __forceinline__ bool hides(int start, int k) const { return start + k >= limit; }   // key k of the unit
+};
+template <>
+struct RowMask<true> {
+    RowSpan r;
+    int first_end, least_first, least_hi, most_lo, least_lo, most;
+    __device__ __forceinline__ RowMask(const SelParams& p, const GroupRow& row, const WindowUnits* u, int len, int64_t pos) {
+        r = row_span(p, len, pos, row.query);
+        if (!row.there) r = RowSpan{0, 0, 0};
+        first_end = u->first_end;
+        least_first = row.there ? r.first : 0x7fffffff;
+        least_hi = row.there ? r.hi : 0x7fffffff;
+        least_lo = row.there ? r.lo : 0x7fffffff;
+        most_lo = r.lo;
+        most = max(r.first, r.hi);
+#pragma unroll
+        for (int m = 1; m < 32; m *= 2) {
+            least_first = min(least_first, __shfl_xor(least_first, m));
+            least_hi = min(least_hi, __shfl_xor(least_hi, m));
+            least_lo = min(least_lo, __shfl_xor(least_lo, m));
+            most_lo = max(most_lo, __shfl_xor(most_lo, m));
+            most = max(most, __shfl_xor(most, m));
+        }
+        least_first = __builtin_amdgcn_readfirstlane(least_first);
+        least_hi = __builtin_amdgcn_readfirstlane(least_hi);
+        least_lo = __builtin_amdgcn_readfirstlane(least_lo);
+        most_lo = __builtin_amdgcn_readfirstlane(most_lo);
+        most = __builtin_amdgcn_readfirstlane(most);
+    }
+    __device__ __forceinline__ bool nothing() const { return most == 0; }
+    __device__ __forceinline__ bool sees() const { return r.first > 0 || r.hi > r.lo; }
+    __device__ __forceinline__ bool idle(int start) const { return start >= most || (start >= first_end && start + kUnit <= least_lo); }
+    __device__ __forceinline__ bool cuts(int start) const { return start < first_end ? start + kUnit > least_first : start + kUnit > least_hi || start < most_lo; }
+    __device__ __forceinline__ bool hides(int start, int k) const {
+        const bool first = start < first_end;
+        const int low = first ? 0 : r.lo, width = first ? r.first : r.hi - r.lo;
+        return (uint32_t)(start + k - low) >= (uint32_t)width;
+    }
+};
+
 // ---- the walk over a list ------------------------------------------------------------------------
 // K and V tiles of 64 keys (two units), double buffered.  NW waves fetch 1-KiB pieces; a wave's pieces lie in one unit.
-template <int NW, int D>
+template <int NW, int D, bool WINDOW = false>
 struct KeyLoader {
     static constexpr int kPieces = 64 * D * 2 / 1024, LPW = kPieces / NW, kPerUnit = kPieces / 2, kRows = 1024 / (2 * D), kChunks = D / 8;
     static_assert(LPW >= 1 && kPerUnit % LPW == 0, "a wave's pieces lie in one unit");
     const uint8_t *K, *V;        // of the head
     int64_t pitch_k, pitch_v;    // bytes
     int last;                    // last key that may be read
+    int first_end;               // windows: first keys are read up to here
     int my_unit, row[LPW], col[LPW];
-    __device__ __forceinline__ KeyLoader(const SelParams& p, const Item& it, int seen, int wave, int lane) {
+    __device__ __forceinline__ KeyLoader(const SelParams& p, const Item& it, int seen, int wave, int lane, int first_keys = 0) {
+        first_end = first_keys;
         K = row_address(p.K, it.b, it.h, 0);
         V = row_address(p.V, it.b, it.h, 0);
         pitch_k = 2 * p.K.stride_n;
@@ -230,7 +346,7 @@ struct KeyLoader {
     // start: of a listed unit, which begins with a key that some row sees.  Keys behind the last of these are not read: it stands for them, and they are
     // masked.
     __device__ __forceinline__ void issue(const uint8_t* head, int64_t pitch, int start, uint8_t* tile, int wave) const {
-        const int left = last - start;
+        const int left = (WINDOW && start < first_end ? first_end - 1 : last) - start;
         const uint8_t* const base = head + start * pitch;
 #pragma unroll
         for (int k = 0; k < LPW; ++k) load_lds(base, (uint32_t)min(row[k], left) * (uint32_t)pitch + col[k], tile + (wave * LPW + k) * 1024);

@@ -41,42 +41,94 @@ __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 // the groups that list the block in tiles of 64 through LDS; two teams of KW waves take 32 rows of a tile each.
 // What goes with a row - where it lies, lse, D, the keys it sees - is worked out by one wave, a tile ahead of the loads that need it, and
 // passed on through LDS; lse and D go there straight from memory.
+template <bool WINDOW>
 struct alignas(16) RowMeta {
     float lse2[64], delta[64];
-    int32_t limit[64];
+    int32_t limit[64], lo[WINDOW ? 64 : 0];   // keys seen: below limit, from lo on (windows)
     const uint8_t* q[64];
     const uint8_t* d[64];
     int32_t masked;   // some row does not see all keys of the tile
 };
 
-template <int KW, bool F16, int D>
+// Attention within a window: the rows that see key tile `item` of the launch, or the part of them that it takes.
+struct WindowItem {
+    int bh, tile, parts, slot;   // slot: of the part's sums, -1: the tile has no other part
+    int i0, ni, z, w;            // rows from z to w of head after head, ni queries from i0 on each
+    __device__ __forceinline__ WindowItem(const SelParams& p, const WindowGradParams& g, int item) {
+        bh = item / g.head_items;
+        const int r = item - bh * g.head_items, firsts = g.first_tiles * g.first_parts;
+        const bool first = r < firsts;
+        parts = first ? g.first_parts : g.near_parts;
+        const int at = first ? r : r - firsts;
+        tile = at / parts + (first ? 0 : g.first_tiles);
+        slot = parts > 1 ? bh * g.head_slots + r : -1;
+        z = at % parts;   // (of the parts)
+    }
+    __device__ __forceinline__ void rows(const SelParams& p, int len, int64_t pos) {
+        const SeqShape& s = p.s;
+        const int64_t k0 = (int64_t)tile * 64, k1 = min(k0 + 64, (int64_t)len);
+        const bool first = k0 < p.sinks, all = p.window == kNoWindow;
+        const int64_t from = s.causal ? k0 : first || all ? INT64_MIN / 2 : k0 - p.window + 1, to = first || all ? INT64_MAX / 2 : k1 + p.window - 1;   // positions
+        i0 = (int)min(max(from - pos, (int64_t)0), (int64_t)s.n_q);
+        ni = max((int)min(max(to - pos, (int64_t)0), (int64_t)s.n_q) - i0, 0);
+        const int n = ni * s.share, per = ((n + parts - 1) / parts + 63) & ~63;
+        z = (int)min((int64_t)z * per, (int64_t)n);
+        w = min(z + per, n);
+    }
+};
+
+template <int KW, bool F16, int D, bool WINDOW>
 __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, GradParams g) {
     using E = Elem<F16>;
     constexpr int NW = 2 * KW, kTile = 64 * D * 2, kPieces = kTile / 1024, LPW = kPieces / NW, kRows = 1024 / (2 * D), kChunks = D / 8;
     __shared__ __attribute__((aligned(2 * kTile))) uint8_t lds[4][kTile];   // Q, Q, dO, dO
-    __shared__ RowMeta meta[4];
+    __shared__ RowMeta<WINDOW> meta[4];
     const SeqShape& s = p.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
     const int team = wave / KW, key_wave = wave % KW;
 
-    // The XCDs walk the heads together, kChunk items at a time each: Q and dO of one or two K/V heads are in use at a time, which the memory-side
-    // cache holds.
-    constexpr int kChunk = 16;
-    const int tiles = (int)g.fd_tiles.d, longs = g.counters[1], work = (longs + g.counters[4]) * tiles;
-    const int turn = (int)blockIdx.x >> 3, item = ((turn / kChunk) * 8 + ((int)blockIdx.x & 7)) * kChunk + turn % kChunk;
-    if (item >= work) return;
-    uint32_t part_id, tile_in_block, b_, h_;
-    fdivmod((uint32_t)item, g.fd_tiles, part_id, tile_in_block);
-    if ((int)part_id >= longs) part_id = (uint32_t)(g.most_parts - 1 - ((int)part_id - longs));   // short parts: from the back
-    const int4 part = g.parts[part_id];
-    const uint32_t bh = (uint32_t)part.x / (uint32_t)s.n_blocks, block = (uint32_t)part.x - bh * (uint32_t)s.n_blocks;
+    int b, h, tile_key0, tile_in_block = 0, tiles = 1, slot;
+    uint32_t bh, b_, h_;
+    int4 part;
+    if constexpr (!WINDOW) {
+        // The XCDs walk the heads together, kChunk items at a time each: Q and dO of one or two K/V heads are in use at a time, which the memory-side
+        // cache holds.
+        constexpr int kChunk = 16;
+        tiles = (int)g.fd_tiles.d;
+        const int longs = g.counters[1], work = (longs + g.counters[4]) * tiles;
+        const int turn = (int)blockIdx.x >> 3, item = ((turn / kChunk) * 8 + ((int)blockIdx.x & 7)) * kChunk + turn % kChunk;
+        if (item >= work) return;
+        uint32_t part_id, in_block;
+        fdivmod((uint32_t)item, g.fd_tiles, part_id, in_block);
+        tile_in_block = (int)in_block;
+        if ((int)part_id >= longs) part_id = (uint32_t)(g.most_parts - 1 - ((int)part_id - longs));   // short parts: from the back
+        part = g.parts[part_id];
+        slot = g.part_slot[part_id];
+        bh = (uint32_t)part.x / (uint32_t)s.n_blocks;
+        tile_key0 = (part.x - (int)bh * s.n_blocks) * s.block + tile_in_block * (32 * KW);
+    }
+    WindowItem near(p, g.window, WINDOW ? ((int)blockIdx.x & 7) * g.window.per_xcd + ((int)blockIdx.x >> 3) : 0);
+    if constexpr (WINDOW) {   // consecutive tiles, which share their rows, go to one XCD
+        if ((int)(blockIdx.x >> 3) >= g.window.per_xcd || ((int)blockIdx.x & 7) * g.window.per_xcd + ((int)blockIdx.x >> 3) >= g.window.items) return;
+        bh = (uint32_t)near.bh;
+        slot = near.slot;
+        tile_key0 = near.tile * 64;
+    }
     fdivmod(bh, p.fd_kv_heads, b_, h_);
-    const int b = (int)b_, h = (int)h_;
-    const int n_tiles = (part.w - part.z + 63) / 64;
+    b = (int)b_;
+    h = (int)h_;
     const int len = seq_len(s, b);
-    const int64_t pos = seq_pos(s, b, len);
+    const int64_t pos = WINDOW ? window_pos(s, b, len) : seq_pos(s, b, len);
+    if constexpr (WINDOW) {
+        near.rows(p, len, pos);
+        part = make_int4(0, 0, near.z, near.w);
+    }
+    const int n_tiles = (part.w - part.z + 63) / 64;
 
-    const int tile_key0 = (int)block * s.block + (int)tile_in_block * (32 * KW), key = tile_key0 + key_wave * 32 + (lane & 31);
+    const int key = tile_key0 + key_wave * 32 + (lane & 31);
+    // What is held against the rows' limits.  (A first key is seen by every row that it is not behind, if causal, else by every row.)
+    const bool first_key = WINDOW && key < p.sinks;
+    const int ahead = first_key ? 0x7fffffff : key, behind = first_key && !s.causal && key < len ? -1 : key;
     f32x16 dk[D / 32], dv[D / 32];
     clear<D>(dk);
     clear<D>(dv);
@@ -93,21 +145,35 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
             for (int i = 0; i < D / 16; ++i) vf[i] = *(const frag8*)(vs + 32 * i);
         }
         // -- rows of the walk
-        const int32_t* const groups = g.groups + part.y;
-        auto find_group = [&](int t) { return groups[fdiv((uint32_t)min(part.z + 64 * t + lane, part.w - 1), g.fd_rows)]; };
+        auto find_group = [&](int t) { return WINDOW ? 0 : (g.groups + part.y)[fdiv((uint32_t)min(part.z + 64 * t + lane, part.w - 1), g.fd_rows)]; };
         auto put_rows = [&](int t, int group) {
             const int at = part.z + 64 * t + lane, in_list = min(at, part.w - 1);
-            const GroupRow r(p, h, group, in_list - (int)(fdiv((uint32_t)in_list, g.fd_rows) * g.fd_rows.d));
-            const bool there = r.there && at < part.w;
-            RowMeta& m = meta[t & 3];
-            m.q[lane] = row_address(p.Q, b, r.head, r.query);
-            m.d[lane] = row_address(g.dO, b, r.head, r.query);
-            const int limit = row_seen(s, len, pos, r.query);
+            int head, query, limit;
+            bool there = at < part.w, cut;
+            RowMeta<WINDOW>& m = meta[t & 3];
+            if constexpr (WINDOW) {
+                const int e = (int)((uint32_t)in_list / (uint32_t)near.ni);
+                head = h * s.share + e;
+                query = near.i0 + in_list - e * near.ni;
+                const RowSpan span = row_span(p, len, pos, query);
+                limit = span.hi;
+                m.lo[lane] = span.lo;
+                cut = (limit < tile_key0 + 64 || span.lo > tile_key0) && span.first < tile_key0 + 64;
+            } else {
+                const GroupRow r(p, h, group, in_list - (int)(fdiv((uint32_t)in_list, g.fd_rows) * g.fd_rows.d));
+                there = r.there && there;
+                head = r.head;
+                query = r.query;
+                limit = row_seen(s, len, pos, query);
+                cut = limit < tile_key0 + 32 * KW;
+            }
+            m.q[lane] = row_address(p.Q, b, head, query);
+            m.d[lane] = row_address(g.dO, b, head, query);
             m.limit[lane] = limit;
-            const bool cut = __builtin_amdgcn_ballot_w64(there && limit < tile_key0 + 32 * KW) != 0;
+            cut = __builtin_amdgcn_ballot_w64(there && cut) != 0;
             if (lane == 0) m.masked = cut;
             // (rows that only fill a tile take the entry behind the last row's, which makes them weigh 0)
-            const int64_t i = there ? ((int64_t)b * s.q_heads + r.head) * s.n_q + r.query : g.stats;
+            const int64_t i = there ? ((int64_t)b * s.q_heads + head) * s.n_q + query : g.stats;
             load_lds_word((const uint8_t*)(g.lse2 + i), (uint8_t*)m.lse2);
             load_lds_word((const uint8_t*)(g.delta + i), (uint8_t*)m.delta);
         };
@@ -123,7 +189,7 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
         static_assert(kRows % 4 == 0, "");
         const int piece_row = wave * LPW * kRows + lane / kChunks, piece_col = (lane % kChunks) ^ tile_swizzle<D>(lane / kChunks);
         auto issue = [&](int t) {
-            const RowMeta& m = meta[t & 3];
+            const RowMeta<WINDOW>& m = meta[t & 3];
             uint8_t *qt = lds[t & 1], *dt = lds[2 + (t & 1)];
             int chunk = piece_col;
             asm volatile("" : "+v"(chunk));   // (columns are formed here: kept, they take two registers each)
@@ -142,7 +208,7 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
         };
         TileReader<D> read(lane, lds[0], team);
         const float c = p.scale_log2;
-        auto rows_block = [&](const RowMeta& m, bool masked) {
+        auto rows_block = [&](const RowMeta<WINDOW>& m, bool masked) {
             const int row0 = 32 * team + 4 * half;   // of this lane in the tile
             // 4 products, each fragment read kAhead products ahead of its own: the sums of dK and dV, K and V leave 64 registers for
             // everything else, and the compiler, left to itself, reads further ahead than that allows.
@@ -180,8 +246,13 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
             }
             if (masked) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key >= m.limit[row0 + 8 * (i >> 2) + (i & 3)]) S[i] = T[i] = 0.f;
+                for (int i = 0; i < 16; ++i) {
+                    const int r = row0 + 8 * (i >> 2) + (i & 3);
+                    bool gone = behind >= m.limit[r];
+                    if constexpr (WINDOW) gone |= ahead < m.lo[r];
+                    S[i] = gone ? 0.f : S[i];
+                    T[i] = gone ? 0.f : T[i];
+                }
             }
             uint32_t pw[8], dw[8];
 #pragma unroll
@@ -210,7 +281,7 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
                 put_rows(t + 2, group_ahead);
                 group_ahead = find_group(t + 3);   // (past the last row: the last row's again)
             }
-            const RowMeta& m = meta[t & 3];
+            const RowMeta<WINDOW>& m = meta[t & 3];
             rows_block(m, __builtin_amdgcn_readfirstlane(m.masked) != 0);
             read.flip();
         }
@@ -241,8 +312,7 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
     add(dv);
     if (team == 1) return;
     const float dk_factor = F16 ? ldexpf(p.scale, -bits) : p.scale, dv_factor = F16 ? ldexpf(1.f, -kWeightBits) : 1.f;
-    const int slot = g.part_slot[part_id];
-    if (slot >= 0) {   // parts are joined by grad_join_kernel
+    if (slot >= 0) {   // parts are joined by grad_join_kernel or grad_window_join_kernel
         float* const dst = g.slots + (((int64_t)slot * tiles + tile_in_block) * 2 * (32 * KW) + key_wave * 32 + (lane & 31)) * D + 4 * half;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
@@ -296,6 +366,34 @@ __global__ __launch_bounds__(256) void grad_join_kernel(SelParams p, GradParams 
     }
 }
 
+// Attention within a window: the same for the tiles in parts, tile blockIdx.y of K/V head blockIdx.z.
+template <bool F16, int D>
+__global__ __launch_bounds__(256) void grad_window_join_kernel(SelParams p, GradParams g) {
+    const SeqShape& s = p.s;
+    const WindowGradParams& w = g.window;
+    const int tile = (int)blockIdx.y, bh = (int)blockIdx.z;
+    const bool first = tile < w.first_tiles;
+    const int parts = first ? w.first_parts : w.near_parts;
+    const int64_t slot = (int64_t)bh * w.head_slots + (first ? tile * w.first_parts : w.first_tiles * w.first_parts + (tile - w.first_tiles) * w.near_parts);
+    const int b = (int)fdiv((uint32_t)bh, p.fd_kv_heads), h = bh - b * s.kv_heads;
+    const float* const src = g.slots + slot * (128 * D);
+    for (int i = (int)blockIdx.x * 256 + threadIdx.x; i < 128 * (D / 4); i += 256 * kJoinShare) {
+        const int which = i / (64 * (D / 4)), row = i / (D / 4) % 64, c = i % (D / 4), key = tile * 64 + row;
+        if (key >= s.n_k) continue;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int k = 0; k < parts; ++k) {
+            const float4 v = *(const float4*)(src + (int64_t)k * (128 * D) + 4 * i);
+            sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+        }
+        const float f = which == 0 ? (F16 ? ldexpf(p.scale, -g.head_bits[bh]) : p.scale) : F16 ? ldexpf(1.f, -kWeightBits) : 1.f;
+        uint2 v;
+        v.x = Elem<F16>::pack(sum.x * f, sum.y * f);
+        v.y = Elem<F16>::pack(sum.z * f, sum.w * f);
+        *(uint2*)((uint8_t*)row_address(which == 0 ? g.dK : g.dV, b, h, key) + 8 * c) = v;
+    }
+}
+
 // ---- dQ ----------------------------------------------------------------------------------------
 // The forward walk with dO beside Q in registers: S^T = K Q^T, dP^T = V dO^T, and dQ^T += K^T dS^T with K read both ways from its tile.
 // Lists of at most this many units are walked twice, for an exact D (see below).  1 024 tokens in groups of 64 x 4 heads, bf16, head_dim 128; a training step without and
@@ -305,15 +403,16 @@ __global__ __launch_bounds__(256) void grad_join_kernel(SelParams p, GradParams 
 constexpr int kFewUnits = 12;
 
 // For the launches that follow: what they count, and what rows that only fill a tile take.
+template <bool WINDOW = false>
 __device__ __forceinline__ void start_lists(const GradParams& g) {
     if (blockIdx.x == 0 && threadIdx.x < 5) {
-        g.counters[threadIdx.x] = 0;
+        if (!WINDOW) g.counters[threadIdx.x] = 0;
         g.delta[g.stats] = 0.f;
         g.lse2[g.stats] = INFINITY;
     }
 }
 
-template <int RW, int TEAMS, bool F16, int D>
+template <int RW, int TEAMS, bool F16, int D, bool WINDOW>
 __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad_queries_kernel(SelParams p, GradParams g) {
     using E = Elem<F16>;
     constexpr int NW = RW * TEAMS, kTile = 64 * D * 2;
@@ -321,7 +420,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
     const Item it(p);
-    start_lists(g);
+    start_lists<WINDOW>(g);
     if (it.idle(p)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int team = TEAMS == 1 ? 0 : wave / RW, row_wave = wave % RW, half = lane >> 5;
@@ -367,30 +466,25 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     }
     auto unscaled = [&](float x) { return F16 ? ldexpf(x, -bits) : x; };
     const int len = seq_len(s, it.b);
-    const int64_t pos = seq_pos(s, it.b, len);
-    const int seen = group_seen(s, len, pos, it.g);
-    const int limit = row.there ? row_seen(s, len, pos, row.query) : 0;
-    int least = row.there ? limit : 0x7fffffff, most = limit;
-#pragma unroll
-    for (int m = 1; m < 32; m *= 2) {
-        least = min(least, __shfl_xor(least, m));
-        most = max(most, __shfl_xor(most, m));
-    }
-    least = __builtin_amdgcn_readfirstlane(least);
-    most = __builtin_amdgcn_readfirstlane(most);
-    const int n_units = seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
+    const int64_t pos = WINDOW ? window_pos(s, it.b, len) : seq_pos(s, it.b, len);
+    const int i0 = it.g * s.q_group, i1 = min(i0 + s.q_group, s.n_q) - 1;
+    const WindowUnits window(p, len, pos, i0, i1);
+    const int seen = WINDOW ? window.near_end : group_seen(s, len, pos, it.g);
+    const RowMask<WINDOW> hidden(p, row, &window, len, pos);
+    const int n_units = WINDOW ? window.n : seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
     const int n_tiles = (n_units + 1) / 2;
     f32x16 dq[D / 32];
     clear<D>(dq);
     const float c = p.scale_log2;
-    const KeyLoader<NW, D> load(p, it, seen, wave, lane);
+    const KeyLoader<NW, D, WINDOW> load(p, it, seen, wave, lane, window.first_end);
     TileReader<D> read(lane, lds[0], team);
-    auto unit_start = [&](int i) { return i < n_units ? __builtin_amdgcn_readfirstlane(s_units[i]) : kNoUnit; };
-    auto unit_load = [&](int i) { return __builtin_amdgcn_readfirstlane(s_units[min(i, n_units - 1)]); };   // (as in the forward walk)
+    auto unit_at = [&](int i) { return WINDOW ? window.start(i) : __builtin_amdgcn_readfirstlane(s_units[i]); };
+    auto unit_start = [&](int i) { return i < n_units ? unit_at(i) : kNoUnit; };
+    auto unit_load = [&](int i) { return unit_at(min(i, n_units - 1)); };   // (as in the forward walk)
     float sum = 0.f;   // over this lane's keys: of P dP while D is being formed, then of dS
     auto block = [&](auto form_d, int hb, int start) {
         constexpr bool kFormD = decltype(form_d)::value;
-        if (start >= most) return;
+        if (hidden.idle(start)) return;
         f32x16 S, T;
 #pragma unroll
         for (int i = 0; i < 16; ++i) S[i] = T[i] = 0.f;
@@ -398,16 +492,16 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
         for (int ks = 0; ks < D / 16; ++ks) S = E::mfma(read.rows(0, hb, ks), qf[ks], S);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) T = E::mfma(read.rows(1, hb, ks), df[ks], T);
-        const bool masked = start + kUnit > least;
+        const bool masked = hidden.cuts(start);
         uint32_t dw[8];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
             float d0 = __builtin_amdgcn_exp2f(fmaf(S[i], c, -lse2)) * (T[i] - delta);
             float d1 = __builtin_amdgcn_exp2f(fmaf(S[i + 1], c, -lse2)) * (T[i + 1] - delta);
             if (masked) {
-                const int key = start + 8 * (i >> 2) + 4 * half + (i & 3);
-                if (key >= limit) d0 = 0.f;
-                if (key + 1 >= limit) d1 = 0.f;
+                const int k = 8 * (i >> 2) + 4 * half + (i & 3);
+                if (hidden.hides(start, k)) d0 = 0.f;
+                if (hidden.hides(start, k + 1)) d1 = 0.f;
             }
             sum += d0 + d1;
             if constexpr (!kFormD) dw[i >> 1] = E::pack(d0, d1);
@@ -426,7 +520,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     // product kAhead later.  Keys that a row does not see get their -infinity as what their scores are added to.
     auto tile = [&](int start0, int start1) {
         constexpr int kAhead = 2, kN = D / 16, kM = 2 * (D / 32), kAll = 4 * kN + 2 * kM;
-        if (start0 >= most && start1 >= most) return;   // nobody in this wave sees the units
+        if (hidden.idle(start0) && hidden.idle(start1)) return;   // nobody in this wave sees the units
         frag8 fr[kAll];
         auto fetch = [&](int i) {   // S T of unit 0, S T of unit 1, dS K of both
             if (i < 4 * kN) fr[i] = read.rows(i / kN % 2, i / (2 * kN), i % kN);
@@ -439,9 +533,9 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int start = u == 0 ? start0 : start1;
-            if (start + kUnit > least) {
+            if (hidden.cuts(start)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) S[u][i] = start + 8 * (i >> 2) + 4 * half + (i & 3) < limit ? 0.f : -INFINITY;
+                for (int i = 0; i < 16; ++i) S[u][i] = hidden.hides(start, 8 * (i >> 2) + 4 * half + (i & 3)) ? -INFINITY : 0.f;
             }
         }
         auto weigh = [&](int u, int j) {   // pair j
@@ -545,7 +639,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     }
     sum = unscaled(over_row(sum));
     if constexpr (F16) {
-        int least = limit > 0 ? say : kMostBits;
+        int least = hidden.sees() ? say : kMostBits;
 #pragma unroll
         for (int m = 1; m < 32; m *= 2) least = min(least, __shfl_xor(least, m));
         if (team == 0 && lane == 0) g.row_bits[it.item * RW + row_wave] = least;
@@ -756,16 +850,16 @@ __global__ __launch_bounds__(256, 2) void grad_queries_narrow_kernel(SelParams p
 template <int KW, bool F16, int D>
 inline void launch_grad_keys(const SelParams& p, const GradParams& g, hipStream_t stream) {
     const int64_t items = (int64_t)g.most_parts * g.fd_tiles.d;
-    hipLaunchKernelGGL((grad_keys_kernel<KW, F16, D>), dim3((unsigned)((items + 127) / 128 * 128)), dim3(KW * 128), 0, stream, p, g);
+    hipLaunchKernelGGL((grad_keys_kernel<KW, F16, D, false>), dim3((unsigned)((items + 127) / 128 * 128)), dim3(KW * 128), 0, stream, p, g);
     if (g.most_joins > 0) {   // workgroups that share a key tile run beside each other (30 us for train_long's; 33 the other way round)
         const unsigned n = g.most_joins * g.fd_tiles.d, rows = n < 32768u ? n : 32768u;
         hipLaunchKernelGGL((grad_join_kernel<F16, D>), dim3(kJoinShare, rows, (n + rows - 1) / rows), dim3(256), 0, stream, p, g, 32 * KW);
     }
 }
-template <int RW, int TEAMS, bool F16, int D>
+template <int RW, int TEAMS, bool F16, int D, bool WINDOW = false>
 inline void launch_grad_queries(const SelParams& p, const GradParams& g, hipStream_t stream) {
-    const size_t dyn = sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1);
-    hipLaunchKernelGGL((grad_queries_kernel<RW, TEAMS, F16, D>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p, g);
+    const size_t dyn = WINDOW ? 0 : sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1);
+    hipLaunchKernelGGL((grad_queries_kernel<RW, TEAMS, F16, D, WINDOW>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p, g);
 }
 
 // tile_rows: 128, 64, 32 or 16; key tiles of 64 or 32 keys
@@ -780,6 +874,21 @@ inline hipError_t launch_bwd(const SelParams& p, const GradParams& g, int tile_r
     launch_grad_lists(p, g, stream);
     if (tile_keys == 64) launch_grad_keys<2, F16, D>(p, g, stream);
     else launch_grad_keys<1, F16, D>(p, g, stream);
+    return hipGetLastError();
+}
+
+// Attention within a window.  tile_rows: 128, 64 or 32
+template <bool F16, int D>
+inline hipError_t launch_window_bwd(const SelParams& p, const GradParams& g, int tile_rows, hipStream_t stream) {
+    if (tile_rows == 128) launch_grad_queries<4, 1, F16, D, true>(p, g, stream);
+    else if (tile_rows == 64) launch_grad_queries<2, 2, F16, D, true>(p, g, stream);
+    else launch_grad_queries<1, 2, F16, D, true>(p, g, stream);
+    if (F16) launch_grad_head_bits(g, stream);
+    const WindowGradParams& w = g.window;
+    hipLaunchKernelGGL((grad_keys_kernel<2, F16, D, true>), dim3((unsigned)(8 * w.per_xcd)), dim3(256), 0, stream, p, g);
+    const int joined = w.near_parts > 1 ? w.tiles : w.first_parts > 1 ? w.first_tiles : 0;
+    if (joined > 0)
+        hipLaunchKernelGGL((grad_window_join_kernel<F16, D>), dim3(kJoinShare, (unsigned)joined, (unsigned)g.heads), dim3(256), 0, stream, p, g);
     return hipGetLastError();
 }
 

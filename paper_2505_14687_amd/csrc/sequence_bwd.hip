@@ -22,6 +22,12 @@ __device__ __forceinline__ void put_head_bits(const GradParams& g, int bh) {
     __syncthreads();
 }
 
+__global__ __launch_bounds__(256) void grad_head_bits_kernel(GradParams g) { put_head_bits<256>(g, (int)blockIdx.x); }
+
+void launch_grad_head_bits(const GradParams& g, hipStream_t stream) {
+    hipLaunchKernelGGL(grad_head_bits_kernel, dim3((unsigned)g.heads), dim3(256), 0, stream, g);
+}
+
 // The bitmap, cleared (by a kernel: recorded into graphs like any other launch), and half's exponents.
 __global__ __launch_bounds__(256) void grad_clear_kernel(GradParams g) {
     if (g.row_bits)

@@ -16,7 +16,7 @@
 
 namespace grat {
 
-template <int RW, int TEAMS, bool F16, int D>
+template <int RW, int TEAMS, bool F16, int D, bool WINDOW>
 __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void selected_fwd_kernel(SelParams p) {
     using E = Elem<F16>;
     constexpr int NW = RW * TEAMS, kTile = 64 * D * 2;
@@ -38,19 +38,13 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const frag8*)(q_src + 32 * ks);
     const int len = seq_len(s, it.b);
-    const int64_t pos = seq_pos(s, it.b, len);
-    const int seen = group_seen(s, len, pos, it.g);
-    const int limit = row.there ? row_seen(s, len, pos, row.query) : 0;   // keys below it are seen
-    int least = row.there ? limit : 0x7fffffff, most = limit;              // of the wave's rows
-#pragma unroll
-    for (int m = 1; m < 32; m *= 2) {
-        least = min(least, __shfl_xor(least, m));
-        most = max(most, __shfl_xor(most, m));
-    }
-    least = __builtin_amdgcn_readfirstlane(least);
-    most = __builtin_amdgcn_readfirstlane(most);
+    const int64_t pos = WINDOW ? window_pos(s, it.b, len) : seq_pos(s, it.b, len);
+    const int i0 = it.g * s.q_group, i1 = min(i0 + s.q_group, s.n_q) - 1;
+    const WindowUnits window(p, len, pos, i0, i1);
+    const int seen = WINDOW ? window.near_end : group_seen(s, len, pos, it.g);
+    const RowMask<WINDOW> hidden(p, row, &window, len, pos);
 
-    const int all_units = seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
+    const int all_units = WINDOW ? window.n : seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
     int u_first = 0, n_units = all_units;
     if (p.splits > 1) {   // an even number of units a part
         const int per = ((all_units + p.splits - 1) / p.splits + 1) & ~1;
@@ -65,18 +59,19 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     float m_ref = -1e38f / fmaxf(c, 1.f);   // (finite, so that a block without a seen key weighs 0)
     float l_run = 0.f;
 
-    const KeyLoader<NW, D> load(p, it, seen, wave, lane);
+    const KeyLoader<NW, D, WINDOW> load(p, it, seen, wave, lane, window.first_end);
     TileReader<D> read(lane, lds[0], team);
+    auto unit_at = [&](int i) { return WINDOW ? window.start(i) : __builtin_amdgcn_readfirstlane(s_units[i]); };
     // (a list's last tile may lack its second unit; one of a part that ends inside the list does not)
-    auto unit_start = [&](int i) { return i < n_units ? __builtin_amdgcn_readfirstlane(s_units[u_first + i]) : kNoUnit; };
+    auto unit_start = [&](int i) { return i < n_units ? unit_at(u_first + i) : kNoUnit; };
     // (what fills a tile in its place is the list's last unit again: a key that is not listed may hold anything, and 0 * NaN is NaN)
-    auto unit_load = [&](int i) { return __builtin_amdgcn_readfirstlane(s_units[u_first + max(min(i, n_units - 1), 0)]); };
+    auto unit_load = [&](int i) { return unit_at(u_first + max(min(i, n_units - 1), 0)); };
 
     auto mask = [&](f32x16& S, int start) {
-        if (start + kUnit > least) {
+        if (hidden.cuts(start)) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (start + 8 * (i >> 2) + 4 * half + (i & 3) >= limit) S[i] = -INFINITY;
+                if (hidden.hides(start, 8 * (i >> 2) + 4 * half + (i & 3))) S[i] = -INFINITY;
         }
     };
     auto weigh = [&](const f32x16& S, uint32_t (&w)[8]) {   // weights against the reference; this lane's sum of them
@@ -111,7 +106,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     if constexpr (TEAMS == 2) {
         // few rows: latency is what counts, a block after the other
         auto block = [&](int start) {
-            if (start >= most) return;   // nobody in this wave sees the unit
+            if (hidden.idle(start)) return;
             f32x16 S;
 #pragma unroll
             for (int i = 0; i < 16; ++i) S[i] = 0.f;
@@ -222,7 +217,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
         constexpr integral_constant<int, 1> odd{};
         if (n_tiles > 0) {
             load.issue(load.K, load.pitch_k, ahead, lds[0], wave);
-            if (most == 0) {   // a wave without a row only fetches
+            if (hidden.nothing()) {   // a wave without a row only fetches
                 for (int t = 0; t <= n_tiles; ++t) {
                     here = ahead;
                     ahead = unit_load(2 * t + 2 + load.my_unit);
@@ -487,10 +482,10 @@ inline void launch_join(const SelParams& p, int tile_rows, hipStream_t stream) {
                        make_fastdiv((uint32_t)p.rows));
 }
 
-template <int RW, int TEAMS, bool F16, int D>
+template <int RW, int TEAMS, bool F16, int D, bool WINDOW = false>
 inline void launch_fwd_tile(const SelParams& p, hipStream_t stream) {
-    const size_t dyn = sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1);
-    hipLaunchKernelGGL((selected_fwd_kernel<RW, TEAMS, F16, D>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p);
+    const size_t dyn = WINDOW ? 0 : sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1);
+    hipLaunchKernelGGL((selected_fwd_kernel<RW, TEAMS, F16, D, WINDOW>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p);
 }
 
 // tile_rows: 256 (head_dim 128), 128, 64, 32 or 16
@@ -505,6 +500,19 @@ inline hipError_t launch_fwd(const SelParams& p, int tile_rows, hipStream_t stre
     else if (tile_rows == 16)
         hipLaunchKernelGGL((selected_fwd_narrow_kernel<F16, D>), dim3(8 * p.per_xcd), dim3(256), sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1),
                            stream, p);
+    if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
+    return hipGetLastError();
+}
+
+// Attention within a window.  tile_rows: 256 (head_dim 128), 128, 64 or 32
+template <bool F16, int D>
+inline hipError_t launch_window(const SelParams& p, int tile_rows, hipStream_t stream) {
+    if constexpr (D == 128) {
+        if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D, true>(p, stream);
+    }
+    if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D, true>(p, stream);
+    else if (tile_rows == 64) launch_fwd_tile<2, 2, F16, D, true>(p, stream);
+    else if (tile_rows == 32) launch_fwd_tile<1, 2, F16, D, true>(p, stream);
     if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
     return hipGetLastError();
 }

@@ -1,0 +1,198 @@
+// Host side of attention within a window: argument validation and dispatch.  No allocation, no synchronisation.
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "grat_window.h"
+#include "sequence_attn.h"
+#include "sequence_checks.h"
+
+namespace grat {
+namespace {
+
+constexpr int64_t kMostFirst = (int64_t)1 << 20;   // first keys that stay visible
+
+// What every operator here reads of a grat_sequence.
+grat_status make_shape(const grat_sequence* s, SeqShape* out) {
+    if (!s) return GRAT_ERR_NULL;
+    if (s->batch < 1 || s->kv_heads < 1 || s->q_heads < 1 || s->n_q < 1 || s->n_k < 1 || s->q_heads % s->kv_heads) return GRAT_ERR_BAD_DIMS;
+    if (!is16(s->dtype) || (s->head_dim != 64 && s->head_dim != 128)) return GRAT_ERR_UNSUPPORTED;
+    if (s->n_q >= kMaxRows || s->n_k >= kMaxRows || (int64_t)s->batch * s->kv_heads > 65535 || s->q_heads > 65535) return GRAT_ERR_UNSUPPORTED;
+    if ((int64_t)s->batch * s->q_heads * s->n_q >= kMaxRows / 2 || (int64_t)s->batch * s->kv_heads * s->n_k >= kMaxRows / 4) return GRAT_ERR_UNSUPPORTED;
+    *out = SeqShape{s->batch, s->q_heads, s->kv_heads, s->q_heads / s->kv_heads, s->n_q, s->n_k, s->n_q, kUnit, 1, 0,
+                    s->causal ? 1 : 0, s->d_k_len, s->d_q_pos};
+    return GRAT_OK;
+}
+
+grat_status set_window(SelParams& p, float scale, int32_t window, int32_t sinks) {
+    if (window < 0 || sinks < 0 || !(scale > 0.f) || !std::isfinite(scale)) return GRAT_ERR_BAD_DIMS;
+    const bool all = window == 0 || sinks >= p.s.n_k;
+    p.window = all ? kNoWindow : window;
+    p.sinks = all ? 0 : sinks;
+    if (p.sinks > kMostFirst) return GRAT_ERR_UNSUPPORTED;
+    p.scale = scale;
+    p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    return GRAT_OK;
+}
+
+// Keys that `queries` neighbouring queries may see beside the first ones, and the other way round.
+int64_t reach(const SelParams& p, int64_t queries, int64_t most) {
+    return p.window == kNoWindow ? most : std::min(most, (p.s.causal ? 1 : 2) * ((int64_t)p.window - 1) + queries);
+}
+
+// Groups of neighbouring queries whose rows fill a tile.
+void set_tiles(SelParams& p, int tile_rows) {
+    SeqShape& s = p.s;
+    s.q_group = std::max(1, std::min(s.n_q, tile_rows / s.share));
+    s.n_groups = (s.n_q + s.q_group - 1) / s.q_group;
+    p.rows = s.q_group * s.share;
+    p.row_tiles = (p.rows + tile_rows - 1) / tile_rows;
+    p.fd_row_tiles = make_fastdiv((uint32_t)p.row_tiles);
+    p.fd_groups = make_fastdiv((uint32_t)s.n_groups);
+    p.fd_kv_heads = make_fastdiv((uint32_t)s.kv_heads);
+    p.fd_q_group = make_fastdiv((uint32_t)s.q_group);
+    p.fd_units = make_fastdiv(1);
+}
+void set_items(SelParams& p, int64_t items, int splits) {
+    p.splits = splits;
+    p.items = (int32_t)(items * splits);
+    p.per_xcd = (p.items + 7) / 8;
+    p.fd_splits = make_fastdiv((uint32_t)splits);
+}
+
+struct WindowPlan {
+    SelParams p{};
+    GradParams g{};
+    int tile_rows = 0;
+    int64_t work = 0;
+};
+
+int fwd_tile_rows(const SelParams& p, int head_dim) {
+    const int64_t rows = (int64_t)p.s.n_q * p.s.share;
+    if (rows <= 32) return 32;
+    if (rows <= 64) return 64;
+    if (head_dim == 128 && (int64_t)p.s.batch * p.s.kv_heads * ((rows + 255) / 256) >= 1024) return 256;
+    return 128;
+}
+int bwd_tile_rows(const SelParams& p) {
+    const int64_t rows = (int64_t)p.s.n_q * p.s.share;
+    return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+}
+
+grat_status make_plan(const grat_sequence* seq, float scale, int32_t window, int32_t sinks, bool backward, void* work, WindowPlan* out) {
+    WindowPlan plan;
+    SelParams& p = plan.p;
+    grat_status st = make_shape(seq, &p.s);
+    if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
+    if (st != GRAT_OK) return st;
+    const SeqShape& s = p.s;
+    const int64_t D = seq->head_dim, heads = (int64_t)s.batch * s.kv_heads;
+    Scratch scratch{(uint8_t*)work};
+    plan.tile_rows = backward ? bwd_tile_rows(p) : fwd_tile_rows(p, (int)D);
+    set_tiles(p, plan.tile_rows);
+    const int64_t items = heads * s.n_groups * p.row_tiles;
+    if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+    // Few workgroups: the keys of each are shared by several (as with lists).
+    const int64_t units = (reach(p, s.q_group, s.n_k) + kUnit - 1) / kUnit + (p.sinks + kUnit - 1) / kUnit, steps = (units + 1) / 2;
+    set_items(p, items, backward || steps < 8 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(256 / items, steps / 2), 64)));
+    if (p.splits > 1) {
+        p.part_o = scratch.take<float>((int64_t)p.items * plan.tile_rows * D);
+        p.part_ml = scratch.take<float>((int64_t)p.items * plan.tile_rows * 2);
+    }
+    if (backward) {
+        GradParams& g = plan.g;
+        WindowGradParams& w = g.window;
+        w.tiles = (s.n_k + 63) / 64;
+        w.first_tiles = (p.sinks + 63) / 64;
+        const int64_t near = reach(p, 64, s.n_q) * s.share, all = (int64_t)s.n_q * s.share;
+        const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(near, 512), heads * w.tiles * near / 768) + 63) / 64 * 64);
+        w.near_parts = (int32_t)((near + part - 1) / part);
+        w.first_parts = std::max(w.near_parts, (int32_t)((all + part - 1) / part));
+        const int64_t firsts = (int64_t)w.first_tiles * w.first_parts, per_head = firsts + (int64_t)(w.tiles - w.first_tiles) * w.near_parts;
+        const int64_t slots = w.near_parts > 1 ? per_head : w.first_parts > 1 ? firsts : 0;
+        if (heads * per_head >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+        w.head_items = (int32_t)per_head;
+        w.head_slots = (int32_t)slots;
+        w.items = (int32_t)(heads * per_head);
+        w.per_xcd = (w.items + 7) / 8;
+        g.fd_tiles = make_fastdiv(1);
+        g.stats = (int64_t)s.batch * s.q_heads * s.n_q;
+        g.delta = scratch.take<float>(g.stats + 1);
+        g.lse2 = scratch.take<float>(g.stats + 1);
+        g.slots = scratch.take<float>(heads * slots * 128 * D);
+        g.heads = (int32_t)heads;
+        if (seq->dtype == GRAT_F16) {
+            g.head_runs = s.n_groups * p.row_tiles * (plan.tile_rows / 32);
+            g.row_bits = scratch.take<int32_t>(heads * g.head_runs);
+            g.head_bits = scratch.take<int32_t>(heads);
+        }
+    }
+    plan.work = scratch.bytes;
+    *out = plan;
+    return GRAT_OK;
+}
+
+}  // namespace
+}  // namespace grat
+
+using namespace grat;
+
+extern "C" int64_t grat_window_attention_work(const grat_sequence* seq, int32_t window, int32_t sinks, int32_t backward) {
+    WindowPlan plan;
+    return make_plan(seq, 1.f, window, sinks, backward != 0, nullptr, &plan) == GRAT_OK ? plan.work : 0;
+}
+
+extern "C" grat_status grat_window_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K, const grat_tensor* V,
+                                                 const grat_tensor* O, float* d_lse, float scale, int32_t window, int32_t sinks, void* d_work,
+                                                 void* hip_stream) {
+    WindowPlan plan;
+    grat_status st = make_plan(seq, scale, window, sinks, false, d_work, &plan);
+    for (const grat_tensor* t : {Q, K, V})
+        if (st == GRAT_OK) st = check_tensor(t, seq->dtype, seq->head_dim);
+    if (st == GRAT_OK) st = check_output(O, seq->dtype, seq->head_dim, seq->batch, seq->q_heads);
+    if (st != GRAT_OK) return st;
+    if (plan.work > 0 && !d_work) return GRAT_ERR_NULL;
+    if (!aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;
+    SelParams& p = plan.p;
+    p.Q = of(Q);
+    p.K = of(K);
+    p.V = of(V);
+    p.O = of(O);
+    p.lse = d_lse;
+    const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
+    const auto launch = f16 ? (wide ? launch_window_fwd_f16_d128 : launch_window_fwd_f16_d64)
+                            : (wide ? launch_window_fwd_bf16_d128 : launch_window_fwd_bf16_d64);
+    return status_of(launch(p, plan.tile_rows, (hipStream_t)hip_stream));
+}
+
+extern "C" grat_status grat_window_attention_bwd(const grat_sequence* seq, const grat_tensor* dO, const grat_tensor* Q, const grat_tensor* K,
+                                                 const grat_tensor* V, const grat_tensor* O, const float* d_lse, const grat_tensor* dQ,
+                                                 const grat_tensor* dK, const grat_tensor* dV, float scale, int32_t window, int32_t sinks,
+                                                 void* d_work, void* hip_stream) {
+    if (!d_lse) return GRAT_ERR_NULL;
+    WindowPlan plan;
+    grat_status st = make_plan(seq, scale, window, sinks, true, d_work, &plan);
+    for (const grat_tensor* t : {dO, Q, K, V, O})
+        if (st == GRAT_OK) st = check_tensor(t, seq->dtype, seq->head_dim);
+    if (st == GRAT_OK) st = check_output(dQ, seq->dtype, seq->head_dim, seq->batch, seq->q_heads);
+    for (const grat_tensor* t : {dK, dV})
+        if (st == GRAT_OK) st = check_output(t, seq->dtype, seq->head_dim, seq->batch, seq->kv_heads);
+    if (st != GRAT_OK) return st;
+    if (!d_work) return GRAT_ERR_NULL;
+    if (!aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;
+    SelParams& p = plan.p;
+    p.Q = of(Q);
+    p.K = of(K);
+    p.V = of(V);
+    p.O = of(O);
+    p.lse = const_cast<float*>(d_lse);
+    GradParams& g = plan.g;
+    g.dO = of(dO);
+    g.dQ = of(dQ);
+    g.dK = of(dK);
+    g.dV = of(dV);
+    const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
+    const auto launch = f16 ? (wide ? launch_window_bwd_f16_d128 : launch_window_bwd_f16_d64)
+                            : (wide ? launch_window_bwd_bf16_d128 : launch_window_bwd_bf16_d64);
+    return status_of(launch(p, g, plan.tile_rows, (hipStream_t)hip_stream));
+}

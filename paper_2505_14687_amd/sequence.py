@@ -91,8 +91,12 @@ def _library() -> ctypes.CDLL:
 
 
 def _call(name: str, *args, written=()):
+    _enter(_library(), name, args, written)
+
+
+def _enter(L: ctypes.CDLL, name: str, args, written):
     """written: the caller's tensors that it writes to; autograd then notices where it had saved one of them."""
-    st = getattr(_library(), name)(*args)
+    st = getattr(L, name)(*args)
     if st != GRAT_OK:
         raise GratError(st, name)
     for t in written:
