@@ -66,13 +66,19 @@ struct WindowLibrary {   // ... and those of grat_window.h
     decltype(&grat_window_attention_work) attention_work;
     decltype(&grat_window_attention_fwd) attention_fwd;
     decltype(&grat_window_attention_bwd) attention_bwd;
+    decltype(&grat_cache_append) append;
+    decltype(&grat_cache_read) read;
+    decltype(&grat_cache_attention_work) cache_work;
+    decltype(&grat_cache_attention_fwd) cache_attention;
 } g_win;
 
 // set_window_library(addresses): in the order above
 PyObject* set_window_library(PyObject*, PyObject* args) {
-    unsigned long long a[3];
-    if (!PyArg_ParseTuple(args, "KKK", a, a + 1, a + 2)) return nullptr;
-    g_win = {(decltype(g_win.attention_work))a[0], (decltype(g_win.attention_fwd))a[1], (decltype(g_win.attention_bwd))a[2]};
+    unsigned long long a[7];
+    if (!PyArg_ParseTuple(args, "KKKKKKK", a, a + 1, a + 2, a + 3, a + 4, a + 5, a + 6)) return nullptr;
+    g_win = {(decltype(g_win.attention_work))a[0], (decltype(g_win.attention_fwd))a[1], (decltype(g_win.attention_bwd))a[2],
+             (decltype(g_win.append))a[3],         (decltype(g_win.read))a[4],          (decltype(g_win.cache_work))a[5],
+             (decltype(g_win.cache_attention))a[6]};
     Py_RETURN_NONE;
 }
 
@@ -664,7 +670,7 @@ PyObject* selected_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// ---- attention within a window (grat_window.h) -----------------------------------------------------
+// ---- attention within a window and over caches (grat_window.h) -----------------------------------------------------
 
 struct Limits {   // window (None: no limit) and sinks
     int32_t window, sinks;
@@ -727,6 +733,118 @@ PyObject* window_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// A cache of the dtype of `like`, or of 8 bits beside its rows' scales.
+struct Cache {
+    const at::Tensor &t, *scale;
+    grat_tensor scales{};
+    Cache(PyObject* cache, PyObject* s, const at::Tensor* like) : t(tensor_of(cache)), scale(s == Py_None ? nullptr : &tensor_of(s)) {
+        need(t.dim() == 4 && t.stride(3) == 1 && t.is_cuda());
+        for (int i = 0; i < 4; ++i) need(t.size(i) >= 1 && t.size(i) <= INT32_MAX);
+        if (like) need(t.device() == like->device());
+        no_gradient(t);
+        if (!scale) {
+            need(like && t.scalar_type() == like->scalar_type());
+            return;
+        }
+        need(t.scalar_type() == at::kFloat8_e4m3fn && scale->scalar_type() == at::kFloat && scale->dim() == 3 && scale->device() == t.device());
+        for (int i = 0; i < 3; ++i) need(scale->size(i) == t.size(i));
+        no_gradient(*scale);
+        scales = {scale->data_ptr(), t.size(0) > 1 ? scale->stride(0) : 0, t.size(1) > 1 ? scale->stride(1) : 0, t.size(2) > 1 ? scale->stride(2) : 1};
+    }
+    const grat_tensor* s() const { return scale ? &scales : nullptr; }
+};
+
+// cache_append(Q or None, K, V, table or None, K_cache, V_cache, start, K_scale, V_scale, positions, layout, axis_pairs, out, stream): Q_out (True where there is no Q)
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return ordinary(n, 14, [&]() -> PyObject* {
+        const bool with_q = a[0] != Py_None;
+        const at::Tensor &k = rows_of(a[1]), &v = rows_of(a[2], &k), &q = with_q ? rows_of(a[0], &k) : k;
+        need(q.size(0) == k.size(0) && q.size(2) == k.size(2) && q.size(3) == k.size(3));
+        same_shape(k, v);
+        need((a[7] == Py_None) == (a[8] == Py_None) && a[3] != Py_None && a[6] != Py_None && (with_q || a[12] == Py_None));
+        const Cache kc(a[4], a[7], &k), vc(a[5], a[8], &k);
+        need(kc.t.size(0) == k.size(0) && kc.t.size(1) == k.size(1) && kc.t.size(3) == k.size(3));
+        same_shape(kc.t, vc.t);
+        RotaryCall call(q, k.size(1), a[3], a[9], Py_None, layout_of(a[10]), a[11], 0);
+        call.args.d_start = (const int32_t*)flat(a[6], at::kInt, {k.size(0)}, k);
+        const hipStream_t stream = current_stream(k, a[13]);
+        const at::Tensor qo = !with_q ? k : a[12] == Py_None ? at::empty_like(q) : rows_of(a[12], &k);
+        same_shape(q, qo);
+        const grat_tensor t[6] = {tensor4(q), tensor4(qo), tensor4(k), tensor4(v), tensor4(kc.t), tensor4(vc.t)};
+        const int32_t rows = (int32_t)kc.t.size(2);
+        const grat_status st = without_gil([&] {
+            return g_win.append(&call.args, with_q ? t : nullptr, with_q ? t + 1 : nullptr, t + 2, t + 3, t + 4, t + 5, kc.s(), vc.s(), rows, stream);
+        });
+        if (st != GRAT_OK) return PyLong_FromLong((long)st);
+        for (const Cache* c : {&kc, &vc}) {
+            written(c->t);
+            if (c->scale) written(*c->scale);
+        }
+        if (with_q) return given_or(a[12], qo);
+        Py_RETURN_TRUE;
+    });
+}
+
+// cache_read(cache, scale, dtype id, k_len, out, stream)
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return ordinary(n, 6, [&]() -> PyObject* {
+        need(a[1] != Py_None);
+        const Cache c(a[0], a[1], nullptr);
+        const int64_t id = int_of(a[2]);
+        need(id >= GRAT_BF16 && id <= GRAT_F16);
+        const at::ScalarType type = id == GRAT_BF16 ? at::kBFloat16 : id == GRAT_F16 ? at::kHalf : at::kFloat;
+        const int32_t* const len = (const int32_t*)flat(a[3], at::kInt, {c.t.size(0)}, c.t, true);
+        const hipStream_t stream = current_stream(c.t, a[5]);
+        const at::Tensor o = a[4] == Py_None ? at::empty(c.t.sizes(), c.t.options().dtype(type)) : rows_of(a[4]);
+        need(o.scalar_type() == type && o.device() == c.t.device());
+        same_shape(c.t, o);
+        const grat_tensor t[2] = {tensor4(c.t), tensor4(o)};
+        return sequence_result(without_gil([&] {
+            return g_win.read((grat_dtype)id, (int32_t)c.t.size(0), (int32_t)c.t.size(1), (int32_t)c.t.size(2), (int32_t)c.t.size(3), t, c.s(), len, t + 1, stream);
+        }), a[4], o);
+    });
+}
+
+// cache_attention(Q, K_cache, V_cache, scale, k_len, K_scale, V_scale, parent, window, sinks, return_lse, out, stream): O or (O, lse)
+PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return ordinary(n, 13, [&]() -> PyObject* {
+        const at::Tensor& q = rows_of(a[0]);
+        need((a[5] == Py_None) == (a[6] == Py_None));
+        const Cache k(a[1], a[5], &q), v(a[2], a[6], &q);
+        const float scale = scale_of(a[3]);
+        const int64_t B = q.size(0), N = q.size(2), Hkv = k.t.size(1);
+        need(k.t.size(0) == B && k.t.size(3) == q.size(3) && q.size(1) % Hkv == 0);
+        same_shape(k.t, v.t);
+        const Limits limits(a[8], a[9]);
+        const int32_t* parent = nullptr;
+        int64_t parent_stride = 0;
+        if (a[7] != Py_None) {
+            const at::Tensor& p = tensor_of(a[7]);
+            need(p.scalar_type() == at::kInt && p.is_contiguous() && p.device() == q.device());
+            need((p.dim() == 1 && p.size(0) == N) || (p.dim() == 2 && (p.size(0) == 1 || p.size(0) == B) && p.size(1) == N));
+            parent = (const int32_t*)p.data_ptr();
+            parent_stride = p.dim() == 2 && p.size(0) > 1 ? N : 0;
+        }
+        const grat_sequence s{dtype_of(q), (int32_t)B, (int32_t)q.size(1), (int32_t)Hkv, (int32_t)q.size(3), (int32_t)N, (int32_t)k.t.size(2),
+                              0, 0, 1, (const int32_t*)flat(a[4], at::kInt, {B}, q, true), nullptr};
+        const bool with_lse = bool_of(a[10]);
+        const hipStream_t stream = current_stream(q, a[12]);
+        const int64_t bytes = g_win.cache_work(&s, limits.window, limits.sinks, k.scale ? 1 : 0);
+        const at::Tensor work = bytes ? scratch(bytes, q) : at::Tensor();
+        const at::Tensor o = a[11] == Py_None ? at::empty_like(q) : rows_of(a[11], &q);
+        same_shape(q, o);
+        const at::Tensor lse = with_lse ? at::empty({B, q.size(1), N}, q.options().dtype(at::kFloat)) : at::Tensor();
+        const grat_tensor t[4] = {tensor4(q), tensor4(k.t), tensor4(v.t), tensor4(o)};
+        float* const lp = with_lse ? (float*)lse.data_ptr() : nullptr;
+        void* const w = bytes ? work.data_ptr() : nullptr;
+        const grat_status st = without_gil([&] {
+            return g_win.cache_attention(&s, t, t + 1, t + 2, k.s(), v.s(), t + 3, lp, scale, limits.window, limits.sinks, parent, parent_stride, w, stream);
+        });
+        if (st != GRAT_OK || !with_lse) return sequence_result(st, a[11], o);
+        return tuple_of({given_or(a[11], o), THPVariable_Wrap(lse)});
+    });
+}
+
 PyMethodDef kMethods[] = {
     {"set_library", set_library, METH_VARARGS, nullptr},
     {"attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, nullptr},
@@ -744,6 +862,9 @@ PyMethodDef kMethods[] = {
     {"set_window_library", set_window_library, METH_VARARGS, nullptr},
     {"window_fwd", (PyCFunction)(void (*)())window_fwd, METH_FASTCALL, nullptr},
     {"window_bwd", (PyCFunction)(void (*)())window_bwd, METH_FASTCALL, nullptr},
+    {"cache_append", (PyCFunction)(void (*)())cache_append, METH_FASTCALL, nullptr},
+    {"cache_read", (PyCFunction)(void (*)())cache_read, METH_FASTCALL, nullptr},
+    {"cache_attention", (PyCFunction)(void (*)())cache_attention, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

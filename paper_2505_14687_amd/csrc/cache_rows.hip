@@ -1,0 +1,208 @@
+// Rows of a cache in 8 bits: written with the new tokens' K turned by their positions, and read back.
+//
+// A row of head_dim numbers x is kept as e4m3 values of x / s and s, the least power of two with max |x| <= 448 s: as e4m3 is a floating format
+// itself, a finer s would gain nothing, and with this one the division and the way back are exact.  Memory (for few tokens the launch) bounds both directions.
+#include <algorithm>
+
+#include "cache_rows.h"
+#include "rotary_pairs.h"
+
+namespace grat {
+
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+
+// 4 numbers as e4m3, rounded to nearest-even; |x| <= 448, NaN and infinities become NaN
+__device__ __forceinline__ uint32_t narrow(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    return (uint32_t)w;
+}
+
+// The power of two of a row whose largest finite |x| is `most`: 448 = 7/8 2^9.
+__device__ __forceinline__ int row_power(float most) {
+    if (!(most > 0.f)) return 0;
+    const int e = __builtin_amdgcn_frexp_expf(most);
+    return max(e - (__builtin_amdgcn_frexp_mantf(most) > 0.875f ? 8 : 9), -126);
+}
+
+// Thread and piece as in rotary_kernel; the lanes of a row, `items` neighbours, find its largest number together.
+template <typename T, bool AXES, bool EIGHT>
+__global__ __launch_bounds__(256) void cache_append_kernel(AppendParams a) {
+    typedef typename Vec16<T>::type vec;
+    constexpr int V = Vec16<T>::n;
+    const RotaryParams& p = a.p;
+    uint32_t slot, item, b, n;
+    fdivmod(threadIdx.x, p.fd_items, slot, item);
+    const uint32_t per_block = 256u / (uint32_t)p.items, token = blockIdx.x * per_block + slot;
+    if (token >= (uint32_t)p.batch * (uint32_t)p.n_tokens) return;   // (items divides a wave: rows end as a whole)
+    fdivmod(token, p.fd_tokens, b, n);
+
+    const int turned = p.rot / (2 * V);
+    const bool turn = (int)item < turned;
+    const int lo = turn && !p.interleaved ? (int)item * V : (int)item * 2 * V;
+    const int hi = turn && !p.interleaved ? lo + p.rot / 2 : lo + V;
+    float cs[V], sn[V];
+    if (turn) pair_angles<T, AXES>(p, (int)b, (int)n, (int)item * V, cs, sn);
+
+    const int all = p.heads[0] + p.heads[1] + p.heads[2];
+    const int64_t row = (int64_t)p.start[b] + n;
+    const bool in_cache = row >= 0 && row < p.n_cache;
+    for (int h0 = blockIdx.y * p.head_chunk, h1 = min(all, h0 + p.head_chunk); h0 < h1; h0 += kHeads) {
+        vec x[kHeads], y[kHeads];
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            int h = min(h0 + i, h1 - 1), t = 0;
+            if (h >= p.heads[0]) { h -= p.heads[0]; t = 1; if (h >= p.heads[1]) { h -= p.heads[1]; t = 2; } }
+            const SeqTensor in = t == 0 ? p.in[0] : t == 1 ? p.in[1] : p.in[2];   // (uniform)
+            const T* const src = (const T*)in.data + b * in.stride_b + h * in.stride_h + n * in.stride_n;
+            x[i] = *(const vec*)(src + lo);
+            y[i] = *(const vec*)(src + hi);
+        }
+#pragma unroll
+        for (int i = 0; i < kHeads; ++i) {
+            if (h0 + i >= h1) break;
+            int h = h0 + i, t = 0;
+            if (h >= p.heads[0]) { h -= p.heads[0]; t = 1; if (h >= p.heads[1]) { h -= p.heads[1]; t = 2; } }
+            const SeqTensor out = t == 0 ? p.out[0] : t == 1 ? p.out[1] : p.out[2];
+            float u[V], v[V];   // the piece's two vectors
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                u[e] = (float)x[i][e];
+                v[e] = (float)y[i][e];
+            }
+            if (turn && t < 2) {
+                if (p.interleaved) {
+#pragma unroll
+                    for (int e = 0; e < V; e += 2) {
+                        const int q = e / 2, q2 = V / 2 + e / 2;
+                        const float f = u[e], c = u[e + 1], f2 = v[e], c2 = v[e + 1];
+                        u[e] = fmaf(cs[q], f, -(sn[q] * c));
+                        u[e + 1] = fmaf(sn[q], f, cs[q] * c);
+                        v[e] = fmaf(cs[q2], f2, -(sn[q2] * c2));
+                        v[e + 1] = fmaf(sn[q2], f2, cs[q2] * c2);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float f = u[e], c = v[e];
+                        u[e] = fmaf(cs[e], f, -(sn[e] * c));
+                        v[e] = fmaf(sn[e], f, cs[e] * c);
+                    }
+                }
+            }
+            if (EIGHT && t > 0) {
+                float most = 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float f = fabsf(u[e]), c = fabsf(v[e]);
+                    most = fmaxf(most, fmaxf(f < INFINITY ? f : 0.f, c < INFINITY ? c : 0.f));
+                }
+                for (int m = 1; m < p.items; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+                const int power = row_power(most);
+                const float inv = ldexpf(1.f, -power);
+                if (!in_cache) continue;
+                uint8_t* const dst = out.data + b * out.stride_b + h * out.stride_h + row * out.stride_n;
+                uint32_t wu[V / 4], wv[V / 4];
+#pragma unroll
+                for (int k = 0; k < V / 4; ++k) {
+                    wu[k] = narrow(u[4 * k] * inv, u[4 * k + 1] * inv, u[4 * k + 2] * inv, u[4 * k + 3] * inv);
+                    wv[k] = narrow(v[4 * k] * inv, v[4 * k + 1] * inv, v[4 * k + 2] * inv, v[4 * k + 3] * inv);
+                }
+                if constexpr (V == 8) {
+                    *(uint2*)(dst + lo) = make_uint2(wu[0], wu[1]);
+                    *(uint2*)(dst + hi) = make_uint2(wv[0], wv[1]);
+                } else {
+                    *(uint32_t*)(dst + lo) = wu[0];
+                    *(uint32_t*)(dst + hi) = wv[0];
+                }
+                const SeqTensor& to = t == 1 ? a.k_scale : a.v_scale;
+                if (item == 0) ((float*)to.data)[b * to.stride_b + h * to.stride_h + row * to.stride_n] = ldexpf(1.f, power);
+            } else {
+                if (t > 0 && !in_cache) continue;
+                T* const dst = (T*)out.data + b * out.stride_b + h * out.stride_h + (t > 0 ? row : (int64_t)n) * out.stride_n;
+                vec xo, yo;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    xo[e] = (T)u[e];
+                    yo[e] = (T)v[e];
+                }
+                *(vec*)(dst + lo) = xo;
+                *(vec*)(dst + hi) = yo;
+            }
+        }
+    }
+}
+
+template <typename T>
+static hipError_t launch_append_type(AppendParams a, bool eight, hipStream_t stream) {
+    RotaryParams& p = a.p;
+    p.items = p.items / (2 * Vec16<T>::n);   // (came as head_dim)
+    p.fd_items = make_fastdiv((uint32_t)p.items);
+    p.fd_tokens = make_fastdiv((uint32_t)p.n_tokens);
+    const int64_t tokens = (int64_t)p.batch * p.n_tokens, per_block = 256 / p.items, blocks = (tokens + per_block - 1) / per_block;
+    const int heads = p.heads[0] + p.heads[1] + p.heads[2];
+    p.head_chunk = head_chunk(blocks, heads);
+    const dim3 grid((unsigned)blocks, (unsigned)((heads + p.head_chunk - 1) / p.head_chunk));
+    if (p.axes > 1) {
+        if (eight) hipLaunchKernelGGL((cache_append_kernel<T, true, true>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((cache_append_kernel<T, true, false>), grid, dim3(256), 0, stream, a);
+    } else {
+        if (eight) hipLaunchKernelGGL((cache_append_kernel<T, false, true>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((cache_append_kernel<T, false, false>), grid, dim3(256), 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_append(const AppendParams& a, grat_dtype dtype, bool eight, hipStream_t stream) {
+    if (dtype == GRAT_BF16) return launch_append_type<__bf16>(a, eight, stream);
+    if (dtype == GRAT_F16) return launch_append_type<_Float16>(a, eight, stream);
+    return launch_append_type<float>(a, eight, stream);
+}
+
+// 16 numbers of a row a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void cache_read_kernel(ReadParams p) {
+    constexpr int V = Vec16<T>::n;
+    typedef typename Vec16<T>::type vec;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= p.pieces) return;
+    uint32_t row, piece, bh, n, b, h;
+    fdivmod((uint32_t)at, p.fd_items, row, piece);
+    fdivmod(row, p.fd_rows, bh, n);
+    fdivmod(bh, p.fd_heads, b, h);
+    T* const dst = (T*)p.out.data + b * p.out.stride_b + h * p.out.stride_h + n * p.out.stride_n + 16 * piece;
+    float x[16];
+    if (!p.k_len || (int)n < p.k_len[b]) {
+        const uint4 raw = *(const uint4*)(p.cache.data + b * p.cache.stride_b + h * p.cache.stride_h + n * p.cache.stride_n + 16 * piece);
+        const float s = ((const float*)p.scale.data)[b * p.scale.stride_b + h * p.scale.stride_h + n * p.scale.stride_n];
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 u = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), v = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
+            x[4 * i] = u[0] * s;
+            x[4 * i + 1] = u[1] * s;
+            x[4 * i + 2] = v[0] * s;
+            x[4 * i + 3] = v[1] * s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i += V) {
+        vec o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = (T)x[i + e];
+        *(vec*)(dst + i) = o;
+    }
+}
+
+hipError_t launch_cache_read(const ReadParams& p, grat_dtype dtype, hipStream_t stream) {
+    const dim3 grid((unsigned)((p.pieces + 255) / 256));
+    if (dtype == GRAT_BF16) hipLaunchKernelGGL((cache_read_kernel<__bf16>), grid, dim3(256), 0, stream, p);
+    else if (dtype == GRAT_F16) hipLaunchKernelGGL((cache_read_kernel<_Float16>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((cache_read_kernel<float>), grid, dim3(256), 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace grat

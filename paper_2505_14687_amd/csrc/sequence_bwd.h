@@ -44,7 +44,7 @@ __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 template <bool WINDOW>
 struct alignas(16) RowMeta {
     float lse2[64], delta[64];
-    int32_t limit[64], lo[WINDOW ? 64 : 0];   // keys seen: below limit, from lo on (windows)
+    int32_t limit[64], lo[WINDOW ? 64 : 1];   // keys seen: below limit, from lo on (windows)
     const uint8_t* q[64];
     const uint8_t* d[64];
     int32_t masked;   // some row does not see all keys of the tile

@@ -9,44 +9,9 @@
 // 3.8 of them the kernel's.
 #include <algorithm>
 
-#include "sequence_common.h"
+#include "rotary_pairs.h"
 
 namespace grat {
-
-template <typename T, bool AXES>
-__device__ __forceinline__ void pair_angles(const RotaryParams& p, int b, int n, int pair0, float* cs, float* sn) {
-    constexpr int V = Vec16<T>::n;
-    const float2* const table = (const float2*)p.table;
-    const int pairs = p.rot / 2;
-    auto row = [&](int pos) { return (int64_t)min(max(pos, 0), p.n_pos - 1) * pairs; };
-    if constexpr (AXES) {
-        const int32_t* at = p.positions + b * p.positions_stride_b + (int64_t)n * p.axes;
-        int64_t r[3];
-#pragma unroll
-        for (int a = 0; a < 3; ++a) r[a] = row(at[min(a, p.axes - 1)]);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const int pair = pair0 + e;
-            const float2 v = table[(pair < p.axis_end[0] ? r[0] : pair < p.axis_end[1] ? r[1] : r[2]) + pair];
-            cs[e] = v.x;
-            sn[e] = p.inverse ? -v.y : v.y;
-        }
-    } else {
-        // (start + n may leave 32 bits; what does is far outside the table either way)
-        const int64_t pos = p.positions ? (int64_t)p.positions[b * p.positions_stride_b + n] : (int64_t)(p.start ? p.start[b] : 0) + n;
-        const float4* src = (const float4*)(table + row((int)min((int64_t)p.n_pos, pos)) + pair0);   // (rows are whole 16-byte vectors)
-#pragma unroll
-        for (int e = 0; e < V; e += 2) {
-            const float4 v = src[e / 2];
-            cs[e] = v.x;
-            sn[e] = p.inverse ? -v.y : v.y;
-            cs[e + 1] = v.z;
-            sn[e + 1] = p.inverse ? -v.w : v.w;
-        }
-    }
-}
-
-constexpr int kHeads = 4;   // in flight at a time
 
 template <typename T, bool AXES>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
@@ -133,10 +98,9 @@ static hipError_t launch_rotary_type(RotaryParams p, hipStream_t stream) {
     const int64_t tokens = (int64_t)p.batch * p.n_tokens, per_block = 256 / p.items;
     const int64_t blocks = (tokens + per_block - 1) / per_block;
     const int heads = p.heads[0] + p.heads[1] + p.heads[2];
-    // Heads of a thread, which share its cos and sin: multiples of kHeads, as many as leave the chip 4 096 workgroups.  (One head a thread: 115 200
-    // tokens of 48 heads on a grid 761 us against 567; 8 191 tokens of 40 heads 66.6 against 65.8; a token each of 32 sequences 5.4 both ways.)
-    const int64_t want = std::max<int64_t>(1, blocks * heads / 4096);
-    p.head_chunk = (int)std::min<int64_t>(heads, (want + kHeads - 1) / kHeads * kHeads);
+    // (One head a thread: 115 200 tokens of 48 heads on a grid 761 us against 567; 8 191 tokens of 40 heads 66.6 against 65.8; a token each of 32
+    // sequences 5.4 both ways.)
+    p.head_chunk = head_chunk(blocks, heads);
     const dim3 grid((unsigned)blocks, (unsigned)((heads + p.head_chunk - 1) / p.head_chunk));
     if (p.axes > 1) hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(256), 0, stream, p);

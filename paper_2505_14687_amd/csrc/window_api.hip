@@ -1,10 +1,11 @@
-// Host side of attention within a window: argument validation and dispatch.  No allocation, no synchronisation.
+// Host side of attention within a window and over caches: argument validation and dispatch.  No allocation, no synchronisation.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
 
+#include "cache_attn.h"
+#include "cache_rows.h"
 #include "grat_window.h"
-#include "sequence_attn.h"
 #include "sequence_checks.h"
 
 namespace grat {
@@ -132,6 +133,87 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t window, int
     return GRAT_OK;
 }
 
+// ---- caches --------------------------------------------------------------------------------------
+// Rows in 8 bits, and their scales.
+grat_status check_eight(const grat_tensor* t, int32_t head_dim) {
+    if (!t || !t->data) return GRAT_ERR_NULL;
+    if (t->stride_n < head_dim || t->stride_b < 0 || t->stride_h < 0) return GRAT_ERR_BAD_DIMS;
+    if (t->stride_n % 16 || t->stride_b % 16 || t->stride_h % 16 || !aligned16(t->data)) return GRAT_ERR_UNSUPPORTED;
+    if (t->stride_n >= ((int64_t)1 << 24) || t->stride_b >= ((int64_t)1 << 46) || t->stride_h >= ((int64_t)1 << 46)) return GRAT_ERR_UNSUPPORTED;
+    return GRAT_OK;
+}
+grat_status check_scale(const grat_tensor* t) {
+    if (!t || !t->data) return GRAT_ERR_NULL;
+    if (t->stride_n < 1 || t->stride_b < 0 || t->stride_h < 0) return GRAT_ERR_BAD_DIMS;
+    if ((uintptr_t)t->data & 3) return GRAT_ERR_UNSUPPORTED;
+    if (t->stride_n >= ((int64_t)1 << 24) || t->stride_b >= ((int64_t)1 << 46) || t->stride_h >= ((int64_t)1 << 46)) return GRAT_ERR_UNSUPPORTED;
+    return GRAT_OK;
+}
+grat_status not_repeated(const grat_tensor* t, int32_t batch, int32_t heads) {   // what is written to
+    return (batch > 1 && t->stride_b == 0) || (heads > 1 && t->stride_h == 0) ? GRAT_ERR_BAD_DIMS : GRAT_OK;
+}
+// A cache of either kind.
+grat_status check_cache(const grat_tensor* t, const grat_tensor* scale, grat_dtype dtype, int32_t head_dim) {
+    if (!scale) return check_tensor(t, dtype, head_dim);
+    const grat_status st = check_eight(t, head_dim);
+    return st == GRAT_OK ? check_scale(scale) : st;
+}
+
+struct CachePlan {
+    CacheParams c{};
+    int sets = 1;
+    int64_t work = 0;
+};
+
+// One group: the rows of all heads that share a K/V head, 16, 32 or 64 a workgroup.
+void set_cache(CachePlan& plan, int32_t head_dim, bool eight, void* work) {
+    SelParams& p = plan.c.p;
+    SeqShape& s = p.s;
+    const int64_t rows = (int64_t)s.n_q * s.share;
+    plan.sets = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const int tile_rows = 16 * plan.sets, keys = eight ? 64 : 32;
+    s.q_group = s.n_q;
+    s.n_groups = 1;
+    p.rows = (int32_t)rows;
+    p.row_tiles = (p.rows + tile_rows - 1) / tile_rows;
+    p.fd_row_tiles = make_fastdiv((uint32_t)p.row_tiles);
+    p.fd_groups = make_fastdiv(1);
+    p.fd_kv_heads = make_fastdiv((uint32_t)s.kv_heads);
+    p.fd_q_group = make_fastdiv((uint32_t)s.q_group);
+    p.fd_units = make_fastdiv(1);
+    const int64_t items = (int64_t)s.batch * s.kv_heads * p.row_tiles;
+    const int64_t units = (reach(p, std::min<int64_t>(s.n_q, tile_rows), s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys, steps = (units + 3) / 4;
+    set_items(p, items, steps < 8 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(256 / items, steps / 2), 64)));
+    Scratch scratch{(uint8_t*)work};
+    if (p.splits > 1) {
+        p.part_o = scratch.take<float>((int64_t)p.items * tile_rows * head_dim);
+        p.part_ml = scratch.take<float>((int64_t)p.items * tile_rows * 2);
+    }
+    plan.work = scratch.bytes;
+}
+
+grat_status make_cache_plan(const grat_sequence* seq, float scale, int32_t window, int32_t sinks, bool eight, bool tree, void* work, CachePlan* out) {
+    CachePlan plan;
+    SelParams& p = plan.c.p;
+    grat_status st = make_shape(seq, &p.s);
+    if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
+    if (st != GRAT_OK) return st;
+    if (tree && p.s.n_q > kMostDrafted) return GRAT_ERR_UNSUPPORTED;
+    p.s.causal = 1;
+    p.s.q_pos = nullptr;
+    set_cache(plan, seq->head_dim, eight, work);
+    if ((int64_t)p.s.batch * p.s.kv_heads * p.row_tiles >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+    *out = plan;
+    return GRAT_OK;
+}
+
+grat_status launch_cache(const CachePlan& plan, const grat_sequence* seq, bool eight, void* hip_stream) {
+    const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
+    const auto launch = f16 ? (wide ? launch_cache_attention_f16_d128 : launch_cache_attention_f16_d64)
+                            : (wide ? launch_cache_attention_bf16_d128 : launch_cache_attention_bf16_d64);
+    return status_of(launch(plan.c, eight, plan.sets, (hipStream_t)hip_stream));
+}
+
 }  // namespace
 }  // namespace grat
 
@@ -195,4 +277,115 @@ extern "C" grat_status grat_window_attention_bwd(const grat_sequence* seq, const
     const auto launch = f16 ? (wide ? launch_window_bwd_f16_d128 : launch_window_bwd_f16_d64)
                             : (wide ? launch_window_bwd_bf16_d128 : launch_window_bwd_bf16_d64);
     return status_of(launch(p, g, plan.tile_rows, (hipStream_t)hip_stream));
+}
+
+extern "C" grat_status grat_cache_append(const grat_rotary_args* args, const grat_tensor* Q, const grat_tensor* Q_out, const grat_tensor* K,
+                                         const grat_tensor* V, const grat_tensor* K_cache, const grat_tensor* V_cache, const grat_tensor* K_scale,
+                                         const grat_tensor* V_scale, int32_t n_cache, void* hip_stream) {
+    if (!args) return GRAT_ERR_NULL;
+    grat_rotary_args r = *args;
+    const bool with_q = Q || Q_out, eight = K_scale || V_scale;
+    if (!with_q) r.q_heads = 1;   // (what is not read)
+    if (!r.d_table) {
+        r.rot = 16;
+        r.axes = 1;
+        r.axis_pairs[0] = 8;
+        r.n_pos = 1;
+        r.d_positions = nullptr;
+        r.d_table = (const float*)16;
+    }
+    AppendParams a{};
+    RotaryParams& p = a.p;
+    grat_status st = make_rotary(&r, true, &p);
+    if (st != GRAT_OK) return st;
+    if (!args->d_table) {
+        p.rot = 0;
+        p.table = nullptr;
+    }
+    if (r.head_dim != 64 && r.head_dim != 128) return GRAT_ERR_UNSUPPORTED;
+    if (!r.d_start) return GRAT_ERR_NULL;
+    if (n_cache < 1 || r.inverse) return GRAT_ERR_BAD_DIMS;
+    if (n_cache >= kMaxRows) return GRAT_ERR_UNSUPPORTED;
+    if (with_q) {
+        st = check_tensor(Q, r.dtype, r.head_dim);
+        if (st == GRAT_OK) st = check_output(Q_out, r.dtype, r.head_dim, r.batch, r.q_heads);
+    }
+    for (const grat_tensor* t : {K, V})
+        if (st == GRAT_OK) st = check_tensor(t, r.dtype, r.head_dim);
+    const grat_tensor *const caches[2] = {K_cache, V_cache}, *const scales[2] = {K_scale, V_scale};
+    for (int i = 0; i < 2 && st == GRAT_OK; ++i) {
+        if (eight && !scales[i]) return GRAT_ERR_NULL;
+        st = check_cache(caches[i], scales[i], r.dtype, r.head_dim);
+        if (st == GRAT_OK) st = not_repeated(caches[i], r.batch, r.kv_heads);
+        if (st == GRAT_OK && eight) st = not_repeated(scales[i], r.batch, r.kv_heads);
+    }
+    if (st != GRAT_OK) return st;
+    if (with_q) {
+        p.in[0] = of(Q);
+        p.out[0] = of(Q_out);
+    } else {
+        p.heads[0] = 0;
+    }
+    p.in[1] = of(K);
+    p.in[2] = of(V);
+    p.out[1] = of(K_cache);
+    p.out[2] = of(V_cache);
+    p.heads[2] = p.heads[1];
+    p.n_cache = n_cache;
+    if (eight) {
+        a.k_scale = of(K_scale);
+        a.v_scale = of(V_scale);
+    }
+    return status_of(launch_cache_append(a, r.dtype, eight, (hipStream_t)hip_stream));
+}
+
+extern "C" grat_status grat_cache_read(grat_dtype dtype, int32_t batch, int32_t heads, int32_t n_rows, int32_t head_dim, const grat_tensor* cache,
+                                       const grat_tensor* scale, const int32_t* d_k_len, const grat_tensor* out, void* hip_stream) {
+    if (batch < 1 || heads < 1 || n_rows < 1) return GRAT_ERR_BAD_DIMS;
+    if (!known(dtype) || (head_dim != 64 && head_dim != 128)) return GRAT_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)batch * heads * n_rows;
+    if ((int64_t)batch * heads > 65535 || n_rows >= kMaxRows || rows >= kMaxRows / 4) return GRAT_ERR_UNSUPPORTED;
+    if (!scale) return GRAT_ERR_NULL;
+    grat_status st = check_cache(cache, scale, dtype, head_dim);
+    if (st == GRAT_OK) st = check_output(out, dtype, head_dim, batch, heads);
+    if (st != GRAT_OK) return st;
+    const ReadParams p{of(cache), of(scale), of(out), d_k_len, rows * (head_dim / 16), make_fastdiv((uint32_t)head_dim / 16), make_fastdiv((uint32_t)n_rows),
+                       make_fastdiv((uint32_t)heads)};
+    return status_of(launch_cache_read(p, dtype, (hipStream_t)hip_stream));
+}
+
+extern "C" int64_t grat_cache_attention_work(const grat_sequence* seq, int32_t window, int32_t sinks, int32_t eight) {
+    CachePlan plan;
+    return make_cache_plan(seq, 1.f, window, sinks, eight != 0, false, nullptr, &plan) == GRAT_OK ? plan.work : 0;
+}
+
+extern "C" grat_status grat_cache_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K_cache, const grat_tensor* V_cache,
+                                                const grat_tensor* K_scale, const grat_tensor* V_scale, const grat_tensor* O, float* d_lse, float scale,
+                                                int32_t window, int32_t sinks, const int32_t* d_parent, int64_t parent_stride_b, void* d_work,
+                                                void* hip_stream) {
+    CachePlan plan;
+    const bool eight = K_scale || V_scale;
+    grat_status st = make_cache_plan(seq, scale, window, sinks, eight, d_parent != nullptr, d_work, &plan);
+    if (st == GRAT_OK) st = check_tensor(Q, seq->dtype, seq->head_dim);
+    if (st == GRAT_OK && eight && (!K_scale || !V_scale)) st = GRAT_ERR_NULL;
+    if (st == GRAT_OK) st = check_cache(K_cache, K_scale, seq->dtype, seq->head_dim);
+    if (st == GRAT_OK) st = check_cache(V_cache, V_scale, seq->dtype, seq->head_dim);
+    if (st == GRAT_OK) st = check_output(O, seq->dtype, seq->head_dim, seq->batch, seq->q_heads);
+    if (st == GRAT_OK && d_parent && parent_stride_b < 0) st = GRAT_ERR_BAD_DIMS;
+    if (st != GRAT_OK) return st;
+    if (plan.work > 0 && !d_work) return GRAT_ERR_NULL;
+    if (!aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;
+    CacheParams& c = plan.c;
+    c.p.Q = of(Q);
+    c.p.K = of(K_cache);
+    c.p.V = of(V_cache);
+    c.p.O = of(O);
+    c.p.lse = d_lse;
+    if (eight) {
+        c.k_scale = of(K_scale);
+        c.v_scale = of(V_scale);
+    }
+    c.parent = d_parent;
+    c.parent_stride_b = parent_stride_b;
+    return launch_cache(plan, seq, eight, hip_stream);
 }

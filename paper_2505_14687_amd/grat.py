@@ -31,8 +31,9 @@ EXPORTS = ("grat_block_list_shape", "grat_build_block_lists", "grat_validate_blo
            "grat_rotary_table", "grat_rotary", "grat_rotary_append", "grat_block_means", "grat_block_scores_work",
            "grat_block_scores", "grat_select_blocks", "grat_selected_attention_work", "grat_selected_attention_fwd",
            "grat_selected_attention_bwd",
-           # attention within a window: window.py
-           "grat_window_attention_work", "grat_window_attention_fwd", "grat_window_attention_bwd")
+           # attention within a window and over caches: window.py
+           "grat_window_attention_work", "grat_window_attention_fwd", "grat_window_attention_bwd", "grat_cache_append", "grat_cache_read",
+           "grat_cache_attention_work", "grat_cache_attention_fwd")
 
 _i32, _i64, _f32, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
 _pi32 = ctypes.POINTER(ctypes.c_int32)
