@@ -15,27 +15,21 @@
 
 namespace grat {
 
-constexpr int kMostDrafted = 256, kTreeWords = 10;   // tokens of a tree; words of a token's line of ancestors, the last two 0
+hipError_t launch_cache_attention_bf16_d128(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
+hipError_t launch_cache_attention_bf16_d64(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
+hipError_t launch_cache_attention_f16_d128(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
+hipError_t launch_cache_attention_f16_d64(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
 
-struct CacheParams {
-    SelParams p;                 // one group: q_group = n_q, rows = n_q * share
-    SeqTensor k_scale, v_scale;  // float; 8 bits
-    const int32_t* parent;       // of a tree, or null
-    int64_t parent_stride_b;
-};
-
-hipError_t launch_cache_attention_bf16_d128(const CacheParams& c, bool eight, int sets, hipStream_t stream);
-hipError_t launch_cache_attention_bf16_d64(const CacheParams& c, bool eight, int sets, hipStream_t stream);
-hipError_t launch_cache_attention_f16_d128(const CacheParams& c, bool eight, int sets, hipStream_t stream);
-hipError_t launch_cache_attention_f16_d64(const CacheParams& c, bool eight, int sets, hipStream_t stream);
+// Keys of a unit.
+constexpr int cache_keys(bool eight, int sets) { return eight && sets < 4 ? 64 : 32; }
 
 // A wave's units of K and V, and its fragments in them.
-template <bool EIGHT, int D>
+template <bool EIGHT, int D, int KEYS>
 struct CacheWave {
-    static constexpr int kKeys = EIGHT ? 64 : 32, kRow = EIGHT ? D : 2 * D, kTile = kKeys * kRow, kChunks = kRow / 16, kRows = 1024 / kRow, kPieces = kTile / 1024;
+    static constexpr int kKeys = KEYS, kRow = EIGHT ? D : 2 * D, kTile = kKeys * kRow, kChunks = kRow / 16, kRows = 1024 / kRow, kPieces = kTile / 1024;
     static constexpr int kLoads = kPieces + (EIGHT ? 1 : 0);   // of a tile: its pieces and its scales
     static constexpr int kM = kKeys / 16, kN = D / 32, kDims = D / 16;
-    static constexpr int kBytes = 2 * kTile + (EIGHT ? 2 * kKeys * 4 : 0);   // K, V, their scales
+    static constexpr int kBytes = 2 * kTile + (EIGHT ? 512 : 0);   // K, V, their scales
     // Chunk c of a row lies at c ^ swizzle(row).  8 bits: ds_read_b128 of 16 consecutive rows, and the transpose read's rows 4 g + e, 16 + 4 g + e of
     // two neighbouring g, fall on the 16 chunk positions of a 256-byte line.
     static __device__ __forceinline__ int swizzle(int row) {
@@ -49,20 +43,19 @@ struct CacheWave {
     int first_end, near_end;     // keys are read below these: the first ones, the others
     int lane;
     uint32_t row_at, col_at;
-    __device__ __forceinline__ CacheWave(const CacheParams& c, const Item& it, uint8_t* lds_, int first_end_, int near_end_, int lane_)
+    __device__ __forceinline__ CacheWave(const SelParams& p, const Item& it, uint8_t* lds_, int first_end_, int near_end_, int lane_)
         : lds(lds_), first_end(first_end_), near_end(near_end_), lane(lane_) {
         constexpr int kSize = EIGHT ? 1 : 2;
-        const SelParams& p = c.p;
         const int r = lane & 15, g = lane >> 4;
         K = p.K.data + kSize * (it.b * p.K.stride_b + it.h * p.K.stride_h);
         V = p.V.data + kSize * (it.b * p.V.stride_b + it.h * p.V.stride_h);
         pitch_k = kSize * p.K.stride_n;
         pitch_v = kSize * p.V.stride_n;
         if constexpr (EIGHT) {
-            ks = c.k_scale.data + 4 * (it.b * c.k_scale.stride_b + it.h * c.k_scale.stride_h);
-            vs = c.v_scale.data + 4 * (it.b * c.v_scale.stride_b + it.h * c.v_scale.stride_h);
-            pitch_ks = 4 * c.k_scale.stride_n;
-            pitch_vs = 4 * c.v_scale.stride_n;
+            ks = p.k_scale.data + 4 * (it.b * p.k_scale.stride_b + it.h * p.k_scale.stride_h);
+            vs = p.v_scale.data + 4 * (it.b * p.v_scale.stride_b + it.h * p.v_scale.stride_h);
+            pitch_ks = 4 * p.k_scale.stride_n;
+            pitch_vs = 4 * p.v_scale.stride_n;
         }
         const uint32_t base = (uint32_t)(uintptr_t)(LDS_PTR(uint8_t))lds;
         row_at = base + r * kRow + ((swizzle(r) ^ g) << 4);
@@ -84,7 +77,7 @@ struct CacheWave {
             const int row = k * kRows + lane / kChunks;
             load_lds(base, (uint32_t)min(row, left) * (uint32_t)pitch + (((lane % kChunks) ^ swizzle(row)) << 4), tile + k * 1024);
         }
-        if constexpr (EIGHT) load_lds_word(scale + (start + (int64_t)min(lane, left)) * scale_pitch, lds + 2 * kTile + which * kKeys * 4);
+        if constexpr (EIGHT) load_lds_word(scale + (start + (int64_t)min(lane, left)) * scale_pitch, lds + 2 * kTile + which * 256);
     }
     __device__ __forceinline__ void fetch_k(int start) const { fetch(K, pitch_k, ks, pitch_ks, start, 0); }
     __device__ __forceinline__ void fetch_v(int start) const { fetch(V, pitch_v, vs, pitch_vs, start, 1); }
@@ -94,7 +87,7 @@ struct CacheWave {
         asm volatile("" ::: "memory");
     }
     __device__ __forceinline__ f32x4 scale(int which, int m) const {   // of keys 16 m + 4 g ..
-        return *(const f32x4*)(lds + 2 * kTile + which * kKeys * 4 + (16 * m + 4 * (lane >> 4)) * 4);
+        return *(const f32x4*)(lds + 2 * kTile + which * 256 + (16 * m + 4 * (lane >> 4)) * 4);
     }
 };
 
@@ -111,45 +104,16 @@ __device__ __forceinline__ frag8 widen(uint2 x) {
     return __builtin_bit_cast(frag8, make_uint4(w[0], w[1], w[2], w[3]));
 }
 
-// The lower n bits, n from 0 to 32 (what is beyond is taken for the nearest).
-__device__ __forceinline__ uint32_t lower_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
-
-// A tree of drafted tokens: token t goes on from token parent[t], or from the newest committed token (-1, and whatever is not a token ahead of t).  Its key
-// lies in row base + t, its position is base + depth.  lines[t]: the tokens of its line, itself among them, that it sees.
-struct Tree {
-    int32_t parent[kMostDrafted], depth[kMostDrafted];
-    uint32_t lines[kMostDrafted * kTreeWords];
-};
-__device__ __forceinline__ void build_tree(Tree& tree, const CacheParams& c, int b, int64_t base) {   // ends with a barrier
-    const int n = c.p.s.n_q, t = (int)threadIdx.x;
-    if (t < n) {
-        const int up = c.parent[b * c.parent_stride_b + t];
-        tree.parent[t] = up >= 0 && up < t ? up : -1;
-        for (int w = 0; w < kTreeWords; ++w) tree.lines[t * kTreeWords + w] = 0;
-    }
-    __syncthreads();
-    if (t < n) {
-        int depth = 0;
-        for (int a = tree.parent[t]; a >= 0; a = tree.parent[a]) ++depth;   // (a parent lies ahead of its child: the walk ends)
-        tree.depth[t] = depth;
-        int at = depth;   // of the token that is looked at
-        for (int a = t; a >= 0; a = tree.parent[a], --at)
-            if (depth - at < c.p.window || base + at < c.p.sinks) tree.lines[t * kTreeWords + (a >> 5)] |= 1u << (a & 31);
-    }
-    __syncthreads();
-}
-
 template <int R, bool EIGHT, bool F16, int D, bool TREE>
-__global__ __launch_bounds__(256, R == 4 ? 1 : 2) void cache_attention_kernel(CacheParams c) {
+__global__ __launch_bounds__(256, R > (EIGHT ? 1 : 2) ? 1 : 2) void cache_attention_kernel(SelParams p) {
     using E = Elem<F16>;
-    using W = CacheWave<EIGHT, D>;
+    using W = CacheWave<EIGHT, D, cache_keys(EIGHT, R)>;
     using EV = Elem<F16 && !EIGHT>;   // of the weights and V
     using Out = NarrowWave<D>;
     constexpr int kLds = 4 * W::kBytes > 4 * 16 * D * 4 ? 4 * W::kBytes : 4 * 16 * D * 4;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds];
     __shared__ float s_m[4][16], s_l[4][16];
     __shared__ Tree tree[1];   // (of no size where nothing refers to it)
-    const SelParams& p = c.p;
     const Item it(p);
     if (it.idle(p)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
@@ -166,7 +130,7 @@ __global__ __launch_bounds__(256, R == 4 ? 1 : 2) void cache_attention_kernel(Ca
         for (int ks = 0; ks < W::kN; ++ks)   // 8 bits: 16 dims of K a lane and 64, as its reads have them
             qf[k][ks] = *(const frag8*)(src + (EIGHT ? 128 * (ks >> 1) + 32 * g + 16 * (ks & 1) : 64 * ks + 16 * g));
     }
-    if constexpr (TREE) build_tree(tree[0], c, it.b, base);
+    if constexpr (TREE) build_tree(tree[0], p, it.b, base);
 
     // what this lane's rows see, and what the workgroup's rows see together
     RowSpan span[R];
@@ -176,9 +140,8 @@ __global__ __launch_bounds__(256, R == 4 ? 1 : 2) void cache_attention_kernel(Ca
     for (int k = 0; k < R; ++k) {
         const GroupRow row(p, it.h, 0, it.tile * (16 * R) + 16 * k + r);
         if constexpr (TREE) {
-            const int committed = max(base, 0);
             line[k] = row.query * kTreeWords;
-            span[k] = RowSpan{min(p.sinks, committed), p.window == kNoWindow ? 0 : (int)max((int64_t)0, min((int64_t)committed, (int64_t)base + tree[0].depth[row.query] - p.window + 1)), committed};
+            span[k] = tree_span(p, tree[0], base, row.query);
         } else {
             span[k] = row_span(p, len, pos, row.query);
         }
@@ -218,15 +181,9 @@ __global__ __launch_bounds__(256, R == 4 ? 1 : 2) void cache_attention_kernel(Ca
     auto unit_start = [&](int i) { return u_first + i < first_units ? (u_first + i) * W::kKeys : near + (u_first + i - first_units) * W::kKeys; };
     // Bit j: row k sees key `start` + j.
     auto sees = [&](int k, bool first, int start) {
-        const int low = first ? 0 : span[k].lo, up = first ? span[k].first : span[k].hi;
-        uint32_t bits = lower_bits(up - start) & ~lower_bits(low - start);
+        uint32_t bits = range_bits(start, first ? 0 : span[k].lo, first ? span[k].first : span[k].hi);
         if constexpr (TREE) {
-            const int off = start - base;   // the drafted token of the unit's first key
-            if (!first && off > -32) {
-                const int w = min(max(off, 0) >> 5, kTreeWords - 2);
-                const uint64_t x = tree[0].lines[line[k] + w] | (uint64_t)tree[0].lines[line[k] + w + 1] << 32;
-                bits |= off < 0 ? (uint32_t)x << -off : (uint32_t)(x >> (off & 31));
-            }
+            if (!first) bits |= line_bits(tree[0].lines + line[k], start - base);
         }
         return bits;
     };
@@ -241,8 +198,9 @@ __global__ __launch_bounds__(256, R == 4 ? 1 : 2) void cache_attention_kernel(Ca
         m_ref[k] = -1e38f / fmaxf(cc, 1.f);   // (finite, so that a unit without a seen key weighs 0)
         l_run[k] = 0.f;
     }
-    const W w(c, it, lds + wave * W::kBytes, first_end, near_end, lane);
-    frag8 kf[W::kM * (EIGHT ? W::kN / 2 : W::kN)], vf[W::kDims];   // 8 bits: 16 numbers each
+    const W w(p, it, lds + wave * W::kBytes, first_end, near_end, lane);
+    frag8 kf[W::kM * (EIGHT ? W::kN / 2 : W::kN)], vf[EIGHT ? 1 : W::kDims];   // 8 bits: 16 numbers of K each
+    uint2 v_raw[EIGHT ? W::kDims : 1][W::kM / 2];
     f32x4 k_scale[W::kM], v_scale[W::kM];
     frag8 weights[R][W::kM / 2];
     auto take_k = [&]() {
@@ -265,8 +223,11 @@ __global__ __launch_bounds__(256, R == 4 ? 1 : 2) void cache_attention_kernel(Ca
             if constexpr (EIGHT) {
                 const uint32_t at = (w.col_at ^ (dt << 4)) + W::kTile;
                 const i32x2 lo = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_PTR(i32x2))(uintptr_t)at);
-                const i32x2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_PTR(i32x2))(uintptr_t)(at + 32 * W::kRow));
-                vf[dt] = __builtin_bit_cast(frag8, make_int4(lo[0], lo[1], hi[0], hi[1]));
+                v_raw[dt][0] = make_uint2((uint32_t)lo[0], (uint32_t)lo[1]);
+                if constexpr (W::kM == 4) {
+                    const i32x2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_PTR(i32x2))(uintptr_t)(at + 32 * W::kRow));
+                    v_raw[dt][W::kM / 2 - 1] = make_uint2((uint32_t)hi[0], (uint32_t)hi[1]);
+                }
             } else {
                 const uint32_t at = (w.col_at ^ (dt << 5)) + W::kTile;
                 const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(uintptr_t)at);
@@ -351,12 +312,11 @@ __global__ __launch_bounds__(256, R == 4 ? 1 : 2) void cache_attention_kernel(Ca
 #pragma unroll
         for (int dt = 0; dt < W::kDims; ++dt)
             if constexpr (EIGHT) {
-                const uint4 raw = __builtin_bit_cast(uint4, vf[dt]);
-                const frag8 x = widen<false>(make_uint2(raw.x, raw.y)), y = widen<false>(make_uint2(raw.z, raw.w));
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    oacc[k][dt] = EV::mfma16(x, weights[k][0], oacc[k][dt]);
-                    oacc[k][dt] = EV::mfma16(y, weights[k][W::kM / 2 - 1], oacc[k][dt]);
+                for (int h = 0; h < W::kM / 2; ++h) {
+                    const frag8 x = widen<false>(v_raw[dt][h]);
+#pragma unroll
+                    for (int k = 0; k < R; ++k) oacc[k][dt] = EV::mfma16(x, weights[k][h], oacc[k][dt]);
                 }
             } else {
 #pragma unroll
@@ -429,25 +389,29 @@ __global__ __launch_bounds__(256, R == 4 ? 1 : 2) void cache_attention_kernel(Ca
 }
 
 template <int R, bool EIGHT, bool F16, int D>
-inline void launch_cache_sets(const CacheParams& c, hipStream_t stream) {
-    const dim3 grid((unsigned)(8 * c.p.per_xcd));
-    if (c.parent) hipLaunchKernelGGL((cache_attention_kernel<R, EIGHT, F16, D, true>), grid, dim3(256), 0, stream, c);
-    else hipLaunchKernelGGL((cache_attention_kernel<R, EIGHT, F16, D, false>), grid, dim3(256), 0, stream, c);
+inline void launch_cache_sets(const SelParams& p, hipStream_t stream) {
+    const dim3 grid((unsigned)(8 * p.per_xcd));
+    if (p.parent) hipLaunchKernelGGL((cache_attention_kernel<R, EIGHT, F16, D, true>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((cache_attention_kernel<R, EIGHT, F16, D, false>), grid, dim3(256), 0, stream, p);
 }
 
-// sets: 1, 2 or 4, of 16 rows a workgroup
+// tile_rows: 16, 32, 64, or, with the kernels of prompts, 128 and 256
 template <bool F16, int D>
-inline hipError_t launch_cache_attention(const CacheParams& c, bool eight, int sets, hipStream_t stream) {
-    if (eight) {
-        if (sets == 1) launch_cache_sets<1, true, F16, D>(c, stream);
-        else if (sets == 2) launch_cache_sets<2, true, F16, D>(c, stream);
-        else launch_cache_sets<4, true, F16, D>(c, stream);
-    } else {
-        if (sets == 1) launch_cache_sets<1, false, F16, D>(c, stream);
-        else if (sets == 2) launch_cache_sets<2, false, F16, D>(c, stream);
-        else launch_cache_sets<4, false, F16, D>(c, stream);
+inline hipError_t launch_cache_attention(const SelParams& p, bool eight, int tile_rows, hipStream_t stream) {
+    if (tile_rows > 64) {
+        if (eight) return p.parent ? launch_cache_tiles<F16, D, kTree, true>(p, tile_rows, stream) : launch_cache_tiles<F16, D, kWindow, true>(p, tile_rows, stream);
+        return p.parent ? launch_cache_tiles<F16, D, kTree, false>(p, tile_rows, stream) : launch_cache_tiles<F16, D, kWindow, false>(p, tile_rows, stream);
     }
-    if (c.p.splits > 1) launch_join<F16, D>(c.p, 16 * sets, stream);
+    if (eight) {
+        if (tile_rows == 16) launch_cache_sets<1, true, F16, D>(p, stream);
+        else if (tile_rows == 32) launch_cache_sets<2, true, F16, D>(p, stream);
+        else launch_cache_sets<4, true, F16, D>(p, stream);
+    } else {
+        if (tile_rows == 16) launch_cache_sets<1, false, F16, D>(p, stream);
+        else if (tile_rows == 32) launch_cache_sets<2, false, F16, D>(p, stream);
+        else launch_cache_sets<4, false, F16, D>(p, stream);
+    }
+    if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
     return hipGetLastError();
 }
 

@@ -3,8 +3,8 @@
 
 namespace grat {
 
-hipError_t launch_cache_attention_bf16_d128(const CacheParams& c, bool eight, int sets, hipStream_t stream) {
-    return launch_cache_attention<false, 128>(c, eight, sets, stream);
+hipError_t launch_cache_attention_bf16_d128(const SelParams& p, bool eight, int tile_rows, hipStream_t stream) {
+    return launch_cache_attention<false, 128>(p, eight, tile_rows, stream);
 }
 
 }  // namespace grat

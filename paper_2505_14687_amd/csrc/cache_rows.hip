@@ -25,12 +25,23 @@ __device__ __forceinline__ int row_power(float most) {
     return max(e - (__builtin_amdgcn_frexp_mantf(most) > 0.875f ? 8 : 9), -126);
 }
 
+// The largest number of 4, 8 or 16 neighbouring lanes.
+__device__ __forceinline__ float row_max(float x, int lanes) {
+    auto with = [&](float y) { return fmaxf(x, y); };
+#define GRAT_DPP(x, control) __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), control, 0xf, 0xf, true))
+    x = with(GRAT_DPP(x, 0xb1));    // lane ^ 1
+    x = with(GRAT_DPP(x, 0x4e));    // lane ^ 2
+    if (lanes > 4) x = with(GRAT_DPP(x, 0x141));    // the other four of eight, in mirror order
+    if (lanes > 8) x = with(GRAT_DPP(x, 0x140));    // the other eight
+#undef GRAT_DPP
+    return x;
+}
+
 // Thread and piece as in rotary_kernel; the lanes of a row, `items` neighbours, find its largest number together.
 template <typename T, bool AXES, bool EIGHT>
-__global__ __launch_bounds__(256) void cache_append_kernel(AppendParams a) {
+__global__ __launch_bounds__(256) void cache_append_kernel(RotaryParams p, SeqTensor k_scale, SeqTensor v_scale) {
     typedef typename Vec16<T>::type vec;
     constexpr int V = Vec16<T>::n;
-    const RotaryParams& p = a.p;
     uint32_t slot, item, b, n;
     fdivmod(threadIdx.x, p.fd_items, slot, item);
     const uint32_t per_block = 256u / (uint32_t)p.items, token = blockIdx.x * per_block + slot;
@@ -49,21 +60,30 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendParams a) {
     const bool in_cache = row >= 0 && row < p.n_cache;
     for (int h0 = blockIdx.y * p.head_chunk, h1 = min(all, h0 + p.head_chunk); h0 < h1; h0 += kHeads) {
         vec x[kHeads], y[kHeads];
+        uint8_t* dst[kHeads];
+        float* scale[kHeads];   // of a row that is kept in 8 bits
+        int kind[kHeads];       // 0: Q, 1: K, 2: V
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) {
             int h = min(h0 + i, h1 - 1), t = 0;
             if (h >= p.heads[0]) { h -= p.heads[0]; t = 1; if (h >= p.heads[1]) { h -= p.heads[1]; t = 2; } }
-            const SeqTensor in = t == 0 ? p.in[0] : t == 1 ? p.in[1] : p.in[2];   // (uniform)
+            // (uniform; an index into the parameters would put them into scratch memory)
+            const SeqTensor in = t == 0 ? p.in[0] : t == 1 ? p.in[1] : p.in[2], out = t == 0 ? p.out[0] : t == 1 ? p.out[1] : p.out[2];
             const T* const src = (const T*)in.data + b * in.stride_b + h * in.stride_h + n * in.stride_n;
+            const bool keep = h0 + i < h1 && (t == 0 || in_cache);
+            const int64_t to = b * out.stride_b + h * out.stride_h + (t > 0 ? row : (int64_t)n) * out.stride_n;
+            dst[i] = keep ? out.data + to * (EIGHT && t > 0 ? 1 : (int)sizeof(T)) : nullptr;
+            kind[i] = t;
+            if constexpr (EIGHT) {
+                const SeqTensor sc = t == 1 ? k_scale : v_scale;
+                scale[i] = (float*)sc.data + b * sc.stride_b + h * sc.stride_h + row * sc.stride_n;
+            }
             x[i] = *(const vec*)(src + lo);
             y[i] = *(const vec*)(src + hi);
         }
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) {
-            if (h0 + i >= h1) break;
-            int h = h0 + i, t = 0;
-            if (h >= p.heads[0]) { h -= p.heads[0]; t = 1; if (h >= p.heads[1]) { h -= p.heads[1]; t = 2; } }
-            const SeqTensor out = t == 0 ? p.out[0] : t == 1 ? p.out[1] : p.out[2];
+            const int t = kind[i];
             float u[V], v[V];   // the piece's two vectors
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -71,22 +91,24 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendParams a) {
                 v[e] = (float)y[i][e];
             }
             if (turn && t < 2) {
+// (each product and sum rounded, as elementary operations would: what lies next to a border of the 8 bits then falls to the same side)
+#pragma clang fp contract(off)
                 if (p.interleaved) {
 #pragma unroll
                     for (int e = 0; e < V; e += 2) {
                         const int q = e / 2, q2 = V / 2 + e / 2;
                         const float f = u[e], c = u[e + 1], f2 = v[e], c2 = v[e + 1];
-                        u[e] = fmaf(cs[q], f, -(sn[q] * c));
-                        u[e + 1] = fmaf(sn[q], f, cs[q] * c);
-                        v[e] = fmaf(cs[q2], f2, -(sn[q2] * c2));
-                        v[e + 1] = fmaf(sn[q2], f2, cs[q2] * c2);
+                        u[e] = cs[q] * f - sn[q] * c;
+                        u[e + 1] = sn[q] * f + cs[q] * c;
+                        v[e] = cs[q2] * f2 - sn[q2] * c2;
+                        v[e + 1] = sn[q2] * f2 + cs[q2] * c2;
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         const float f = u[e], c = v[e];
-                        u[e] = fmaf(cs[e], f, -(sn[e] * c));
-                        v[e] = fmaf(sn[e], f, cs[e] * c);
+                        u[e] = cs[e] * f - sn[e] * c;
+                        v[e] = sn[e] * f + cs[e] * c;
                     }
                 }
             }
@@ -97,37 +119,34 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendParams a) {
                     const float f = fabsf(u[e]), c = fabsf(v[e]);
                     most = fmaxf(most, fmaxf(f < INFINITY ? f : 0.f, c < INFINITY ? c : 0.f));
                 }
-                for (int m = 1; m < p.items; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+                most = row_max(most, p.items);
                 const int power = row_power(most);
                 const float inv = ldexpf(1.f, -power);
-                if (!in_cache) continue;
-                uint8_t* const dst = out.data + b * out.stride_b + h * out.stride_h + row * out.stride_n;
                 uint32_t wu[V / 4], wv[V / 4];
 #pragma unroll
                 for (int k = 0; k < V / 4; ++k) {
                     wu[k] = narrow(u[4 * k] * inv, u[4 * k + 1] * inv, u[4 * k + 2] * inv, u[4 * k + 3] * inv);
                     wv[k] = narrow(v[4 * k] * inv, v[4 * k + 1] * inv, v[4 * k + 2] * inv, v[4 * k + 3] * inv);
                 }
-                if constexpr (V == 8) {
-                    *(uint2*)(dst + lo) = make_uint2(wu[0], wu[1]);
-                    *(uint2*)(dst + hi) = make_uint2(wv[0], wv[1]);
-                } else {
-                    *(uint32_t*)(dst + lo) = wu[0];
-                    *(uint32_t*)(dst + hi) = wv[0];
+                if (dst[i]) {
+                    if constexpr (V == 8) {
+                        *(uint2*)(dst[i] + lo) = make_uint2(wu[0], wu[1]);
+                        *(uint2*)(dst[i] + hi) = make_uint2(wv[0], wv[1]);
+                    } else {
+                        *(uint32_t*)(dst[i] + lo) = wu[0];
+                        *(uint32_t*)(dst[i] + hi) = wv[0];
+                    }
+                    if (item == 0) *scale[i] = ldexpf(1.f, power);
                 }
-                const SeqTensor& to = t == 1 ? a.k_scale : a.v_scale;
-                if (item == 0) ((float*)to.data)[b * to.stride_b + h * to.stride_h + row * to.stride_n] = ldexpf(1.f, power);
-            } else {
-                if (t > 0 && !in_cache) continue;
-                T* const dst = (T*)out.data + b * out.stride_b + h * out.stride_h + (t > 0 ? row : (int64_t)n) * out.stride_n;
+            } else if (dst[i]) {
                 vec xo, yo;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     xo[e] = (T)u[e];
                     yo[e] = (T)v[e];
                 }
-                *(vec*)(dst + lo) = xo;
-                *(vec*)(dst + hi) = yo;
+                *(vec*)((T*)dst[i] + lo) = xo;
+                *(vec*)((T*)dst[i] + hi) = yo;
             }
         }
     }
@@ -144,11 +163,11 @@ static hipError_t launch_append_type(AppendParams a, bool eight, hipStream_t str
     p.head_chunk = head_chunk(blocks, heads);
     const dim3 grid((unsigned)blocks, (unsigned)((heads + p.head_chunk - 1) / p.head_chunk));
     if (p.axes > 1) {
-        if (eight) hipLaunchKernelGGL((cache_append_kernel<T, true, true>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((cache_append_kernel<T, true, false>), grid, dim3(256), 0, stream, a);
+        if (eight) hipLaunchKernelGGL((cache_append_kernel<T, true, true>), grid, dim3(256), 0, stream, p, a.k_scale, a.v_scale);
+        else hipLaunchKernelGGL((cache_append_kernel<T, true, false>), grid, dim3(256), 0, stream, p, a.k_scale, a.v_scale);
     } else {
-        if (eight) hipLaunchKernelGGL((cache_append_kernel<T, false, true>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((cache_append_kernel<T, false, false>), grid, dim3(256), 0, stream, a);
+        if (eight) hipLaunchKernelGGL((cache_append_kernel<T, false, true>), grid, dim3(256), 0, stream, p, a.k_scale, a.v_scale);
+        else hipLaunchKernelGGL((cache_append_kernel<T, false, false>), grid, dim3(256), 0, stream, p, a.k_scale, a.v_scale);
     }
     return hipGetLastError();
 }

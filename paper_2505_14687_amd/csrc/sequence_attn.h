@@ -28,6 +28,9 @@ struct SelParams {
     float* part_o;                // splits > 1: [items][rows of a tile][D], with part_ml [items][rows of a tile][2]
     float* part_ml;
     int32_t window, sinks;        // attention within a window: no lists, q_group is the launch's own
+    SeqTensor k_scale, v_scale;   // K and V in 8 bits: a float a row
+    const int32_t* parent;        // drafted tokens, or null
+    int64_t parent_stride_b;
 };
 constexpr int32_t kNoWindow = 0x7fffffff;
 
@@ -246,22 +249,74 @@ struct WindowUnits {
     int first_end, first_units, near, near_end, n;
     __device__ __forceinline__ WindowUnits(const SelParams& p, int len, int64_t pos, int i0, int i1) {
         const RowSpan a = row_span(p, len, pos, i0), z = row_span(p, len, pos, i1);
-        first_end = z.first;
+        set(z.first, a.lo, z.hi);
+    }
+    // ... of a tree: its first token is one that goes on from a committed one, and no other sees more of these.
+    __device__ __forceinline__ WindowUnits(const SelParams& p, int len) {
+        const int base = len - p.s.n_q, committed = max(base, 0);
+        set(min(p.sinks, committed), p.window == kNoWindow ? 0 : max(0, min(committed, base - p.window + 1)), len);
+    }
+    __device__ __forceinline__ void set(int first, int lo, int hi) {   // (the same in all lanes, which what it is computed from does not always say)
+        first_end = __builtin_amdgcn_readfirstlane(first);
         first_units = (first_end + kUnit - 1) / kUnit;
-        near = max(a.lo, first_end);
-        near_end = z.hi;
+        near_end = __builtin_amdgcn_readfirstlane(hi);
+        near = max(__builtin_amdgcn_readfirstlane(lo), first_end);
         n = first_units + (max(near_end - near, 0) + kUnit - 1) / kUnit;
     }
     __device__ __forceinline__ int start(int i) const { return i < first_units ? i * kUnit : near + (i - first_units) * kUnit; }
 };
 
-// What a lane's row does not see of a unit, of 32 rows a wave.
-template <bool WINDOW>
+// A tree of drafted tokens: token t goes on from token parent[t], or from the newest committed token (-1, and whatever is not a token ahead of t).  Its key
+// lies in row base + t, its position is base + depth.  lines[t]: the tokens of its line, itself among them, that it sees.
+constexpr int kMostDrafted = 256, kTreeWords = 10;   // tokens of a tree; words of a line, the last two 0
+struct Tree {
+    int32_t parent[kMostDrafted], depth[kMostDrafted];
+    uint32_t lines[kMostDrafted * kTreeWords];
+};
+__device__ __forceinline__ void build_tree(Tree& tree, const SelParams& p, int b, int base) {   // by at least kMostDrafted threads; ends with a barrier
+    const int n = p.s.n_q, t = (int)threadIdx.x;
+    if (t < n) {
+        const int up = p.parent[b * p.parent_stride_b + t];
+        tree.parent[t] = up >= 0 && up < t ? up : -1;
+        for (int w = 0; w < kTreeWords; ++w) tree.lines[t * kTreeWords + w] = 0;
+    }
+    __syncthreads();
+    if (t < n) {
+        int depth = 0;
+        for (int a = tree.parent[t]; a >= 0; a = tree.parent[a]) ++depth;   // (a parent lies ahead of its child: the walk ends)
+        tree.depth[t] = depth;
+        int at = depth;   // of the token that is looked at
+        for (int a = t; a >= 0; a = tree.parent[a], --at)
+            if (depth - at < p.window || base + at < p.sinks) tree.lines[t * kTreeWords + (a >> 5)] |= 1u << (a & 31);
+    }
+    __syncthreads();
+}
+// What a drafted token sees of the committed ones, with hi their number.
+__device__ __forceinline__ RowSpan tree_span(const SelParams& p, const Tree& tree, int base, int t) {
+    const int committed = max(base, 0);
+    const int64_t lo = (int64_t)base + tree.depth[t] - p.window + 1;
+    return RowSpan{min(p.sinks, committed), p.window == kNoWindow ? 0 : (int)max((int64_t)0, min((int64_t)committed, lo)), committed};
+}
+// The lower n bits, n from 0 to 32 (what is beyond is taken for the nearest).
+__device__ __forceinline__ uint32_t lower_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+// Bit k: key start + k lies in [low, up).
+__device__ __forceinline__ uint32_t range_bits(int start, int low, int up) { return lower_bits(up - start) & ~lower_bits(low - start); }
+// ... : is the key of a drafted token that a row with this line sees; off: the token of the first of them.
+__device__ __forceinline__ uint32_t line_bits(const uint32_t* line, int off) {
+    if (off <= -32) return 0;
+    const int w = min(max(off, 0) >> 5, kTreeWords - 2);
+    const uint64_t x = line[w] | (uint64_t)line[w + 1] << 32;
+    return off < 0 ? (uint32_t)x << -off : (uint32_t)(x >> (off & 31));
+}
+
+// What a lane's row does not see of a unit, of 32 rows a wave: of lists, of a window, of a tree.
+enum Walk { kLists = 0, kWindow = 1, kTree = 2 };
+template <int WALK>
 struct RowMask;
 template <>
-struct RowMask<false> {   // keys behind the row's own
+struct RowMask<kLists> {   // keys behind the row's own
     int limit, least, most;   // keys below it are seen; of the wave's rows
-    __device__ __forceinline__ RowMask(const SelParams& p, const GroupRow& row, const WindowUnits*, int len, int64_t pos) {
+    __device__ __forceinline__ RowMask(const SelParams& p, const GroupRow& row, const WindowUnits&, const Tree*, int len, int64_t pos) {
         limit = row.there ? row_seen(p.s, len, pos, row.query) : 0;
         least = row.there ? limit : 0x7fffffff;
         most = limit;
@@ -280,13 +335,17 @@ struct RowMask<false> {   // keys behind the row's own
     __device__ __forceinline__ bool hides(int start, int k) const { return start + k >= limit; }   // key k of the unit
 };
 template <>
-struct RowMask<true> {
+struct RowMask<kWindow> {
     RowSpan r;
     int first_end, least_first, least_hi, most_lo, least_lo, most;
-    __device__ __forceinline__ RowMask(const SelParams& p, const GroupRow& row, const WindowUnits* u, int len, int64_t pos) {
-        r = row_span(p, len, pos, row.query);
+    __device__ __forceinline__ RowMask() {}
+    __device__ __forceinline__ RowMask(const SelParams& p, const GroupRow& row, const WindowUnits& u, const Tree*, int len, int64_t pos) {
+        of(row, u, row_span(p, len, pos, row.query));
+    }
+    __device__ __forceinline__ void of(const GroupRow& row, const WindowUnits& u, RowSpan span) {
+        r = span;
         if (!row.there) r = RowSpan{0, 0, 0};
-        first_end = u->first_end;
+        first_end = u.first_end;
         least_first = row.there ? r.first : 0x7fffffff;
         least_hi = row.there ? r.hi : 0x7fffffff;
         least_lo = row.there ? r.lo : 0x7fffffff;
@@ -314,6 +373,26 @@ struct RowMask<true> {
         const bool first = start < first_end;
         const int low = first ? 0 : r.lo, width = first ? r.first : r.hi - r.lo;
         return (uint32_t)(start + k - low) >= (uint32_t)width;
+    }
+};
+
+template <>
+struct RowMask<kTree> : RowMask<kWindow> {   // the committed tokens as a window, and a line of drafted ones
+    const uint32_t* line;
+    int base;
+    bool there;
+    __device__ __forceinline__ RowMask(const SelParams& p, const GroupRow& row, const WindowUnits& u, const Tree* tree, int len, int64_t) {
+        base = len - p.s.n_q;
+        there = row.there;
+        line = tree->lines + row.query * kTreeWords;
+        of(row, u, tree_span(p, *tree, base, row.query));
+    }
+    __device__ __forceinline__ bool nothing() const { return __builtin_amdgcn_ballot_w64(there) == 0; }
+    __device__ __forceinline__ bool idle(int) const { return false; }
+    __device__ __forceinline__ uint32_t bits(int start) const {   // bit k: the row sees key k of the unit
+        const bool first = start < first_end;
+        const uint32_t drafted = line_bits(line, start - base);
+        return range_bits(start, first ? 0 : r.lo, first ? r.first : r.hi) | (first || !there ? 0 : drafted);
     }
 };
 
@@ -354,6 +433,71 @@ struct KeyLoader {
     __device__ __forceinline__ void issue(int start, uint8_t* k_tile, uint8_t* v_tile, int wave) const {
         issue(K, pitch_k, start, k_tile, wave);
         issue(V, pitch_v, start, v_tile, wave);
+    }
+};
+
+// The same of K and V in 8 bits, by way of registers: e4m3 values times their row's scale are rounded to the element type (scales that are powers of two leave
+// nothing to round; half saturates) and stored as the direct loads would have them.
+template <int NW, bool F16, int D>
+struct EightLoader {
+    static constexpr int kOwnRows = 64 / NW, kC = kOwnRows * (D / 16) / 64;   // rows of a wave; chunks of 16 numbers a lane
+    static_assert(kC >= 1, "");
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    struct Raw {
+        u32x4 x[kC];
+        float s[kC];
+    };
+    const uint8_t *K, *V, *ks, *vs;
+    int64_t pitch_k, pitch_v, pitch_ks, pitch_vs;   // bytes
+    int last, first_end, my_unit, first_row, chunk;
+    __device__ __forceinline__ EightLoader(const SelParams& p, const Item& it, int seen, int wave, int lane, int first_keys) {
+        K = p.K.data + it.b * p.K.stride_b + it.h * p.K.stride_h;
+        V = p.V.data + it.b * p.V.stride_b + it.h * p.V.stride_h;
+        ks = p.k_scale.data + 4 * (it.b * p.k_scale.stride_b + it.h * p.k_scale.stride_h);
+        vs = p.v_scale.data + 4 * (it.b * p.v_scale.stride_b + it.h * p.v_scale.stride_h);
+        pitch_k = p.K.stride_n;
+        pitch_v = p.V.stride_n;
+        pitch_ks = 4 * p.k_scale.stride_n;
+        pitch_vs = 4 * p.v_scale.stride_n;
+        last = seen - 1;
+        first_end = first_keys;
+        my_unit = wave * kOwnRows / kUnit;
+        first_row = wave * kOwnRows + lane / (D / 16);   // in the tile
+        chunk = lane % (D / 16);
+    }
+    __device__ __forceinline__ void issue(const uint8_t* head, int64_t pitch, const uint8_t* scales, int64_t scale_pitch, int start, Raw& raw) const {
+        const int left = (start < first_end ? first_end - 1 : last) - start;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            const int64_t row = start + min((first_row + c * (1024 / D)) & (kUnit - 1), left);
+            raw.x[c] = *(const u32x4*)(head + row * pitch + 16 * chunk);
+            raw.s[c] = *(const float*)(scales + row * scale_pitch);
+        }
+    }
+    __device__ __forceinline__ void issue_k(int start, Raw& raw) const { issue(K, pitch_k, ks, pitch_ks, start, raw); }
+    __device__ __forceinline__ void issue_v(int start, Raw& raw) const { issue(V, pitch_v, vs, pitch_vs, start, raw); }
+    __device__ __forceinline__ void store(const Raw& raw, uint8_t* tile) const {
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            const int row = first_row + c * (1024 / D);
+            uint8_t* const to = tile + row * 2 * D;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t word = raw.x[c][2 * j + (i >> 1)];
+                    const f32x2 v = i & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)word, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)word, false);
+                    float lo = v[0] * raw.s[c], hi = v[1] * raw.s[c];
+                    if constexpr (F16) {   // (NaN stays)
+                        lo = lo > 65504.f ? 65504.f : lo < -65504.f ? -65504.f : lo;
+                        hi = hi > 65504.f ? 65504.f : hi < -65504.f ? -65504.f : hi;
+                    }
+                    w[i] = Elem<F16>::pack(lo, hi);
+                }
+                *(uint4*)(to + (((2 * chunk + j) ^ tile_swizzle<D>(row)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
     }
 };
 

@@ -470,7 +470,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     const int i0 = it.g * s.q_group, i1 = min(i0 + s.q_group, s.n_q) - 1;
     const WindowUnits window(p, len, pos, i0, i1);
     const int seen = WINDOW ? window.near_end : group_seen(s, len, pos, it.g);
-    const RowMask<WINDOW> hidden(p, row, &window, len, pos);
+    const RowMask<WINDOW ? kWindow : kLists> hidden(p, row, window, nullptr, len, pos);
     const int n_units = WINDOW ? window.n : seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
     const int n_tiles = (n_units + 1) / 2;
     f32x16 dq[D / 32];

@@ -16,9 +16,11 @@
 
 namespace grat {
 
-template <int RW, int TEAMS, bool F16, int D, bool WINDOW>
+template <int RW, int TEAMS, bool F16, int D, int WALK, bool EIGHT>
 __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void selected_fwd_kernel(SelParams p) {
     using E = Elem<F16>;
+    constexpr bool WINDOW = WALK != kLists;
+    static_assert(!EIGHT || TEAMS == 1, "8 bits: many rows");
     constexpr int NW = RW * TEAMS, kTile = 64 * D * 2;
     __shared__ __attribute__((aligned(2 * kTile))) uint8_t lds[4][kTile];   // K, K, V, V
     __shared__ int32_t s_n;
@@ -39,10 +41,12 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const frag8*)(q_src + 32 * ks);
     const int len = seq_len(s, it.b);
     const int64_t pos = WINDOW ? window_pos(s, it.b, len) : seq_pos(s, it.b, len);
+    __shared__ Tree s_tree[1];   // (not there where nothing refers to it)
+    if constexpr (WALK == kTree) build_tree(s_tree[0], p, it.b, len - s.n_q);
     const int i0 = it.g * s.q_group, i1 = min(i0 + s.q_group, s.n_q) - 1;
-    const WindowUnits window(p, len, pos, i0, i1);
+    const WindowUnits window = WALK == kTree ? WindowUnits(p, len) : WindowUnits(p, len, pos, i0, i1);
     const int seen = WINDOW ? window.near_end : group_seen(s, len, pos, it.g);
-    const RowMask<WINDOW> hidden(p, row, &window, len, pos);
+    const RowMask<WALK> hidden(p, row, window, WALK == kTree ? s_tree : nullptr, len, pos);
 
     const int all_units = WINDOW ? window.n : seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
     int u_first = 0, n_units = all_units;
@@ -59,7 +63,8 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     float m_ref = -1e38f / fmaxf(c, 1.f);   // (finite, so that a block without a seen key weighs 0)
     float l_run = 0.f;
 
-    const KeyLoader<NW, D, WINDOW> load(p, it, seen, wave, lane, window.first_end);
+    using Loader = std::conditional_t<EIGHT, EightLoader<EIGHT ? NW : 4, F16, D>, KeyLoader<NW, D, WINDOW>>;
+    const Loader load(p, it, seen, wave, lane, window.first_end);
     TileReader<D> read(lane, lds[0], team);
     auto unit_at = [&](int i) { return WINDOW ? window.start(i) : __builtin_amdgcn_readfirstlane(s_units[i]); };
     // (a list's last tile may lack its second unit; one of a part that ends inside the list does not)
@@ -69,6 +74,12 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
 
     auto mask = [&](f32x16& S, int start) {
         if (hidden.cuts(start)) {
+            if constexpr (WALK == kTree) {
+                const uint32_t bits = hidden.bits(start) >> (4 * half);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) S[i] = bits >> (8 * (i >> 2) + (i & 3)) & 1 ? S[i] : -INFINITY;
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (hidden.hides(start, 8 * (i >> 2) + 4 * half + (i & 3))) S[i] = -INFINITY;
@@ -150,8 +161,14 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
             here = ahead;
             ahead = unit_load(2 * t + 2 + load.my_unit);
             tile_barrier();
-            if (t + 1 < n_tiles) load.issue(load.K, load.pitch_k, ahead, lds[kOdd ^ 1], wave);
-            if (kScores) load.issue(load.V, load.pitch_v, here, lds[2 + kOdd], wave);
+            std::conditional_t<EIGHT, typename EightLoader<EIGHT ? NW : 4, F16, D>::Raw, int> next_k, this_v;   // 8 bits: stored at the step's end
+            if constexpr (EIGHT) {
+                if (t + 1 < n_tiles) load.issue_k(ahead, next_k);
+                if (kScores) load.issue_v(here, this_v);
+            } else {
+                if (t + 1 < n_tiles) load.issue(load.K, load.pitch_k, ahead, lds[kOdd ^ 1], wave);
+                if (kScores) load.issue(load.V, load.pitch_v, here, lds[2 + kOdd], wave);
+            }
             frag8 fr[2 * kItems];
             auto fetch = [&](int i) {
                 const int h = i / kItems, j = i % kItems;
@@ -209,6 +226,10 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
                 }
             }
             late = start1;
+            if constexpr (EIGHT) {
+                if (t + 1 < n_tiles) load.store(next_k, lds[kOdd ^ 1]);
+                if (kScores) load.store(this_v, lds[2 + kOdd]);
+            }
         };
         using std::false_type;
         using std::true_type;
@@ -216,14 +237,32 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
         constexpr integral_constant<int, 0> even{};
         constexpr integral_constant<int, 1> odd{};
         if (n_tiles > 0) {
-            load.issue(load.K, load.pitch_k, ahead, lds[0], wave);
+            auto fetch_k = [&](int start, uint8_t* tile) {
+                if constexpr (EIGHT) {
+                    typename Loader::Raw raw;
+                    load.issue_k(start, raw);
+                    load.store(raw, tile);
+                } else {
+                    load.issue(load.K, load.pitch_k, start, tile, wave);
+                }
+            };
+            auto fetch_v = [&](int start, uint8_t* tile) {
+                if constexpr (EIGHT) {
+                    typename Loader::Raw raw;
+                    load.issue_v(start, raw);
+                    load.store(raw, tile);
+                } else {
+                    load.issue(load.V, load.pitch_v, start, tile, wave);
+                }
+            };
+            fetch_k(ahead, lds[0]);
             if (hidden.nothing()) {   // a wave without a row only fetches
                 for (int t = 0; t <= n_tiles; ++t) {
                     here = ahead;
                     ahead = unit_load(2 * t + 2 + load.my_unit);
                     tile_barrier();
-                    if (t + 1 < n_tiles) load.issue(load.K, load.pitch_k, ahead, lds[(t + 1) & 1], wave);
-                    if (t < n_tiles) load.issue(load.V, load.pitch_v, here, lds[2 + (t & 1)], wave);
+                    if (t + 1 < n_tiles) fetch_k(ahead, lds[(t + 1) & 1]);
+                    if (t < n_tiles) fetch_v(here, lds[2 + (t & 1)]);
                 }
             } else {
                 step(even, true_type{}, false_type{}, 0);
@@ -482,10 +521,10 @@ inline void launch_join(const SelParams& p, int tile_rows, hipStream_t stream) {
                        make_fastdiv((uint32_t)p.rows));
 }
 
-template <int RW, int TEAMS, bool F16, int D, bool WINDOW = false>
+template <int RW, int TEAMS, bool F16, int D, int WALK = kLists, bool EIGHT = false>
 inline void launch_fwd_tile(const SelParams& p, hipStream_t stream) {
-    const size_t dyn = WINDOW ? 0 : sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1);
-    hipLaunchKernelGGL((selected_fwd_kernel<RW, TEAMS, F16, D, WINDOW>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p);
+    const size_t dyn = WALK == kLists ? sizeof(int32_t) * ((size_t)p.max_blocks * p.fd_units.d + 1) : 0;
+    hipLaunchKernelGGL((selected_fwd_kernel<RW, TEAMS, F16, D, WALK, EIGHT>), dim3(8 * p.per_xcd), dim3(RW * TEAMS * 64), dyn, stream, p);
 }
 
 // tile_rows: 256 (head_dim 128), 128, 64, 32 or 16
@@ -508,11 +547,22 @@ inline hipError_t launch_fwd(const SelParams& p, int tile_rows, hipStream_t stre
 template <bool F16, int D>
 inline hipError_t launch_window(const SelParams& p, int tile_rows, hipStream_t stream) {
     if constexpr (D == 128) {
-        if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D, true>(p, stream);
+        if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D, kWindow>(p, stream);
     }
-    if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D, true>(p, stream);
-    else if (tile_rows == 64) launch_fwd_tile<2, 2, F16, D, true>(p, stream);
-    else if (tile_rows == 32) launch_fwd_tile<1, 2, F16, D, true>(p, stream);
+    if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D, kWindow>(p, stream);
+    else if (tile_rows == 64) launch_fwd_tile<2, 2, F16, D, kWindow>(p, stream);
+    else if (tile_rows == 32) launch_fwd_tile<1, 2, F16, D, kWindow>(p, stream);
+    if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
+    return hipGetLastError();
+}
+
+// The rows of new tokens over a cache, of 16 or 8 bits, as a chain or a tree.  tile_rows: 256 (head_dim 128) or 128
+template <bool F16, int D, int WALK, bool EIGHT>
+inline hipError_t launch_cache_tiles(const SelParams& p, int tile_rows, hipStream_t stream) {
+    if constexpr (D == 128) {
+        if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D, WALK, EIGHT>(p, stream);
+    }
+    if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D, WALK, EIGHT>(p, stream);
     if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
     return hipGetLastError();
 }

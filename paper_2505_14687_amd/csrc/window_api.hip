@@ -41,10 +41,10 @@ int64_t reach(const SelParams& p, int64_t queries, int64_t most) {
     return p.window == kNoWindow ? most : std::min(most, (p.s.causal ? 1 : 2) * ((int64_t)p.window - 1) + queries);
 }
 
-// Groups of neighbouring queries whose rows fill a tile.
-void set_tiles(SelParams& p, int tile_rows) {
+// Groups of neighbouring queries of at most `group_rows` rows (where one query has no more), in tiles.
+void set_tiles(SelParams& p, int group_rows, int tile_rows) {
     SeqShape& s = p.s;
-    s.q_group = std::max(1, std::min(s.n_q, tile_rows / s.share));
+    s.q_group = std::max(1, std::min(s.n_q, group_rows / s.share));
     s.n_groups = (s.n_q + s.q_group - 1) / s.q_group;
     p.rows = s.q_group * s.share;
     p.row_tiles = (p.rows + tile_rows - 1) / tile_rows;
@@ -90,7 +90,7 @@ grat_status make_plan(const grat_sequence* seq, float scale, int32_t window, int
     const int64_t D = seq->head_dim, heads = (int64_t)s.batch * s.kv_heads;
     Scratch scratch{(uint8_t*)work};
     plan.tile_rows = backward ? bwd_tile_rows(p) : fwd_tile_rows(p, (int)D);
-    set_tiles(p, plan.tile_rows);
+    set_tiles(p, plan.tile_rows, plan.tile_rows);
     const int64_t items = heads * s.n_groups * p.row_tiles;
     if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
     // Few workgroups: the keys of each are shared by several (as with lists).
@@ -160,49 +160,39 @@ grat_status check_cache(const grat_tensor* t, const grat_tensor* scale, grat_dty
 }
 
 struct CachePlan {
-    CacheParams c{};
-    int sets = 1;
+    SelParams p{};
+    int tile_rows = 0;
     int64_t work = 0;
 };
 
-// One group: the rows of all heads that share a K/V head, 16, 32 or 64 a workgroup.
-void set_cache(CachePlan& plan, int32_t head_dim, bool eight, void* work) {
-    SelParams& p = plan.c.p;
-    SeqShape& s = p.s;
-    const int64_t rows = (int64_t)s.n_q * s.share;
-    plan.sets = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int tile_rows = 16 * plan.sets, keys = eight ? 64 : 32;
-    s.q_group = s.n_q;
-    s.n_groups = 1;
-    p.rows = (int32_t)rows;
-    p.row_tiles = (p.rows + tile_rows - 1) / tile_rows;
-    p.fd_row_tiles = make_fastdiv((uint32_t)p.row_tiles);
-    p.fd_groups = make_fastdiv(1);
-    p.fd_kv_heads = make_fastdiv((uint32_t)s.kv_heads);
-    p.fd_q_group = make_fastdiv((uint32_t)s.q_group);
-    p.fd_units = make_fastdiv(1);
-    const int64_t items = (int64_t)s.batch * s.kv_heads * p.row_tiles;
-    const int64_t units = (reach(p, std::min<int64_t>(s.n_q, tile_rows), s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys, steps = (units + 3) / 4;
-    set_items(p, items, steps < 8 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(256 / items, steps / 2), 64)));
-    Scratch scratch{(uint8_t*)work};
-    if (p.splits > 1) {
-        p.part_o = scratch.take<float>((int64_t)p.items * tile_rows * head_dim);
-        p.part_ml = scratch.take<float>((int64_t)p.items * tile_rows * 2);
-    }
-    plan.work = scratch.bytes;
-}
+// Rows of a workgroup, of the `rows` of all heads that share a K/V head: few are worked on by waves that share the keys (cache_attn.h), more in the
+// tiles of prompts.
+int cache_tile_rows(int64_t rows, int head_dim) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows > 128 && head_dim == 128 ? 256 : 128; }
 
 grat_status make_cache_plan(const grat_sequence* seq, float scale, int32_t window, int32_t sinks, bool eight, bool tree, void* work, CachePlan* out) {
     CachePlan plan;
-    SelParams& p = plan.c.p;
-    grat_status st = make_shape(seq, &p.s);
+    SelParams& p = plan.p;
+    SeqShape& s = p.s;
+    grat_status st = make_shape(seq, &s);
     if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
     if (st != GRAT_OK) return st;
-    if (tree && p.s.n_q > kMostDrafted) return GRAT_ERR_UNSUPPORTED;
-    p.s.causal = 1;
-    p.s.q_pos = nullptr;
-    set_cache(plan, seq->head_dim, eight, work);
-    if ((int64_t)p.s.batch * p.s.kv_heads * p.row_tiles >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+    if (tree && s.n_q > kMostDrafted) return GRAT_ERR_UNSUPPORTED;
+    s.causal = 1;
+    s.q_pos = nullptr;
+    plan.tile_rows = cache_tile_rows((int64_t)s.n_q * s.share, seq->head_dim);
+    const bool few = plan.tile_rows <= 64;
+    set_tiles(p, few || tree ? s.n_q * s.share : plan.tile_rows, plan.tile_rows);   // few rows and trees are one group
+    const int64_t items = (int64_t)s.batch * s.kv_heads * s.n_groups * p.row_tiles;
+    if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+    const int keys = few ? 4 * cache_keys(eight, plan.tile_rows / 16) : 64;   // of a workgroup's step
+    const int64_t steps = (reach(p, s.q_group, s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys;
+    set_items(p, items, steps < 8 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(256 / items, steps / 2), 64)));
+    Scratch scratch{(uint8_t*)work};
+    if (p.splits > 1) {
+        p.part_o = scratch.take<float>((int64_t)p.items * plan.tile_rows * seq->head_dim);
+        p.part_ml = scratch.take<float>((int64_t)p.items * plan.tile_rows * 2);
+    }
+    plan.work = scratch.bytes;
     *out = plan;
     return GRAT_OK;
 }
@@ -211,7 +201,7 @@ grat_status launch_cache(const CachePlan& plan, const grat_sequence* seq, bool e
     const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
     const auto launch = f16 ? (wide ? launch_cache_attention_f16_d128 : launch_cache_attention_f16_d64)
                             : (wide ? launch_cache_attention_bf16_d128 : launch_cache_attention_bf16_d64);
-    return status_of(launch(plan.c, eight, plan.sets, (hipStream_t)hip_stream));
+    return status_of(launch(plan.p, eight, plan.tile_rows, (hipStream_t)hip_stream));
 }
 
 }  // namespace
@@ -375,17 +365,17 @@ extern "C" grat_status grat_cache_attention_fwd(const grat_sequence* seq, const 
     if (st != GRAT_OK) return st;
     if (plan.work > 0 && !d_work) return GRAT_ERR_NULL;
     if (!aligned16(d_work)) return GRAT_ERR_UNSUPPORTED;
-    CacheParams& c = plan.c;
-    c.p.Q = of(Q);
-    c.p.K = of(K_cache);
-    c.p.V = of(V_cache);
-    c.p.O = of(O);
-    c.p.lse = d_lse;
+    SelParams& p = plan.p;
+    p.Q = of(Q);
+    p.K = of(K_cache);
+    p.V = of(V_cache);
+    p.O = of(O);
+    p.lse = d_lse;
     if (eight) {
-        c.k_scale = of(K_scale);
-        c.v_scale = of(V_scale);
+        p.k_scale = of(K_scale);
+        p.v_scale = of(V_scale);
     }
-    c.parent = d_parent;
-    c.parent_stride_b = parent_stride_b;
+    p.parent = d_parent;
+    p.parent_stride_b = parent_stride_b;
     return launch_cache(plan, seq, eight, hip_stream);
 }

@@ -186,6 +186,9 @@ SHAPES = [
     (2, 4, 4, 40, 200, 6, 70, [200, 100], True),                 # a window shorter than the tree
     (2, 4, 2, 20, 64, 5, 3, [12, 25], True),                     # drafted tokens without a row; first keys among the drafted
     (1, 20, 1, 1, 5000, 4096, 4, None, True),                    # a tree of one token
+    (2, 8, 2, 90, 700, 100, 3, [700, 311], False),               # 360 rows: a chain in the tiles of prompts
+    (2, 12, 4, 60, 1800, 1500, 40, [1800, 59], True),            # 180 rows; a row without a key
+    (1, 48, 2, 16, 1000, None, 0, [990], True),                  # 384 rows: two tiles
 ]
 
 
