@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256, R > (EIGHT ? 1 : 2) ? 1 : 2) void cache_attent
     const int first_units = (first_end + W::kKeys - 1) / W::kKeys, all_units = first_units + (max(near_end - near, 0) + W::kKeys - 1) / W::kKeys;
     int u_first = 0, n_units = all_units;
     if (p.splits > 1) {
-        const int per = (all_units + p.splits - 1) / p.splits;
+        const int per = ((all_units + p.splits - 1) / p.splits + 3) & ~3;   // (a unit of every wave at a time)
         u_first = min(it.split * per, all_units);
         n_units = min(per, all_units - u_first);
     }

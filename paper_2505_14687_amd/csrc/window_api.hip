@@ -186,7 +186,12 @@ grat_status make_cache_plan(const grat_sequence* seq, float scale, int32_t windo
     if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
     const int keys = few ? 4 * cache_keys(eight, plan.tile_rows / 16) : 64;   // of a workgroup's step
     const int64_t steps = (reach(p, s.q_group, s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys;
-    set_items(p, items, steps < 8 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(256 / items, steps / 2), 64)));
+    // A launch that leaves compute units idle has keys shared by several workgroups, up to one a compute unit.  Few rows: parts of one or two steps, about 16 of them,
+    // or of more where that fills the chip; 4 steps or more (one token on 8 heads, us, in parts of 2 steps and by this rule: 17 steps 11.9 and 10.8, 8 steps
+    // 10.3 and 9.3, 32 steps 12.3 both, in parts of one 13.4; 2 steps 7.5 in one part).  Many rows: 2 steps or more, as lists have them.
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / items, 64));
+    const int64_t per = std::max((steps + most - 1) / most, std::min<int64_t>(std::max<int64_t>((steps + 8) / 16, 1), 2));
+    set_items(p, items, few ? (steps < 4 ? 1 : (int)std::min<int64_t>((steps + per - 1) / per, most)) : steps < 8 ? 1 : (int)std::min<int64_t>(steps / 2, most));
     Scratch scratch{(uint8_t*)work};
     if (p.splits > 1) {
         p.part_o = scratch.take<float>((int64_t)p.items * plan.tile_rows * seq->head_dim);
