@@ -73,7 +73,7 @@ grat_status grat_window_attention_bwd(const grat_sequence* seq, const grat_tenso
  *          its position from its depth): axes and d_positions as for grat_rotary; NULL: row i is at position d_start[b] + i.  d_table NULL:
  *          nothing is turned; rot, axes, positions and n_pos are not read.
  *   Q, Q_out   both NULL: K and V alone; q_heads is not read.  Q_out may be Q.  Else no output may overlap an input.
- * Turned in fp32 and rounded once, to the cache's type.  Supported: as grat_rotary; head_dim 64 or 128.
+ * Turned in fp32 and rounded once, to the cache's type.  Supported: as grat_rotary; head_dim 64 or 128; n_cache < 2^30; batch * n_tokens * (q_heads + 2 kv_heads) < 2^35.
  */
 grat_status grat_cache_append(const grat_rotary_args* args, const grat_tensor* Q, const grat_tensor* Q_out, const grat_tensor* K,
                               const grat_tensor* V, const grat_tensor* K_cache, const grat_tensor* V_cache, const grat_tensor* K_scale,

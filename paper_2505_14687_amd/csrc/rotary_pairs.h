@@ -4,8 +4,6 @@
 
 namespace grat {
 
-constexpr int kHeads = 4;   // in flight at a time
-
 // cos and sin of the V pairs from pair0 on, of token n of sequence b.
 template <typename T, bool AXES>
 __device__ __forceinline__ void pair_angles(const RotaryParams& p, int b, int n, int pair0, float* cs, float* sn) {
@@ -40,9 +38,9 @@ __device__ __forceinline__ void pair_angles(const RotaryParams& p, int b, int n,
     }
 }
 
-// Heads of a thread, which share its cos and sin: multiples of kHeads, as many as leave the chip 4 096 workgroups.
-inline int head_chunk(int64_t blocks, int heads) {
-    const int64_t want = blocks * heads / 4096 > 1 ? blocks * heads / 4096 : 1, chunk = (want + kHeads - 1) / kHeads * kHeads;
+// Heads of a thread, which share its cos and sin: multiples of `own`, as many as leave the chip 4 096 workgroups.
+inline int head_chunk(int64_t blocks, int heads, int own) {
+    const int64_t want = blocks * heads / 4096 > 1 ? blocks * heads / 4096 : 1, chunk = (want + own - 1) / own * own;
     return (int)(chunk < heads ? chunk : heads);
 }
 

@@ -13,6 +13,8 @@
 
 namespace grat {
 
+constexpr int kHeads = 4;   // in flight at a time
+
 template <typename T, bool AXES>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
     typedef typename Vec16<T>::type vec;
@@ -100,7 +102,7 @@ static hipError_t launch_rotary_type(RotaryParams p, hipStream_t stream) {
     const int heads = p.heads[0] + p.heads[1] + p.heads[2];
     // (One head a thread: 115 200 tokens of 48 heads on a grid 761 us against 567; 8 191 tokens of 40 heads 66.6 against 65.8; a token each of 32
     // sequences 5.4 both ways.)
-    p.head_chunk = head_chunk(blocks, heads);
+    p.head_chunk = head_chunk(blocks, heads, kHeads);
     const dim3 grid((unsigned)blocks, (unsigned)((heads + p.head_chunk - 1) / p.head_chunk));
     if (p.axes > 1) hipLaunchKernelGGL((rotary_kernel<T, true>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((rotary_kernel<T, false>), grid, dim3(256), 0, stream, p);

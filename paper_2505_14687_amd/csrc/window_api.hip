@@ -301,6 +301,7 @@ extern "C" grat_status grat_cache_append(const grat_rotary_args* args, const gra
     if (!r.d_start) return GRAT_ERR_NULL;
     if (n_cache < 1 || r.inverse) return GRAT_ERR_BAD_DIMS;
     if (n_cache >= kMaxRows) return GRAT_ERR_UNSUPPORTED;
+    if ((int64_t)r.batch * r.n_tokens * (r.q_heads + 2 * (int64_t)r.kv_heads) >= (int64_t)1 << 35) return GRAT_ERR_UNSUPPORTED;
     if (with_q) {
         st = check_tensor(Q, r.dtype, r.head_dim);
         if (st == GRAT_OK) st = check_output(Q_out, r.dtype, r.head_dim, r.batch, r.q_heads);
