@@ -23,7 +23,6 @@ SOURCES = ["grat_api.hip", "block_lists.hip", "attn_f32.hip", "mfma_probe.hip", 
            "sequence_fwd_bf16_d128.hip", "sequence_fwd_bf16_d64.hip", "sequence_fwd_f16_d128.hip", "sequence_fwd_f16_d64.hip",
            "sequence_bwd_bf16_d128.hip", "sequence_bwd_bf16_d64.hip", "sequence_bwd_f16_d128.hip", "sequence_bwd_f16_d64.hip",
            "window_api.hip", "cache_rows.hip", "cache_attn_bf16_d128.hip", "cache_attn_bf16_d64.hip", "cache_attn_f16_d128.hip", "cache_attn_f16_d64.hip",
-           "window_fwd_bf16_d128.hip", "window_fwd_bf16_d64.hip", "window_fwd_f16_d128.hip", "window_fwd_f16_d64.hip",
            "window_bwd_bf16_d128.hip", "window_bwd_bf16_d64.hip", "window_bwd_f16_d128.hip", "window_bwd_f16_d64.hip"]
 
 HIPCC_FLAGS = [

@@ -15,10 +15,6 @@
 
 namespace grat {
 
-hipError_t launch_cache_attention_bf16_d128(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
-hipError_t launch_cache_attention_bf16_d64(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
-hipError_t launch_cache_attention_f16_d128(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
-hipError_t launch_cache_attention_f16_d64(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
 
 // Keys of a unit.
 constexpr int cache_keys(bool eight, int sets) { return eight && sets < 4 ? 64 : 32; }
@@ -105,7 +101,7 @@ __device__ __forceinline__ frag8 widen(uint2 x) {
 }
 
 template <int R, bool EIGHT, bool F16, int D, bool TREE>
-__global__ __launch_bounds__(256, R > (EIGHT ? 1 : 2) ? 1 : 2) void cache_attention_kernel(SelParams p) {
+__global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_kernel(SelParams p) {
     using E = Elem<F16>;
     using W = CacheWave<EIGHT, D, cache_keys(EIGHT, R)>;
     using EV = Elem<F16 && !EIGHT>;   // of the weights and V
@@ -388,6 +384,7 @@ __global__ __launch_bounds__(256, R > (EIGHT ? 1 : 2) ? 1 : 2) void cache_attent
     }
 }
 
+// 16 R rows a workgroup
 template <int R, bool EIGHT, bool F16, int D>
 inline void launch_cache_sets(const SelParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)(8 * p.per_xcd));
@@ -395,22 +392,27 @@ inline void launch_cache_sets(const SelParams& p, hipStream_t stream) {
     else hipLaunchKernelGGL((cache_attention_kernel<R, EIGHT, F16, D, false>), grid, dim3(256), 0, stream, p);
 }
 
-// tile_rows: 16, 32, 64, or, with the kernels of prompts, 128 and 256
+// tile_rows: 16, 32; 64; 128, or 256 (head_dim 128)
+template <bool F16, int D, int WALK, bool EIGHT>
+inline void launch_cache_tiles(const SelParams& p, int tile_rows, hipStream_t stream) {
+    if constexpr (D == 128) {
+        if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D, WALK, EIGHT>(p, stream);
+    }
+    if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D, WALK, EIGHT>(p, stream);
+    else if (tile_rows == 64) {
+        if constexpr (EIGHT) launch_cache_sets<4, true, F16, D>(p, stream);
+        else launch_fwd_tile<2, 2, F16, D, WALK>(p, stream);
+    }
+    else if (tile_rows == 32) launch_cache_sets<2, EIGHT, F16, D>(p, stream);
+    else if (tile_rows == 16) launch_cache_sets<1, EIGHT, F16, D>(p, stream);
+}
+
 template <bool F16, int D>
 inline hipError_t launch_cache_attention(const SelParams& p, bool eight, int tile_rows, hipStream_t stream) {
-    if (tile_rows > 64) {
-        if (eight) return p.parent ? launch_cache_tiles<F16, D, kTree, true>(p, tile_rows, stream) : launch_cache_tiles<F16, D, kWindow, true>(p, tile_rows, stream);
-        return p.parent ? launch_cache_tiles<F16, D, kTree, false>(p, tile_rows, stream) : launch_cache_tiles<F16, D, kWindow, false>(p, tile_rows, stream);
-    }
-    if (eight) {
-        if (tile_rows == 16) launch_cache_sets<1, true, F16, D>(p, stream);
-        else if (tile_rows == 32) launch_cache_sets<2, true, F16, D>(p, stream);
-        else launch_cache_sets<4, true, F16, D>(p, stream);
-    } else {
-        if (tile_rows == 16) launch_cache_sets<1, false, F16, D>(p, stream);
-        else if (tile_rows == 32) launch_cache_sets<2, false, F16, D>(p, stream);
-        else launch_cache_sets<4, false, F16, D>(p, stream);
-    }
+    if (eight && p.parent) launch_cache_tiles<F16, D, kTree, true>(p, tile_rows, stream);
+    else if (eight) launch_cache_tiles<F16, D, kWindow, true>(p, tile_rows, stream);
+    else if (p.parent) launch_cache_tiles<F16, D, kTree, false>(p, tile_rows, stream);
+    else launch_cache_tiles<F16, D, kWindow, false>(p, tile_rows, stream);
     if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
     return hipGetLastError();
 }

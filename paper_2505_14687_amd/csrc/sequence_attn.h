@@ -75,11 +75,11 @@ hipError_t launch_selected_bwd_f16_d128(const SelParams& p, const GradParams& g,
 hipError_t launch_selected_bwd_f16_d64(const SelParams& p, const GradParams& g, int tile_rows, int tile_keys, hipStream_t stream);
 void launch_grad_lists(const SelParams& p, const GradParams& g, hipStream_t stream);
 void launch_grad_head_bits(const GradParams& g, hipStream_t stream);
-// ... of attention within a window (window_fwd_*.hip, window_bwd_*.hip)
-hipError_t launch_window_fwd_bf16_d128(const SelParams& p, int tile_rows, hipStream_t stream);
-hipError_t launch_window_fwd_bf16_d64(const SelParams& p, int tile_rows, hipStream_t stream);
-hipError_t launch_window_fwd_f16_d128(const SelParams& p, int tile_rows, hipStream_t stream);
-hipError_t launch_window_fwd_f16_d64(const SelParams& p, int tile_rows, hipStream_t stream);
+// ... of attention within a window and over caches (cache_attn_*.hip, window_bwd_*.hip).  eight: K and V in 8 bits; p.parent: a tree
+hipError_t launch_cache_attention_bf16_d128(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
+hipError_t launch_cache_attention_bf16_d64(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
+hipError_t launch_cache_attention_f16_d128(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
+hipError_t launch_cache_attention_f16_d64(const SelParams& p, bool eight, int tile_rows, hipStream_t stream);
 hipError_t launch_window_bwd_bf16_d128(const SelParams& p, const GradParams& g, int tile_rows, hipStream_t stream);
 hipError_t launch_window_bwd_bf16_d64(const SelParams& p, const GradParams& g, int tile_rows, hipStream_t stream);
 hipError_t launch_window_bwd_f16_d128(const SelParams& p, const GradParams& g, int tile_rows, hipStream_t stream);

@@ -543,28 +543,4 @@ inline hipError_t launch_fwd(const SelParams& p, int tile_rows, hipStream_t stre
     return hipGetLastError();
 }
 
-// Attention within a window.  tile_rows: 256 (head_dim 128), 128, 64 or 32
-template <bool F16, int D>
-inline hipError_t launch_window(const SelParams& p, int tile_rows, hipStream_t stream) {
-    if constexpr (D == 128) {
-        if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D, kWindow>(p, stream);
-    }
-    if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D, kWindow>(p, stream);
-    else if (tile_rows == 64) launch_fwd_tile<2, 2, F16, D, kWindow>(p, stream);
-    else if (tile_rows == 32) launch_fwd_tile<1, 2, F16, D, kWindow>(p, stream);
-    if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
-    return hipGetLastError();
-}
-
-// The rows of new tokens over a cache, of 16 or 8 bits, as a chain or a tree.  tile_rows: 256 (head_dim 128) or 128
-template <bool F16, int D, int WALK, bool EIGHT>
-inline hipError_t launch_cache_tiles(const SelParams& p, int tile_rows, hipStream_t stream) {
-    if constexpr (D == 128) {
-        if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D, WALK, EIGHT>(p, stream);
-    }
-    if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D, WALK, EIGHT>(p, stream);
-    if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
-    return hipGetLastError();
-}
-
 }  // namespace grat

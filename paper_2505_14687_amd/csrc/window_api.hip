@@ -61,72 +61,121 @@ void set_items(SelParams& p, int64_t items, int splits) {
     p.fd_splits = make_fastdiv((uint32_t)splits);
 }
 
-struct WindowPlan {
+// ---- forward -------------------------------------------------------------------------------------
+struct ForwardPlan {
+    SelParams p{};
+    int tile_rows = 0;
+    int64_t work = 0;
+};
+
+// Rows of a workgroup, of the `rows` of all heads that share a K/V head: one tile where they fit, else 256 if that makes four rounds of the chip, else 128 (windows of
+// 1 024, us in tiles of 256 and of 128: 32 768 tokens of 8 heads 614 and 598, 8 192 tokens 144 and 151; windows of 4 096 1 855 and 1 890, of 256 258 and 251).
+int fwd_tile_rows(const SeqShape& s, int head_dim) {
+    const int64_t rows = (int64_t)s.n_q * s.share;
+    if (rows <= 64) return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    if (head_dim == 128 && rows > 128 && (rows <= 256 || (int64_t)s.batch * s.kv_heads * ((rows + 255) / 256) >= 1024)) return 256;
+    return 128;
+}
+
+grat_status make_forward(const grat_sequence* seq, float scale, int32_t window, int32_t sinks, bool eight, bool tree, void* work, ForwardPlan* out) {
+    ForwardPlan plan;
+    SelParams& p = plan.p;
+    const SeqShape& s = p.s;
+    grat_status st = make_shape(seq, &p.s);
+    if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
+    if (st != GRAT_OK) return st;
+    if (tree && s.n_q > kMostDrafted) return GRAT_ERR_UNSUPPORTED;
+    plan.tile_rows = fwd_tile_rows(s, seq->head_dim);
+    const bool few = plan.tile_rows <= (eight ? 64 : 32);   // four waves that share the keys (cache_attn.h)
+    set_tiles(p, tree ? s.n_q * s.share : plan.tile_rows, plan.tile_rows);   // (a tree is one group)
+    const int64_t items = (int64_t)s.batch * s.kv_heads * s.n_groups * p.row_tiles;
+    if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+    const int keys = few ? 4 * cache_keys(eight, plan.tile_rows / 16) : 64;   // of a workgroup's step
+    const int64_t steps = (reach(p, s.q_group, s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys;
+    // A launch that leaves compute units idle has keys shared by several workgroups, up to one a compute unit.  Few rows: parts of one or two steps, about 16 of them,
+    // or of more where that fills the chip; 4 steps or more (one token on 8 heads, us, in parts of 2 steps and by this rule: 17 steps 11.9 and 10.8, 8 steps
+    // 10.3 and 9.3, 32 steps 12.3 both, in parts of one 13.4; 2 steps 7.5 in one part).  Many rows: 2 steps or more, as lists have them.
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / items, 64));
+    const int64_t per = std::max((steps + most - 1) / most, std::min<int64_t>(std::max<int64_t>((steps + 8) / 16, 1), 2));
+    set_items(p, items, few ? (steps < 4 ? 1 : (int)std::min<int64_t>((steps + per - 1) / per, most)) : steps < 8 ? 1 : (int)std::min<int64_t>(steps / 2, most));
+    Scratch scratch{(uint8_t*)work};
+    if (p.splits > 1) {
+        p.part_o = scratch.take<float>((int64_t)p.items * plan.tile_rows * seq->head_dim);
+        p.part_ml = scratch.take<float>((int64_t)p.items * plan.tile_rows * 2);
+    }
+    plan.work = scratch.bytes;
+    *out = plan;
+    return GRAT_OK;
+}
+
+grat_status launch_forward(const ForwardPlan& plan, const grat_sequence* seq, bool eight, void* hip_stream) {
+    const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
+    const auto launch = f16 ? (wide ? launch_cache_attention_f16_d128 : launch_cache_attention_f16_d64)
+                            : (wide ? launch_cache_attention_bf16_d128 : launch_cache_attention_bf16_d64);
+    return status_of(launch(plan.p, eight, plan.tile_rows, (hipStream_t)hip_stream));
+}
+
+// A cache's queries are the newest tokens.
+grat_sequence newest(const grat_sequence& s) {
+    grat_sequence t = s;
+    t.causal = 1;
+    t.d_q_pos = nullptr;
+    return t;
+}
+
+// ---- gradient ------------------------------------------------------------------------------------
+struct GradPlan {
     SelParams p{};
     GradParams g{};
     int tile_rows = 0;
     int64_t work = 0;
 };
 
-int fwd_tile_rows(const SelParams& p, int head_dim) {
-    const int64_t rows = (int64_t)p.s.n_q * p.s.share;
-    if (rows <= 32) return 32;
-    if (rows <= 64) return 64;
-    if (head_dim == 128 && (int64_t)p.s.batch * p.s.kv_heads * ((rows + 255) / 256) >= 1024) return 256;
-    return 128;
-}
-int bwd_tile_rows(const SelParams& p) {
-    const int64_t rows = (int64_t)p.s.n_q * p.s.share;
+int bwd_tile_rows(const SeqShape& s) {
+    const int64_t rows = (int64_t)s.n_q * s.share;
     return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
 
-grat_status make_plan(const grat_sequence* seq, float scale, int32_t window, int32_t sinks, bool backward, void* work, WindowPlan* out) {
-    WindowPlan plan;
+grat_status make_gradient(const grat_sequence* seq, float scale, int32_t window, int32_t sinks, void* work, GradPlan* out) {
+    GradPlan plan;
     SelParams& p = plan.p;
+    GradParams& g = plan.g;
+    WindowGradParams& w = g.window;
+    const SeqShape& s = p.s;
     grat_status st = make_shape(seq, &p.s);
     if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
     if (st != GRAT_OK) return st;
-    const SeqShape& s = p.s;
     const int64_t D = seq->head_dim, heads = (int64_t)s.batch * s.kv_heads;
-    Scratch scratch{(uint8_t*)work};
-    plan.tile_rows = backward ? bwd_tile_rows(p) : fwd_tile_rows(p, (int)D);
+    plan.tile_rows = bwd_tile_rows(s);
     set_tiles(p, plan.tile_rows, plan.tile_rows);
     const int64_t items = heads * s.n_groups * p.row_tiles;
     if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
-    // Few workgroups: the keys of each are shared by several (as with lists).
-    const int64_t units = (reach(p, s.q_group, s.n_k) + kUnit - 1) / kUnit + (p.sinks + kUnit - 1) / kUnit, steps = (units + 1) / 2;
-    set_items(p, items, backward || steps < 8 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min(256 / items, steps / 2), 64)));
-    if (p.splits > 1) {
-        p.part_o = scratch.take<float>((int64_t)p.items * plan.tile_rows * D);
-        p.part_ml = scratch.take<float>((int64_t)p.items * plan.tile_rows * 2);
-    }
-    if (backward) {
-        GradParams& g = plan.g;
-        WindowGradParams& w = g.window;
-        w.tiles = (s.n_k + 63) / 64;
-        w.first_tiles = (p.sinks + 63) / 64;
-        const int64_t near = reach(p, 64, s.n_q) * s.share, all = (int64_t)s.n_q * s.share;
-        const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(near, 512), heads * w.tiles * near / 768) + 63) / 64 * 64);
-        w.near_parts = (int32_t)((near + part - 1) / part);
-        w.first_parts = std::max(w.near_parts, (int32_t)((all + part - 1) / part));
-        const int64_t firsts = (int64_t)w.first_tiles * w.first_parts, per_head = firsts + (int64_t)(w.tiles - w.first_tiles) * w.near_parts;
-        const int64_t slots = w.near_parts > 1 ? per_head : w.first_parts > 1 ? firsts : 0;
-        if (heads * per_head >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
-        w.head_items = (int32_t)per_head;
-        w.head_slots = (int32_t)slots;
-        w.items = (int32_t)(heads * per_head);
-        w.per_xcd = (w.items + 7) / 8;
-        g.fd_tiles = make_fastdiv(1);
-        g.stats = (int64_t)s.batch * s.q_heads * s.n_q;
-        g.delta = scratch.take<float>(g.stats + 1);
-        g.lse2 = scratch.take<float>(g.stats + 1);
-        g.slots = scratch.take<float>(heads * slots * 128 * D);
-        g.heads = (int32_t)heads;
-        if (seq->dtype == GRAT_F16) {
-            g.head_runs = s.n_groups * p.row_tiles * (plan.tile_rows / 32);
-            g.row_bits = scratch.take<int32_t>(heads * g.head_runs);
-            g.head_bits = scratch.take<int32_t>(heads);
-        }
+    set_items(p, items, 1);
+    // Parts of the rows that see a key tile: a window's, or fewer where that leaves compute units idle (as with lists).
+    w.tiles = (s.n_k + 63) / 64;
+    w.first_tiles = (p.sinks + 63) / 64;
+    const int64_t near = reach(p, 64, s.n_q) * s.share, all = (int64_t)s.n_q * s.share;
+    const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(near, 512), heads * w.tiles * near / 768) + 63) / 64 * 64);
+    w.near_parts = (int32_t)((near + part - 1) / part);
+    w.first_parts = std::max(w.near_parts, (int32_t)((all + part - 1) / part));
+    const int64_t firsts = (int64_t)w.first_tiles * w.first_parts, per_head = firsts + (int64_t)(w.tiles - w.first_tiles) * w.near_parts;
+    const int64_t slots = w.near_parts > 1 ? per_head : w.first_parts > 1 ? firsts : 0;
+    if (heads * per_head >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+    w.head_items = (int32_t)per_head;
+    w.head_slots = (int32_t)slots;
+    w.items = (int32_t)(heads * per_head);
+    w.per_xcd = (w.items + 7) / 8;
+    Scratch scratch{(uint8_t*)work};
+    g.fd_tiles = make_fastdiv(1);
+    g.stats = (int64_t)s.batch * s.q_heads * s.n_q;
+    g.delta = scratch.take<float>(g.stats + 1);
+    g.lse2 = scratch.take<float>(g.stats + 1);
+    g.slots = scratch.take<float>(heads * slots * 128 * D);
+    g.heads = (int32_t)heads;
+    if (seq->dtype == GRAT_F16) {
+        g.head_runs = s.n_groups * p.row_tiles * (plan.tile_rows / 32);
+        g.row_bits = scratch.take<int32_t>(heads * g.head_runs);
+        g.head_bits = scratch.take<int32_t>(heads);
     }
     plan.work = scratch.bytes;
     *out = plan;
@@ -159,71 +208,23 @@ grat_status check_cache(const grat_tensor* t, const grat_tensor* scale, grat_dty
     return st == GRAT_OK ? check_scale(scale) : st;
 }
 
-struct CachePlan {
-    SelParams p{};
-    int tile_rows = 0;
-    int64_t work = 0;
-};
-
-// Rows of a workgroup, of the `rows` of all heads that share a K/V head: few are worked on by waves that share the keys (cache_attn.h), more in the
-// tiles of prompts.
-int cache_tile_rows(int64_t rows, int head_dim) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows > 128 && head_dim == 128 ? 256 : 128; }
-
-grat_status make_cache_plan(const grat_sequence* seq, float scale, int32_t window, int32_t sinks, bool eight, bool tree, void* work, CachePlan* out) {
-    CachePlan plan;
-    SelParams& p = plan.p;
-    SeqShape& s = p.s;
-    grat_status st = make_shape(seq, &s);
-    if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
-    if (st != GRAT_OK) return st;
-    if (tree && s.n_q > kMostDrafted) return GRAT_ERR_UNSUPPORTED;
-    s.causal = 1;
-    s.q_pos = nullptr;
-    plan.tile_rows = cache_tile_rows((int64_t)s.n_q * s.share, seq->head_dim);
-    const bool few = plan.tile_rows <= 64;
-    set_tiles(p, few || tree ? s.n_q * s.share : plan.tile_rows, plan.tile_rows);   // few rows and trees are one group
-    const int64_t items = (int64_t)s.batch * s.kv_heads * s.n_groups * p.row_tiles;
-    if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
-    const int keys = few ? 4 * cache_keys(eight, plan.tile_rows / 16) : 64;   // of a workgroup's step
-    const int64_t steps = (reach(p, s.q_group, s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys;
-    // A launch that leaves compute units idle has keys shared by several workgroups, up to one a compute unit.  Few rows: parts of one or two steps, about 16 of them,
-    // or of more where that fills the chip; 4 steps or more (one token on 8 heads, us, in parts of 2 steps and by this rule: 17 steps 11.9 and 10.8, 8 steps
-    // 10.3 and 9.3, 32 steps 12.3 both, in parts of one 13.4; 2 steps 7.5 in one part).  Many rows: 2 steps or more, as lists have them.
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / items, 64));
-    const int64_t per = std::max((steps + most - 1) / most, std::min<int64_t>(std::max<int64_t>((steps + 8) / 16, 1), 2));
-    set_items(p, items, few ? (steps < 4 ? 1 : (int)std::min<int64_t>((steps + per - 1) / per, most)) : steps < 8 ? 1 : (int)std::min<int64_t>(steps / 2, most));
-    Scratch scratch{(uint8_t*)work};
-    if (p.splits > 1) {
-        p.part_o = scratch.take<float>((int64_t)p.items * plan.tile_rows * seq->head_dim);
-        p.part_ml = scratch.take<float>((int64_t)p.items * plan.tile_rows * 2);
-    }
-    plan.work = scratch.bytes;
-    *out = plan;
-    return GRAT_OK;
-}
-
-grat_status launch_cache(const CachePlan& plan, const grat_sequence* seq, bool eight, void* hip_stream) {
-    const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
-    const auto launch = f16 ? (wide ? launch_cache_attention_f16_d128 : launch_cache_attention_f16_d64)
-                            : (wide ? launch_cache_attention_bf16_d128 : launch_cache_attention_bf16_d64);
-    return status_of(launch(plan.p, eight, plan.tile_rows, (hipStream_t)hip_stream));
-}
-
 }  // namespace
 }  // namespace grat
 
 using namespace grat;
 
 extern "C" int64_t grat_window_attention_work(const grat_sequence* seq, int32_t window, int32_t sinks, int32_t backward) {
-    WindowPlan plan;
-    return make_plan(seq, 1.f, window, sinks, backward != 0, nullptr, &plan) == GRAT_OK ? plan.work : 0;
+    ForwardPlan f;
+    GradPlan g;
+    if (backward) return make_gradient(seq, 1.f, window, sinks, nullptr, &g) == GRAT_OK ? g.work : 0;
+    return make_forward(seq, 1.f, window, sinks, false, false, nullptr, &f) == GRAT_OK ? f.work : 0;
 }
 
 extern "C" grat_status grat_window_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K, const grat_tensor* V,
                                                  const grat_tensor* O, float* d_lse, float scale, int32_t window, int32_t sinks, void* d_work,
                                                  void* hip_stream) {
-    WindowPlan plan;
-    grat_status st = make_plan(seq, scale, window, sinks, false, d_work, &plan);
+    ForwardPlan plan;
+    grat_status st = make_forward(seq, scale, window, sinks, false, false, d_work, &plan);
     for (const grat_tensor* t : {Q, K, V})
         if (st == GRAT_OK) st = check_tensor(t, seq->dtype, seq->head_dim);
     if (st == GRAT_OK) st = check_output(O, seq->dtype, seq->head_dim, seq->batch, seq->q_heads);
@@ -236,10 +237,7 @@ extern "C" grat_status grat_window_attention_fwd(const grat_sequence* seq, const
     p.V = of(V);
     p.O = of(O);
     p.lse = d_lse;
-    const bool f16 = seq->dtype == GRAT_F16, wide = seq->head_dim == 128;
-    const auto launch = f16 ? (wide ? launch_window_fwd_f16_d128 : launch_window_fwd_f16_d64)
-                            : (wide ? launch_window_fwd_bf16_d128 : launch_window_fwd_bf16_d64);
-    return status_of(launch(p, plan.tile_rows, (hipStream_t)hip_stream));
+    return launch_forward(plan, seq, false, hip_stream);
 }
 
 extern "C" grat_status grat_window_attention_bwd(const grat_sequence* seq, const grat_tensor* dO, const grat_tensor* Q, const grat_tensor* K,
@@ -247,8 +245,8 @@ extern "C" grat_status grat_window_attention_bwd(const grat_sequence* seq, const
                                                  const grat_tensor* dK, const grat_tensor* dV, float scale, int32_t window, int32_t sinks,
                                                  void* d_work, void* hip_stream) {
     if (!d_lse) return GRAT_ERR_NULL;
-    WindowPlan plan;
-    grat_status st = make_plan(seq, scale, window, sinks, true, d_work, &plan);
+    GradPlan plan;
+    grat_status st = make_gradient(seq, scale, window, sinks, d_work, &plan);
     for (const grat_tensor* t : {dO, Q, K, V, O})
         if (st == GRAT_OK) st = check_tensor(t, seq->dtype, seq->head_dim);
     if (st == GRAT_OK) st = check_output(dQ, seq->dtype, seq->head_dim, seq->batch, seq->q_heads);
@@ -351,17 +349,22 @@ extern "C" grat_status grat_cache_read(grat_dtype dtype, int32_t batch, int32_t 
 }
 
 extern "C" int64_t grat_cache_attention_work(const grat_sequence* seq, int32_t window, int32_t sinks, int32_t eight) {
-    CachePlan plan;
-    return make_cache_plan(seq, 1.f, window, sinks, eight != 0, false, nullptr, &plan) == GRAT_OK ? plan.work : 0;
+    if (!seq) return 0;
+    const grat_sequence q = newest(*seq);
+    ForwardPlan chain, tree;   // (a tree of more tokens than there may be is refused by the call itself)
+    if (make_forward(&q, 1.f, window, sinks, eight != 0, false, nullptr, &chain) != GRAT_OK) return 0;
+    return make_forward(&q, 1.f, window, sinks, eight != 0, true, nullptr, &tree) == GRAT_OK ? std::max(chain.work, tree.work) : chain.work;
 }
 
 extern "C" grat_status grat_cache_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K_cache, const grat_tensor* V_cache,
                                                 const grat_tensor* K_scale, const grat_tensor* V_scale, const grat_tensor* O, float* d_lse, float scale,
                                                 int32_t window, int32_t sinks, const int32_t* d_parent, int64_t parent_stride_b, void* d_work,
                                                 void* hip_stream) {
-    CachePlan plan;
+    if (!seq) return GRAT_ERR_NULL;
+    const grat_sequence q = newest(*seq);
     const bool eight = K_scale || V_scale;
-    grat_status st = make_cache_plan(seq, scale, window, sinks, eight, d_parent != nullptr, d_work, &plan);
+    ForwardPlan plan;
+    grat_status st = make_forward(&q, scale, window, sinks, eight, d_parent != nullptr, d_work, &plan);
     if (st == GRAT_OK) st = check_tensor(Q, seq->dtype, seq->head_dim);
     if (st == GRAT_OK && eight && (!K_scale || !V_scale)) st = GRAT_ERR_NULL;
     if (st == GRAT_OK) st = check_cache(K_cache, K_scale, seq->dtype, seq->head_dim);
@@ -383,5 +386,5 @@ extern "C" grat_status grat_cache_attention_fwd(const grat_sequence* seq, const 
     }
     p.parent = d_parent;
     p.parent_stride_b = parent_stride_b;
-    return launch_cache(plan, seq, eight, hip_stream);
+    return launch_forward(plan, seq, eight, hip_stream);
 }
