@@ -110,8 +110,10 @@ __global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_k
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds];
     __shared__ float s_m[4][16], s_l[4][16];
     __shared__ Tree tree[1];   // (of no size where nothing refers to it)
-    const Item it(p);
+    Item it(p);
     if (it.idle(p)) return;
+    int part_units = 0;
+    if (!it.share(p, part_units)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), r = lane & 15, g = lane >> 4;
     const SeqShape& s = p.s;
     const int len = seq_len(s, it.b);
@@ -128,10 +130,11 @@ __global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_k
     }
     if constexpr (TREE) build_tree(tree[0], p, it.b, base);
 
-    // what this lane's rows see, and what the workgroup's rows see together
+    // what this lane's rows see, and what the workgroup's rows see together (all of the group's)
     RowSpan span[R];
     int line[TREE ? R : 1];   // trees: the row's line, in words
-    int first_end = 0, near = 0x7fffffff, near_end = 0, least_first = 0x7fffffff, least_hi = 0x7fffffff, most_lo = 0;
+    const auto [first_end, near, near_end] = uniform(TREE ? tree_range(p, len) : rows_range(p, len, pos, 0, s.n_q - 1));
+    int least_first = 0x7fffffff, least_hi = 0x7fffffff, most_lo = 0;
 #pragma unroll
     for (int k = 0; k < R; ++k) {
         const GroupRow row(p, it.h, 0, it.tile * (16 * R) + 16 * k + r);
@@ -142,9 +145,6 @@ __global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_k
             span[k] = row_span(p, len, pos, row.query);
         }
         if (row.there) {
-            first_end = max(first_end, span[k].first);
-            if (TREE || span[k].hi > span[k].lo) near = min(near, span[k].lo);
-            near_end = max(near_end, TREE ? len : span[k].hi);
             least_first = min(least_first, span[k].first);
             least_hi = min(least_hi, span[k].hi);
             most_lo = max(most_lo, span[k].lo);
@@ -154,23 +154,17 @@ __global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_k
     }
 #pragma unroll
     for (int m = 1; m < 16; m *= 2) {
-        first_end = max(first_end, __shfl_xor(first_end, m));
-        near = min(near, __shfl_xor(near, m));
-        near_end = max(near_end, __shfl_xor(near_end, m));
         least_first = min(least_first, __shfl_xor(least_first, m));
         least_hi = min(least_hi, __shfl_xor(least_hi, m));
         most_lo = max(most_lo, __shfl_xor(most_lo, m));
     }
-    first_end = __builtin_amdgcn_readfirstlane(first_end);
-    near = max(__builtin_amdgcn_readfirstlane(near), first_end);
-    near_end = __builtin_amdgcn_readfirstlane(near_end);
     least_first = __builtin_amdgcn_readfirstlane(least_first);
     least_hi = __builtin_amdgcn_readfirstlane(least_hi);
     most_lo = __builtin_amdgcn_readfirstlane(most_lo);
     const int first_units = (first_end + W::kKeys - 1) / W::kKeys, all_units = first_units + (max(near_end - near, 0) + W::kKeys - 1) / W::kKeys;
     int u_first = 0, n_units = all_units;
     if (p.splits > 1) {
-        const int per = ((all_units + p.splits - 1) / p.splits + 3) & ~3;   // (a unit of every wave at a time)
+        const int per = part_units ? part_units : ((all_units + p.splits - 1) / p.splits + 3) & ~3;   // (a unit of every wave at a time)
         u_first = min(it.split * per, all_units);
         n_units = min(per, all_units - u_first);
     }

@@ -31,6 +31,7 @@ struct SelParams {
     SeqTensor k_scale, v_scale;   // K and V in 8 bits: a float a row
     const int32_t* parent;        // drafted tokens, or null
     int64_t parent_stride_b;
+    int32_t slots, part_keys, part_step;   // parts that the sequences share (Parts), or 0; keys of a unit; units that a workgroup takes at a time
 };
 constexpr int32_t kNoWindow = 0x7fffffff;
 
@@ -41,6 +42,7 @@ struct WindowGradParams {
     int32_t first_parts, near_parts;    // parts of either kind of tile
     int32_t items, per_xcd;             // of the launch
     int32_t head_items, head_slots;     // items and places in `slots` of a K/V head
+    int32_t own_bits;                   // half: every workgroup works out its head's exponent itself
 };
 
 // What the gradient needs beside SelParams, in the caller's scratch memory.
@@ -207,6 +209,7 @@ struct Item {
         b = (int)bb; h = (int)hh; g = (int)gg; tile = (int)m; split = (int)s;
     }
     __device__ __forceinline__ bool idle(const SelParams& p) const { return (int)(blockIdx.x >> 3) >= p.per_xcd || item >= p.items; }
+    __device__ __forceinline__ bool share(const SelParams& p, int& units);
     __device__ __forceinline__ int64_t list(const SelParams& p) const { return ((int64_t)b * p.s.kv_heads + h) * p.s.n_groups + g; }
 };
 
@@ -245,26 +248,72 @@ __device__ __forceinline__ RowSpan row_span(const SelParams& p, int len, int64_t
 }
 // The keys that the rows [i0, i1] see, as units of 32 keys: of the first keys from key 0 on, then from the first key of row i0's window on that is
 // not among these.  A unit's keys that no row sees are not read: the last one that some row sees stands for them.
-struct WindowUnits {
-    int first_end, first_units, near, near_end, n;
-    __device__ __forceinline__ WindowUnits(const SelParams& p, int len, int64_t pos, int i0, int i1) {
-        const RowSpan a = row_span(p, len, pos, i0), z = row_span(p, len, pos, i1);
-        set(z.first, a.lo, z.hi);
-    }
-    // ... of a tree: its first token is one that goes on from a committed one, and no other sees more of these.
-    __device__ __forceinline__ WindowUnits(const SelParams& p, int len) {
-        const int base = len - p.s.n_q, committed = max(base, 0);
-        set(min(p.sinks, committed), p.window == kNoWindow ? 0 : max(0, min(committed, base - p.window + 1)), len);
-    }
-    __device__ __forceinline__ void set(int first, int lo, int hi) {   // (the same in all lanes, which what it is computed from does not always say)
-        first_end = __builtin_amdgcn_readfirstlane(first);
+struct KeyRange {
+    int first_end, near, near_end;
+    __device__ __forceinline__ int units(int keys) const { return (first_end + keys - 1) / keys + (max(near_end - near, 0) + keys - 1) / keys; }
+};
+__device__ __forceinline__ KeyRange rows_range(const SelParams& p, int len, int64_t pos, int i0, int i1) {
+    const RowSpan a = row_span(p, len, pos, i0), z = row_span(p, len, pos, i1);
+    return KeyRange{z.first, max(a.lo, z.first), z.hi};
+}
+// ... of a tree: its first token is one that goes on from a committed one, and no other sees more of these.
+__device__ __forceinline__ KeyRange tree_range(const SelParams& p, int len) {
+    const int base = len - p.s.n_q, committed = max(base, 0), first = min(p.sinks, committed);
+    return KeyRange{first, max(p.window == kNoWindow ? 0 : max(0, min(committed, base - p.window + 1)), first), len};
+}
+// (The same in all lanes, which what it is computed from does not always say.)
+__device__ __forceinline__ KeyRange uniform(const KeyRange& r) {
+    return KeyRange{__builtin_amdgcn_readfirstlane(r.first_end), __builtin_amdgcn_readfirstlane(r.near), __builtin_amdgcn_readfirstlane(r.near_end)};
+}
+struct WindowUnits : KeyRange {
+    int first_units, n;
+    __device__ __forceinline__ explicit WindowUnits(const KeyRange& r) : KeyRange(uniform(r)) {
         first_units = (first_end + kUnit - 1) / kUnit;
-        near_end = __builtin_amdgcn_readfirstlane(hi);
-        near = max(__builtin_amdgcn_readfirstlane(lo), first_end);
-        n = first_units + (max(near_end - near, 0) + kUnit - 1) / kUnit;
+        n = units(kUnit);
     }
     __device__ __forceinline__ int start(int i) const { return i < first_units ? i * kUnit : near + (i - first_units) * kUnit; }
 };
+
+// Sequences of lengths that the host does not know, whose keys few workgroups share: the parts of all of them, p.slots for a K/V head's row tile, are
+// of about equal length, and not shorter than pays.  A sequence a lane, at most 64.  (64 drafted tokens x 4 heads over 4 caches of 10 240 to 16 384 keys 83.1 -> 76.5 us.)
+__device__ __forceinline__ int sum_up_to(int x) {   // of the lanes up to this one
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // lane - 1, - 2, - 4, - 8 of its row of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // the row ahead, the two rows ahead
+    return x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+}
+struct Parts {
+    int n, end, per;   // parts of this lane's sequence, and of all up to it; units of a part
+    __device__ __forceinline__ explicit Parts(const SelParams& p) {   // by whole waves
+        const SeqShape& s = p.s;
+        const int lane = threadIdx.x & 63, b = min(lane, s.batch - 1), len = seq_len(s, b);
+        const KeyRange r = p.parent ? tree_range(p, len) : rows_range(p, len, window_pos(s, b, len), 0, s.n_q - 1);
+        const int units = lane < s.batch ? r.units(p.part_keys) : 0, step = p.part_step, all = __builtin_amdgcn_readlane(sum_up_to(units), 63);
+        // (least: two steps of 64 keys of many rows; one of few, two where there are 24 and more)
+        const int least = step < 4 || all >= 24 * step * s.batch ? 2 * step : step;
+        per = (max((all + p.slots - 1) / p.slots, least) + step - 1) / step * step;
+        for (;; per += (per / 16 + step) / step * step) {   // (as soon as a part holds the longest one there are no more parts than sequences)
+            n = (units + per - 1) / per;
+            end = sum_up_to(n);
+            if (__builtin_amdgcn_readlane(end, 63) <= p.slots) break;
+        }
+    }
+    // The sequence that part k belongs to, p.s.batch if none.
+    __device__ __forceinline__ int of(int k) const { return __popcll(__builtin_amdgcn_ballot_w64(end <= k)); }
+};
+
+// Where p.slots says so, `split` is a part of all sequences': finds whose, and the units that it takes.  False: there is none.
+__device__ __forceinline__ bool Item::share(const SelParams& p, int& units) {
+    if (p.slots == 0) return true;
+    const Parts parts(p);
+    b = parts.of(split);
+    if (b >= p.s.batch) return false;
+    split -= __builtin_amdgcn_readlane(parts.end, b) - __builtin_amdgcn_readlane(parts.n, b);
+    units = parts.per;
+    return true;
+}
 
 // A tree of drafted tokens: token t goes on from token parent[t], or from the newest committed token (-1, and whatever is not a token ahead of t).  Its key
 // lies in row base + t, its position is base + depth.  lines[t]: the tokens of its line, itself among them, that it sees.

@@ -132,7 +132,25 @@ __global__ __launch_bounds__(KW * 128, KW) void grad_keys_kernel(SelParams p, Gr
     f32x16 dk[D / 32], dv[D / 32];
     clear<D>(dk);
     clear<D>(dv);
-    const int bits = F16 ? __builtin_amdgcn_readfirstlane(g.head_bits[bh]) : 0;
+    int bits = 0;
+    if constexpr (F16) {
+        if (WINDOW && g.window.own_bits) {   // (the launch that does it for all costs more than a few hundred numbers read by each: @BITS@)
+            __shared__ int32_t s_least[NW];
+            const int32_t* const runs = g.row_bits + (int64_t)bh * g.head_runs;
+            int least = kMostBits;
+            for (int i = threadIdx.x; i < g.head_runs; i += NW * 64) least = min(least, runs[i]);
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) least = min(least, __shfl_xor(least, m));
+            if (lane == 0) s_least[wave] = least;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < NW; ++w) least = min(least, s_least[w]);
+            bits = __builtin_amdgcn_readfirstlane(least) - 1;
+            if (near.tile == 0 && near.z == 0 && threadIdx.x == 0) g.head_bits[bh] = bits;   // for the join
+        } else {
+            bits = __builtin_amdgcn_readfirstlane(g.head_bits[bh]);
+        }
+    }
     const float grad_factor = ldexpf(1.f, bits - kWeightBits);   // (half: dS from the P that dV takes)
     if (n_tiles > 0 && tile_key0 < len) {
         frag8 kf[D / 16], vf[D / 16];
@@ -468,7 +486,7 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void grad
     const int len = seq_len(s, it.b);
     const int64_t pos = WINDOW ? window_pos(s, it.b, len) : seq_pos(s, it.b, len);
     const int i0 = it.g * s.q_group, i1 = min(i0 + s.q_group, s.n_q) - 1;
-    const WindowUnits window(p, len, pos, i0, i1);
+    const WindowUnits window(rows_range(p, len, pos, i0, i1));
     const int seen = WINDOW ? window.near_end : group_seen(s, len, pos, it.g);
     const RowMask<WINDOW ? kWindow : kLists> hidden(p, row, window, nullptr, len, pos);
     const int n_units = WINDOW ? window.n : seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
@@ -883,7 +901,7 @@ inline hipError_t launch_window_bwd(const SelParams& p, const GradParams& g, int
     if (tile_rows == 128) launch_grad_queries<4, 1, F16, D, true>(p, g, stream);
     else if (tile_rows == 64) launch_grad_queries<2, 2, F16, D, true>(p, g, stream);
     else launch_grad_queries<1, 2, F16, D, true>(p, g, stream);
-    if (F16) launch_grad_head_bits(g, stream);
+    if (F16 && !g.window.own_bits) launch_grad_head_bits(g, stream);
     const WindowGradParams& w = g.window;
     hipLaunchKernelGGL((grad_keys_kernel<2, F16, D, true>), dim3((unsigned)(8 * w.per_xcd)), dim3(256), 0, stream, p, g);
     const int joined = w.near_parts > 1 ? w.tiles : w.first_parts > 1 ? w.first_tiles : 0;

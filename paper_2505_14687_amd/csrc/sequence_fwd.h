@@ -25,8 +25,10 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     __shared__ __attribute__((aligned(2 * kTile))) uint8_t lds[4][kTile];   // K, K, V, V
     __shared__ int32_t s_n;
     extern __shared__ int32_t s_units[];
-    const Item it(p);
+    Item it(p);
     if (it.idle(p)) return;
+    int part_units = 0;
+    if (WINDOW && !it.share(p, part_units)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int team = TEAMS == 1 ? 0 : wave / RW, row_wave = wave % RW;
     const int half = lane >> 5;
@@ -44,14 +46,14 @@ __global__ __launch_bounds__(RW * TEAMS * 64, RW * TEAMS == 2 ? 1 : 2) void sele
     __shared__ Tree s_tree[1];   // (not there where nothing refers to it)
     if constexpr (WALK == kTree) build_tree(s_tree[0], p, it.b, len - s.n_q);
     const int i0 = it.g * s.q_group, i1 = min(i0 + s.q_group, s.n_q) - 1;
-    const WindowUnits window = WALK == kTree ? WindowUnits(p, len) : WindowUnits(p, len, pos, i0, i1);
+    const WindowUnits window(WALK == kTree ? tree_range(p, len) : rows_range(p, len, pos, i0, i1));
     const int seen = WINDOW ? window.near_end : group_seen(s, len, pos, it.g);
     const RowMask<WALK> hidden(p, row, window, WALK == kTree ? s_tree : nullptr, len, pos);
 
     const int all_units = WINDOW ? window.n : seen > 0 ? list_units(p, it.list(p), seen, s_units, &s_n) : 0;
     int u_first = 0, n_units = all_units;
     if (p.splits > 1) {   // an even number of units a part
-        const int per = ((all_units + p.splits - 1) / p.splits + 1) & ~1;
+        const int per = part_units ? part_units : ((all_units + p.splits - 1) / p.splits + 1) & ~1;
         u_first = min(it.split * per, all_units);
         n_units = min(per, all_units - u_first);
     }
@@ -476,17 +478,23 @@ __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int til
     fdivmod(list, p.fd_groups, bh, g);
     fdivmod(bh, p.fd_kv_heads, b, h);
     const GroupRow row(p, (int)h, (int)g, (int)r);
-    const int64_t first = (((int64_t)list * p.row_tiles + r / tile_rows) * p.splits) * tile_rows + r % tile_rows;   // + split * tile_rows
+    int64_t first = (((int64_t)list * p.row_tiles + r / tile_rows) * p.splits) * tile_rows + r % tile_rows;   // + split * tile_rows
+    int parts = p.splits;
+    if (p.slots > 0) {   // (the lists are the K/V heads of the sequences)
+        const Parts share(p);
+        parts = __shfl(share.n, (int)b);
+        first = (((int64_t)h * p.row_tiles + r / tile_rows) * p.slots + __shfl(share.end, (int)b) - parts) * tile_rows + r % tile_rows;
+    }
     const float2* const ml = (const float2*)p.part_ml + first;
     const float4* const po = (const float4*)p.part_o + first * L + lane;
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = 0; i0 < p.splits; i0 += 8) {
+    for (int i0 = 0; i0 < parts; i0 += 8) {
         float2 v[8];
         float4 x[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int i = min(i0 + k, p.splits - 1);
+            const int i = min(i0 + k, parts - 1);
             v[k] = ml[(int64_t)i * tile_rows];
             x[k] = po[(int64_t)i * tile_rows * L];
         }
@@ -499,7 +507,7 @@ __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int til
         m = top;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float f = i0 + k < p.splits ? __builtin_amdgcn_exp2f((v[k].x - m) * p.scale_log2) : 0.f;
+            const float f = i0 + k < parts ? __builtin_amdgcn_exp2f((v[k].x - m) * p.scale_log2) : 0.f;
             l = fmaf(f, v[k].y, l);
             o = make_float4(fmaf(f, x[k].x, o.x), fmaf(f, x[k].y, o.y), fmaf(f, x[k].z, o.z), fmaf(f, x[k].w, o.w));
         }

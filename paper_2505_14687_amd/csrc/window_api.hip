@@ -98,6 +98,12 @@ grat_status make_forward(const grat_sequence* seq, float scale, int32_t window, 
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / items, 64));
     const int64_t per = std::max((steps + most - 1) / most, std::min<int64_t>(std::max<int64_t>((steps + 8) / 16, 1), 2));
     set_items(p, items, few ? (steps < 4 ? 1 : (int)std::min<int64_t>((steps + per - 1) / per, most)) : steps < 8 ? 1 : (int)std::min<int64_t>(steps / 2, most));
+    if (p.splits > 1 && s.k_len && s.batch <= 64 && s.n_groups == 1) {   // lengths of their own: parts of about equal length
+        p.slots = s.batch * p.splits;
+        p.part_keys = few ? keys / 4 : kUnit;
+        p.part_step = few ? 4 : 2;
+        p.fd_splits = make_fastdiv((uint32_t)p.slots);
+    }
     Scratch scratch{(uint8_t*)work};
     if (p.splits > 1) {
         p.part_o = scratch.take<float>((int64_t)p.items * plan.tile_rows * seq->head_dim);
@@ -176,6 +182,7 @@ grat_status make_gradient(const grat_sequence* seq, float scale, int32_t window,
         g.head_runs = s.n_groups * p.row_tiles * (plan.tile_rows / 32);
         g.row_bits = scratch.take<int32_t>(heads * g.head_runs);
         g.head_bits = scratch.take<int32_t>(heads);
+        w.own_bits = g.head_runs <= 512;
     }
     plan.work = scratch.bytes;
     *out = plan;

@@ -257,6 +257,17 @@ def test_peaked_weights(shape, dtype, gain, eight):
 
 
 @pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("B,N,M,tree", [(64, 1, 2500, False), (65, 1, 2500, False), (7, 40, 3000, True), (2, 3, 20000, False), (1, 1, 30000, False),
+                                        (3, 150, 2000, False)])
+def test_lengths_of_their_own(B, N, M, tree, eight):
+    """Sequences that share workgroups by their lengths: empty, short, as long as the cache; one more than share."""
+    gen = np.random.default_rng(B + N)
+    k_len = [int(n) for n in gen.integers(0, M + 1, B)]
+    k_len[0], k_len[-1] = min(M, 777), 0 if B > 2 else M // 3
+    run_case((B, 2, 1, N, M, None if N > 1 else 1800, 3 if N == 1 else 0, k_len, tree), "bf16", 64, eight, seed=360 + B)
+
+
+@pytest.mark.parametrize("eight", [False, True])
 def test_one_tree_for_all_sequences(eight):
     B, Hq, Hkv, N, M, d = 3, 4, 2, 9, 77, 64
     up = ints([-1, 0, 0, 1, 1, 2, 5, -1, 7])
