@@ -2,7 +2,7 @@
 // or over all keys.
 //
 // Bound by fetching K and V, which no other rows share.  A workgroup is four waves that take every fourth unit of the keys (or of a share of
-// them, `splits`) and wait for nothing but their own loads; each holds all of the workgroup's rows, 16 R of them.  The 16x16x32 instruction, with the rows as its columns:
+// them, `splits`) and wait for nothing but their own loads; each holds all of the workgroup's rows, 16 or 32.  The 16x16x32 instruction, with the rows as its columns:
 // T^T (16 keys x 16 rows) leaves lane (row r = lane % 16, g = lane / 16) with keys 16 m + 4 g + i, and Z^T[16 dims, row] += X'^T T is contracted over
 // 32 keys in that order: elements 0 .. 3 keys 4 g + i, 4 .. 7 keys 16 + 4 g + i.
 // A unit is 32 keys in 16 bits and 64 in 8, the same bytes: as soon as K's (or V's) has landed in LDS it is read into registers, and the next
@@ -16,8 +16,9 @@
 namespace grat {
 
 
-// Keys of a unit.
-constexpr int cache_keys(bool eight, int sets) { return eight && sets < 4 ? 64 : 32; }
+// Keys of a unit.  8 bits: 64, and where two workgroups of 32 rows read the same keys, 32, which leaves registers for two of them on a compute unit (head_dim 128;
+// 64 rows, 8 caches of 8 192 keys: 41.8 us against 57.1, and 52.7 in one workgroup of 64 rows, whose accumulators do not fit beside the rest).
+constexpr int cache_keys(bool eight, int head_dim, int row_tiles) { return eight && (head_dim < 128 || row_tiles == 1) ? 64 : 32; }
 
 // A wave's units of K and V, and its fragments in them.
 template <bool EIGHT, int D, int KEYS>
@@ -100,10 +101,10 @@ __device__ __forceinline__ frag8 widen(uint2 x) {
     return __builtin_bit_cast(frag8, make_uint4(w[0], w[1], w[2], w[3]));
 }
 
-template <int R, bool EIGHT, bool F16, int D, bool TREE>
-__global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_kernel(SelParams p) {
+template <int R, int KEYS, bool EIGHT, bool F16, int D, bool TREE>
+__global__ __launch_bounds__(256, R * KEYS * D > 64 * 128 ? 1 : 2) void cache_attention_kernel(SelParams p) {
     using E = Elem<F16>;
-    using W = CacheWave<EIGHT, D, cache_keys(EIGHT, R)>;
+    using W = CacheWave<EIGHT, D, KEYS>;
     using EV = Elem<F16 && !EIGHT>;   // of the weights and V
     using Out = NarrowWave<D>;
     constexpr int kLds = 4 * W::kBytes > 4 * 16 * D * 4 ? 4 * W::kBytes : 4 * 16 * D * 4;
@@ -133,7 +134,8 @@ __global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_k
     // what this lane's rows see, and what the workgroup's rows see together (all of the group's)
     RowSpan span[R];
     int line[TREE ? R : 1];   // trees: the row's line, in words
-    const auto [first_end, near, near_end] = uniform(TREE ? tree_range(p, len) : rows_range(p, len, pos, 0, s.n_q - 1));
+    const KeyRange keys = uniform(TREE ? tree_range(p, len) : rows_range(p, len, pos, 0, s.n_q - 1));
+    const int first_end = keys.first_end, near = keys.near;
     int least_first = 0x7fffffff, least_hi = 0x7fffffff, most_lo = 0;
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -161,7 +163,7 @@ __global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_k
     least_first = __builtin_amdgcn_readfirstlane(least_first);
     least_hi = __builtin_amdgcn_readfirstlane(least_hi);
     most_lo = __builtin_amdgcn_readfirstlane(most_lo);
-    const int first_units = (first_end + W::kKeys - 1) / W::kKeys, all_units = first_units + (max(near_end - near, 0) + W::kKeys - 1) / W::kKeys;
+    const int first_units = (first_end + W::kKeys - 1) / W::kKeys, all_units = keys.units(W::kKeys);
     int u_first = 0, n_units = all_units;
     if (p.splits > 1) {
         const int per = part_units ? part_units : ((all_units + p.splits - 1) / p.splits + 3) & ~3;   // (a unit of every wave at a time)
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_k
         m_ref[k] = -1e38f / fmaxf(cc, 1.f);   // (finite, so that a unit without a seen key weighs 0)
         l_run[k] = 0.f;
     }
-    const W w(p, it, lds + wave * W::kBytes, first_end, near_end, lane);
+    const W w(p, it, lds + wave * W::kBytes, first_end, keys.near_end, lane);
     frag8 kf[W::kM * (EIGHT ? W::kN / 2 : W::kN)], vf[EIGHT ? 1 : W::kDims];   // 8 bits: 16 numbers of K each
     uint2 v_raw[EIGHT ? W::kDims : 1][W::kM / 2];
     f32x4 k_scale[W::kM], v_scale[W::kM];
@@ -379,26 +381,27 @@ __global__ __launch_bounds__(256, EIGHT && R > 1 ? 1 : 2) void cache_attention_k
 }
 
 // 16 R rows a workgroup
-template <int R, bool EIGHT, bool F16, int D>
+template <int R, int KEYS, bool EIGHT, bool F16, int D>
 inline void launch_cache_sets(const SelParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)(8 * p.per_xcd));
-    if (p.parent) hipLaunchKernelGGL((cache_attention_kernel<R, EIGHT, F16, D, true>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((cache_attention_kernel<R, EIGHT, F16, D, false>), grid, dim3(256), 0, stream, p);
+    if (p.parent) hipLaunchKernelGGL((cache_attention_kernel<R, KEYS, EIGHT, F16, D, true>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((cache_attention_kernel<R, KEYS, EIGHT, F16, D, false>), grid, dim3(256), 0, stream, p);
 }
 
-// tile_rows: 16, 32; 64; 128, or 256 (head_dim 128)
+// tile_rows: 16, 32; 64 (16 bits); 128, or 256 (head_dim 128)
 template <bool F16, int D, int WALK, bool EIGHT>
 inline void launch_cache_tiles(const SelParams& p, int tile_rows, hipStream_t stream) {
     if constexpr (D == 128) {
         if (tile_rows == 256) launch_fwd_tile<8, 1, F16, D, WALK, EIGHT>(p, stream);
     }
     if (tile_rows == 128) launch_fwd_tile<4, 1, F16, D, WALK, EIGHT>(p, stream);
-    else if (tile_rows == 64) {
-        if constexpr (EIGHT) launch_cache_sets<4, true, F16, D>(p, stream);
-        else launch_fwd_tile<2, 2, F16, D, WALK>(p, stream);
+    if constexpr (!EIGHT) {
+        if (tile_rows == 64) launch_fwd_tile<2, 2, F16, D, WALK>(p, stream);
     }
-    else if (tile_rows == 32) launch_cache_sets<2, EIGHT, F16, D>(p, stream);
-    else if (tile_rows == 16) launch_cache_sets<1, EIGHT, F16, D>(p, stream);
+    constexpr int one = cache_keys(EIGHT, D, 1), two = cache_keys(EIGHT, D, 2);
+    if (tile_rows == 32 && p.row_tiles == 1) launch_cache_sets<2, one, EIGHT, F16, D>(p, stream);
+    else if (tile_rows == 32) launch_cache_sets<2, two, EIGHT, F16, D>(p, stream);
+    else if (tile_rows == 16) launch_cache_sets<1, one, EIGHT, F16, D>(p, stream);
 }
 
 template <bool F16, int D>

@@ -70,9 +70,9 @@ struct ForwardPlan {
 
 // Rows of a workgroup, of the `rows` of all heads that share a K/V head: one tile where they fit, else 256 if that makes four rounds of the chip, else 128 (windows of
 // 1 024, us in tiles of 256 and of 128: 32 768 tokens of 8 heads 614 and 598, 8 192 tokens 144 and 151; windows of 4 096 1 855 and 1 890, of 256 258 and 251).
-int fwd_tile_rows(const SeqShape& s, int head_dim) {
+int fwd_tile_rows(const SeqShape& s, int head_dim, bool eight) {
     const int64_t rows = (int64_t)s.n_q * s.share;
-    if (rows <= 64) return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    if (rows <= 64) return rows <= 16 ? 16 : rows <= 32 || eight ? 32 : 64;
     if (head_dim == 128 && rows > 128 && (rows <= 256 || (int64_t)s.batch * s.kv_heads * ((rows + 255) / 256) >= 1024)) return 256;
     return 128;
 }
@@ -85,17 +85,17 @@ grat_status make_forward(const grat_sequence* seq, float scale, int32_t window, 
     if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
     if (st != GRAT_OK) return st;
     if (tree && s.n_q > kMostDrafted) return GRAT_ERR_UNSUPPORTED;
-    plan.tile_rows = fwd_tile_rows(s, seq->head_dim);
-    const bool few = plan.tile_rows <= (eight ? 64 : 32);   // four waves that share the keys (cache_attn.h)
-    set_tiles(p, tree ? s.n_q * s.share : plan.tile_rows, plan.tile_rows);   // (a tree is one group)
+    plan.tile_rows = fwd_tile_rows(s, seq->head_dim, eight);
+    const bool few = plan.tile_rows <= 32;   // four waves that share the keys (cache_attn.h)
+    set_tiles(p, tree || few ? s.n_q * s.share : plan.tile_rows, plan.tile_rows);   // (these are one group)
     const int64_t items = (int64_t)s.batch * s.kv_heads * s.n_groups * p.row_tiles;
     if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
-    const int keys = few ? 4 * cache_keys(eight, plan.tile_rows / 16) : 64;   // of a workgroup's step
+    const int keys = few ? 4 * cache_keys(eight, seq->head_dim, p.row_tiles) : 64;   // of a workgroup's step
     const int64_t steps = (reach(p, s.q_group, s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys;
-    // A launch that leaves compute units idle has keys shared by several workgroups, up to one a compute unit.  Few rows: parts of one or two steps, about 16 of them,
+    // A launch that leaves compute units idle has keys shared by several workgroups, up to one a compute unit (two tiles of few rows: two).  Few rows: parts of one or two steps, about 16 of them,
     // or of more where that fills the chip; 4 steps or more (one token on 8 heads, us, in parts of 2 steps and by this rule: 17 steps 11.9 and 10.8, 8 steps
     // 10.3 and 9.3, 32 steps 12.3 both, in parts of one 13.4; 2 steps 7.5 in one part).  Many rows: 2 steps or more, as lists have them.
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / items, 64));
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>((few && p.row_tiles > 1 ? 512 : 256) / items, 64));
     const int64_t per = std::max((steps + most - 1) / most, std::min<int64_t>(std::max<int64_t>((steps + 8) / 16, 1), 2));
     set_items(p, items, few ? (steps < 4 ? 1 : (int)std::min<int64_t>((steps + per - 1) / per, most)) : steps < 8 ? 1 : (int)std::min<int64_t>(steps / 2, most));
     if (p.splits > 1 && s.k_len && s.batch <= 64 && s.n_groups == 1) {   // lengths of their own: parts of about equal length
