@@ -35,7 +35,7 @@ extern "C" {
  * batch * kv_heads, q_heads <= 65535; batch * q_heads * n_q < 2^29; batch * kv_heads * n_k < 2^28; sinks <= 2^20 where that is below n_k.
  * Scores, reference maximum, sum and output accumulate in fp32; the weights are rounded to the element type (nearest-even) for the product
  * with V, their sum is not.  Rows are worked on together, 32 to 256 of neighbouring positions and of the heads that share a K/V head: a NaN or infinite V that one of
- * them sees reaches all of them (0 * NaN).  Keys that none of them sees are never read.
+ * them sees can reach all of them (0 * NaN).  Keys that none of them sees are never read.
  */
 int64_t grat_window_attention_work(const grat_sequence* seq, int32_t window, int32_t sinks, int32_t backward);
 grat_status grat_window_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K, const grat_tensor* V,
@@ -60,6 +60,7 @@ grat_status grat_window_attention_bwd(const grat_sequence* seq, const grat_tenso
  * Caches in 8 bits.  Of each row (one token of one K/V head) the head_dim numbers x are kept as e4m3 values (1 + 4 + 3 bits, largest 448, no
  * infinity), one byte each, rounded to nearest-even from x / s, beside s, one float a row: the least power of two with max |x| <= 448 s,
  * at least 2^-126, over the finite x; 1 for a row of zeros.  NaN and infinities become NaN.  A value is off by at most 2^-4 of itself, or 2^-10 s.
+ * (GRAT_F16: 240 2^8 is the largest that a number below 65 520 becomes: 256 2^8 would be infinite when it is read back.)
  * grat_cache_read and grat_cache_attention_fwd take any finite scale.
  *   The cache's grat_tensor is in bytes (strides in elements of one byte, as its pointer multiples of 16); a scale's (b, h, n) at data +
  *   b*stride_b + h*stride_h + n*stride_n floats, strides >= 0 and below 2^46, stride_n >= 1 and below 2^24; scales that are written as in grat_sequence.h.
@@ -99,9 +100,11 @@ grat_status grat_cache_read(grat_dtype dtype, int32_t batch, int32_t heads, int3
  *   window, sinks, O, d_lse, scale   as for grat_window_attention_fwd
  *   d_work     scratch memory of grat_cache_attention_work(seq, window, sinks, eight) bytes, eight: caches in 8 bits; 16-byte aligned
  * Supported: as grat_window_attention_fwd; trees: n_q <= 256.  For few rows (n_q * q_heads / kv_heads up to a few hundred); more are correct, but
- * every 64 rows read the cache anew.
- * Arithmetic as there; in 8 bits the weights times V's scales are rounded to bfloat16 (also with GRAT_F16).  A NaN or infinite V that one of 64
- * rows sees reaches all of them.
+ * every 128 or 256 rows read the cache anew.
+ * Arithmetic as there.  8 bits, up to 64 rows a K/V head: K's scale is taken to the scores in fp32, and the weights times V's scales are rounded to
+ * bfloat16 (also with GRAT_F16).  More rows: values times scales are rounded to seq->dtype first (scales that are powers of two leave bfloat16 nothing to
+ * round; half saturates at 65 504), and the weights as there.  A NaN or infinite V that one of a sequence's new tokens sees
+ * can reach all of them (0 * NaN).
  */
 int64_t grat_cache_attention_work(const grat_sequence* seq, int32_t window, int32_t sinks, int32_t eight);
 grat_status grat_cache_attention_fwd(const grat_sequence* seq, const grat_tensor* Q, const grat_tensor* K_cache, const grat_tensor* V_cache,

@@ -52,8 +52,9 @@ def e4m3(x):
     return np.where(fine, np.rint(v / step) * step, np.nan)
 
 
-def quantise(x):
-    """(values, scales) of rows in 8 bits: the least power of two, from 2^-126 on, with max |x| <= 448 s; 1 for rows of zeros."""
+def quantise(x, half=False):
+    """(values, scales) of rows in 8 bits: the least power of two, from 2^-126 on, with max |x| <= 448 s; 1 for rows of zeros.  Of half: what would become
+    256 2^8, which half does not hold, 240 2^8."""
     x = np.asarray(x, dtype=np.float64)
     most = np.where(np.isfinite(x), np.abs(x), 0.0).max(-1)
     power = np.zeros(most.shape, dtype=np.int64)
@@ -63,4 +64,6 @@ def quantise(x):
             while most[at] > 448 * 2.0 ** power[at]:
                 power[at] += 1
     s = 2.0 ** power
+    if half:
+        x = np.where((s[..., None] == 256) & (np.abs(x) < 65520), np.clip(x, -240 * 256, 240 * 256), x)
     return e4m3(x / s[..., None]), s

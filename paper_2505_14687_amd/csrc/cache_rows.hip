@@ -3,6 +3,7 @@
 // A row of head_dim numbers x is kept as e4m3 values of x / s and s, the least power of two with max |x| <= 448 s: as e4m3 is a floating format
 // itself, a finer s would gain nothing, and with this one the division and the way back are exact.  Memory (for few tokens the launch) bounds both directions.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_rows.h"
 #include "rotary_pairs.h"
@@ -128,6 +129,16 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RotaryParams p, SeqTe
                 most = row_max(most, p.items);
                 const int power = row_power(most);
                 const float inv = ldexpf(1.f, -power);
+                if constexpr (std::is_same_v<T, _Float16>) {   // what half holds stays finite when it is read back: 256 2^8 would not
+                    if (power == 8) {
+                        const float top = 240.f * 256.f;
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            u[e] = fabsf(u[e]) < 65520.f ? fminf(fmaxf(u[e], -top), top) : u[e];
+                            v[e] = fabsf(v[e]) < 65520.f ? fminf(fmaxf(v[e], -top), top) : v[e];
+                        }
+                    }
+                }
                 uint32_t wu[V / 4], wv[V / 4];
 #pragma unroll
                 for (int k = 0; k < V / 4; ++k) {

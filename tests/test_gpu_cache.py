@@ -62,7 +62,7 @@ def test_rows_are_the_oracles(dtype, d, where):
     start = [20, -5]                                                  # the first sequence's last rows, the second's first are outside
     assert grat.grat_cache_append(None, K, V, None, kc, vc, ints(start), K_scale=ks, V_scale=vs) is None
     for x, c, s in ((K, kc, ks), (V, vc, vs)):
-        values, scales = orc.quantise(f64(x))
+        values, scales = orc.quantise(f64(x), dtype == "f16")
         got, got_s = f64(c.float()), f64(s)
         want, want_s = np.full_like(got, np.nan), np.full_like(got_s, np.nan)
         for b in range(B):
@@ -288,6 +288,22 @@ def test_one_tree_for_all_sequences(eight):
     Ow, _, bO, _, _, _ = bounds(f64(Q), f64(X), f64(X), 0.1, np.repeat(see[:, None], Hkv, 1), "bf16")
     for up in (None, ints(line)):
         within(f64(grat.grat_cache_attention_fwd(Q, c, c, 0.1, parent=up, window=20, sinks=2, **a)), Ow, bO + 8 * EPS * np.abs(f64(X)).max(), "O")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_scales_of_any_value_and_many_rows(dtype):
+    """More than 64 rows: the values that the cache stands for are rounded to the tensors' type first (half saturates)."""
+    B, H, M, N, d = 1, 2, 500, 70, 128
+    gen = torch.Generator().manual_seed(337)
+    c = [torch.randn((B, H, M, d), generator=gen).to(EIGHT).cuda() for _ in range(2)]
+    s = [(0.1 + torch.rand((B, H, M), generator=gen)).cuda() for _ in range(2)]
+    s[1][:, :, 3] = 3e4
+    K, V = (f64((x.float() * y[..., None]).clamp(-65504, 65504).to(TYPES[dtype])) if dtype == "f16" else f64((x.float() * y[..., None]).to(TYPES[dtype]))
+            for x, y in zip(c, s))
+    Q = normal((B, 4, N, d), dtype, 338)
+    O = grat.grat_cache_attention_fwd(Q, *c, 0.09, K_scale=s[0], V_scale=s[1])
+    Ow, _, bO, _, _, _ = bounds(f64(Q), K, V, 0.09, np.repeat(orc.window_seen(N, M, B)[:, None], H, 1), dtype)
+    within(f64(O), Ow, bO, "O")
 
 
 def test_scales_of_any_value():

@@ -35,6 +35,8 @@ PROMPTS = [
     (1, 16, 1, 33, 1000, 500, 4, [999], None, True),
     (1, 2, 2, 700, 700, 2000, 900, None, None, True),              # a window longer than the sequence, first keys as many
     (1, 80, 2, 40, 90, 50, 33, [90], None, True),                  # 40 heads to a K/V head
+    (1, 150, 1, 9, 70, 20, 2, None, None, True),                   # more heads to a K/V head than a row tile has
+    (1, 150, 1, 9, 70, 20, 0, [70], [64], False),                  # ... both directions, positions behind the last key
 ]
 
 
