@@ -68,12 +68,25 @@ struct ForwardPlan {
     int64_t work = 0;
 };
 
+// Prompts that tiles of 128 rows would spread over the chip about once, and whose rows see few keys: tiles of 64, whose two teams take half of the keys each.  us with tiles
+// of 128 and of 64, forward of 8 heads on as many (16 tiles of 128 rows for 2 048 tokens of one):
+//   window 129, 2 047 tokens of 1 to 4 sequences   head_dim 64   11.0 8.5   11.7 10.2   14.6 11.8   14.9 13.4   (training step 47.0 38.5   52.5 47.3   67.0 58.8   71.8 74.6)
+//                                                  head_dim 128  13.3 11.7   14.0 14.1   18.4 21.5   19.3 24.9   (62.2 53.8   74.8 71.4   92.4 99.0   108 123)
+//   2 048 tokens, window 1 500, 2 000, 2 500       head_dim 64   25.9 21.9   29.5 26.9   32.8 32.1   head_dim 128  34.4 31.6   38.1 39.1   41.9 46.5
+bool few_tiles(const SelParams& p, int head_dim) {
+    const SeqShape& s = p.s;
+    const int64_t tiles = (int64_t)s.batch * s.kv_heads * (((int64_t)s.n_q * s.share + 127) / 128);
+    return tiles <= (head_dim == 64 ? 384 : 256) && reach(p, 128, s.n_k) <= (head_dim == 64 ? 40 : 24) * 64;
+}
+
 // Rows of a workgroup, of the `rows` of all heads that share a K/V head: one tile where they fit, else 256 if that makes four rounds of the chip, else 128 (windows of
 // 1 024, us in tiles of 256 and of 128: 32 768 tokens of 8 heads 614 and 598, 8 192 tokens 144 and 151; windows of 4 096 1 855 and 1 890, of 256 258 and 251).
-int fwd_tile_rows(const SeqShape& s, int head_dim, bool eight) {
+int fwd_tile_rows(const SelParams& p, int head_dim, bool eight) {
+    const SeqShape& s = p.s;
     const int64_t rows = (int64_t)s.n_q * s.share;
     if (rows <= 64) return rows <= 16 ? 16 : rows <= 32 || eight ? 32 : 64;
     if (head_dim == 128 && rows > 128 && (rows <= 256 || (int64_t)s.batch * s.kv_heads * ((rows + 255) / 256) >= 1024)) return 256;
+    if (!eight && few_tiles(p, head_dim)) return 64;
     return 128;
 }
 
@@ -85,7 +98,7 @@ grat_status make_forward(const grat_sequence* seq, float scale, int32_t window, 
     if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
     if (st != GRAT_OK) return st;
     if (tree && s.n_q > kMostDrafted) return GRAT_ERR_UNSUPPORTED;
-    plan.tile_rows = fwd_tile_rows(s, seq->head_dim, eight);
+    plan.tile_rows = fwd_tile_rows(p, seq->head_dim, eight);
     const bool few = plan.tile_rows <= 32;   // four waves that share the keys (cache_attn.h)
     set_tiles(p, tree || few ? s.n_q * s.share : plan.tile_rows, plan.tile_rows);   // (these are one group)
     const int64_t items = (int64_t)s.batch * s.kv_heads * s.n_groups * p.row_tiles;
@@ -137,9 +150,10 @@ struct GradPlan {
     int64_t work = 0;
 };
 
-int bwd_tile_rows(const SeqShape& s) {
+int bwd_tile_rows(const SelParams& p, int head_dim) {
+    const SeqShape& s = p.s;
     const int64_t rows = (int64_t)s.n_q * s.share;
-    return rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    return rows <= 32 ? 32 : rows <= 64 || few_tiles(p, head_dim) ? 64 : 128;
 }
 
 grat_status make_gradient(const grat_sequence* seq, float scale, int32_t window, int32_t sinks, void* work, GradPlan* out) {
@@ -152,7 +166,7 @@ grat_status make_gradient(const grat_sequence* seq, float scale, int32_t window,
     if (st == GRAT_OK) st = set_window(p, scale, window, sinks);
     if (st != GRAT_OK) return st;
     const int64_t D = seq->head_dim, heads = (int64_t)s.batch * s.kv_heads;
-    plan.tile_rows = bwd_tile_rows(s);
+    plan.tile_rows = bwd_tile_rows(p, (int)D);
     set_tiles(p, plan.tile_rows, plan.tile_rows);
     const int64_t items = heads * s.n_groups * p.row_tiles;
     if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
