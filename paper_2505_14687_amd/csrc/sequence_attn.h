@@ -321,22 +321,108 @@ constexpr int kMostDrafted = 256, kTreeWords = 10;   // tokens of a tree; words 
 struct Tree {
     int32_t parent[kMostDrafted], depth[kMostDrafted];
     uint32_t lines[kMostDrafted * kTreeWords];
+    int32_t deep[10];
 };
-__device__ __forceinline__ void build_tree(Tree& tree, const SelParams& p, int b, int base) {   // by at least kMostDrafted threads; ends with a barrier
-    const int n = p.s.n_q, t = (int)threadIdx.x;
+// Lines are doubled, of all tokens at once: round k knows the 2^k tokens from a token upward, and the one above these.  Within a window a line's tokens are gathered by
+// the bits of its length.  Up to 64 tokens by each wave for itself, more through LDS.  (One token upward after the other a line of 256 tokens took 40 us and one of 64 ten;
+// now 6 and two.)
+__device__ __forceinline__ void build_small_tree(Tree& tree, const SelParams& p, int b, int base) {
+    const int n = p.s.n_q, t = (int)(threadIdx.x & 63);
+    const bool limited = p.window < n;
+    int up = -1, from = t;   // above the line so far, above `near`
     if (t < n) {
-        const int up = p.parent[b * p.parent_stride_b + t];
-        tree.parent[t] = up >= 0 && up < t ? up : -1;
-        for (int w = 0; w < kTreeWords; ++w) tree.lines[t * kTreeWords + w] = 0;
+        up = p.parent[b * p.parent_stride_b + t];
+        if (up < 0 || up >= t) up = -1;
+    }
+    int depth = up >= 0;
+    uint64_t line = 1ull << t, near = 0;
+    for (int k = 0;; ++k) {   // (ends at 2^k >= n at the latest: a parent lies ahead of its child)
+        const bool last = __builtin_amdgcn_ballot_w64(up >= 0) == 0;
+        if (limited && (last ? p.window >> k : p.window >> k & 1)) {
+            const uint64_t x = __shfl(line, max(from, 0));
+            const int above = __shfl(up, max(from, 0));
+            near |= from >= 0 ? x : 0;
+            from = from >= 0 ? above : -1;
+        }
+        if (last) break;
+        const uint64_t x = __shfl(line, max(up, 0));
+        const int d = __shfl(depth, max(up, 0)), above = __shfl(up, max(up, 0));
+        line |= up >= 0 ? x : 0;
+        depth += up >= 0 ? d : 0;
+        up = up >= 0 ? above : -1;
+    }
+    if (limited) line = near | (line & __builtin_amdgcn_ballot_w64(base + depth < p.sinks));   // (tokens that stay visible for their positions)
+    if (threadIdx.x < 64 && t < n) {
+        uint32_t* const to = tree.lines + t * kTreeWords;
+        to[0] = (uint32_t)line;
+        to[1] = (uint32_t)(line >> 32);
+#pragma unroll
+        for (int w = 2; w < kTreeWords; ++w) to[w] = 0;
+        tree.depth[t] = depth;
+    }
+    __syncthreads();
+}
+__device__ __forceinline__ void build_tree(Tree& tree, const SelParams& p, int b, int base) {   // by at least kMostDrafted threads; ends with a barrier
+    if (p.s.n_q <= 64) return build_small_tree(tree, p, b, base);
+    constexpr int kWords = kTreeWords - 2;
+    const int n = p.s.n_q, t = (int)threadIdx.x, words = (n + 31) >> 5;
+    const bool limited = p.window < n;
+    uint32_t line[kWords], near[kWords];
+    int up = -1, from = t < n ? t : -1;   // above the line so far, above `near`
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        line[w] = t >> 5 == w ? 1u << (t & 31) : 0;
+        near[w] = 0;
+    }
+    if (t < 10) tree.deep[t] = 0;
+    if (t < n) {
+        up = p.parent[b * p.parent_stride_b + t];
+        if (up < 0 || up >= t) up = -1;
+        for (int w = words; w < kTreeWords; ++w) tree.lines[t * kTreeWords + w] = 0;
+    }
+    int depth = up >= 0;
+    __syncthreads();
+    for (int k = 0;; ++k) {   // (ends at 2^k >= n at the latest: a parent lies ahead of its child)
+        if (t < n) {
+            tree.parent[t] = up;
+            tree.depth[t] = depth;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w)
+                if (w < words) tree.lines[t * kTreeWords + w] = line[w];
+            if (up >= 0) tree.deep[k] = 1;
+        }
+        __syncthreads();
+        const bool last = tree.deep[k] == 0;
+        if (limited && (last ? p.window >> k : p.window >> k & 1) && from >= 0) {
+#pragma unroll
+            for (int w = 0; w < kWords; ++w)
+                if (w < words) near[w] |= tree.lines[from * kTreeWords + w];
+            from = tree.parent[from];
+        }
+        if (last) break;
+        if (up >= 0) {
+#pragma unroll
+            for (int w = 0; w < kWords; ++w)
+                if (w < words) line[w] |= tree.lines[up * kTreeWords + w];
+            depth += tree.depth[up];
+            up = tree.parent[up];
+        }
+        __syncthreads();
+    }
+    if (!limited) return;
+    if (p.sinks > base) {   // tokens that stay visible for their positions
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+            uint32_t shallow = 0;
+            for (int a = 32 * w; a < min(n, 32 * w + 32); ++a) shallow |= (uint32_t)(base + tree.depth[a] < p.sinks) << (a & 31);
+            near[w] |= line[w] & shallow;
+        }
     }
     __syncthreads();
     if (t < n) {
-        int depth = 0;
-        for (int a = tree.parent[t]; a >= 0; a = tree.parent[a]) ++depth;   // (a parent lies ahead of its child: the walk ends)
-        tree.depth[t] = depth;
-        int at = depth;   // of the token that is looked at
-        for (int a = t; a >= 0; a = tree.parent[a], --at)
-            if (depth - at < p.window || base + at < p.sinks) tree.lines[t * kTreeWords + (a >> 5)] |= 1u << (a & 31);
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+            if (w < words) tree.lines[t * kTreeWords + w] = near[w];
     }
     __syncthreads();
 }

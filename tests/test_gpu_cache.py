@@ -215,10 +215,11 @@ def fill(x, see, eight):
     return c, s, grat.grat_cache_read(c, s, torch.float32)
 
 
-def run_case(shape, dtype, d, eight, seed=300, gain=1.0):
+def run_case(shape, dtype, d, eight, seed=300, gain=1.0, up=None):
     B, Hq, Hkv, N, M, window, sinks, k_len, tree = shape
     gen = np.random.default_rng(seed)
-    up = parents(gen, B, N) if tree else None
+    if tree and up is None:
+        up = parents(gen, B, N)
     see = orc.tree_seen(up, M, window, sinks, k_len) if tree else orc.window_seen(N, M, B, window, sinks, True, k_len)
     Q = normal((B, Hq, N, d), dtype, seed, "tokens", gain)
     kc, ks, K = fill(normal((B, Hkv, M, d), dtype, seed + 1, "heads"), see, eight)
@@ -265,6 +266,16 @@ def test_lengths_of_their_own(B, N, M, tree, eight):
     k_len = [int(n) for n in gen.integers(0, M + 1, B)]
     k_len[0], k_len[-1] = min(M, 777), 0 if B > 2 else M // 3
     run_case((B, 2, 1, N, M, None if N > 1 else 1800, 3 if N == 1 else 0, k_len, tree), "bf16", 64, eight, seed=360 + B)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("N,window,sinks,k_len", [(256, None, 0, 300), (256, 255, 0, 256), (256, 100, 0, 300), (256, 1, 0, 270), (256, 7, 30, 266), (200, 64, 250, 310),
+                                                  (65, 63, 0, 80), (64, 64, 0, 64), (64, 3, 5, 61), (33, 32, 0, 33), (2, 1, 0, 9), (2, 1, 9, 9)])
+def test_trees_of_long_lines(N, window, sinks, k_len, eight):
+    """One line of N tokens, and one of two branches that leave it half way."""
+    up = np.arange(N)[None].repeat(2, 0) - 1
+    up[1, N // 2 + 1:] = np.maximum(np.arange(N // 2 + 1, N) - 2, N // 2)
+    run_case((2, 2, 1, N, 320, window, sinks, [k_len, k_len], True), "bf16", 64, eight, seed=340, up=up)
 
 
 @pytest.mark.parametrize("eight", [False, True])
