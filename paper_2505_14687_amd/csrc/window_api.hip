@@ -107,10 +107,11 @@ grat_status make_forward(const grat_sequence* seq, float scale, int32_t window, 
     const int64_t steps = (reach(p, s.q_group, s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys;
     // A launch that leaves compute units idle has keys shared by several workgroups, up to one a compute unit (two tiles of few rows: two).  Few rows: parts of one or two steps, about 16 of them,
     // or of more where that fills the chip; 4 steps or more (one token on 8 heads, us, in parts of 2 steps and by this rule: 17 steps 11.9 and 10.8, 8 steps
-    // 10.3 and 9.3, 32 steps 12.3 both, in parts of one 13.4; 2 steps 7.5 in one part).  Many rows: 2 steps or more, as lists have them.
+    // 10.3 and 9.3, 32 steps 12.3 both, in parts of one 13.4; 2 steps 7.5 in one part).  Many rows, whose parts' results weigh as much as their keys do:
+    // 2 steps or more up to 8 parts, 4 or more beyond (64 rows over 4 000 keys in 31 and in 15 parts 19.0 and 16.9, 96 rows 21.1 and 19.1; 120 rows over 1 015 in 8 and 4 12.7 and 13.7).
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>((few && p.row_tiles > 1 ? 512 : 256) / items, 64));
     const int64_t per = std::max((steps + most - 1) / most, std::min<int64_t>(std::max<int64_t>((steps + 8) / 16, 1), 2));
-    set_items(p, items, few ? (steps < 4 ? 1 : (int)std::min<int64_t>((steps + per - 1) / per, most)) : steps < 8 ? 1 : (int)std::min<int64_t>(steps / 2, most));
+    set_items(p, items, few ? (steps < 4 ? 1 : (int)std::min<int64_t>((steps + per - 1) / per, most)) : steps < 8 ? 1 : (int)std::min<int64_t>(steps < 32 ? std::min<int64_t>(steps / 2, 8) : steps / 4, most));
     if (p.splits > 1 && s.k_len && s.batch <= 64 && s.n_groups == 1) {   // lengths of their own: parts of about equal length
         p.slots = s.batch * p.splits;
         p.part_keys = few ? keys / 4 : kUnit;
