@@ -5,7 +5,7 @@
 // them, `splits`) and wait for nothing but their own loads; each holds all of the workgroup's rows, 16 or 32.  The 16x16x32 instruction, with the rows as its columns:
 // T^T (16 keys x 16 rows) leaves lane (row r = lane % 16, g = lane / 16) with keys 16 m + 4 g + i, and Z^T[16 dims, row] += X'^T T is contracted over
 // 32 keys in that order: elements 0 .. 3 keys 4 g + i, 4 .. 7 keys 16 + 4 g + i.
-// A unit is 32 keys in 16 bits and 64 in 8, the same bytes: as soon as K's (or V's) has landed in LDS it is read into registers, and the next
+// A unit is 32 keys, or 64: as soon as K's (or V's) has landed in LDS it is read into registers, and the next
 // one's loads go out into the same place.
 // 8 bits: e4m3 values become the 16-bit type of the product in registers, without loss.  A row's scale is taken to the score of its K in fp32, and to the weight of
 // its V ahead of the weight's rounding.  Weights times scales may leave half's range, so they and V are bfloat16 there, whatever Q is: 2^-9 of a weight
@@ -15,10 +15,10 @@
 
 namespace grat {
 
-
-// Keys of a unit.  8 bits: 64, and where two workgroups of 32 rows read the same keys, 32, which leaves registers for two of them on a compute unit (head_dim 128;
-// 64 rows, 8 caches of 8 192 keys: 41.8 us against 57.1, and 52.7 in one workgroup of 64 rows, whose accumulators do not fit beside the rest).
-constexpr int cache_keys(bool eight, int head_dim, int row_tiles) { return eight && (head_dim < 128 || row_tiles == 1) ? 64 : 32; }
+// Keys of a unit: 32, and 64 in 8 bits at head_dim 64, for chains (32 caches of 8 192 keys, a token each 51 us
+// against 57, 8 tokens of 16 caches 34 against 38; but trees of 8 tokens 45 against 39, and at head_dim 128, where two workgroups of 32 rows then share a compute unit,
+// a token each 98 against 94, trees of 8 tokens 63 against 58).
+constexpr int cache_keys(bool eight, int head_dim, bool tree) { return eight && head_dim == 64 && !tree ? 64 : 32; }
 
 // A wave's units of K and V, and its fragments in them.
 template <bool EIGHT, int D, int KEYS>
@@ -102,7 +102,7 @@ __device__ __forceinline__ frag8 widen(uint2 x) {
 }
 
 template <int R, int KEYS, bool EIGHT, bool F16, int D, bool TREE>
-__global__ __launch_bounds__(256, R * KEYS * D > 64 * 128 ? 1 : 2) void cache_attention_kernel(SelParams p) {
+__global__ __launch_bounds__(256, 2) void cache_attention_kernel(SelParams p) {
     using E = Elem<F16>;
     using W = CacheWave<EIGHT, D, KEYS>;
     using EV = Elem<F16 && !EIGHT>;   // of the weights and V
@@ -319,6 +319,11 @@ __global__ __launch_bounds__(256, R * KEYS * D > 64 * 128 ? 1 : 2) void cache_at
         int next = unit_start(wave);
         w.fetch_k(next);
         w.fetch_v(next);
+        // (Q has landed: left to itself the compiler, which does not know of the loads into LDS, has its first use in the loop wait for all of them, in every step)
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+#pragma unroll
+            for (int ks = 0; ks < W::kN; ++ks) asm volatile("" : "+v"(qf[k][ks]));
         for (int i = wave; i < n_units; i += 4) {
             const int start = next;
             const bool more = i + 4 < n_units, first = start < first_end;
@@ -381,11 +386,11 @@ __global__ __launch_bounds__(256, R * KEYS * D > 64 * 128 ? 1 : 2) void cache_at
 }
 
 // 16 R rows a workgroup
-template <int R, int KEYS, bool EIGHT, bool F16, int D>
+template <int R, bool EIGHT, bool F16, int D>
 inline void launch_cache_sets(const SelParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)(8 * p.per_xcd));
-    if (p.parent) hipLaunchKernelGGL((cache_attention_kernel<R, KEYS, EIGHT, F16, D, true>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((cache_attention_kernel<R, KEYS, EIGHT, F16, D, false>), grid, dim3(256), 0, stream, p);
+    if (p.parent) hipLaunchKernelGGL((cache_attention_kernel<R, cache_keys(EIGHT, D, true), EIGHT, F16, D, true>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((cache_attention_kernel<R, cache_keys(EIGHT, D, false), EIGHT, F16, D, false>), grid, dim3(256), 0, stream, p);
 }
 
 // tile_rows: 16, 32; 64 (16 bits); 128, or 256 (head_dim 128)
@@ -398,10 +403,8 @@ inline void launch_cache_tiles(const SelParams& p, int tile_rows, hipStream_t st
     if constexpr (!EIGHT) {
         if (tile_rows == 64) launch_fwd_tile<2, 2, F16, D, WALK>(p, stream);
     }
-    constexpr int one = cache_keys(EIGHT, D, 1), two = cache_keys(EIGHT, D, 2);
-    if (tile_rows == 32 && p.row_tiles == 1) launch_cache_sets<2, one, EIGHT, F16, D>(p, stream);
-    else if (tile_rows == 32) launch_cache_sets<2, two, EIGHT, F16, D>(p, stream);
-    else if (tile_rows == 16) launch_cache_sets<1, one, EIGHT, F16, D>(p, stream);
+    if (tile_rows == 32) launch_cache_sets<2, EIGHT, F16, D>(p, stream);
+    else if (tile_rows == 16) launch_cache_sets<1, EIGHT, F16, D>(p, stream);
 }
 
 template <bool F16, int D>

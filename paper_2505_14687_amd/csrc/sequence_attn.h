@@ -322,6 +322,7 @@ struct Tree {
     int32_t parent[kMostDrafted], depth[kMostDrafted];
     uint32_t lines[kMostDrafted * kTreeWords];
     int32_t deep[10];
+    uint32_t shallow[kTreeWords - 2];
 };
 // Lines are doubled, of all tokens at once: round k knows the 2^k tokens from a token upward, and the one above these.  Within a window a line's tokens are gathered by
 // the bits of its length.  Up to 64 tokens by each wave for itself, more through LDS.  (One token upward after the other a line of 256 tokens took 40 us and one of 64 ten;
@@ -410,19 +411,16 @@ __device__ __forceinline__ void build_tree(Tree& tree, const SelParams& p, int b
         __syncthreads();
     }
     if (!limited) return;
-    if (p.sinks > base) {   // tokens that stay visible for their positions
-#pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-            uint32_t shallow = 0;
-            for (int a = 32 * w; a < min(n, 32 * w + 32); ++a) shallow |= (uint32_t)(base + tree.depth[a] < p.sinks) << (a & 31);
-            near[w] |= line[w] & shallow;
-        }
+    const uint64_t shallow = __builtin_amdgcn_ballot_w64(base + depth < p.sinks);   // tokens that stay visible for their positions
+    if ((t & 63) == 0 && t < 32 * kWords) {
+        tree.shallow[t >> 5] = (uint32_t)shallow;
+        tree.shallow[(t >> 5) + 1] = (uint32_t)(shallow >> 32);
     }
     __syncthreads();
     if (t < n) {
 #pragma unroll
         for (int w = 0; w < kWords; ++w)
-            if (w < words) tree.lines[t * kTreeWords + w] = near[w];
+            if (w < words) tree.lines[t * kTreeWords + w] = near[w] | (line[w] & tree.shallow[w]);
     }
     __syncthreads();
 }

@@ -79,13 +79,22 @@ bool few_tiles(const SelParams& p, int head_dim) {
     return tiles <= (head_dim == 64 ? 384 : 256) && reach(p, 128, s.n_k) <= (head_dim == 64 ? 40 : 24) * 64;
 }
 
-// Rows of a workgroup, of the `rows` of all heads that share a K/V head: one tile where they fit, else 256 if that makes four rounds of the chip, else 128 (windows of
-// 1 024, us in tiles of 256 and of 128: 32 768 tokens of 8 heads 614 and 598, 8 192 tokens 144 and 151; windows of 4 096 1 855 and 1 890, of 256 258 and 251).
+// Rows of a workgroup, of the `rows` of all heads that share a K/V head.
+// 16 and 32: the kernel of few rows, whose tiles each fetch all of the head's keys; so rows that see much the same keys, few of them (64; 96 in 8 bits) or with few keys.  us
+// in tiles of 64 to 256 rows and of 32, 32 heads on 8: 64 rows over 4 000 keys 16 bits 17.1 15.4, 16 sequences over 8 192 112 108, head_dim 64 13.3 11.9 and 65.8 56.8;
+// 96 rows of 16 sequences over 4 096 8 bits 65.3 56.8, 16 bits 64.1 80.6; 256 rows over 4 096 8 bits 29.2 21.8, 16 bits 27.9 21.7, head_dim 64 18.5 15.5; of 4 sequences
+// 35.8 38.3, 35.5 35.3, 25.6 25.6; 128 rows of 4 sequences over 8 192, 16 bits, 40.1 48.5, head_dim 64 25.3 24.9.
+// 256 if that is one tile or makes four rounds of the chip, else 128 (windows of 1 024, us in tiles of 256 and of 128: 32 768 tokens of 8 heads 614 and 598, 8 192 tokens
+// 144 and 151; windows of 4 096 1 855 and 1 890, of 256 258 and 251).
 int fwd_tile_rows(const SelParams& p, int head_dim, bool eight) {
     const SeqShape& s = p.s;
-    const int64_t rows = (int64_t)s.n_q * s.share;
-    if (rows <= 64) return rows <= 16 ? 16 : rows <= 32 || eight ? 32 : 64;
-    if (head_dim == 128 && rows > 128 && (rows <= 256 || (int64_t)s.batch * s.kv_heads * ((rows + 255) / 256) >= 1024)) return 256;
+    const int64_t rows = (int64_t)s.n_q * s.share, tiles = (rows + 31) / 32, heads = (int64_t)s.batch * s.kv_heads;
+    const bool alike = p.window / 4 >= s.n_q;
+    const int64_t keys = heads * tiles * reach(p, s.n_q, s.n_k);   // that tiles of 32 rows fetch
+    if (rows <= 32) return rows <= 16 ? 16 : 32;
+    if ((rows <= 64 && eight) || (alike && (rows <= (eight ? 96 : 64) || (rows <= 256 && keys <= (head_dim == 64 ? 1 << 20 : 1 << 19))))) return 32;
+    if (rows <= 64) return 64;
+    if (head_dim == 128 && rows > 128 && (rows <= 256 || heads * ((rows + 255) / 256) >= 1024)) return 256;
     if (!eight && few_tiles(p, head_dim)) return 64;
     return 128;
 }
@@ -103,7 +112,7 @@ grat_status make_forward(const grat_sequence* seq, float scale, int32_t window, 
     set_tiles(p, tree || few ? s.n_q * s.share : plan.tile_rows, plan.tile_rows);   // (these are one group)
     const int64_t items = (int64_t)s.batch * s.kv_heads * s.n_groups * p.row_tiles;
     if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
-    const int keys = few ? 4 * cache_keys(eight, seq->head_dim, p.row_tiles) : 64;   // of a workgroup's step
+    const int keys = few ? 4 * cache_keys(eight, seq->head_dim, tree) : 64;   // of a workgroup's step
     const int64_t steps = (reach(p, s.q_group, s.n_k) + keys - 1) / keys + (p.sinks + keys - 1) / keys;
     // A launch that leaves compute units idle has keys shared by several workgroups, up to one a compute unit (two tiles of few rows: two).  Few rows: parts of one or two steps, about 16 of them,
     // or of more where that fills the chip; 4 steps or more (one token on 8 heads, us, in parts of 2 steps and by this rule: 17 steps 11.9 and 10.8, 8 steps
