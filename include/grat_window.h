@@ -102,7 +102,7 @@ grat_status grat_cache_read(grat_dtype dtype, int32_t batch, int32_t heads, int3
  * Supported: as grat_window_attention_fwd; trees: n_q <= 256.  For few rows (n_q * q_heads / kv_heads up to a few hundred); more are correct, but
  * every 128 or 256 rows (32 where their keys are few) read the cache anew.
  * Arithmetic as there.  8 bits, few rows a K/V head (up to 64; up to 256 where their keys are few): K's scale is taken to the scores in fp32, and the weights times
- * V's scales are rounded to bfloat16 (also with GRAT_F16).  More rows: values times scales are rounded to seq->dtype first (scales that are powers of two leave bfloat16
+ * V's scales are rounded to bfloat16 (GRAT_F16: to the sum of two such numbers, 2^-17).  More rows: values times scales are rounded to seq->dtype first (scales that are powers of two leave bfloat16
  * nothing to round; half saturates at 65 504), and the weights as there.  A NaN or infinite V that one of a sequence's new tokens sees
  * can reach all of them (0 * NaN).
  */

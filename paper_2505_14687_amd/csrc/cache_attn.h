@@ -8,8 +8,8 @@
 // A unit is 32 keys, or 64: as soon as K's (or V's) has landed in LDS it is read into registers, and the next
 // one's loads go out into the same place.
 // 8 bits: e4m3 values become the 16-bit type of the product in registers, without loss.  A row's scale is taken to the score of its K in fp32, and to the weight of
-// its V ahead of the weight's rounding.  Weights times scales may leave half's range, so they and V are bfloat16 there, whatever Q is: 2^-9 of a weight
-// beside the 2^-4 that V's values were rounded by.
+// its V ahead of the weight's rounding.  Weights times scales may leave half's range, so they and V are bfloat16 there, whatever Q is; with half's Q a weight
+// is two bfloat16 numbers, the second what the first leaves over, and V's product is formed with both.
 #pragma once
 #include "sequence_fwd.h"
 
@@ -194,7 +194,8 @@ __global__ __launch_bounds__(256, 2) void cache_attention_kernel(SelParams p) {
     frag8 kf[W::kM * (EIGHT ? W::kN / 2 : W::kN)], vf[EIGHT ? 1 : W::kDims];   // 8 bits: 16 numbers of K each
     uint2 v_raw[EIGHT ? W::kDims : 1][W::kM / 2];
     f32x4 k_scale[W::kM], v_scale[W::kM];
-    frag8 weights[R][W::kM / 2];
+    constexpr bool kTwice = EIGHT && F16;   // weights of two bfloat16 numbers
+    frag8 weights[R][W::kM / 2], rest[kTwice ? R : 1][W::kM / 2];
     auto take_k = [&]() {
 #pragma unroll
         for (int m = 0; m < W::kM; ++m)
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256, 2) void cache_attention_kernel(SelParams p) {
                 }
             }
         }
-        uint32_t pw[2 * W::kM];
+        uint32_t pw[2 * W::kM], pr[2 * W::kM];
         auto weigh = [&]() {
             const float mc = m_ref[k] * cc;
             float ls = 0.f;
@@ -276,7 +277,9 @@ __global__ __launch_bounds__(256, 2) void cache_attention_kernel(SelParams p) {
             for (int i = 0; i < 2 * W::kM; ++i) {
                 const int m = i >> 1, e = 2 * (i & 1);
                 const float a = __builtin_amdgcn_exp2f(fmaf(X[m][e], cc, -mc)), b = __builtin_amdgcn_exp2f(fmaf(X[m][e + 1], cc, -mc));
-                pw[i] = EIGHT ? EV::pack(a * v_scale[m][e], b * v_scale[m][e + 1]) : EV::pack(a, b);
+                const float x = EIGHT ? a * v_scale[m][e] : a, y = EIGHT ? b * v_scale[m][e + 1] : b;
+                pw[i] = EV::pack(x, y);
+                if constexpr (kTwice) pr[i] = EV::pack(x - __builtin_bit_cast(float, pw[i] << 16), y - __builtin_bit_cast(float, pw[i] & 0xffff0000u));
                 ls += a + b;
             }
             return ls;
@@ -297,8 +300,10 @@ __global__ __launch_bounds__(256, 2) void cache_attention_kernel(SelParams p) {
         }
         l_run[k] += ls;
 #pragma unroll
-        for (int h = 0; h < W::kM / 2; ++h)
+        for (int h = 0; h < W::kM / 2; ++h) {
             weights[k][h] = __builtin_bit_cast(frag8, make_uint4(pw[4 * h], pw[4 * h + 1], pw[4 * h + 2], pw[4 * h + 3]));
+            if constexpr (kTwice) rest[k][h] = __builtin_bit_cast(frag8, make_uint4(pr[4 * h], pr[4 * h + 1], pr[4 * h + 2], pr[4 * h + 3]));
+        }
     };
     auto products = [&]() {
 #pragma unroll
@@ -308,7 +313,10 @@ __global__ __launch_bounds__(256, 2) void cache_attention_kernel(SelParams p) {
                 for (int h = 0; h < W::kM / 2; ++h) {
                     const frag8 x = widen<false>(v_raw[dt][h]);
 #pragma unroll
-                    for (int k = 0; k < R; ++k) oacc[k][dt] = EV::mfma16(x, weights[k][h], oacc[k][dt]);
+                    for (int k = 0; k < R; ++k) {
+                        oacc[k][dt] = EV::mfma16(x, weights[k][h], oacc[k][dt]);
+                        if constexpr (kTwice) oacc[k][dt] = EV::mfma16(x, rest[k][h], oacc[k][dt]);
+                    }
                 }
             } else {
 #pragma unroll

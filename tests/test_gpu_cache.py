@@ -234,7 +234,7 @@ def run_case(shape, dtype, d, eight, seed=300, gain=1.0, up=None):
         Ow, lw, bO, bl, _, _ = bounds(f64(Q), f64(K), f64(V), scale, mask, dtype)
         if eight:
             PV = sequence_oracle.attention(f64(Q), f64(K), np.abs(f64(V)), scale, mask)[0]
-            bO = bO + (ROUND["bf16"] - ROUND[dtype] + 8 * EPS) * PV
+            bO = bO + 8 * EPS * PV
     within(f64(O), Ow, bO, "O")
     got = f64(lse)
     assert np.array_equal(np.isneginf(got), np.isneginf(lw)), "rows that see nothing"
@@ -318,8 +318,8 @@ def test_scales_of_any_value_and_many_rows(dtype, N):
     O = grat.grat_cache_attention_fwd(Q, *c, 0.09, K_scale=s[0], V_scale=s[1])
     mask = np.repeat(orc.window_seen(N, M, B)[:, None], H, 1)
     Ow, _, bO, _, _, _ = bounds(f64(Q), K, V, 0.09, mask, dtype)
-    if 2 * N <= 256:   # the weights in bfloat16, as in run_case
-        bO = bO + (ROUND["bf16"] - ROUND[dtype] + 8 * EPS) * sequence_oracle.attention(f64(Q), K, np.abs(V), 0.09, mask)[0]
+    if 2 * N <= 256:   # scales beside the values, as in run_case
+        bO = bO + 8 * EPS * sequence_oracle.attention(f64(Q), K, np.abs(V), 0.09, mask)[0]
     within(f64(O), Ow, bO, "O")
 
 
