@@ -1,7 +1,8 @@
 // Rows of a cache in 8 bits: written with the new tokens' K turned by their positions, and read back.
 //
 // A row of head_dim numbers x is kept as e4m3 values of x / s and s, the least power of two with max |x| <= 448 s: as e4m3 is a floating format
-// itself, a finer s would gain nothing, and with this one the division and the way back are exact.  Memory (for few tokens the launch) bounds both directions.
+// itself, a finer s would gain nothing, and with this one the division and the way back are exact.  Memory (for few tokens the launch) bounds both directions: 2 x 8 191 tokens of 32 + 2 x 8 heads written 82 us
+// (4.5 TB/s in and out), 8 caches of 16 384 keys at most read back 74 us (5.1 TB/s), a token each of 32 sequences 5.5.
 #include <algorithm>
 #include <type_traits>
 
@@ -13,7 +14,6 @@ namespace grat {
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 
 constexpr int kOwnHeads = 2;   // of a thread, in flight at a time (a token each of 32 sequences 5.4 us; 4 heads 6.3, 8 heads 9.6; 8 192 tokens alike)
-
 
 // 4 numbers as e4m3, rounded to nearest-even; |x| <= 448, NaN and infinities become NaN
 __device__ __forceinline__ uint32_t narrow(float a, float b, float c, float d) {

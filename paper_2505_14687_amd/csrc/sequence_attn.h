@@ -1,4 +1,4 @@
-// Attention over lists of key blocks, on the matrix cores of gfx950: what the forward and the gradient kernels share.
+// Attention over lists of key blocks, within a window and over caches, on the matrix cores of gfx950: what the forward and the gradient kernels share.
 //
 // The rows of a query group - q_group queries of each of the heads that share a K/V head, head by head - all walk the group's list, so every
 // (row tile, key unit) product is a dense one; only the newest keys and the end of a sequence need a mask.  The products are the
@@ -7,6 +7,10 @@
 // rows 8 (r / 4) + 4 half + r % 4 of its own row c per 32, and that layout, packed to 16 bits, is the B operand of
 // Z^T += X'^T T if the contraction index is enumerated in the same order.  X'^T fragments come out of row-major tiles
 // through the LDS transpose read.
+//
+// A window needs no list: what the rows of a group see together is two runs of keys, the first ones and those near (KeyRange), and the
+// walk's units of 32 keys follow from their number (WindowUnits).  Rows of a group are neighbours, so a mask is needed at the ends of the runs only.  Drafted tokens
+// see the committed ones as a window's rows do, and of their own number a line, kept as bits (Tree).
 #pragma once
 #include "mfma_elem.h"
 #include "sequence_common.h"
@@ -569,7 +573,8 @@ struct KeyLoader {
     }
 };
 
-// The same of K and V in 8 bits, by way of registers: e4m3 values times their row's scale are rounded to the element type (scales that are powers of two leave
+// The same of K and V in 8 bits, by way of registers (a load into LDS cannot widen them; a tile of 256 rows walks a cache of 8 bits as fast as one of 16: 64 tokens of 4
+// sequences over 8 192 keys 48 us against 51): e4m3 values times their row's scale are rounded to the element type (scales that are powers of two leave
 // nothing to round; half saturates) and stored as the direct loads would have them.
 template <int NW, bool F16, int D>
 struct EightLoader {
