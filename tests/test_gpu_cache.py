@@ -189,6 +189,12 @@ SHAPES = [
     (2, 8, 2, 90, 700, 100, 3, [700, 311], False),               # 360 rows: a chain in the tiles of prompts
     (2, 12, 4, 60, 1800, 1500, 40, [1800, 59], True),            # 180 rows; a row without a key
     (1, 48, 2, 16, 1000, None, 0, [990], True),                  # 384 rows: two tiles
+    (2, 4, 1, 64, 1500, 200, 3, [1500, 777], True),              # 256 rows that see different keys
+    (2, 4, 1, 50, 900, 100, 5, [900, 333], False),               # 200 rows, a chain
+    (2, 2, 1, 30, 700, 64, 2, [700, 100], False),                # 60 rows
+    (2, 2, 1, 30, 700, 64, 2, [700, 100], True),
+    (1, 1, 1, 256, 3000, 900, 2, [2900], True),                  # 256 rows in several parts
+    (2, 1, 1, 250, 3000, 900, 2, [2900, 1300], False),           # ... of sequences of their own lengths
 ]
 
 

@@ -118,6 +118,19 @@ def test_larger(shape, dtype, pick):
     run_case(shape, dtype, 128, where="tokens", backward=True, seed=61, pick=pick)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("bf16", 64), ("f16", 128)])
+@pytest.mark.parametrize("shape,pick", [
+    ((16, 32, 32, 100, 130, 20, 3, None, None, True), [(0, 0), (7, 31), (15, 5)]),           # many short prompts: 128 rows
+    ((16, 32, 32, 100, 130, 20, 3, [130] * 8 + [40] * 8, None, False), [(0, 0), (15, 5)]),
+    ((1, 2, 1, 150, 2700, 2650, 3, None, None, True), None),                                 # a chunk on many keys
+    ((1, 1, 1, 250, 2000, 300, 2, [1700], None, True), None),                                # 250 rows that see different keys
+    ((1, 1, 1, 250, 3000, 990, 2, None, None, True), None),                                  # ... in several parts
+    ((1, 4, 1, 60, 4000, 1000, 2, None, None, True), None),                                  # 240 rows that see the same
+])
+def test_tiles_of_rows(shape, pick, dtype, d):
+    run_case(shape, dtype, d, where="tokens", backward=True, seed=71, pick=pick)
+
+
 def test_gradient_against_differences():
     """Directional differences of sum(O dO) in the kernels' own forward pass, in half; the bound as for attention over lists."""
     shape = (1, 2, 1, 40, 90, 20, 5, None, None, True)
