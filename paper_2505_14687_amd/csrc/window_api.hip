@@ -84,8 +84,8 @@ bool few_tiles(const SelParams& p, int head_dim) {
 // in tiles of 64 to 256 rows and of 32, 32 heads on 8: 64 rows over 4 000 keys 16 bits 17.1 15.4, 16 sequences over 8 192 112 108, head_dim 64 13.3 11.9 and 65.8 56.8;
 // 96 rows of 16 sequences over 4 096 8 bits 65.3 56.8, 16 bits 64.1 80.6; 256 rows over 4 096 8 bits 29.2 21.8, 16 bits 27.9 21.7, head_dim 64 18.5 15.5; of 4 sequences
 // 35.8 38.3, 35.5 35.3, 25.6 25.6; 128 rows of 4 sequences over 8 192, 16 bits, 40.1 48.5, head_dim 64 25.3 24.9.
-// 256 if that is one tile or makes four rounds of the chip, else 128 (windows of 1 024, us in tiles of 256 and of 128: 32 768 tokens of 8 heads 614 and 598, 8 192 tokens
-// 144 and 151; windows of 4 096 1 855 and 1 890, of 256 258 and 251).
+// 256 if that is one tile, or makes four rounds of the chip and its walk is long, else 128, of which two share a compute unit and cover each other's start and end (32 768
+// tokens, 32 heads on 8, us in tiles of 256 and of 128: window 64 204 161, 256 288 253, 512 398 371, 1 024 621 601, 2 048 1 056 1 051, 4 096 1 855 1 890).
 int fwd_tile_rows(const SelParams& p, int head_dim, bool eight) {
     const SeqShape& s = p.s;
     const int64_t rows = (int64_t)s.n_q * s.share, tiles = (rows + 31) / 32, heads = (int64_t)s.batch * s.kv_heads;
@@ -94,7 +94,7 @@ int fwd_tile_rows(const SelParams& p, int head_dim, bool eight) {
     if (rows <= 32) return rows <= 16 ? 16 : 32;
     if ((rows <= 64 && eight) || (alike && (rows <= (eight ? 96 : 64) || (rows <= 256 && keys <= (head_dim == 64 ? 1 << 20 : 1 << 19))))) return 32;
     if (rows <= 64) return 64;
-    if (head_dim == 128 && rows > 128 && (rows <= 256 || heads * ((rows + 255) / 256) >= 1024)) return 256;
+    if (head_dim == 128 && rows > 128 && (rows <= 256 || (heads * ((rows + 255) / 256) >= 1024 && reach(p, 64, s.n_k) > 2560))) return 256;
     if (!eight && few_tiles(p, head_dim)) return 64;
     return 128;
 }

@@ -111,7 +111,8 @@ def test_peaked_weights(dtype, gain, shape):
     ((1, 8, 2, 2100, 2100, 300, 4, None, None, True), "bf16", [(0, 1)]),
     ((1, 4, 4, 1500, 1500, 700, 100, None, None, False), "f16", [(0, 3)]),
     ((1, 4, 1, 1500, 3000, None, 0, None, None, True), "bf16", None),
-    ((4, 32, 8, 2047, 2047, 200, 3, [2047, 1500, 70, 0], None, True), "bf16", [(0, 0), (1, 6), (2, 7), (3, 2)]),   # workgroups of 256 rows
+    ((4, 32, 8, 2047, 2047, 200, 3, [2047, 1500, 70, 0], None, True), "bf16", [(0, 0), (1, 6), (2, 7), (3, 2)]),   # many workgroups
+    ((4, 32, 32, 2700, 2700, None, 0, [2700, 1500, 70, 0], None, True), "bf16", [(0, 0), (1, 30), (2, 7), (3, 2)]),                # of 256 rows
     ((2, 12, 4, 11000, 600, 80, 5, None, [0, 30], True), "f16", [(1, 2)]),                                        # more queries than keys
 ])
 def test_larger(shape, dtype, pick):
