@@ -181,13 +181,16 @@ grat_status make_gradient(const grat_sequence* seq, float scale, int32_t window,
     const int64_t items = heads * s.n_groups * p.row_tiles;
     if (items >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
     set_items(p, items, 1);
-    // Parts of the rows that see a key tile: a window's, or fewer where that leaves compute units idle (as with lists).
+    // Parts of the rows that see a key tile: a window's, or fewer where that leaves compute units idle, which take two workgroups each (2 048 tokens, 32 heads on 8, window
+    // 512, training step 137 us in 1.5 rounds of parts, 124 in one).  The rows that see first keys are cut as the others, or into 32 where four rounds cover longer parts
+    // (16 384 tokens, window 128 545 -> 523; on one K/V head 172 -> 227).
     w.tiles = (s.n_k + 63) / 64;
     w.first_tiles = (p.sinks + 63) / 64;
     const int64_t near = reach(p, 64, s.n_q) * s.share, all = (int64_t)s.n_q * s.share;
-    const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(near, 512), heads * w.tiles * near / 768) + 63) / 64 * 64);
+    const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(near, 512), heads * w.tiles * near / 512) + 63) / 64 * 64);
+    const int64_t first_part = heads * w.tiles >= 2048 ? std::max(part, (all / 32 + 63) / 64 * 64) : part;
     w.near_parts = (int32_t)((near + part - 1) / part);
-    w.first_parts = std::max(w.near_parts, (int32_t)((all + part - 1) / part));
+    w.first_parts = std::max(w.near_parts, (int32_t)((all + first_part - 1) / first_part));
     const int64_t firsts = (int64_t)w.first_tiles * w.first_parts, per_head = firsts + (int64_t)(w.tiles - w.first_tiles) * w.near_parts;
     const int64_t slots = w.near_parts > 1 ? per_head : w.first_parts > 1 ? firsts : 0;
     if (heads * per_head >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
