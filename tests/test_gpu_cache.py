@@ -417,3 +417,36 @@ def test_together_streams_and_graphs():
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(out, eager[i])), f"replay with data {i}"
         step(*sets[(i + 1) % 3], copies())
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("N,M,tree", [(1, 5000, False), (20, 3000, True), (150, 900, False)])
+def test_a_graph_with_other_lengths(N, M, tree, eight):
+    """Lengths and parents are read where they lie: a graph replays with others, as eager calls have them."""
+    B, Hq, Hkv, d = 5, 4, 2, 64
+    x = normal((B, Hkv, M, d), "bf16", 400)
+    c, s = (x, None) if not eight else empty_cache(B, Hkv, M, d)
+    if eight:
+        grat.grat_cache_append(None, x, x, None, c, c, ints([0] * B), K_scale=s, V_scale=s)
+    Q = normal((B, Hq, N, d), "bf16", 401)
+    gen = np.random.default_rng(402)
+    lengths = [ints([M] * B), ints([0, 1, N, M // 2, M]), ints([int(n) for n in gen.integers(0, M + 1, B)])]
+    trees = [ints(parents(np.random.default_rng(403 + i), B, N)) if tree else None for i in range(3)]
+    k_len, up = lengths[0].clone(), trees[0].clone() if tree else None
+
+    def call(k, t):
+        return grat.grat_cache_attention_fwd(Q, c, c, 0.125, k_len=k, K_scale=s, V_scale=s, parent=t, return_lse=True)
+
+    eager = [call(k, t) for k, t in zip(lengths, trees)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call(k_len, up)
+    for i in (1, 0, 2, 1):
+        k_len.copy_(lengths[i])
+        if tree:
+            up.copy_(trees[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager[i])), f"replay with data {i}"
+        call(lengths[(i + 1) % 3], trees[(i + 1) % 3])
