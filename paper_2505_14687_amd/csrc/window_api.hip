@@ -183,12 +183,15 @@ grat_status make_gradient(const grat_sequence* seq, float scale, int32_t window,
     set_items(p, items, 1);
     // Parts of the rows that see a key tile: a window's, or fewer where that leaves compute units idle, which take two workgroups each (2 048 tokens, 32 heads on 8, window
     // 512, training step 137 us in 1.5 rounds of parts, 124 in one).  The rows that see first keys are cut as the others, or into 32 where four rounds cover longer parts
-    // (16 384 tokens, window 128 545 -> 523; on one K/V head 172 -> 227).
+    // (16 384 tokens, window 128 545 -> 523; on one K/V head 172 -> 227), and into no more than make two rounds of all first tiles: a part's sums are twice what dK and dV take of its
+    // tile, in scratch memory.  Gradient of 16 384 tokens, 32 heads on 8, window 128, first keys 1 024 and 4 096: cut by their length alone 1 350 us and 273 MB, 4 171 and
+    // 1 078; for one round 1 166 and 38, 3 311 and 4; two 1 186 and 71, 3 289 and 71; four 1 258 and 138, 3 346 and 138.  8 heads on one, 4 096: 1 280, 1 371, 1 178, 1 115 us.
     w.tiles = (s.n_k + 63) / 64;
     w.first_tiles = (p.sinks + 63) / 64;
     const int64_t near = reach(p, 64, s.n_q) * s.share, all = (int64_t)s.n_q * s.share;
     const int64_t part = std::max<int64_t>(256, (std::min(std::max<int64_t>(near, 512), heads * w.tiles * near / 512) + 63) / 64 * 64);
-    const int64_t first_part = heads * w.tiles >= 2048 ? std::max(part, (all / 32 + 63) / 64 * 64) : part;
+    const int64_t even = std::max(heads * w.tiles >= 2048 ? all / 32 : 0, std::min(all, heads * w.first_tiles * all / 1024));
+    const int64_t first_part = std::max(part, (even + 63) / 64 * 64);
     w.near_parts = (int32_t)((near + part - 1) / part);
     w.first_parts = std::max(w.near_parts, (int32_t)((all + first_part - 1) / first_part));
     const int64_t firsts = (int64_t)w.first_tiles * w.first_parts, per_head = firsts + (int64_t)(w.tiles - w.first_tiles) * w.near_parts;

@@ -216,3 +216,14 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(out, eager[i])), f"replay with data {i}"
         step(*sets[(i + 1) % 3])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("shape,pick", [
+    ((4, 32, 32, 1100, 1100, 64, 70, [1100, 1100, 900, 66], None, True), [(0, 0), (2, 31), (3, 5)]),    # many tiles: two of first keys in parts beside others of one
+    ((4, 64, 32, 1100, 1100, 64, 70, None, None, False), [(1, 17)]),                                    # ... both directions
+    ((16, 32, 32, 300, 300, 40, 130, [300] * 15 + [131], None, True), [(0, 0), (9, 30), (15, 7)]),      # three tiles of first keys, as many as fill the chip: one part each
+    ((1, 8, 1, 2500, 2500, 70, 600, None, None, True), None),                                           # few heads: first tiles in more parts than the others
+])
+def test_gradient_of_first_keys_in_parts(shape, pick, dtype, d):
+    run_case(shape, dtype, d, where="tokens", backward=True, seed=111, pick=pick)

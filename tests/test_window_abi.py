@@ -351,3 +351,18 @@ def test_axes_of_one_element_and_inputs_that_repeat(given):
                 grat.grat_cache_attention_fwd(f(q), cc, cc, 0.1, K_scale=ss, V_scale=ss, **s))
     for a, b in zip(several(lambda t: t), several(lambda t: t.contiguous())):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("batch,q_heads,kv_heads,n,window,sinks,causal", [
+    (8, 32, 8, 16384, 128, 4096, 1), (1, 32, 8, 32768, 64, 8192, 1), (1, 32, 8, 16384, 128, 1024, 1), (1, 32, 8, 16384, 128, 4096, 1), (1, 8, 1, 16384, 128, 4096, 1),
+    (4, 32, 32, 16384, 128, 4, 1), (8, 32, 8, 4096, 128, 1000, 1), (2, 16, 2, 8192, 300, 700, 0), (1, 4, 4, 2047, 64, 2000, 1), (1, 1, 1, 1 << 20, 5, 1 << 19, 1),
+])
+def test_work_of_many_first_keys_stays_small(batch, q_heads, kv_heads, n, window, sinks, causal):
+    """The rows that see a tile of first keys are cut into parts until these fill the chip, no further: at most two rounds of 512 workgroups in parts (and one part more a tile), beside
+    what the other tiles take where there are few of them (512 parts, and one more a tile); a part's sums are 2 * 64 * head_dim floats."""
+    L = wn._library()
+    s = seq(batch=batch, q_heads=q_heads, kv_heads=kv_heads, n_q=n, n_k=n, causal=causal)
+    heads, tiles, firsts = batch * kv_heads, -(-n // 64), -(-sinks // 64)
+    most = (1024 + heads * firsts if heads * firsts < 1024 else 0) + (512 + heads * tiles if heads * tiles < 512 else 0)
+    rows = 8 * batch * q_heads * n
+    assert rows <= L.grat_window_attention_work(ref(s), window, sinks, 1) <= rows + most * 2 * 64 * 128 * 4 + 4096
