@@ -196,7 +196,7 @@ grat_status make_gradient(const grat_sequence* seq, float scale, int32_t window,
     w.first_parts = std::max(w.near_parts, (int32_t)((all + first_part - 1) / first_part));
     const int64_t firsts = (int64_t)w.first_tiles * w.first_parts, per_head = firsts + (int64_t)(w.tiles - w.first_tiles) * w.near_parts;
     const int64_t slots = w.near_parts > 1 ? per_head : w.first_parts > 1 ? firsts : 0;
-    if (heads * per_head >= (1 << 23)) return GRAT_ERR_UNSUPPORTED;
+    // (Fewer than 2^23 items in all for whatever is supported: heads * tiles < 2^22 + 2^16, and there is more than one part only of tiles that leave these few.)
     w.head_items = (int32_t)per_head;
     w.head_slots = (int32_t)slots;
     w.items = (int32_t)(heads * per_head);

@@ -366,3 +366,28 @@ def test_work_of_many_first_keys_stays_small(batch, q_heads, kv_heads, n, window
     most = (1024 + heads * firsts if heads * firsts < 1024 else 0) + (512 + heads * tiles if heads * tiles < 512 else 0)
     rows = 8 * batch * q_heads * n
     assert rows <= L.grat_window_attention_work(ref(s), window, sinks, 1) <= rows + most * 2 * 64 * 128 * 4 + 4096
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("d,dtype", [(128, 0), (64, 2)])
+@pytest.mark.parametrize("shape", [
+    dict(batch=1, q_heads=32, kv_heads=32, n_q=1 << 20, n_k=1 << 20), dict(batch=32, q_heads=32, kv_heads=4, n_q=1 << 18, n_k=1 << 20),
+    dict(batch=1, q_heads=1, kv_heads=1, n_q=(1 << 28) - 1, n_k=(1 << 28) - 1), dict(batch=1, q_heads=1, kv_heads=1, n_q=(1 << 29) - 1, n_k=5),
+    dict(batch=1, q_heads=1, kv_heads=1, n_q=1, n_k=(1 << 28) - 1), dict(batch=255, q_heads=257, kv_heads=257, n_q=4000, n_k=4000),
+    dict(batch=1, q_heads=65535, kv_heads=65535, n_q=8191, n_k=4095), dict(batch=1, q_heads=65535, kv_heads=1, n_q=8192, n_k=1 << 20),
+    dict(batch=1, q_heads=65, kv_heads=1, n_q=(1 << 29) // 65 - 1, n_k=1 << 20), dict(batch=1, q_heads=129, kv_heads=1, n_q=(1 << 29) // 129 - 1, n_k=1 << 20),
+    dict(batch=127, q_heads=129 * 4, kv_heads=4, n_q=(1 << 29) // (127 * 129 * 4), n_k=200000),
+])
+def test_the_gradient_takes_what_the_forward_call_takes(shape, d, dtype, eight):
+    """Up to the limits that the header names no size is refused.  (A tensor is missing: only what is looked at ahead of it can refuse the call.)"""
+    L = wn._library()
+    t, e, sc = tensor(n=d), tensor(n=d), scales()
+    s = seq(d=d, dtype=dtype, **shape)
+    for causal in (1, 0):
+        s.causal = causal
+        for window, sinks in ((0, 0), (1, 0), (128, 4), (2 ** 31 - 1, 1), (64, min(shape["n_k"] - 1, 1 << 19)), (4096, min(shape["n_k"] - 1, 1 << 20)), (300, 2 ** 31 - 1)):
+            assert L.grat_window_attention_fwd(ref(s), None, ref(t), ref(t), ref(t), None, 0.1, window, sinks, FAKE, None) == NULL
+            assert L.grat_window_attention_bwd(ref(s), None, *[ref(t)] * 4, FAKE, *[ref(t)] * 3, 0.1, window, sinks, FAKE, None) == NULL
+            assert L.grat_window_attention_work(ref(s), window, sinks, 1) >= 8 * shape["batch"] * shape["q_heads"] * shape["n_q"]
+            kv = (ref(e), ref(e), ref(sc), ref(sc)) if eight else (ref(t), ref(t), None, None)
+            assert L.grat_cache_attention_fwd(ref(s), None, *kv, ref(t), None, 0.1, window, sinks, None, 0, FAKE, None) == NULL
