@@ -68,15 +68,23 @@ struct ForwardPlan {
     int64_t work = 0;
 };
 
-// Prompts that tiles of 128 rows would spread over the chip about once, and whose rows see few keys: tiles of 64, whose two teams take half of the keys each.  us with tiles
+// Prompts that tiles of 128 rows would spread over the chip about once: tiles of 64, whose two teams take half of the keys each.  us with tiles
 // of 128 and of 64, forward of 8 heads on as many (16 tiles of 128 rows for 2 048 tokens of one):
 //   window 129, 2 047 tokens of 1 to 4 sequences   head_dim 64   11.0 8.5   11.7 10.2   14.6 11.8   14.9 13.4   (training step 47.0 38.5   52.5 47.3   67.0 58.8   71.8 74.6)
 //                                                  head_dim 128  13.3 11.7   14.0 14.1   18.4 21.5   19.3 24.9   (62.2 53.8   74.8 71.4   92.4 99.0   108 123)
-//   2 048 tokens, window 1 500, 2 000, 2 500       head_dim 64   25.9 21.9   29.5 26.9   32.8 32.1   head_dim 128  34.4 31.6   38.1 39.1   41.9 46.5
-bool few_tiles(const SelParams& p, int head_dim) {
-    const SeqShape& s = p.s;
-    const int64_t tiles = (int64_t)s.batch * s.kv_heads * (((int64_t)s.n_q * s.share + 127) / 128);
-    return tiles <= (head_dim == 64 ? 384 : 256) && reach(p, 128, s.n_k) <= (head_dim == 64 ? 40 : 24) * 64;
+// The gradient's dQ gains at any number of keys (2 048 queries of 1 and 2 sequences behind 6 144 tokens, gradient, window 1 000, 3 000, none: head_dim 64 58.5 51.3   112.5 94.4
+// 247.5 201.4 and 70.2 66.8   142.8 134.1   308 285; head_dim 128 81.5 75.6   156.8 141.8   336.6 298.3 and 107.4 108.8   220.5 222.0   463 464).
+int64_t tiles_of_128(const SelParams& p) { return (int64_t)p.s.batch * p.s.kv_heads * (((int64_t)p.s.n_q * p.s.share + 127) / 128); }
+bool few_tiles(const SelParams& p, int head_dim) { return tiles_of_128(p) <= (head_dim == 64 ? 384 : 256); }
+
+// ... forward, while rows see few keys: the same queries, windows
+//   1 500, 1 800, 2 100          head_dim 128, 1 sequence   34.2 30.6   36.7 35.2   38.7 38.9     2   37.5 38.9   42.9 45.2   47.3 50.6   (1 300, 1 400: 32.8 32.7   33.7 33.8)
+//   2 500, 2 900, 3 200, 6 000   head_dim 64, 1 sequence    32.8 31.9   35.5 35.6   37.1 38.0   56.0 65.5     2   43.6 38.8   48.7 43.3   51.9 46.4   90.6 80.8     3   56.3 51.4   63.1 57.9
+//   67.3 62.1   117 110
+bool few_tiles_forward(const SelParams& p, int head_dim) {
+    const bool half_chip = tiles_of_128(p) <= 128;
+    const int64_t most = head_dim == 128 ? (half_chip ? 2048 : 1536) : half_chip ? 2816 : p.s.n_k;
+    return few_tiles(p, head_dim) && reach(p, 128, p.s.n_k) <= most;
 }
 
 // Rows of a workgroup, of the `rows` of all heads that share a K/V head.
@@ -95,7 +103,7 @@ int fwd_tile_rows(const SelParams& p, int head_dim, bool eight) {
     if ((rows <= 64 && eight) || (alike && (rows <= (eight ? 96 : 64) || (rows <= 256 && keys <= (head_dim == 64 ? 1 << 20 : 1 << 19))))) return 32;
     if (rows <= 64) return 64;
     if (head_dim == 128 && rows > 128 && (rows <= 256 || (heads * ((rows + 255) / 256) >= 1024 && reach(p, 64, s.n_k) > 2560))) return 256;
-    if (!eight && few_tiles(p, head_dim)) return 64;
+    if (!eight && few_tiles_forward(p, head_dim)) return 64;
     return 128;
 }
 

@@ -391,3 +391,12 @@ def test_the_gradient_takes_what_the_forward_call_takes(shape, d, dtype, eight):
             assert L.grat_window_attention_work(ref(s), window, sinks, 1) >= 8 * shape["batch"] * shape["q_heads"] * shape["n_q"]
             kv = (ref(e), ref(e), ref(sc), ref(sc)) if eight else (ref(t), ref(t), None, None)
             assert L.grat_cache_attention_fwd(ref(s), None, *kv, ref(t), None, 0.1, window, sinks, None, 0, FAKE, None) == NULL
+
+
+def test_tiles_of_prompts_follow_what_was_measured():
+    """Scratch memory tells the tiles: 2 048 tokens of 8 heads make 128 of 128 rows, two parts each, or 256 of 64 rows in one part."""
+    L = wn._library()
+    for d, windows in ((128, {1500: 64, 1800: 64, 2100: 128}), (64, {2500: 64, 3200: 128})):
+        s = seq(d=d, q_heads=8, kv_heads=8, n_q=2048, n_k=8192)
+        for window, tile in windows.items():
+            assert L.grat_window_attention_work(ref(s), window, 0, 0) == (0 if tile == 64 else 2 * 128 * 128 * (d + 2) * 4), (d, window)
