@@ -41,6 +41,9 @@ int64_t reach(const SelParams& p, int64_t queries, int64_t most) {
     return p.window == kNoWindow ? most : std::min(most, (p.s.causal ? 1 : 2) * ((int64_t)p.window - 1) + queries);
 }
 
+// Keys that they see, with the first ones.
+int64_t seen(const SelParams& p, int64_t queries) { return std::min<int64_t>(p.s.n_k, reach(p, queries, p.s.n_k) + p.sinks); }
+
 // Groups of neighbouring queries of at most `group_rows` rows (where one query has no more), in tiles.
 void set_tiles(SelParams& p, int group_rows, int tile_rows) {
     SeqShape& s = p.s;
@@ -84,25 +87,29 @@ bool few_tiles(const SelParams& p, int head_dim) { return tiles_of_128(p) <= (he
 bool few_tiles_forward(const SelParams& p, int head_dim) {
     const bool half_chip = tiles_of_128(p) <= 128;
     const int64_t most = head_dim == 128 ? (half_chip ? 2048 : 1536) : half_chip ? 2816 : p.s.n_k;
-    return few_tiles(p, head_dim) && reach(p, 128, p.s.n_k) <= most;
+    return few_tiles(p, head_dim) && seen(p, 128) <= most;
 }
 
 // Rows of a workgroup, of the `rows` of all heads that share a K/V head.
 // 16 and 32: the kernel of few rows, whose tiles each fetch all of the head's keys; so rows that see much the same keys, few of them (64; 96 in 8 bits) or with few keys.  us
 // in tiles of 64 to 256 rows and of 32, 32 heads on 8: 64 rows over 4 000 keys 16 bits 17.1 15.4, 16 sequences over 8 192 112 108, head_dim 64 13.3 11.9 and 65.8 56.8;
 // 96 rows of 16 sequences over 4 096 8 bits 65.3 56.8, 16 bits 64.1 80.6; 256 rows over 4 096 8 bits 29.2 21.8, 16 bits 27.9 21.7, head_dim 64 18.5 15.5; of 4 sequences
-// 35.8 38.3, 35.5 35.3, 25.6 25.6; 128 rows of 4 sequences over 8 192, 16 bits, 40.1 48.5, head_dim 64 25.3 24.9.
+// 35.8 38.3, 35.5 35.3, 25.6 25.6; 128 rows of 4 sequences over 8 192, 16 bits, 40.1 48.5.  256 rows of 4 sequences, window 256 and 1 024, 4 096, 16 384 first keys, 16 bits 25.2 22.9   35.0
+// 37.1   82.1 124.6, 8 bits 26.9 23.1   37.2 39.6   82.2 108.4; window 64 and 1 024 first keys 24.2 21.6.  head_dim 64 goes further: 256 rows of 4 sequences over 16 384 and
+// 65 536 67.6 65.6   238 260, in 8 bits, whatever the number of keys, 78.8 65.7   285 233; of 16 sequences over 4 096 and 16 384 63.9 55.3   234 253, 8 bits 74.1 64.6   281 230.
 // 256 if that is one tile, or makes four rounds of the chip and its walk is long, else 128, of which two share a compute unit and cover each other's start and end (32 768
-// tokens, 32 heads on 8, us in tiles of 256 and of 128: window 64 204 161, 256 288 253, 512 398 371, 1 024 621 601, 2 048 1 056 1 051, 4 096 1 855 1 890).
+// tokens, 32 heads on 8, us in tiles of 256 and of 128: window 64 204 161, 256 288 253, 512 398 371, 1 024 621 601, 2 048 1 056 1 051, 4 096 1 855 1 890; window 64 and 2 600, 4 096,
+// 8 192 first keys 1 265 1 302, 1 830 1 906, 3 360 3 466).
 int fwd_tile_rows(const SelParams& p, int head_dim, bool eight) {
     const SeqShape& s = p.s;
     const int64_t rows = (int64_t)s.n_q * s.share, tiles = (rows + 31) / 32, heads = (int64_t)s.batch * s.kv_heads;
-    const bool alike = p.window / 4 >= s.n_q;
-    const int64_t keys = heads * tiles * reach(p, s.n_q, s.n_k);   // that tiles of 32 rows fetch
+    const bool alike = ((int64_t)p.window + p.sinks) / 4 >= s.n_q;
+    const int64_t keys = heads * tiles * seen(p, s.n_q);   // that tiles of 32 rows fetch
+    const bool few_keys = head_dim == 64 ? eight || keys <= 1 << 22 : keys <= 1 << 19;
     if (rows <= 32) return rows <= 16 ? 16 : 32;
-    if ((rows <= 64 && eight) || (alike && (rows <= (eight ? 96 : 64) || (rows <= 256 && keys <= (head_dim == 64 ? 1 << 20 : 1 << 19))))) return 32;
+    if ((rows <= 64 && eight) || (alike && (rows <= (eight ? 96 : 64) || (rows <= 256 && few_keys)))) return 32;
     if (rows <= 64) return 64;
-    if (head_dim == 128 && rows > 128 && (rows <= 256 || (heads * ((rows + 255) / 256) >= 1024 && reach(p, 64, s.n_k) > 2560))) return 256;
+    if (head_dim == 128 && rows > 128 && (rows <= 256 || (heads * ((rows + 255) / 256) >= 1024 && seen(p, 64) > 2560))) return 256;
     if (!eight && few_tiles_forward(p, head_dim)) return 64;
     return 128;
 }

@@ -450,3 +450,14 @@ def test_a_graph_with_other_lengths(N, M, tree, eight):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, eager[i])), f"replay with data {i}"
         call(lengths[(i + 1) % 3], trees[(i + 1) % 3])
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("shape", [
+    (2, 8, 2, 60, 5000, 20, 700, [4990, 611], False),                # 240 rows
+    (1, 8, 2, 64, 9000, 64, 6100, [8000], True),                     # ... of a tree, in several parts
+    (3, 6, 2, 40, 3000, 25, 2000, [3000, 30, 1999], True),           # first keys beyond the committed ones
+])
+def test_more_first_keys_than_others(shape, dtype, d, eight):
+    run_case(shape, dtype, d, eight, seed=410)

@@ -227,3 +227,15 @@ def test_streams_and_graphs():
 ])
 def test_gradient_of_first_keys_in_parts(shape, pick, dtype, d):
     run_case(shape, dtype, d, where="tokens", backward=True, seed=111, pick=pick)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("shape,pick", [
+    ((1, 8, 2, 60, 5000, 20, 700, [4990], None, True), None),                                           # 240 rows that see much the same first keys
+    ((2, 8, 2, 64, 9000, 64, 6100, [9000, 40], [8700, -30], True), None),                               # ... in several parts; rows ahead of the first key
+    ((2, 8, 2, 40, 3000, 25, 2000, None, [100, 2900], False), None),
+    ((1, 8, 8, 2048, 4200, 100, 4000, None, None, True), [(0, 3)]),                                     # prompts that see more first keys than others
+    ((4, 32, 32, 2700, 2700, 64, 2500, [2700, 2700, 2600, 900], None, True), [(0, 0), (3, 30)]),        # of 256 rows
+])
+def test_more_first_keys_than_others(shape, pick, dtype, d):
+    run_case(shape, dtype, d, where="tokens", backward=True, seed=121, pick=pick)

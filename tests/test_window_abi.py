@@ -400,3 +400,17 @@ def test_tiles_of_prompts_follow_what_was_measured():
         s = seq(d=d, q_heads=8, kv_heads=8, n_q=2048, n_k=8192)
         for window, tile in windows.items():
             assert L.grat_window_attention_work(ref(s), window, 0, 0) == (0 if tile == 64 else 2 * 128 * 128 * (d + 2) * 4), (d, window)
+
+
+@pytest.mark.parametrize("eight", [0, 1])
+@pytest.mark.parametrize("batch,heads,n_q,window,sinks,d", [
+    (4, 8, 64, 256, 16384, 128), (1, 8, 64, 256, 16384, 128), (4, 8, 64, 256, 1025, 128), (4, 8, 64, 64, 1985, 128), (8, 8, 40, 100, 6005, 128), (4, 8, 64, 63, 2050, 64),
+    (1, 2, 600, 129, 8001, 128), (1, 2, 700, 129, 8001, 64),
+])
+def test_tiles_count_first_keys(batch, heads, n_q, window, sinks, d, eight):
+    """Rows that see many first keys and a short window are worked on as rows that see as many keys near them.  (Scratch memory tells the tiles.)"""
+    L = wn._library()
+    both = batch, 4 * heads, heads
+    mine = seq(0, *both, d=d, n_q=n_q, n_k=1 << 15)
+    same = seq(0, *both, d=d, n_q=n_q, n_k=window - 1 + n_q + sinks)
+    assert L.grat_cache_attention_work(ref(mine), window, sinks, eight) == L.grat_cache_attention_work(ref(same), 0, 0, eight) > 0
