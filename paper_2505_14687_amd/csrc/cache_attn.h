@@ -424,7 +424,8 @@ inline hipError_t launch_cache_attention(const SelParams& p, bool eight, int til
     else if (eight) launch_cache_tiles<F16, D, kWindow, true>(p, tile_rows, stream);
     else if (p.parent) launch_cache_tiles<F16, D, kTree, false>(p, tile_rows, stream);
     else launch_cache_tiles<F16, D, kWindow, false>(p, tile_rows, stream);
-    if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
+    if (p.slots > 0) launch_join<F16, D, true>(p, tile_rows, stream);
+    else if (p.splits > 1) launch_join<F16, D>(p, tile_rows, stream);
     return hipGetLastError();
 }
 

@@ -469,8 +469,9 @@ __global__ __launch_bounds__(256, 2) void selected_fwd_narrow_kernel(SelParams p
 }
 
 // Joins the parts of a split list, weighted by 2^(c (m - max m)).  D / 4 lanes share a row's dims; eight parts are in flight at a time.  (1 024 rows of
-// two parts 4.0 us.  More lanes a row, one for every part, do not shorten it.)
-template <bool F16, int D>
+// two parts 4.0 us.  More lanes a row, one for every part, do not shorten it.)  SHARED: the sequences share the parts (Parts); a kernel for both kinds costs
+// lists 0.5 us (a token on 32 768 listed keys of 8 heads 33.0 against 32.5, of 4 sequences 48.1 against 47.2).
+template <bool F16, int D, bool SHARED>
 __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int tile_rows, FastDiv fd_rows) {
     constexpr int L = D / 4, RPB = 256 / L;   // lanes of a row, rows of a workgroup
     const SeqShape& s = p.s;
@@ -483,7 +484,7 @@ __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int til
     const GroupRow row(p, (int)h, (int)g, (int)r);
     int64_t first = (((int64_t)list * p.row_tiles + r / tile_rows) * p.splits) * tile_rows + r % tile_rows;   // + split * tile_rows
     int parts = p.splits;
-    if (p.slots > 0) {   // (the lists are the K/V heads of the sequences)
+    if constexpr (SHARED) {   // (the lists are the K/V heads of the sequences)
         const Parts share(p);
         parts = __shfl(share.n, (int)b);
         first = (((int64_t)h * p.row_tiles + r / tile_rows) * p.slots + __shfl(share.end, (int)b) - parts) * tile_rows + r % tile_rows;
@@ -525,10 +526,10 @@ __global__ __launch_bounds__(256) void selected_join_kernel(SelParams p, int til
         p.lse[((int64_t)b * s.q_heads + row.head) * s.n_q + row.query] = (m * p.scale_log2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-template <bool F16, int D>
+template <bool F16, int D, bool SHARED = false>
 inline void launch_join(const SelParams& p, int tile_rows, hipStream_t stream) {
     const int64_t rows = (int64_t)p.s.batch * p.s.kv_heads * p.s.n_groups * p.rows, per = 1024 / D;
-    hipLaunchKernelGGL((selected_join_kernel<F16, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p, tile_rows,
+    hipLaunchKernelGGL((selected_join_kernel<F16, D, SHARED>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p, tile_rows,
                        make_fastdiv((uint32_t)p.rows));
 }
 
