@@ -3,8 +3,8 @@
 Rows: without rotation everything is exact (the scale is a power of two), so values and scales have to be the oracle's.  A turned number is off by 3 e of
 |c x| + |s y| (two products and a sum in fp32, cos and sin rounded once; e = 2^-24), which may take it to the neighbouring e4m3 value where it is next to a border:
 it is within its own rounding, 2^-4 of itself or 2^-10 s, of the number before rounding.
-Attention: the bounds of test_gpu_sequence_attention.py on the values that the cache stands for; in 8 bits weights are rounded to bfloat16 (u = 2^-8)
-whatever the type, and the scales cost two more fp32 roundings."""
+Attention: the bounds of test_gpu_sequence_attention.py on the values that the cache stands for; in 8 bits weights are rounded to bfloat16 (u = 2^-8), of half to
+two such numbers (2^-17), and the scales cost two more fp32 roundings."""
 import math
 
 import numpy as np
@@ -461,3 +461,22 @@ def test_a_graph_with_other_lengths(N, M, tree, eight):
 ])
 def test_more_first_keys_than_others(shape, dtype, d, eight):
     run_case(shape, dtype, d, eight, seed=410)
+
+
+@pytest.mark.parametrize("N", [3, 7, 20])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_of_any_value_in_half_lose_nothing(N, d):
+    """Few rows of half over 8 bits: a weight is two bfloat16 numbers, the second what the first leaves over, so that it is off by at most 2^-17 of itself (the rest
+    is at most 2^-8, half a step of 2^-7 above 1, and rounded by half a step of 2^-16) in the place of the 2^-11 that `bounds` counts; scales that are no powers of two
+    cost two fp32 roundings on the way, as in run_case.  (Weights of one bfloat16 number are 1.5 to 3.7 times beyond it.)"""
+    B, H, M = 2, 2, 300
+    gen = torch.Generator().manual_seed(431)
+    c = [torch.randn((B, H, M, d), generator=gen).to(EIGHT).cuda() for _ in range(2)]
+    s = [(0.1 + torch.rand((B, H, M), generator=gen)).cuda() for _ in range(2)]
+    K, V = (f64(x.float()) * f64(y)[..., None] for x, y in zip(c, s))
+    Q = normal((B, 4, N, d), "f16", 432)
+    mask = np.repeat(orc.window_seen(N, M, B)[:, None], H, 1)
+    Ow, _, bO, _, _, _ = bounds(f64(Q), K, V, 0.09, mask, "f16")
+    PV = sequence_oracle.attention(f64(Q), K, np.abs(V), 0.09, mask)[0]
+    O = grat.grat_cache_attention_fwd(Q, *c, 0.09, K_scale=s[0], V_scale=s[1])
+    within(f64(O), Ow, bO + (2.0 ** -17 + 8 * EPS - ROUND["f16"]) * PV, "O")
