@@ -31,13 +31,14 @@ struct SelParams {
     FastDiv fd_splits, fd_row_tiles, fd_groups, fd_kv_heads, fd_q_group, fd_units;   // fd_units: by block / 32
     float* part_o;                // splits > 1: [items][rows of a tile][D], with part_ml [items][rows of a tile][2]
     float* part_ml;
-    int32_t window, sinks;        // attention within a window: no lists, q_group is the launch's own
+    int64_t window;               // attention within a window: no lists, q_group is the launch's own
+    int32_t sinks;
     SeqTensor k_scale, v_scale;   // K and V in 8 bits: a float a row
     const int32_t* parent;        // drafted tokens, or null
     int64_t parent_stride_b;
     int32_t slots, part_keys, part_step;   // parts that the sequences share (Parts), or 0; keys of a unit; units that a workgroup takes at a time
 };
-constexpr int32_t kNoWindow = 0x7fffffff;
+constexpr int64_t kNoWindow = (int64_t)1 << 40;   // more than any two positions are apart
 
 // The walk over keys of attention within a window: key tiles of 64 keys, the rows that see a tile cut into parts of about equal length.  Rows that see
 // one of the first keys are as many as there are, of others at most a window's.
@@ -244,9 +245,8 @@ __device__ __forceinline__ int64_t window_pos(const SeqShape& s, int b, int len)
 __device__ __forceinline__ RowSpan row_span(const SelParams& p, int len, int64_t pos, int i) {
     const int64_t at = pos + i;
     RowSpan r;
-    const bool all = p.window == kNoWindow;
-    r.hi = (int)max((int64_t)0, min((int64_t)len, p.s.causal ? at + 1 : all ? (int64_t)len : at + p.window));
-    r.lo = all ? 0 : (int)max((int64_t)0, min((int64_t)r.hi, at - p.window + 1));
+    r.hi = (int)max((int64_t)0, min((int64_t)len, p.s.causal ? at + 1 : at + p.window));
+    r.lo = (int)max((int64_t)0, min((int64_t)r.hi, at - p.window + 1));
     r.first = min(p.sinks, p.s.causal ? r.hi : len);
     return r;
 }
@@ -263,7 +263,7 @@ __device__ __forceinline__ KeyRange rows_range(const SelParams& p, int len, int6
 // ... of a tree: its first token is one that goes on from a committed one, and no other sees more of these.
 __device__ __forceinline__ KeyRange tree_range(const SelParams& p, int len) {
     const int base = len - p.s.n_q, committed = max(base, 0), first = min(p.sinks, committed);
-    return KeyRange{first, max(p.window == kNoWindow ? 0 : max(0, min(committed, base - p.window + 1)), first), len};
+    return KeyRange{first, (int)max((int64_t)first, min((int64_t)committed, base - p.window + 1)), len};
 }
 // (The same in all lanes, which what it is computed from does not always say.)
 __device__ __forceinline__ KeyRange uniform(const KeyRange& r) {
@@ -334,6 +334,7 @@ struct Tree {
 __device__ __forceinline__ void build_small_tree(Tree& tree, const SelParams& p, int b, int base) {
     const int n = p.s.n_q, t = (int)(threadIdx.x & 63);
     const bool limited = p.window < n;
+    const int window = (int)min(p.window, (int64_t)n);
     int up = -1, from = t;   // above the line so far, above `near`
     if (t < n) {
         up = p.parent[b * p.parent_stride_b + t];
@@ -343,7 +344,7 @@ __device__ __forceinline__ void build_small_tree(Tree& tree, const SelParams& p,
     uint64_t line = 1ull << t, near = 0;
     for (int k = 0;; ++k) {   // (ends at 2^k >= n at the latest: a parent lies ahead of its child)
         const bool last = __builtin_amdgcn_ballot_w64(up >= 0) == 0;
-        if (limited && (last ? p.window >> k : p.window >> k & 1)) {
+        if (limited && (last ? window >> k : window >> k & 1)) {
             const uint64_t x = __shfl(line, max(from, 0));
             const int above = __shfl(up, max(from, 0));
             near |= from >= 0 ? x : 0;
@@ -372,6 +373,7 @@ __device__ __forceinline__ void build_tree(Tree& tree, const SelParams& p, int b
     constexpr int kWords = kTreeWords - 2;
     const int n = p.s.n_q, t = (int)threadIdx.x, words = (n + 31) >> 5;
     const bool limited = p.window < n;
+    const int window = (int)min(p.window, (int64_t)n);
     uint32_t line[kWords], near[kWords];
     int up = -1, from = t < n ? t : -1;   // above the line so far, above `near`
 #pragma unroll
@@ -398,7 +400,7 @@ __device__ __forceinline__ void build_tree(Tree& tree, const SelParams& p, int b
         }
         __syncthreads();
         const bool last = tree.deep[k] == 0;
-        if (limited && (last ? p.window >> k : p.window >> k & 1) && from >= 0) {
+        if (limited && (last ? window >> k : window >> k & 1) && from >= 0) {
 #pragma unroll
             for (int w = 0; w < kWords; ++w)
                 if (w < words) near[w] |= tree.lines[from * kTreeWords + w];
@@ -432,7 +434,7 @@ __device__ __forceinline__ void build_tree(Tree& tree, const SelParams& p, int b
 __device__ __forceinline__ RowSpan tree_span(const SelParams& p, const Tree& tree, int base, int t) {
     const int committed = max(base, 0);
     const int64_t lo = (int64_t)base + tree.depth[t] - p.window + 1;
-    return RowSpan{min(p.sinks, committed), p.window == kNoWindow ? 0 : (int)max((int64_t)0, min((int64_t)committed, lo)), committed};
+    return RowSpan{min(p.sinks, committed), (int)max((int64_t)0, min((int64_t)committed, lo)), committed};
 }
 // The lower n bits, n from 0 to 32 (what is beyond is taken for the nearest).
 __device__ __forceinline__ uint32_t lower_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }

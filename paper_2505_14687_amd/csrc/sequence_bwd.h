@@ -71,8 +71,8 @@ struct WindowItem {
     __device__ __forceinline__ void rows(const SelParams& p, int len, int64_t pos) {
         const SeqShape& s = p.s;
         const int64_t k0 = (int64_t)tile * 64, k1 = min(k0 + 64, (int64_t)len);
-        const bool first = k0 < p.sinks, all = p.window == kNoWindow;
-        const int64_t from = s.causal ? k0 : first || all ? INT64_MIN / 2 : k0 - p.window + 1, to = first || all ? INT64_MAX / 2 : k1 + p.window - 1;   // positions
+        const bool first = k0 < p.sinks;
+        const int64_t from = s.causal ? k0 : first ? INT64_MIN / 2 : k0 - p.window + 1, to = first ? INT64_MAX / 2 : k1 + p.window - 1;   // positions
         i0 = (int)min(max(from - pos, (int64_t)0), (int64_t)s.n_q);
         ni = max((int)min(max(to - pos, (int64_t)0), (int64_t)s.n_q) - i0, 0);
         const int n = ni * s.share, per = ((n + parts - 1) / parts + 63) & ~63;

@@ -38,7 +38,7 @@ grat_status set_window(SelParams& p, float scale, int32_t window, int32_t sinks)
 
 // Keys that `queries` neighbouring queries may see beside the first ones, and the other way round.
 int64_t reach(const SelParams& p, int64_t queries, int64_t most) {
-    return p.window == kNoWindow ? most : std::min(most, (p.s.causal ? 1 : 2) * ((int64_t)p.window - 1) + queries);
+    return std::min(most, (p.s.causal ? 1 : 2) * (p.window - 1) + queries);
 }
 
 // Keys that they see, with the first ones.
@@ -103,7 +103,7 @@ bool few_tiles_forward(const SelParams& p, int head_dim) {
 int fwd_tile_rows(const SelParams& p, int head_dim, bool eight) {
     const SeqShape& s = p.s;
     const int64_t rows = (int64_t)s.n_q * s.share, tiles = (rows + 31) / 32, heads = (int64_t)s.batch * s.kv_heads;
-    const bool alike = ((int64_t)p.window + p.sinks) / 4 >= s.n_q;
+    const bool alike = (p.window + p.sinks) / 4 >= s.n_q;
     const int64_t keys = heads * tiles * seen(p, s.n_q);   // that tiles of 32 rows fetch
     const bool few_keys = head_dim == 64 ? eight || keys <= 1 << 22 : keys <= 1 << 19;
     if (rows <= 32) return rows <= 16 ? 16 : 32;

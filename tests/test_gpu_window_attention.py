@@ -239,3 +239,13 @@ def test_gradient_of_first_keys_in_parts(shape, pick, dtype, d):
 ])
 def test_more_first_keys_than_others(shape, pick, dtype, d):
     run_case(shape, dtype, d, where="tokens", backward=True, seed=121, pick=pick)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 2), (2 ** 31 - 2, 0), (None, 0), (1, 3)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n", [5, 70])
+def test_positions_at_the_ends_of_their_type(n, causal, window, sinks, dtype, d):
+    """The longest window is a limit all the same: it ends between the first keys for positions next to 2^31 and -2^31."""
+    shape = (4, 4, 2, n, 140, window, sinks, [140, 140, 130, 140], [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 30, -2 ** 31 + 69], causal)
+    run_case(shape, dtype, d, where="tokens", backward=True, seed=131)
