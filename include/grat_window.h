@@ -47,7 +47,7 @@ grat_status grat_window_attention_fwd(const grat_sequence* seq, const grat_tenso
  * head add up in its dK and dV.  Rows of dK and dV that no query sees, also those behind the valid keys, get 0.  Every output is written
  * once, nothing is added atomically: the same inputs give the same bits.
  *   d_work     grat_window_attention_work(seq, window, sinks, 1) bytes, 16-byte aligned: 8 bytes a query row, and 2 * 64 * head_dim * 4 for every part
- *              of the 64-key tiles that many rows see (those of the first keys; all of them where there are few)
+ *              of the 64-key tiles that many rows see (those of the first keys; all of them where there are few), of which there are fewer than 2 560
  * Supported: as the forward call.  The softmax weights and the score gradients are rounded to the element type for the products; all sums
  * in fp32.  GRAT_F16: with the powers of two of grat_selected_attention_bwd.
  */

@@ -16,8 +16,9 @@
 // takes 7 % less).
 //
 // Within a window the keys' rows are a run of neighbours, so nothing is turned round (WindowItem): D and dQ | dK, dV | joined parts, those of tiles that many rows
-// see (the first keys').  16 384 tokens, 32 heads on 8, window 1 024, bf16: dQ 433 us (950 TFLOP/s), dK and dV 672 to 694 (790 TFLOP/s and more; neighbouring key tiles read
-// the same rows, 650 MB fetched for 3.9 GB of the lists), join 5.
+// see (the first keys').  16 384 tokens, 32 heads on 8, window 1 024, bf16: dQ 427 to 433 us (950 TFLOP/s), dK and dV 672 to 694 (790 TFLOP/s and more; neighbouring key tiles read
+// the same rows, 650 MB fetched for 3.9 GB of the lists), join 5.  Four first keys are 60 us of it, as at window 128 (a training step 511 us, 453 without): their tile takes every
+// row, for 64 keys.
 #pragma once
 #include <type_traits>
 

@@ -9,8 +9,9 @@
 // the matrix pipe busy for 47 % of the cycles.  What holds it back: a block more takes 29 us (8 to 64 blocks: 363, 606, 1 080, 2 008), 1 185 TFLOP/s, and 140 us go
 // by without the walk: 225 registers leave one workgroup of 8 waves to a compute unit, so nothing covers its start (count, list, Q, first K tile, one after the
 // other) and its end (O through LDS), 9 us each time.  Few rows: bound by fetching K and V, see NarrowWave.
-// Windows, without a list's look-up: 32 768 tokens, 32 heads on 8, window 1 024, bf16 600 to 606 us, 900 TFLOP/s of what the rows see (a tile of 32 queries walks 3 % more), the
-// matrix pipe busy for 48 % of the cycles.  head_dim 64, where every product has twice the exponentials: the same 360 us, 755 TFLOP/s, 17 % for 4 001 keys and windows of 300.
+// Windows, without a list's look-up: 32 768 tokens, 32 heads on 8, window 1 024, bf16 590 to 612 us by the card, 890 to 920 TFLOP/s of what the rows see (a tile of 32 queries
+// walks 3 % more), the matrix pipe busy for 48 % of the cycles.  head_dim 64, where every product has twice the exponentials: the same 360 to 385 us, 705 to 755 TFLOP/s, 17 % for
+// 4 001 keys and windows of 300.
 #pragma once
 #include <type_traits>
 
